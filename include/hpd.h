@@ -63,6 +63,8 @@ typedef enum {
 #define HPD_DEVERR_TIMEOUT 0x40u    /* a bounded device-side wait expired */
 #define HPD_DEVERR_POOL 0x80u       /* KV append / rollback: free-page stack short or inconsistent */
 #define HPD_DEVERR_FORK_CAP 0x100u  /* fork: more branches than the output capacity */
+#define HPD_DEVERR_CHUNK_CAP 0x200u /* chunk slots: more new tokens than max_tokens */
+#define HPD_DEVERR_POSITION 0x400u  /* a position outside [0, max_pos) */
 
 /* Tokens per KV page of the paged private cache. */
 #define HPD_PAGE_TOKENS 16
@@ -338,6 +340,132 @@ typedef struct {
 } hpd_fork_args;
 
 hpd_status hpd_fork_children(const hpd_fork_args *args, hpd_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Chunks of new tokens over the paged cache: what puts a page's prefix there
+ * (its vision tokens, then its layout tokens; the prefix that
+ * prefix_page_table describes above), chunk by chunk or token by token.  A step
+ * over S sequences makes one hpd_chunk_slots call, then in every layer one
+ * hpd_qk_norm_rope and one hpd_chunk_attn.  A sequence may bring any number of
+ * new tokens, none among them; one new token is ordinary decoding.  The new
+ * tokens of all sequences stand one after another (row t of T).
+ *
+ * A cache row ("slot") is 16 * page + offset: row t of k_new lies at k_cache +
+ * slot * H_kv * D.
+ * ------------------------------------------------------------------------ */
+
+/* Pages and slots of the new tokens, from the lengths alone.
+ * Logical page i of sequence s is allocated exactly when i < ceil(len / 16).
+ * The pages that new_len opens are taken from the free-page stack in sequence
+ * order (the order of hpd_kv_append, which does this for one number of rows
+ * for all) and entered in page_table; token t = chunk_cu[s] + i is at position
+ * pos[t] = seq_len[s] + i and in cache row slot[t].  Rows past the last new
+ * token get slot -1 and position 0.
+ * All or nothing: on a negative or overlong length (HPD_DEVERR_BRANCH_LEN),
+ * more new tokens than max_tokens (HPD_DEVERR_CHUNK_CAP) or a short or
+ * inconsistent stack (HPD_DEVERR_POOL), lengths, tables and the stack's top
+ * stay as they are, chunk_cu is all 0 and every slot -1, so that the calls
+ * that follow write and attend nothing.  A page id outside [0, num_pages) is
+ * flagged HPD_DEVERR_PAGE_ID and its tokens get slot -1.
+ * seq_len_out may be seq_len and free_top_out may be free_top (updated in
+ * place); other arrays must not overlap.  One launch. */
+typedef struct {
+  const int32_t *new_len;     /* [S] new tokens of each sequence, >= 0             */
+  const int32_t *seq_len;     /* [S] tokens in the cache before the call           */
+  int32_t *page_table;        /* [S][max_pages], extended in place                 */
+  const int32_t *free_pages;  /* [num_pages] stack of free page ids                */
+  const int32_t *free_top;    /* [1] number of ids on the stack                    */
+  int32_t *seq_len_out;       /* [S] lengths with the new tokens                   */
+  int32_t *free_top_out;      /* [1]                                               */
+  int32_t *chunk_cu;          /* [S + 1] first row of each sequence's new tokens   */
+  int32_t *slot;              /* [max_tokens]                                      */
+  int32_t *pos;               /* [max_tokens], or NULL                             */
+  void *workspace;            /* 256-byte aligned, >= 256 bytes, cleared once by
+                                 hpd_workspace_init; one call at a time            */
+  int S;                      /* 1 .. 16,384 sequences                             */
+  int max_pages, num_pages;   /* >= 1; 16 * num_pages and 16 * max_pages < 2^31    */
+  int max_tokens;             /* >= 1 rows of slot and pos                         */
+} hpd_chunk_slots_args;
+
+hpd_status hpd_chunk_slots(const hpd_chunk_slots_args *args, hpd_stream_t stream);
+
+/* Norms of queries and keys for each head, their rotation by position, and
+ * the write of keys and values to the cache, in one pass.
+ *   x' = x * rsqrt(mean(x^2) + eps) * weight        over the D values of a head
+ *   (x'_i, x'_{i + D/2}) rotated by the angle of table row pos[axis[i]][t]:
+ *   y_i = x'_i cos - x'_{i+D/2} sin,  y_{i+D/2} = x'_{i+D/2} cos + x'_i sin
+ * in 32 bits, rounded once.  q_out[t] takes the queries; cache row slot[t] the
+ * keys, and the values as they are.  A negative slot's keys and values are not
+ * written.  With several axes (time, height and width of an image's tokens)
+ * frequency i turns by the position on axis[i]; text has one axis.
+ * rope holds cos and sin of every position and frequency, so that any base or
+ * scaling of the angles is the caller's (hpd.rope_table makes the ordinary one).
+ * A position outside [0, max_pos) is flagged HPD_DEVERR_POSITION and clamped, a
+ * slot >= num_slots flagged HPD_DEVERR_PAGE_ID and not written.
+ * q, k and v may be columns of one projection's rows (strides in values).
+ * q_out may be q when q_stride is H_q * D; other buffers must not overlap.
+ * One launch. */
+typedef struct {
+  const void *q, *k, *v;    /* bf16, head h of row t at q + t * q_stride + h * D   */
+  int64_t q_stride, k_stride, v_stride; /* multiples of 8                          */
+  const void *q_weight, *k_weight;      /* bf16 [D]; NULL: that norm has no weight */
+  const float *rope;        /* [max_pos][D / 2][2]: cos, sin                       */
+  const int32_t *pos;       /* [n_axes][T]                                         */
+  const int32_t *slot;      /* [T]                                                 */
+  void *q_out;              /* bf16 [T][H_q][D]                                    */
+  void *k_cache, *v_cache;  /* bf16 [num_slots][H_kv][D]                           */
+  void *workspace;          /* 256-byte aligned, >= 256 bytes, cleared once; word 0
+                               the error word                                      */
+  int64_t num_slots;        /* >= 1 cache rows: 16 * num_pages                     */
+  float eps;                /* >= 0                                                */
+  int T;                    /* >= 0 rows                                           */
+  int H_q, H_kv, D;         /* D in {64, 128}; H_q, H_kv >= 1                      */
+  int n_axes;               /* 1 .. 4                                              */
+  int max_pos;              /* >= 1 rows of rope                                   */
+  uint8_t axis[64];         /* axis of each of the D / 2 frequencies, < n_axes     */
+} hpd_qk_norm_rope_args;   /* bf16, fp32 pointers 16-byte aligned, int32 4-byte    */
+
+hpd_status hpd_qk_norm_rope(const hpd_qk_norm_rope_args *args, hpd_stream_t stream);
+
+/* Attention of the new tokens over the paged cache.
+ * Sequence s has seq_len[s] tokens in the cache, its n = chunk_cu[s+1] -
+ * chunk_cu[s] new ones among them as the last.  Its i-th new token sees keys
+ *   j < max(seq_len[s] - n + i + 1, full_len[s])   and j < seq_len[s],
+ * i.e. its own past and itself and, with full_len, the first full_len[s] tokens
+ * whatever its place (an image's tokens see one another).  Key j is slot j % 16
+ * of page page_table[s][j / 16].  Scores, softmax, lse and heads as in
+ * hpd_branch_attn; a row that sees no key (more new tokens than seq_len) gets
+ * out 0 and lse -inf.  Cache rows at or past seq_len[s] may hold anything, NaN
+ * too.  Rows at or past chunk_cu[S] are not written.
+ * Lengths out of range are clamped and flagged HPD_DEVERR_BRANCH_LEN, offsets
+ * HPD_DEVERR_BRANCH_CU, page ids HPD_DEVERR_PAGE_ID (and read as page 0). */
+typedef struct {
+  const void *q;              /* bf16, head h of row t at q + t * q_stride + h * D */
+  int64_t q_stride;           /* values, a multiple of 8; 0 = H_q * D              */
+  const int32_t *chunk_cu;    /* [S + 1], non-decreasing, 0 .. T                   */
+  const int32_t *seq_len;     /* [S], 0 <= seq_len <= 16 * max_pages               */
+  const int32_t *full_len;    /* [S] or NULL (0)                                   */
+  const void *k_cache, *v_cache; /* bf16 [num_pages][16][H_kv][D]                  */
+  const int32_t *page_table;  /* [S][max_pages]                                    */
+  int S;                      /* >= 1 sequences                                    */
+  int T;                      /* >= 1 rows of q, out and lse                       */
+  int H_q, H_kv, D;           /* H_q % H_kv == 0, H_q / H_kv <= 16; D in {64, 128} */
+  int num_pages, max_pages;   /* >= 1                                              */
+  int max_seq_len;            /* host upper bound on seq_len, for planning only;
+                                 0 = 16 * max_pages                                */
+  float scale;                /* softmax scale; 0 = 1/sqrt(D)                      */
+  void *out;                  /* bf16 [T][H_q][D]                                  */
+  float *lse;                 /* fp32 [T][H_q], natural log; may be NULL           */
+  void *workspace;            /* 256-byte aligned, initialised once by
+                                 hpd_workspace_init; one call at a time            */
+  size_t workspace_bytes;
+} hpd_chunk_attn_args;       /* q, out and caches 16-byte aligned                   */
+
+/* Bytes of workspace hpd_chunk_attn needs for these host scalars; 0 if they are
+ * invalid.  Device pointers are not read. */
+size_t hpd_chunk_attn_workspace_size(const hpd_chunk_attn_args *args);
+
+hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *args, hpd_stream_t stream);
 
 /* Self-test of the bounded device waits (no counterpart in the paper): one
  * warp waits on an mbarrier phase that nothing completes and for a

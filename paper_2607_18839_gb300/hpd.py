@@ -20,7 +20,8 @@ STATUS = {0: "HPD_OK", 1: "HPD_ERR_INVALID_ARG", 2: "HPD_ERR_UNSUPPORTED",
           3: "HPD_ERR_WORKSPACE", 4: "HPD_ERR_CUDA", 5: "HPD_ERR_TIMEOUT"}
 
 DEVERR = {0x1: "PREFIX_CU", 0x2: "BRANCH_CU", 0x4: "BRANCH_LEN", 0x8: "PAGE_ID",
-          0x10: "FORK_LEN", 0x40: "TIMEOUT"}
+          0x10: "FORK_LEN", 0x40: "TIMEOUT", 0x80: "POOL", 0x100: "FORK_CAP",
+          0x200: "CHUNK_CAP", 0x400: "POSITION"}
 
 # Every entry point declared in include/hpd.h.
 EXPORTS = ("hpd_branch_attn_workspace_size", "hpd_workspace_init", "hpd_branch_attn",
@@ -28,7 +29,8 @@ EXPORTS = ("hpd_branch_attn_workspace_size", "hpd_workspace_init", "hpd_branch_a
            "hpd_pmtp_accept", "hpd_decode_step", "hpd_decode_step_concurrent",
            "hpd_read_errors", "hpd_status_string", "hpd_last_cuda_error", "hpd_version",
            "hpd_branch_attn_noalloc", "hpd_wait_selftest", "hpd_kv_append", "hpd_kv_rollback",
-           "hpd_fork_children")
+           "hpd_fork_children", "hpd_chunk_slots", "hpd_qk_norm_rope",
+           "hpd_chunk_attn_workspace_size", "hpd_chunk_attn")
 
 # Scratch bytes built into libhpd for hpd_branch_attn_noalloc.
 NOALLOC_WORKSPACE_BYTES = 32 << 20
@@ -86,6 +88,39 @@ class hpd_fork_args(ctypes.Structure):
         ("max_pages", ctypes.c_int), ("cap", ctypes.c_int)]
 
 
+class hpd_chunk_slots_args(ctypes.Structure):
+    """Mirror of the C struct of the same name."""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "new_len", "seq_len", "page_table", "free_pages", "free_top", "seq_len_out", "free_top_out",
+        "chunk_cu", "slot", "pos", "workspace")] + [
+        (n, ctypes.c_int) for n in ("S", "max_pages", "num_pages", "max_tokens")]
+
+
+class hpd_qk_norm_rope_args(ctypes.Structure):
+    """Mirror of the C struct of the same name."""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v")] + [
+        (n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + [
+        (n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "rope", "pos", "slot", "q_out",
+                                       "k_cache", "v_cache", "workspace")] + [
+        ("num_slots", ctypes.c_int64), ("eps", ctypes.c_float)] + [
+        (n, ctypes.c_int) for n in ("T", "H_q", "H_kv", "D", "n_axes", "max_pos")] + [
+        ("axis", ctypes.c_uint8 * 64)]
+
+
+class hpd_chunk_attn_args(ctypes.Structure):
+    """Mirror of the C struct of the same name."""
+
+    _fields_ = [("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64)] + [
+        (n, ctypes.c_void_p) for n in ("chunk_cu", "seq_len", "full_len", "k_cache", "v_cache",
+                                       "page_table")] + [
+        (n, ctypes.c_int) for n in ("S", "T", "H_q", "H_kv", "D", "num_pages", "max_pages",
+                                    "max_seq_len")] + [
+        ("scale", ctypes.c_float), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -136,6 +171,14 @@ def load(path: str = LIB_PATH):
     lib.hpd_kv_rollback.argtypes = [ctypes.POINTER(hpd_kv_args), P, P]
     lib.hpd_fork_children.restype = I
     lib.hpd_fork_children.argtypes = [ctypes.POINTER(hpd_fork_args), P]
+    lib.hpd_chunk_slots.restype = I
+    lib.hpd_chunk_slots.argtypes = [ctypes.POINTER(hpd_chunk_slots_args), P]
+    lib.hpd_qk_norm_rope.restype = I
+    lib.hpd_qk_norm_rope.argtypes = [ctypes.POINTER(hpd_qk_norm_rope_args), P]
+    lib.hpd_chunk_attn_workspace_size.restype = S
+    lib.hpd_chunk_attn_workspace_size.argtypes = [ctypes.POINTER(hpd_chunk_attn_args)]
+    lib.hpd_chunk_attn.restype = I
+    lib.hpd_chunk_attn.argtypes = [ctypes.POINTER(hpd_chunk_attn_args), P]
     _lib = lib
     return lib
 
@@ -228,6 +271,22 @@ def hpd_kv_append(args: hpd_kv_args, stream_handle) -> None:
 def hpd_kv_rollback(args: hpd_kv_args, accepted_len_ptr: int, stream_handle) -> None:
     _check("hpd_kv_rollback", load().hpd_kv_rollback(ctypes.byref(args), accepted_len_ptr,
                                                       stream_handle))
+
+
+def hpd_chunk_slots(args: hpd_chunk_slots_args, stream_handle) -> None:
+    _check("hpd_chunk_slots", load().hpd_chunk_slots(ctypes.byref(args), stream_handle))
+
+
+def hpd_qk_norm_rope(args: hpd_qk_norm_rope_args, stream_handle) -> None:
+    _check("hpd_qk_norm_rope", load().hpd_qk_norm_rope(ctypes.byref(args), stream_handle))
+
+
+def hpd_chunk_attn_workspace_size(args: hpd_chunk_attn_args) -> int:
+    return int(load().hpd_chunk_attn_workspace_size(ctypes.byref(args)))
+
+
+def hpd_chunk_attn(args: hpd_chunk_attn_args, stream_handle) -> None:
+    _check("hpd_chunk_attn", load().hpd_chunk_attn(ctypes.byref(args), stream_handle))
 
 
 def hpd_branch_attn_noalloc(args: hpd_branch_attn_args, stream_handle: Optional[int]) -> None:
@@ -449,3 +508,185 @@ def fork_children(out_tokens, accepted_len, is_layout, layout_pos, fork_token, b
                          n_docs, max_pages, cap)
     _check("hpd_fork_children", load().hpd_fork_children(ctypes.byref(args), handle))
     return new
+
+
+def _need(what: str, t, dtype, shape, strides_free=False):
+    """A tensor of the wrong type or shape never reaches a kernel."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or \
+            len(t.shape) != len(shape) or \
+            any(n is not None and n != have for n, have in zip(shape, t.shape)) or \
+            not (strides_free or t.is_contiguous()):
+        have = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t)
+        raise HpdError(what, 1, f"expected a {'' if strides_free else 'contiguous '}CUDA {dtype} "
+                                f"{tuple('any' if n is None else n for n in shape)}, got {have}")
+
+
+def rope_table(max_pos: int, D: int, theta: float = 1e6, device="cuda"):
+    """cos and sin of position * theta^(-2 i / D) for qk_norm_rope: fp32
+    [max_pos, D / 2, 2], the angles taken in 64 bits."""
+    import torch
+    i = torch.arange(D // 2, dtype=torch.float64, device=device)
+    a = torch.arange(max_pos, dtype=torch.float64, device=device)[:, None] * theta ** (-2.0 * i / D)
+    return torch.stack((a.cos(), a.sin()), -1).float().contiguous()
+
+
+class ChunkSlots:
+    """Pages and slots of each step's new tokens (hpd_chunk_slots) for the
+    sequences of one page table.  Owns the outputs: chunk_cu [S + 1], slot and
+    pos [max_tokens], and the error word's workspace.  in_place: lengths and
+    the stack's top are updated where they are; otherwise the new ones go to
+    ``seq_len`` and ``free_top`` of this object and the given ones stay."""
+
+    def __init__(self, page_table, seq_len, free_pages, free_top, max_tokens, in_place=True):
+        import torch
+        S, max_pages = page_table.shape
+        i32 = torch.int32
+        _need("ChunkSlots", page_table, i32, (None, None))
+        _need("ChunkSlots", seq_len, i32, (S,))
+        _need("ChunkSlots", free_pages, i32, (None,))
+        _need("ChunkSlots", free_top, i32, (1,))
+        dev = page_table.device
+        self.page_table, self.free_pages = page_table, free_pages
+        self._seq_in, self._top_in = seq_len, free_top
+        self.seq_len = seq_len if in_place else torch.empty_like(seq_len)
+        self.free_top = free_top if in_place else torch.empty_like(free_top)
+        self.chunk_cu = torch.empty(S + 1, dtype=i32, device=dev)
+        self.slot = torch.empty(max_tokens, dtype=i32, device=dev)
+        self.pos = torch.empty(max_tokens, dtype=i32, device=dev)
+        self.workspace = torch.zeros(256, dtype=torch.uint8, device=dev)
+        self.args = hpd_chunk_slots_args(
+            None, _ptr(seq_len), _ptr(page_table), _ptr(free_pages), _ptr(free_top),
+            _ptr(self.seq_len), _ptr(self.free_top), _ptr(self.chunk_cu), _ptr(self.slot),
+            _ptr(self.pos), _ptr(self.workspace), S, max_pages, free_pages.shape[0], max_tokens)
+
+    def __call__(self, new_len, stream=None) -> "ChunkSlots":
+        """new_len: int32 [S] device tensor."""
+        import torch
+        _need("ChunkSlots", new_len, torch.int32, (self.args.S,))
+        self.args.new_len = new_len.data_ptr()
+        hpd_chunk_slots(self.args, _stream_handle(stream))
+        return self
+
+    def errors(self, stream=None) -> int:
+        return hpd_read_errors(_ptr(self.workspace), _stream_handle(stream))
+
+
+class QkNormRope:
+    """Per-head norms, rotation and cache write of a layer (hpd_qk_norm_rope).
+    q_weight / k_weight: bf16 [D] or None; rope: fp32 [max_pos, D / 2, 2]
+    (rope_table); sections: how many of the D / 2 frequencies turn by each
+    axis' position, in order, or ``axis``: the axis of every frequency."""
+
+    def __init__(self, H_q, H_kv, D, q_weight, k_weight, rope, sections=None, axis=None, eps=1e-6):
+        import torch
+        if axis is None:
+            axis = [a for a, n in enumerate(sections or (D // 2,)) for _ in range(n)]
+        if len(axis) != D // 2 or not all(0 <= a < 4 for a in axis):
+            raise HpdError("QkNormRope", 1, "an axis below 4 for each of the D / 2 frequencies")
+        for w in (q_weight, k_weight):
+            if w is not None:
+                _need("QkNormRope", w, torch.bfloat16, (D,))
+        _need("QkNormRope", rope, torch.float32, (None, D // 2, 2))
+        self.H_q, self.H_kv, self.D = H_q, H_kv, D
+        self._keep = (q_weight, k_weight, rope)
+        self.n_axes = max(axis) + 1
+        self.workspace = torch.zeros(256, dtype=torch.uint8, device=rope.device)
+        self.args = hpd_qk_norm_rope_args()
+        a = self.args
+        a.q_weight, a.k_weight, a.rope = _ptr(q_weight), _ptr(k_weight), _ptr(rope)
+        a.workspace, a.eps = _ptr(self.workspace), eps
+        a.H_q, a.H_kv, a.D, a.n_axes, a.max_pos = H_q, H_kv, D, self.n_axes, rope.shape[0]
+        a.axis[:D // 2] = axis
+        self.q_out = None
+
+    def __call__(self, qkv, pos, slot, k_cache, v_cache, q_out=None, stream=None):
+        """qkv: bf16 [T, at least (H_q + 2 H_kv) D], the projection's rows
+        (queries, keys, values; rows may be strided); pos: int32 [n_axes, T] or
+        [T]; slot: int32 [T]; caches bf16 [pages, 16, H_kv, D].  Returns the
+        queries [T, H_q, D] (q_out, or a tensor that this object keeps)."""
+        import torch
+        a, T = self.args, qkv.shape[0]
+        H_q, H_kv, D = self.H_q, self.H_kv, self.D
+        bf = torch.bfloat16
+        _need("QkNormRope", qkv, bf, (None, None), strides_free=True)
+        if qkv.shape[1] < (H_q + 2 * H_kv) * D or qkv.stride(1) != 1:
+            raise HpdError("QkNormRope", 1, "rows of at least (H_q + 2 H_kv) D values side by side")
+        _need("QkNormRope", pos, torch.int32, (T,) if pos.dim() == 1 else (self.n_axes, T))
+        if pos.dim() == 1 and self.n_axes != 1:
+            raise HpdError("QkNormRope", 1, f"positions on {self.n_axes} axes")
+        _need("QkNormRope", slot, torch.int32, (None,))
+        _need("QkNormRope", k_cache, bf, (None, 16, H_kv, D))
+        _need("QkNormRope", v_cache, bf, k_cache.shape)
+        if slot.shape[0] < T:
+            raise HpdError("QkNormRope", 1, "a slot for each row")
+        if q_out is None:
+            if self.q_out is None or self.q_out.shape[0] < T:
+                self.q_out = torch.empty((T, H_q, D), dtype=bf, device=qkv.device)
+            q_out = self.q_out[:T]
+        else:
+            _need("QkNormRope", q_out, bf, (T, H_q, D))
+        at, row = qkv.data_ptr(), qkv.stride(0)
+        a.q, a.k, a.v = at, at + 2 * H_q * D, at + 2 * (H_q + H_kv) * D
+        a.q_stride = a.k_stride = a.v_stride = row
+        a.pos, a.slot, a.q_out = pos.data_ptr(), slot.data_ptr(), q_out.data_ptr()
+        a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
+        a.num_slots, a.T = k_cache.shape[0] * 16, T
+        hpd_qk_norm_rope(a, _stream_handle(stream))
+        return q_out
+
+    def errors(self, stream=None) -> int:
+        return hpd_read_errors(_ptr(self.workspace), _stream_handle(stream))
+
+
+class ChunkAttn:
+    """Attention of up to max_tokens new tokens over the paged cache
+    (hpd_chunk_attn).  Owns out [max_tokens, H_q, D], lse [max_tokens, H_q]
+    and the workspace."""
+
+    def __init__(self, H_q, k_cache, v_cache, page_table, max_tokens, max_seq_len=0, scale=0.0,
+                 stream=None):
+        import torch
+        bf = torch.bfloat16
+        _need("ChunkAttn", k_cache, bf, (None, 16, None, None))
+        _need("ChunkAttn", v_cache, bf, k_cache.shape)
+        _need("ChunkAttn", page_table, torch.int32, (None, None))
+        num_pages, _, H_kv, D = k_cache.shape
+        S, max_pages = page_table.shape
+        dev = k_cache.device
+        self._keep = (k_cache, v_cache, page_table)
+        self.out = torch.empty((max_tokens, H_q, D), dtype=bf, device=dev)
+        self.lse = torch.empty((max_tokens, H_q), dtype=torch.float32, device=dev)
+        a = self.args = hpd_chunk_attn_args()
+        a.k_cache, a.v_cache, a.page_table = _ptr(k_cache), _ptr(v_cache), _ptr(page_table)
+        a.S, a.T, a.H_q, a.H_kv, a.D = S, max_tokens, H_q, H_kv, D
+        a.num_pages, a.max_pages, a.max_seq_len, a.scale = num_pages, max_pages, max_seq_len, scale
+        a.out, a.lse = _ptr(self.out), _ptr(self.lse)
+        nbytes = hpd_chunk_attn_workspace_size(a)
+        if nbytes == 0:
+            raise HpdError("hpd_chunk_attn_workspace_size", 1, "invalid shape")
+        self.max_tokens = max_tokens
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        a.workspace, a.workspace_bytes = _ptr(self.workspace), nbytes
+        hpd_workspace_init(_ptr(self.workspace), nbytes, _stream_handle(stream))
+
+    def __call__(self, q, chunk_cu, seq_len, full_len=None, stream=None):
+        """q: bf16 [T, H_q, D] (heads side by side, rows may be strided), T up
+        to max_tokens; chunk_cu int32 [S + 1], seq_len and full_len int32 [S].
+        Returns (out, lse) of the T rows."""
+        import torch
+        a, T = self.args, q.shape[0]
+        _need("ChunkAttn", q, torch.bfloat16, (None, a.H_q, a.D), strides_free=True)
+        if T > self.max_tokens or T < 1 or q.stride(2) != 1 or q.stride(1) != a.D:
+            raise HpdError("ChunkAttn", 1, "1 to max_tokens rows with their heads side by side")
+        _need("ChunkAttn", chunk_cu, torch.int32, (a.S + 1,))
+        _need("ChunkAttn", seq_len, torch.int32, (a.S,))
+        if full_len is not None:
+            _need("ChunkAttn", full_len, torch.int32, (a.S,))
+        a.q, a.q_stride, a.T = q.data_ptr(), q.stride(0) if T > 1 else 0, T
+        a.chunk_cu, a.seq_len, a.full_len = chunk_cu.data_ptr(), seq_len.data_ptr(), _ptr(full_len)
+        hpd_chunk_attn(a, _stream_handle(stream))
+        return (self.out, self.lse) if T == self.max_tokens else (self.out[:T], self.lse[:T])
+
+    def errors(self, stream=None) -> int:
+        return hpd_read_errors(_ptr(self.workspace), _stream_handle(stream))
