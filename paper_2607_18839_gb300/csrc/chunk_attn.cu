@@ -1,15 +1,75 @@
 // chunk_attn.cu -- attention of a chunk of new tokens over the paged cache
-// (hpd_chunk_attn): one warp to a row and head, 32 keys at a time with a running
-// maximum and sum.
+// (hpd_chunk_attn) on 5th-generation tensor cores.
+//
+//   row (i, h) of sequence s, h = g G + e:  keys j < lim_i,
+//     lim_i = min(L, max(L - n + i + 1, full))
+//   S = scale Q K^T over them, P = exp(S - max), out = P V / sum P,
+//   lse = max + log sum P
+//
+// The rows that read KV head g are stacked, token by token, into tiles of 128
+// (row r of a tile: token r / G, head g G + r % G; with a G that does not divide
+// 128 its last rows are unused), and a tile walks the 128-key blocks, 8 pages
+// each, up to the last key that one of its rows sees.
+//
+// Work units: (tile, KV head, split of the tile's blocks).  One CTA per SM
+// takes units from an atomic counter; its roles run one unit apart, so that
+// nothing drains between units:
+//   warp 10     scheduler: finds the next unit in the step's lengths and puts
+//               its metadata into one of two slots while the other is in use
+//   warps 0, 11 TMA producers of K (and each unit's Q tile ahead of it) and V:
+//               three-stage rings, 128-byte swizzle; a block whose pages are
+//               consecutive in the pool is one box, else eight
+//   warp 1      Q tile into TMEM (tcgen05.cp), S = Q K^T into one of two buffers
+//   warp 12     O += P V, P read from TMEM where S was
+//   warps 2..9  softmax: two warpgroups, each with half of a block's keys and
+//               half of O's columns; a thread owns one row
+// A row's base is its maximum over the first block it sees keys of (the two
+// threads of a row exchange it there and nowhere else); later exponentials are
+// taken against it.  That is exact to the same relative error as a running
+// maximum as long as nothing overflows: a unit in which a score exceeds its base
+// by more than 2^64, or O is not finite, runs once more with running maxima.
+// Which units do is a matter of their own scores and values alone, so that a
+// call's bits do not depend on which CTA took which unit.
+// P goes to the tensor cores in two parts: while the exponentials of a half's
+// second 32 keys are taken, P V of the first 32 runs.
+//
+// Rows that see no key are written by the scheduler.  Cache rows past a
+// sequence's end may hold anything: pages past it are not loaded (their box lies
+// outside the map and reads zeros), the rows behind it in its last page
+// are zeroed in shared memory before P V, and scores there are masked.
+// A value that is not finite in a row that some of a tile's rows see and others do
+// not would reach the others as 0 times it: rows whose O is not finite after
+// the second pass, and that such a value may have reached, are computed once
+// more from what they see, one row at a time.
+// All waits are bounded, as in the branch attention kernel.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
-#include "common.cuh"
+#include "tc_common.cuh"
 
 namespace hpd {
 namespace {
 
-struct ChunkArgs {
+using namespace sm100;
+using tc::kBlk;
+using tc::kRows;
+
+constexpr uint32_t kTmemCols = 512;
+constexpr int kPagesPerBlock = kBlk / kPage;
+constexpr int kSoftmaxWarps = 8;
+constexpr int kSchedWarp = 2 + kSoftmaxWarps;
+constexpr int kVWarp = kSchedWarp + 1;
+constexpr int kPvWarp = kVWarp + 1;
+constexpr int kThreads = 32 * (kPvWarp + 1);
+constexpr uint32_t kMetaConsumers = 4 + kSoftmaxWarps;
+constexpr int kStages = 3;
+constexpr int kGroup = 256;      // sequences whose lengths the scheduler holds at once
+constexpr int kMaxSplits = 32;
+constexpr int kNoUnit = (1 << 30) - 1;  // every unit's number is below
+constexpr uint64_t kBlockLimitNs = 10000;  // of a unit's time: a block takes some 0.7 us
+
+struct ChunkParams {
   const __nv_bfloat16 *q;
   long long q_stride;
   const int32_t *chunk_cu, *seq_len, *full_len;
@@ -18,80 +78,861 @@ struct ChunkArgs {
   int S, T, H_q, H_kv, G, num_pages, max_pages;
   float scale_log2;
   __nv_bfloat16 *out;
+  bool out_align32;
   float *lse;
   uint32_t *err;
+  int *unit_ctr;   // [2] next unit and finished CTAs, zero between calls
+  int s_max;       // most splits of a tile; 1: none
+  float *o_part;   // [s_max][T][H_q][D]
+  float *l_part;   // [s_max][T][H_q]
+  int *row_split;  // [T] splits of the row's tile
+  FastDiv div_G, div_Hkv;
 };
 
-constexpr int kWarps = 4;
+// Metadata of one unit, written by the scheduler warp.
+struct UnitMeta {
+  int valid;     // 0: no units left
+  int g, split, nsplit;
+  int seq;
+  int tok0;      // first row (of T) of the tile
+  int nrows;     // stacked rows
+  int lim0;      // keys that the tile's first token sees by its place (a token more each)
+  int full, L;   // keys that every token sees; tokens of the sequence
+  int pages;     // pages up to the last key that the tile sees
+  int blk_lo, n_blocks;
+  int exact;     // every block's base is the running maximum
+};
 
 template <int D>
-__global__ void __launch_bounds__(32 * kWarps) chunk_attn_simple_kernel(const ChunkArgs a) {
-  __shared__ float s_q[kWarps][D];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long item = static_cast<long long>(blockIdx.x) * kWarps + warp;
-  pdl_wait();
-  pdl_trigger();
-  if (item >= static_cast<long long>(a.T) * a.H_q) return;
-  const int t = static_cast<int>(item / a.H_q), h = static_cast<int>(item % a.H_q), g = h / a.G;
-  // the row's sequence (offsets clamped into 0 .. T)
-  int s = -1, c0 = 0, c1 = 0;
-  for (int i = 0; i < a.S && s < 0; ++i) {
-    c0 = min(max(a.chunk_cu[i], 0), a.T);
-    c1 = min(max(a.chunk_cu[i + 1], 0), a.T);
-    if (c1 < c0 || c0 != a.chunk_cu[i] || c1 != a.chunk_cu[i + 1]) flag_error(a.err, HPD_DEVERR_BRANCH_CU);
-    if (t >= c0 && t < c1) s = i;
-  }
-  if (s < 0) return;
-  int L = a.seq_len[s];
-  if (L < 0 || L > a.max_pages * kPage) {
-    flag_error(a.err, HPD_DEVERR_BRANCH_LEN);
-    L = min(max(L, 0), a.max_pages * kPage);
-  }
-  int lim = L - (c1 - c0) + (t - c0) + 1;
-  if (a.full_len) lim = max(lim, a.full_len[s]);
-  lim = min(lim, L);
-  for (int c = lane; c < D; c += 32)
-    s_q[warp][c] = __bfloat162float(a.q[t * a.q_stride + h * D + c]);
+struct Layout {
+  static constexpr int kChunks = D / 64;                // 64-column (128-byte) boxes
+  static constexpr uint32_t kChunkBytes = kRows * 128;  // 128 rows x 128 bytes
+  static constexpr uint32_t kTileBytes = kChunks * kChunkBytes;
+  // a block's pages: 8-key groups of kChunks x 1024 bytes
+  static constexpr uint32_t kGroupBytes = kChunks * 1024, kPageBytes = 2 * kGroupBytes;
+  static constexpr uint32_t kK = 0;
+  static constexpr uint32_t kV = kK + kStages * kTileBytes;
+  static constexpr uint32_t kBytes = kV + kStages * kTileBytes;
+  static constexpr uint32_t kDynSmem = kBytes + 1024;   // slack to align to 1024
+  // TMEM columns: S of block buffer i, O, Q rows of unit slot u
+  static constexpr uint32_t kColO = 256;
+  static __device__ __forceinline__ uint32_t col_s(int i) { return i ? 128u : 0u; }
+  static __device__ __forceinline__ uint32_t col_q(int u) { return u ? 448u : 384u; }
+};
+
+struct __align__(8) Shared {
+  uint64_t meta_full[2], meta_empty[2];
+  uint64_t k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages];
+  // per S buffer: scores written; P written, by part; P V done (the buffer is
+  // free and O holds the block)
+  uint64_t s_full[2], p_full[2][2], s_free[2];
+  uint64_t o_full, o_empty;
+  uint64_t mma_done[2];
+  uint32_t tmem_base;
+  int abort;
+  float xmax[2][2][kRows];  // [half][block parity][row]
+  float xsum[2][2][kRows];  // [unit parity][half][row]
+  int xseq[2][2][4];        // [max | sum][half][quadrant]
+  unsigned redo;            // units (by number in this CTA, modulo 32) to run once more
+  int units_done;           // softmax warps that finished a unit's epilogue
+  int unit_id[32];          // the last units issued
+  UnitMeta meta[2];
+  // the scheduler's group of sequences: units before each, first rows, lengths, splits
+  int g_units[kGroup + 1], g_cu[kGroup + 1], g_len[kGroup], g_split[kGroup];
+};
+
+__device__ __forceinline__ void set_abort(Shared &sh, uint32_t *err) {
+  atomicExch(&sh.abort, 1);
+  flag_error(err, HPD_DEVERR_TIMEOUT);
+}
+__device__ __forceinline__ bool aborted(const Shared &sh) {
+  return *reinterpret_cast<const volatile int *>(&sh.abort) != 0;
+}
+__device__ __forceinline__ void publish_seq(int *flag, int seq) {
   __syncwarp();
+  if ((threadIdx.x & 31) == 0)
+    asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(flag)), "r"(seq)
+                 : "memory");
+}
+__device__ __forceinline__ int load_seq(const int *flag) {
+  int v;
+  asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(v) : "r"(smem_u32(flag)) : "memory");
+  return v;
+}
+__device__ __noinline__ bool await_seq_slow(const int *flag, int seq, const int *abort) {
+  const uint64_t t0 = globaltimer();
+  for (uint32_t i = 1; load_seq(flag) < seq; ++i)
+    if ((i & 63u) == 0 &&
+        (*reinterpret_cast<const volatile int *>(abort) || globaltimer() - t0 > kWaitLimitNs))
+      return false;
+  return true;
+}
+__device__ __forceinline__ bool await_seq(const int *flag, int seq, const Shared &sh) {
+  return load_seq(flag) >= seq || await_seq_slow(flag, seq, &sh.abort);
+}
+
+// Natural log of 2^m * l with one rounding at the result's size.
+__device__ __forceinline__ float lse_of(float m, float l) {
+  const int e = static_cast<int>(__float_as_uint(l) >> 23) - 127;
+  const float f = __uint_as_float((__float_as_uint(l) & 0x007fffffu) | 0x3f800000u);
+  return fmaf(static_cast<float>(e), kLn2, fmaf(m, kLn2, logf(f)));
+}
+
+// Half a block of a row's softmax against a base that is there (see
+// tc::softmax_half_based): publish(part) once P of the half's first (second) 32
+// keys is in TMEM.  hi: visible columns of the half.  Returns false when a score
+// lies above the window of the base.
+template <class Publish>
+__device__ __forceinline__ bool softmax_based(uint32_t s_addr, bool plain, int hi, float sl2, float m_run,
+                                              float &l_half, Publish publish) {
   const float NEG_INF = -__int_as_float(0x7f800000);
+  if (!plain && __all_sync(0xffffffffu, hi <= 0)) {  // no row of the warp sees a key of the half
+    uint32_t z[32];
+#pragma unroll
+    for (int c = 0; c < 32; ++c) z[c] = 0u;
+    tmem_st32(s_addr, z);
+    publish(0);
+    publish(1);
+    return true;
+  }
+  const bool raw = sl2 > 0.f;
+  const float mul = raw ? sl2 : 1.f, base = m_run == NEG_INF ? 0.f : m_run;
+  uint32_t v[64];
+  float2 sum4[4];
+  float mx4[4];
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    sum4[a] = make_float2(0.f, 0.f);
+    mx4[a] = NEG_INF;
+  }
+  tmem_ld32(s_addr, v);
+  tmem_ld_wait32(v);
+  tmem_ld32(s_addr + 32, v + 32);
+  if (!plain) tc::mask32(v, 0, hi, !raw, sl2);
+  tc::exp32<true, false>(s_addr, v, mul, base, sum4, mx4);
+  publish(0);
+  tmem_ld_wait32(v + 32);
+  if (!plain) tc::mask32(v + 32, 0, hi - 32, !raw, sl2);
+  tc::exp32<true, false>(s_addr + 16, v + 32, mul, base, sum4, mx4);
+  publish(1);
+  l_half += tc::sum_of(sum4);
+  return fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * mul <= base + tc::kWindowLog2;
+}
+
+// One row over keys [lo, hi) of its sequence by one warp, from global memory and
+// nothing but what the row sees: for rows that a value of another row's keys may
+// have reached through the tensor cores.  Writes half h of the normalised row's
+// columns (o_f, or o_b if o_f is null).
+template <int D>
+__device__ __noinline__ void one_row(const ChunkParams &p, int seq, int token, int head, int lo, int hi, int h,
+                                     float *o_f, __nv_bfloat16 *o_b) {
+  const int lane = threadIdx.x & 31, g = p.div_G(head);
+  const float NEG_INF = -__int_as_float(0x7f800000);
+  const __nv_bfloat16 *q = p.q + token * p.q_stride + head * D;
   float m = NEG_INF, l = 0.f, o[D / 32];
+#pragma unroll
   for (int c = 0; c < D / 32; ++c) o[c] = 0.f;
-  for (int j0 = 0; j0 < lim; j0 += 32) {
+#pragma unroll 1
+  for (int j0 = lo; j0 < hi; j0 += 32) {
     const int j = j0 + lane;
     int pg = 0;
     float x = NEG_INF;
-    if (j < lim) {
-      pg = a.page_table[static_cast<size_t>(s) * a.max_pages + j / kPage];
-      if (pg < 0 || pg >= a.num_pages) {
-        flag_error(a.err, HPD_DEVERR_PAGE_ID);
-        pg = 0;
-      }
-      const __nv_bfloat16 *k = a.k_cache + ((static_cast<size_t>(pg) * kPage + j % kPage) * a.H_kv + g) * D;
+    if (j < hi) {
+      pg = p.page_table[static_cast<size_t>(seq) * p.max_pages + j / kPage];
+      if (static_cast<unsigned>(pg) >= static_cast<unsigned>(p.num_pages)) pg = 0;
+      const __nv_bfloat162 *k = reinterpret_cast<const __nv_bfloat162 *>(
+          p.k_cache + ((static_cast<size_t>(pg) * kPage + j % kPage) * p.H_kv + g) * D);
+      const __nv_bfloat162 *q2 = reinterpret_cast<const __nv_bfloat162 *>(q);
       x = 0.f;
-      for (int c = 0; c < D; ++c) x = fmaf(s_q[warp][c], __bfloat162float(k[c]), x);
-      x *= a.scale_log2;
+#pragma unroll 8
+      for (int c = 0; c < D / 2; ++c) {
+        const float2 a = __bfloat1622float2(q2[c]), b = __bfloat1622float2(k[c]);
+        x = fmaf(a.x, b.x, fmaf(a.y, b.y, x));
+      }
+      x *= p.scale_log2;
     }
     float mx = x;
+#pragma unroll 1
     for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
     const float m_new = fmaxf(m, mx), base = m_new == NEG_INF ? 0.f : m_new;
-    const float alpha = exp2f(m - base), p = exp2f(x - base);
+    const float alpha = exp2f(m - base), e = exp2f(x - base);
     m = m_new;
-    float sum = p;
+    float sum = e;
+#pragma unroll 1
     for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
     l = l * alpha + sum;
+#pragma unroll
     for (int c = 0; c < D / 32; ++c) o[c] *= alpha;
-    for (int i = 0; i < min(32, lim - j0); ++i) {
-      const float pi = __shfl_sync(0xffffffffu, p, i);
+    const int n = min(32, hi - j0);
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      const float ei = __shfl_sync(0xffffffffu, e, i);
       const int pgi = __shfl_sync(0xffffffffu, pg, i);
-      const __nv_bfloat16 *v =
-          a.v_cache + ((static_cast<size_t>(pgi) * kPage + (j0 + i) % kPage) * a.H_kv + g) * D;
-      for (int c = 0; c < D / 32; ++c) o[c] = fmaf(pi, __bfloat162float(v[c * 32 + lane]), o[c]);
+      const __nv_bfloat16 *v = p.v_cache + ((static_cast<size_t>(pgi) * kPage + (j0 + i) % kPage) * p.H_kv + g) * D;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) o[c] = fmaf(ei, __bfloat162float(v[c * 32 + lane]), o[c]);
     }
   }
   const float inv = l > 0.f ? 1.f / l : l;
-  for (int c = 0; c < D / 32; ++c) a.out[item * D + c * 32 + lane] = __float2bfloat16(o[c] * inv);
-  if (lane == 0 && a.lse) a.lse[item] = l > 0.f || l != l ? (m + log2f(l)) * kLn2 : NEG_INF;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    if (c / (D / 64) != h) continue;
+    if (o_f) o_f[c * 32 + lane] = o[c] * inv;
+    else o_b[c * 32 + lane] = __float2bfloat16(o[c] * inv);
+  }
 }
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                      const __grid_constant__ CUtensorMap tm_k8, const __grid_constant__ CUtensorMap tm_v8,
+                      const __grid_constant__ CUtensorMap tm_q, const ChunkParams p) {
+  using L = Layout<D>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Shared sh;
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = p.G;
+  const int TT = kRows / G;  // tokens of a tile
+  const float NEG_INF = -__int_as_float(0x7f800000);
+  auto bar = [](uint64_t &b) { return smem_u32(&b); };
+  auto wait_bar = [&](uint64_t &b, int parity) {
+    return __all_sync(0xffffffffu, mbar_wait(bar(b), parity, &sh.abort));
+  };
+
+  if (tid == 0) {
+    sh.abort = 0;
+    sh.redo = 0u;
+    sh.units_done = 0;
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(bar(sh.k_full[s]), 1);
+      mbar_init(bar(sh.v_full[s]), 1);
+      mbar_init(bar(sh.k_empty[s]), 1);
+      mbar_init(bar(sh.v_empty[s]), 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bar(sh.meta_full[s]), 1);
+      mbar_init(bar(sh.meta_empty[s]), kMetaConsumers);
+      mbar_init(bar(sh.s_full[s]), 1);
+      mbar_init(bar(sh.p_full[s][0]), kSoftmaxWarps);
+      mbar_init(bar(sh.p_full[s][1]), kSoftmaxWarps);
+      mbar_init(bar(sh.s_free[s]), 1);
+    }
+    mbar_init(bar(sh.o_full), 1);
+    mbar_init(bar(sh.o_empty), kSoftmaxWarps);
+    mbar_init(bar(sh.mma_done[0]), 1);
+    mbar_init(bar(sh.mma_done[1]), 1);
+    fence_mbar_init();
+  }
+  if (tid < 16) (&sh.xseq[0][0][0])[tid] = 0;
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&sh.tmem_base), kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem_base;
+  pdl_wait();     // queries, cache, tables and lengths as the kernels before leave them
+  pdl_trigger();  // the merge of the splits may launch; it waits for this grid
+
+  if (warp == kSchedWarp) {
+    // ------------------------------------------------------- scheduler --
+    // Units are numbered sequence by sequence, in each its tiles from the last
+    // (longest) to the first, in each its splits and then its KV heads.
+    int g0 = -kGroup, before = 0, group_units = 0;  // the group held, units before it and of it
+    auto load_group = [&](int s0, int units_before) {
+      g0 = s0;
+      before = units_before;
+      int tiles[kGroup / 32], blocks[kGroup / 32];
+      long long total = 0;
+#pragma unroll
+      for (int k = 0; k < kGroup / 32; ++k) {
+        const int s = s0 + k * 32 + lane;
+        tiles[k] = blocks[k] = 0;
+        if (s < p.S) {
+          const int a0 = p.chunk_cu[s], a1 = p.chunk_cu[s + 1], len = p.seq_len[s];
+          const int c0 = min(max(a0, 0), p.T), c1 = max(c0, min(a1, p.T));
+          if (a0 != c0 || a1 != c1) flag_error(p.err, HPD_DEVERR_BRANCH_CU);
+          const int cap = p.max_pages * kPage, Ls = min(max(len, 0), cap);
+          if (Ls != len) flag_error(p.err, HPD_DEVERR_BRANCH_LEN);
+          tiles[k] = (c1 - c0 + TT - 1) / TT;
+          blocks[k] = ceil_div_i(Ls, kBlk);
+          total += static_cast<long long>(tiles[k]) * blocks[k];
+          sh.g_cu[k * 32 + lane] = c0;
+          // (a row range that the next sequence's offset contradicts)
+          sh.g_len[k * 32 + lane] = Ls;
+          if (k * 32 + lane == kGroup - 1 || s == p.S - 1) sh.g_cu[k * 32 + lane + 1] = c1;
+        }
+      }
+      // Blocks of a split: what one CTA's share of all blocks is.
+      int per = 1 << 30;
+      if (p.s_max > 1) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        total *= p.H_kv;
+        per = max(2, static_cast<int>((total + gridDim.x - 1) / gridDim.x));
+      }
+      // (sums that stop at kNoUnit, which offsets out of order could pass)
+      auto add = [](int a, int b) { return min(a + b, kNoUnit); };
+      int base = 0;
+#pragma unroll
+      for (int k = 0; k < kGroup / 32; ++k) {
+        if (s0 + k * 32 >= p.S) break;
+        const int nsplit = p.s_max > 1 ? min(p.s_max, max(1, (blocks[k] + per - 1) / per)) : 1;
+        const int units = min(tiles[k] * nsplit * p.H_kv, kNoUnit);
+        int incl = units;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, incl, o);
+          if (lane >= o) incl = add(incl, v);
+        }
+        const int prior = __shfl_up_sync(0xffffffffu, incl, 1);
+        sh.g_units[k * 32 + lane] = add(base, lane ? prior : 0);
+        sh.g_split[k * 32 + lane] = nsplit;
+        base = add(base, __shfl_sync(0xffffffffu, incl, 31));
+      }
+      group_units = base;
+      __syncwarp();
+    };
+    load_group(0, 0);
+    unsigned redo = 0;  // units to run once more
+    int nb_last = 0, nb_before = 0;
+    auto take_redo = [&] {
+      unsigned r = 0;
+      if (lane == 0 && *static_cast<volatile unsigned *>(&sh.redo)) r = atomicExch(&sh.redo, 0u);
+      return __shfl_sync(0xffffffffu, r, 0);
+    };
+    // The unit's place in the group held (moved there); false: no such unit.
+    auto locate = [&](int u) {
+      if (u < before) load_group(0, 0);
+      while (u - before >= group_units) {
+        if (g0 + kGroup >= p.S) return false;
+        load_group(g0 + kGroup, min(before + group_units, kNoUnit));
+      }
+      return u < kNoUnit;
+    };
+    for (int k = 0;; ++k) {
+      const int slot = k & 1;
+      if (k >= 2 && !wait_bar(sh.meta_empty[slot], ((k >> 1) - 1) & 1)) {
+        if (lane == 0) set_abort(sh, p.err);
+        break;
+      }
+      UnitMeta &M = sh.meta[slot];
+      bool have = false;
+      for (;;) {
+        int u = 0;
+        if (!redo) redo = take_redo();
+        const bool again = redo != 0;
+        if (again) {
+          u = sh.unit_id[__ffs(redo) - 1];
+          redo &= redo - 1;
+        } else {
+          if (lane == 0) u = atomicAdd(p.unit_ctr, 1);
+          u = __shfl_sync(0xffffffffu, u, 0);
+          if (__any_sync(0xffffffffu, aborted(sh))) break;
+        }
+        if (!locate(u)) {
+          // none left, once the units still running (the last two) need no second
+          // pass; who gives up here has set the abort word and the error
+          const uint64_t limit = kWaitLimitNs + (static_cast<uint64_t>(nb_last) + nb_before) * kBlockLimitNs;
+          if (!__all_sync(0xffffffffu, await_count(smem_u32(&sh.units_done), kSoftmaxWarps * k, &sh.abort, p.err,
+                                                   HPD_DEVERR_TIMEOUT, limit)))
+            break;
+          redo = take_redo();
+          if (!redo) break;
+          continue;
+        }
+        int lo = 0, hi = min(kGroup, p.S - g0);  // the last sequence that starts at or before the unit
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (sh.g_units[mid] <= u - before) lo = mid; else hi = mid;
+        }
+        const int c0 = sh.g_cu[lo], n = max(0, sh.g_cu[lo + 1] - c0), len = sh.g_len[lo], nsplit = sh.g_split[lo];
+        const int full = p.full_len ? min(max(p.full_len[g0 + lo], 0), len) : 0;
+        int idx = u - before - sh.g_units[lo];
+        const int us = p.div_Hkv(idx), g = idx - us * p.H_kv;
+        const int ut = nsplit > 1 ? us / nsplit : us, split = us - ut * nsplit;
+        const int tile = (n + TT - 1) / TT - 1 - ut;
+        const int i0 = tile * TT, ntok = min(TT, n - i0), nrows = ntok * G;
+        const int lim0 = len - n + i0 + 1;
+        const int kmax = min(max(max(lim0 + ntok - 1, full), 0), len);
+        const int N = ceil_div_i(kmax, kBlk);
+        const int blk_lo = nsplit > 1 ? static_cast<int>(static_cast<long long>(split) * N / nsplit) : 0;
+        const int blk_hi = nsplit > 1 ? static_cast<int>(static_cast<long long>(split + 1) * N / nsplit) : N;
+        if (p.s_max > 1 && g == 0 && split == 0)
+          for (int r = lane; r < ntok; r += 32) p.row_split[c0 + i0 + r] = nsplit;
+        if (blk_hi <= blk_lo) {
+          // no key: zero output, or an empty partial
+#pragma unroll 1
+          for (int r = lane; r < nrows; r += 32) {
+            const int rt = p.div_G(r);
+            const size_t pair = static_cast<size_t>(c0 + i0 + rt) * p.H_q + g * G + r - rt * G;
+            if (nsplit == 1) {
+              uint4 *o = reinterpret_cast<uint4 *>(p.out + pair * D);
+#pragma unroll 1
+              for (int c = 0; c < D / 8; ++c) o[c] = make_uint4(0u, 0u, 0u, 0u);
+              if (p.lse) p.lse[pair] = NEG_INF;
+            } else {
+              p.l_part[static_cast<size_t>(split) * p.T * p.H_q + pair] = NEG_INF;
+            }
+          }
+          continue;
+        }
+        if (lane == 0) {
+          M.valid = 1;
+          M.g = g;
+          M.split = split;
+          M.nsplit = nsplit;
+          M.seq = g0 + lo;
+          M.tok0 = c0 + i0;
+          M.nrows = nrows;
+          M.lim0 = lim0;
+          M.full = full;
+          M.L = len;
+          M.pages = ceil_div_i(kmax, kPage);
+          M.blk_lo = blk_lo;
+          M.n_blocks = blk_hi - blk_lo;
+          M.exact = again;
+          sh.unit_id[k & 31] = u;
+        }
+        nb_before = nb_last;
+        nb_last = blk_hi - blk_lo;
+        have = true;
+        break;
+      }
+      if (!have && lane == 0) M.valid = 0;
+      __syncwarp();
+      __threadfence_block();
+      if (lane == 0) mbar_arrive(bar(sh.meta_full[slot]));
+      if (!have) break;
+    }
+  } else if (warp == 0 || warp == kVWarp) {
+    // ------------------------------------------------------- producers --
+    const bool is_k = warp == 0;
+    if (lane == 0) {
+      prefetch_tmap(&tm_q);
+      prefetch_tmap(&tm_k);
+      prefetch_tmap(&tm_v);
+      prefetch_tmap(&tm_k8);
+      prefetch_tmap(&tm_v8);
+    }
+    __syncwarp();
+    uint64_t *const full = is_k ? sh.k_full : sh.v_full, *const empty = is_k ? sh.k_empty : sh.v_empty;
+    const CUtensorMap *const page_map = is_k ? &tm_k : &tm_v, *const run_map = is_k ? &tm_k8 : &tm_v8;
+    const uint32_t ring = sbase + (is_k ? L::kK : L::kV);
+    int issued = 0;  // ring entries
+    bool ok = true;
+    for (int k = 0; ok; ++k) {
+      const int slot = k & 1;
+      if (!(ok = wait_bar(sh.meta_full[slot], (k >> 1) & 1))) break;
+      const UnitMeta M = sh.meta[slot];
+      __syncwarp();
+      if (lane == 0 && M.valid) mbar_arrive(bar(sh.meta_empty[slot]));
+      if (!M.valid) break;
+      const int32_t *const row = p.page_table + static_cast<size_t>(M.seq) * p.max_pages;
+      // page i of a block in lane i < 8, looked up a block ahead; pages past the
+      // last one that the tile sees lie outside the map
+      auto look_up = [&](int j) {
+        const int i = (M.blk_lo + j) * kPagesPerBlock + lane;
+        return lane < kPagesPerBlock && j < M.n_blocks && i < M.pages ? row[i] : p.num_pages;
+      };
+      int pg = look_up(0);
+#pragma unroll 1
+      for (int j = is_k ? -1 : 0; j < M.n_blocks; ++j) {
+        const int e = issued, s = e % kStages;
+        if (e >= kStages && !(ok = wait_bar(empty[s], ((e / kStages) - 1) & 1))) break;
+        ++issued;
+        const uint32_t dst = ring + s * L::kTileBytes, b = bar(full[s]);
+        if (j < 0) {  // the unit's Q tile
+          mbar_arrive_expect_tx_elect(b, L::kChunks * TT * G * 128);
+#pragma unroll 1
+          for (int c = 0; c < L::kChunks; ++c)
+            tma_load_3d_elect(dst + c * L::kChunkBytes, &tm_q, b, c * 64, M.g * G, M.tok0);
+          continue;
+        }
+        const int next = look_up(j + 1);
+        if (static_cast<unsigned>(pg) > static_cast<unsigned>(p.num_pages) ||
+            (pg == p.num_pages && lane < kPagesPerBlock &&
+             (M.blk_lo + j) * kPagesPerBlock + lane < M.pages)) {
+          flag_error(p.err, HPD_DEVERR_PAGE_ID);
+          pg = 0;
+        }
+        mbar_arrive_expect_tx_elect(b, L::kTileBytes);
+        const int right = __shfl_down_sync(0xffffffffu, pg, 1);
+        const unsigned run = __ballot_sync(0xffffffffu, lane < kPagesPerBlock - 1 && right == pg + 1);
+        const bool one = p.num_pages >= kPagesPerBlock && (run & 0x7fu) == 0x7fu;
+        if (lane < (one ? 1 : kPagesPerBlock))
+          tma_load_5d(dst + lane * L::kPageBytes, one ? run_map : page_map, b, 0, 0, 0, 2 * pg, M.g);
+        __syncwarp();
+        pg = next;
+      }
+    }
+    if (!ok && lane == 0) set_abort(sh, p.err);
+    // no exit while a copy into this CTA's shared memory is in flight
+    for (int e = max(0, issued - kStages); e < issued; ++e) mbar_wait(bar(full[e % kStages]), (e / kStages) & 1);
+  } else if (warp == 1) {
+    // ---------------------------------------------------- Q K^T issuer --
+    constexpr uint32_t idesc_qk = idesc_bf16_f32(kRows, kBlk, false);
+    const uint64_t dq0 = smem_desc_sw128(sbase + L::kK, 16, 1024);
+    const uint64_t dk0 = smem_desc_sw128(sbase + L::kK, 16, L::kGroupBytes);
+    const bool issuer = elect_one();
+    uint32_t sk = 0, pk = 0;  // K ring: stage, phase
+    int jg = 0;               // blocks issued
+    bool ok = true;
+    for (int k = 0; ok; ++k) {
+      const int slot = k & 1;
+      if (!(ok = wait_bar(sh.meta_full[slot], (k >> 1) & 1))) break;
+      const bool valid = sh.meta[slot].valid != 0;
+      const int nb = sh.meta[slot].n_blocks;
+      __syncwarp();
+      if (!valid) break;
+      if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
+      // entry -1 of the unit: its Q, copied into TMEM slot k & 1 (in order with the
+      // MMAs: unit k - 2's Q K^T are done with the slot)
+      for (int j = -1; j < nb; ++j) {
+        if (!(ok = wait_bar(sh.k_full[sk], pk))) break;
+        // the S buffer is free once P V of the block before last has read P
+        if (j >= 0 && jg >= 2 && !(ok = wait_bar(sh.s_free[jg & 1], ((jg >> 1) - 1) & 1))) break;
+        tc_fence_after();
+        if (issuer) {
+          const uint32_t off = (sk * L::kTileBytes) >> 4;
+          if (j < 0) {
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              tmem_cp_128x256b(tmem + L::col_q(slot) + kk * 8,
+                               dq0 + off + (((kk >> 2) * L::kChunkBytes + (kk & 3) * 32) >> 4));
+          } else {
+            const uint32_t col = tmem + L::col_s(jg & 1);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              mma_ts_one(col, tmem + L::col_q(slot) + kk * 8, dk0 + off + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4),
+                         idesc_qk, kk > 0);
+            mma_commit_one(bar(sh.s_full[jg & 1]));
+          }
+          mma_commit_one(bar(sh.k_empty[sk]));
+        }
+        __syncwarp();
+        if (++sk == kStages) {
+          sk = 0;
+          pk ^= 1u;
+        }
+        jg += j >= 0;
+      }
+    }
+    if (!ok && lane == 0) set_abort(sh, p.err);
+  } else if (warp == kPvWarp) {
+    // ------------------------------------------------------ P V issuer --
+    constexpr uint32_t idesc_pv = idesc_bf16_f32(kRows, D, true);
+    const uint64_t dv0 = smem_desc_sw128(sbase + L::kV, 1024, L::kGroupBytes);
+    const bool issuer = elect_one();
+    uint32_t sv = 0, pv = 0;  // V ring: stage, phase
+    int jg = 0;               // blocks issued
+    bool ok = true;
+    for (int k = 0; ok; ++k) {
+      const int slot = k & 1;
+      if (!(ok = wait_bar(sh.meta_full[slot], (k >> 1) & 1))) break;
+      const bool valid = sh.meta[slot].valid != 0;
+      const int nb = sh.meta[slot].n_blocks, len = sh.meta[slot].L;
+      // the block with rows behind the sequence's end in its last page
+      const int j_tail = len % kPage ? len / kBlk - sh.meta[slot].blk_lo : -1;
+      __syncwarp();
+      if (!valid) break;
+      if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
+      // O last held the unit before, whose epilogue must have read it
+      if (k >= 1 && !(ok = wait_bar(sh.o_empty, (k - 1) & 1))) break;
+      for (int j = 0; j < nb; ++j) {
+        if (!(ok = wait_bar(sh.v_full[sv], pv))) break;
+        if (j == j_tail) {  // a weight of zero would not keep out what is not finite there
+          const uint32_t v0 = sbase + L::kV + sv * L::kTileBytes;
+          for (int i = (len % kBlk) * (L::kChunks * 8) + lane; i < (len % kBlk / kPage + 1) * kPage * (L::kChunks * 8);
+               i += 32) {
+            const int r = i / (L::kChunks * 8), c = i % (L::kChunks * 8);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v0 + (r >> 3) * L::kGroupBytes +
+                                                                         (c >> 3) * 1024 + (r & 7) * 128 + (c & 7) * 16),
+                         "r"(0)
+                         : "memory");
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+        // O (+)= P V: 16 keys per MMA, P in the S buffer (half h of the keys at
+        // column 64 h), the first 32 keys of both halves and then the second
+        const uint64_t vd = dv0 + ((sv * L::kTileBytes) >> 4);
+        const uint32_t col = tmem + L::col_s(jg & 1);
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          if (!(ok = wait_bar(sh.p_full[jg & 1][part], (jg >> 1) & 1))) break;
+          tc_fence_after();
+          if (issuer) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int kk = (i >> 1) * 4 + part * 2 + (i & 1);
+              mma_ts_one(tmem + L::kColO, col + kk * 8 + (kk >= 4 ? 32 : 0), vd + kk * ((2 * L::kGroupBytes) >> 4),
+                         idesc_pv, (j > 0 || part > 0 || i > 0) ? 1u : 0u);
+            }
+          }
+          __syncwarp();
+        }
+        if (!ok) break;
+        if (issuer) {
+          mma_commit_one(bar(sh.s_free[jg & 1]));
+          mma_commit_one(bar(sh.v_empty[sv]));
+          if (j == nb - 1) mma_commit_one(bar(sh.o_full));
+        }
+        __syncwarp();
+        if (++sv == kStages) {
+          sv = 0;
+          pv ^= 1u;
+        }
+        ++jg;
+      }
+    }
+    if (!ok && lane == 0) set_abort(sh, p.err);
+  } else {
+    // --------------------------------------------------------- softmax --
+    const int h = (warp - 2) >> 2;        // column half
+    const int quad = warp & 3;            // TMEM lane quadrant this warp may access
+    const int r_in = quad * 32 + lane;    // row within the tile
+    const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    const float sl2 = p.scale_log2;
+    const uint32_t o_col = L::kColO + h * (D / 2);
+    int jbase = 0;
+    bool ok = true;
+    for (int k = 0; ok; ++k) {
+      const int slot = k & 1;
+      if (!(ok = wait_bar(sh.meta_full[slot], (k >> 1) & 1))) break;
+      const UnitMeta M = sh.meta[slot];
+      __syncwarp();
+      if (!M.valid) break;
+      if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
+      const bool valid = r_in < M.nrows, idle = quad * 32 >= M.nrows;
+      const int rt = p.div_G(r_in), token = M.tok0 + rt, head = M.g * G + r_in - rt * G;
+      // (rows that are no query count as seeing everything, so that their warp
+      // needs no masks for them; their results are not stored)
+      const int lim = valid ? min(max(M.lim0 + rt, M.full), M.L) : 1 << 30;
+      const int n_plain = sl2 > 0.f ? max(__reduce_min_sync(0xffffffffu, lim), 0) / kBlk : 0;
+      const size_t pair = static_cast<size_t>(token) * p.H_q + head;
+      float m_run = NEG_INF, l_half = 0.f;
+      bool inside = true;  // the scores stay in the window of their base
+      bool based = false;  // every row of the warp has its base
+      auto await_s = [&](int jg) {
+        if (!wait_bar(sh.s_full[jg & 1], (jg >> 1) & 1)) return false;
+        tc_fence_after();
+        return true;
+      };
+      for (int j = 0; j < M.n_blocks; ++j) {
+        const int jg = jbase + j, si = jg & 1;
+        auto publish = [&](int part) {
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(sh.p_full[si][part]));
+        };
+        if (!(ok = await_s(jg))) break;
+        if (idle) {  // whatever is there instead of P reaches only rows that are not stored
+          publish(0);
+          publish(1);
+          continue;
+        }
+        const uint32_t s_addr = t_lane + L::col_s(si) + h * 64;
+        const int jb = M.blk_lo + j;
+        if (based && !M.exact && jb < n_plain) {  // nothing to decide
+          inside &= softmax_based(s_addr, true, 64, sl2, m_run, l_half, publish);
+          continue;
+        }
+        const int hi = min(lim - jb * kBlk, kBlk);
+        const bool find_max =
+            M.exact || (!based && __any_sync(0xffffffffu, valid && m_run == NEG_INF && hi > 0));
+        if (!find_max) {
+          inside &= softmax_based(s_addr, false, hi - h * 64, sl2, m_run, l_half, publish);
+          continue;
+        }
+        const int par = jg & 1;
+        bool xok = true;
+        auto xchg = [&](float mx) {
+          sh.xmax[h][par][r_in] = mx;
+          publish_seq(&sh.xseq[0][h][quad], jg + 1);
+          xok = await_seq(&sh.xseq[0][h ^ 1][quad], jg + 1, sh);
+          return fmaxf(mx, sh.xmax[h ^ 1][par][r_in]);
+        };
+        const float alpha =
+            tc::softmax_half_max<false>(s_addr, -h * 64, hi - h * 64, sl2, m_run, l_half, xchg);
+        if (!(ok = __all_sync(0xffffffffu, xok))) break;
+        based = __all_sync(0xffffffffu, !valid || m_run != NEG_INF);
+        // Before O may be rescaled, P V of block jg - 1 must have landed.  The
+        // test is exact: P V (jg + 1) of the same buffer needs this block's first.
+        if (__any_sync(0xffffffffu, j > 0 && alpha != 1.f)) {
+          if (!(ok = wait_bar(sh.s_free[si ^ 1], ((jg - 1) >> 1) & 1))) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D / 2; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(t_lane + o_col + c, o);
+            tmem_ld_wait32(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tmem_st32(t_lane + o_col + c, o);
+          }
+        }
+        publish(0);
+        publish(1);
+      }
+      if (!ok) break;
+      // ---------------------------------------------------- epilogue --
+      bool redo = false, mend = false;
+      if (!idle) {
+        // row sum over both halves (two buffers in turn: a half may be a unit ahead)
+        sh.xsum[k & 1][h][r_in] = l_half;
+        publish_seq(&sh.xseq[1][h][quad], k + 1);
+        if (!(ok = __all_sync(0xffffffffu, await_seq(&sh.xseq[1][h ^ 1][quad], k + 1, sh)))) break;
+      } else if (lane == 0) {  // (the count goes on for the units that this quadrant has rows of)
+        asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.xseq[1][h][quad])), "r"(k + 1)
+                     : "memory");
+      }
+      if (!(ok = wait_bar(sh.o_full, k & 1))) break;
+      tc_fence_after();
+      const size_t slot_pair = static_cast<size_t>(M.split) * p.T * p.H_q + pair;
+      if (!idle) {
+        const float l_run = l_half + sh.xsum[k & 1][h ^ 1][r_in];
+        // (a sum that is NaN stays one)
+        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+        const float lse = l_run == 0.f ? NEG_INF : l_run > 0.f ? lse_of(m_run, l_run) : l_run;
+        float2 finite = make_float2(0.f, 0.f);  // NaN once an infinity or NaN is added
+#pragma unroll 1
+        for (int c = 0; c < D / 2; c += 32) {
+          uint32_t o[32];
+          tmem_ld32(t_lane + o_col + c, o);
+          tmem_ld_wait32(o);
+          if (!valid) continue;
+#pragma unroll
+          for (int e = 0; e < 32; e += 2)
+            finite = __ffma2_rn(make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), make_float2(0.f, 0.f),
+                                finite);
+          const int dc = h * (D / 2) + c;  // output column
+          if (M.nsplit == 1) {
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              w[e] = pack_bf16x2(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+            __nv_bfloat16 *dst = p.out + pair * D + dc;
+            if (p.out_align32) {
+              st_global_v8(dst, w);
+              st_global_v8(dst + 16, w + 8);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 16; e += 4)
+                reinterpret_cast<uint4 *>(dst)[e / 4] = make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]);
+            }
+          } else {
+            float *dst = p.o_part + slot_pair * D + dc;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) st_global_v8(dst + e, o + e);
+          }
+        }
+        if (valid && h == 0) {
+          if (M.nsplit == 1) {
+            if (p.lse) p.lse[pair] = lse;
+          } else {
+            p.l_part[slot_pair] = lse;
+          }
+        }
+        const bool odd = valid && !(finite.x == 0.f && finite.y == 0.f);
+        redo = __any_sync(0xffffffffu, !M.exact && (odd || (valid && !inside)));
+        // a key that the tile sees and this row does not
+        mend = M.exact && odd && lim < M.pages * kPage && lim < M.L && l_run == l_run;
+      }
+      // O may be overwritten by the next unit once every warp has read it
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(bar(sh.o_empty));
+        if (redo) atomicOr(&sh.redo, 1u << (k & 31));
+        __threadfence_block();
+        atomicAdd(&sh.units_done, 1);
+      }
+      for (unsigned rows = __ballot_sync(0xffffffffu, mend); rows; rows &= rows - 1) {
+        const int src = __ffs(rows) - 1;
+        const int row_token = __shfl_sync(0xffffffffu, token, src), row_head = __shfl_sync(0xffffffffu, head, src);
+        const int row_lim = __shfl_sync(0xffffffffu, lim, src);
+        const size_t at = static_cast<size_t>(row_token) * p.H_q + row_head;
+        const int k0 = M.blk_lo * kBlk, k1 = min(row_lim, (M.blk_lo + M.n_blocks) * kBlk);
+        one_row<D>(p, M.seq, row_token, row_head, k0, k1, h,
+                   M.nsplit == 1 ? nullptr : p.o_part + (static_cast<size_t>(M.split) * p.T * p.H_q + at) * D,
+                   p.out + at * D);
+      }
+      jbase += M.n_blocks;
+    }
+    if (!ok && lane == 0) set_abort(sh, p.err);
+  }
+
+  // ------------------------------------------------------------ teardown --
+  if (warp == 1 || warp == kPvWarp) {
+    uint64_t &done = sh.mma_done[warp == 1 ? 0 : 1];
+    mma_commit(bar(done));
+    mbar_wait(bar(done), 0);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+  // the last CTA to finish resets the unit counters for the next call
+  if (tid == 0) {
+    __threadfence();
+    if (atomicAdd(p.unit_ctr + 1, 1) == static_cast<int>(gridDim.x) - 1) {
+      atomicExch(p.unit_ctr, 0);
+      atomicExch(p.unit_ctr + 1, 0);
+    }
+  }
+}
+
+// Joins the splits of the rows that have several: one warp a (row, head).
+//   lse = log sum_s exp(lse_s),  out = sum_s exp(lse_s - lse) out_s
+constexpr int kMergeWarps = 4;
+template <int D>
+__global__ void __launch_bounds__(32 * kMergeWarps) chunk_merge_kernel(const ChunkParams p) {
+  const int lane = threadIdx.x & 31;
+  const size_t pair = static_cast<size_t>(blockIdx.x) * kMergeWarps + (threadIdx.x >> 5);
+  const size_t pairs = static_cast<size_t>(p.T) * p.H_q;
+  pdl_wait();
+  pdl_trigger();
+  if (pair >= pairs) return;
+  const int t = static_cast<int>(pair / p.H_q);
+  const int n = min(p.row_split[t], p.s_max);
+  if (t >= p.chunk_cu[p.S] || n <= 1) return;
+  const float NEG_INF = -__int_as_float(0x7f800000);
+  const float l = lane < n ? p.l_part[lane * pairs + pair] : NEG_INF;
+  float m = l;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float base = m == NEG_INF ? 0.f : m;
+  float w = exp2f((l - base) * kLog2e), sum = w;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  constexpr int kV = D / 32;  // values of a lane
+  float acc[kV];
+#pragma unroll
+  for (int c = 0; c < kV; ++c) acc[c] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const float ws = __shfl_sync(0xffffffffu, w, s);
+    if (ws == 0.f) continue;  // (an empty partial is not written)
+    const float *src = p.o_part + (s * pairs + pair) * D + lane * kV;
+#pragma unroll
+    for (int c = 0; c < kV; ++c) acc[c] = fmaf(ws, src[c], acc[c]);
+  }
+  uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + pair * D) + lane * (kV / 2);
+#pragma unroll
+  for (int c = 0; c < kV; c += 2) dst[c / 2] = pack_bf16x2(acc[c] * inv, acc[c + 1] * inv);
+  if (lane == 0 && p.lse) p.lse[pair] = sum == 0.f ? NEG_INF : m + logf(sum);
+}
+
+// ------------------------------------------------------------------ host --
 
 hpd_status check_scalars(const hpd_chunk_attn_args *a) {
   if (!a) return HPD_ERR_INVALID_ARG;
@@ -102,7 +943,102 @@ hpd_status check_scalars(const hpd_chunk_attn_args *a) {
   if (a->H_q / a->H_kv > 16 || (a->D != 64 && a->D != 128)) return HPD_ERR_UNSUPPORTED;
   if (a->q_stride != 0 && a->q_stride < static_cast<int64_t>(a->H_q) * a->D) return HPD_ERR_INVALID_ARG;
   if (static_cast<long long>(a->max_pages) * kPage >= (1LL << 30)) return HPD_ERR_UNSUPPORTED;
+  if (static_cast<long long>(a->num_pages) * kPage >= (1LL << 31)) return HPD_ERR_UNSUPPORTED;
+  // units (at most a row and head each, kMaxSplits times) stay below kNoUnit
+  if (static_cast<long long>(a->T) * a->H_q >= (1LL << 30) / kMaxSplits) return HPD_ERR_UNSUPPORTED;
   return HPD_OK;
+}
+
+constexpr int kPlanSms = 152;  // SMs the split plan assumes (GB300)
+constexpr size_t kAlign = 256;
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+struct ChunkPlan {
+  int s_max;
+  long long units;  // upper bound
+  size_t off_opart, off_lpart, off_rows, bytes;
+};
+
+// Splits are allowed where the call's tiles are too few for the SMs.  Only host
+// scalars enter (the kernel then splits by the true lengths): the time of the
+// longest sequences' tiles, in blocks, unsplit against the best number of
+// splits, a unit's start and end counted as 3 blocks, the merge as 6.
+ChunkPlan make_plan(const hpd_chunk_attn_args *a) {
+  ChunkPlan pl{};
+  const int G = a->H_q / a->H_kv, TT = kRows / G;
+  const long long seqs = std::min(a->S, a->T);
+  const long long tiles = std::max<long long>(seqs, (a->T + TT - 1) / TT) * a->H_kv;
+  const int cap = a->max_pages * kPage;
+  const int longest = a->max_seq_len > 0 ? std::min(a->max_seq_len, cap) : cap;
+  const int N = std::max(1, (longest + kBlk - 1) / kBlk);
+  auto time = [&](int sp) {
+    return (tiles * sp + kPlanSms - 1) / kPlanSms * ((N + sp - 1) / sp + 3) + (sp > 1 ? 6 : 0);
+  };
+  int best = 1;
+  if (a->S <= kGroup)
+    for (int sp = 2; sp <= std::min(N, kMaxSplits); ++sp)
+      if (time(sp) < time(best)) best = sp;
+  pl.s_max = best == 1 ? 1 : a->S == 1 ? best : std::min(kMaxSplits, 2 * best);
+  const long long tiles_max = (a->T + seqs * (TT - 1)) / TT;
+  pl.units = tiles_max * a->H_kv * pl.s_max;
+  const size_t pairs = static_cast<size_t>(a->T) * a->H_q;
+  pl.off_opart = kAlign;
+  pl.off_lpart = pl.off_rows = pl.bytes = kAlign;
+  if (pl.s_max > 1) {
+    pl.off_lpart = align_up(pl.off_opart + pl.s_max * pairs * a->D * sizeof(float));
+    pl.off_rows = align_up(pl.off_lpart + pl.s_max * pairs * sizeof(float));
+    pl.bytes = align_up(pl.off_rows + static_cast<size_t>(a->T) * sizeof(int));
+  }
+  return pl;
+}
+
+cudaError_t make_q_map(CUtensorMap *map, const ChunkParams &p, int D) {
+  auto fn = tc::encode_fn();
+  if (!fn) return cudaErrorNotSupported;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(p.H_q),
+                              static_cast<cuuint64_t>(p.T)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(D) * 2, static_cast<cuuint64_t>(p.q_stride) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(p.G), static_cast<cuuint32_t>(kRows / p.G)};
+  const cuuint32_t es[3] = {1, 1, 1};
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16 *>(p.q), dims, strides,
+                        box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int D>
+cudaError_t launch(const ChunkParams &p, long long units, cudaStream_t s) {
+  using L = Layout<D>;
+  static_assert(L::kDynSmem + sizeof(Shared) <= 227 * 1024, "shared memory");
+  CUtensorMap tk, tv, tk8, tv8, tq;
+  const int run = std::min(kPagesPerBlock, p.num_pages);  // box never longer than the pool
+  cudaError_t e = make_q_map(&tq, p, D);
+  if (e == cudaSuccess) e = tc::make_page_map(&tk, p.k_cache, D, p.H_kv, p.num_pages);
+  if (e == cudaSuccess) e = tc::make_page_map(&tv, p.v_cache, D, p.H_kv, p.num_pages);
+  if (e == cudaSuccess) e = tc::make_page_map(&tk8, p.k_cache, D, p.H_kv, p.num_pages, run);
+  if (e == cudaSuccess) e = tc::make_page_map(&tv8, p.v_cache, D, p.H_kv, p.num_pages, run);
+  int dev = 0;
+  if (e == cudaSuccess) e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  static std::atomic<uint64_t> configured{0};
+  static std::atomic<int> sms[64];
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(configured.load(std::memory_order_acquire) & bit)) {
+    int n = 0;
+    e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(chunk_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               static_cast<int>(L::kDynSmem));
+    if (e != cudaSuccess) return e;
+    sms[dev & 63].store(n);
+    configured.fetch_or(bit, std::memory_order_acq_rel);
+  }
+  const unsigned grid = static_cast<unsigned>(std::min<long long>(units, sms[dev & 63].load()));
+  e = launch_kernel(true, chunk_attn_kernel<D>, dim3(grid), dim3(kThreads), L::kDynSmem, s, tk, tv, tk8, tv8, tq, p);
+  if (e != cudaSuccess || p.s_max == 1) return e;
+  const size_t pairs = static_cast<size_t>(p.T) * p.H_q;
+  return launch_kernel(true, chunk_merge_kernel<D>, dim3(static_cast<unsigned>((pairs + kMergeWarps - 1) / kMergeWarps)),
+                       dim3(32 * kMergeWarps), 0, s, p);
 }
 
 }  // namespace
@@ -111,7 +1047,7 @@ hpd_status check_scalars(const hpd_chunk_attn_args *a) {
 extern "C" {
 
 size_t hpd_chunk_attn_workspace_size(const hpd_chunk_attn_args *a) {
-  return hpd::check_scalars(a) == HPD_OK ? 256 : 0;
+  return hpd::check_scalars(a) == HPD_OK ? hpd::make_plan(a).bytes : 0;
 }
 
 hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *a, hpd_stream_t stream) {
@@ -126,10 +1062,12 @@ hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *a, hpd_stream_t stream) {
                         static_cast<const void *>(a->full_len), static_cast<const void *>(a->page_table),
                         static_cast<const void *>(a->lse)})
     if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return HPD_ERR_INVALID_ARG;
-  if (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 255u) != 0 ||
-      a->workspace_bytes < hpd_chunk_attn_workspace_size(a))
+  const ChunkPlan pl = make_plan(a);
+  if (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & (kAlign - 1)) != 0 ||
+      a->workspace_bytes < pl.bytes)
     return HPD_ERR_WORKSPACE;
-  ChunkArgs k{};
+  uint8_t *ws = static_cast<uint8_t *>(a->workspace);
+  ChunkParams k{};
   k.q = static_cast<const __nv_bfloat16 *>(a->q);
   k.q_stride = a->q_stride ? a->q_stride : static_cast<long long>(a->H_q) * a->D;
   k.chunk_cu = a->chunk_cu;
@@ -147,14 +1085,18 @@ hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *a, hpd_stream_t stream) {
   k.max_pages = a->max_pages;
   k.scale_log2 = (a->scale != 0.f ? a->scale : 1.0f / std::sqrt(static_cast<float>(a->D))) * kLog2e;
   k.out = static_cast<__nv_bfloat16 *>(a->out);
+  k.out_align32 = (reinterpret_cast<uintptr_t>(a->out) & 31u) == 0;
   k.lse = a->lse;
-  k.err = static_cast<uint32_t *>(a->workspace);
-  const long long ctas = (static_cast<long long>(a->T) * a->H_q + kWarps - 1) / kWarps;
-  if (ctas > INT32_MAX) return HPD_ERR_UNSUPPORTED;
+  k.err = reinterpret_cast<uint32_t *>(ws);
+  k.unit_ctr = reinterpret_cast<int *>(ws + 8);
+  k.s_max = pl.s_max;
+  k.o_part = reinterpret_cast<float *>(ws + pl.off_opart);
+  k.l_part = reinterpret_cast<float *>(ws + pl.off_lpart);
+  k.row_split = reinterpret_cast<int *>(ws + pl.off_rows);
+  k.div_G.set(k.G);
+  k.div_Hkv.set(k.H_kv);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const dim3 grid(static_cast<unsigned>(ctas)), block(32 * kWarps);
-  const cudaError_t e = a->D == 64 ? launch_kernel(true, chunk_attn_simple_kernel<64>, grid, block, 0, s, k)
-                                   : launch_kernel(true, chunk_attn_simple_kernel<128>, grid, block, 0, s, k);
+  const cudaError_t e = a->D == 64 ? launch<64>(k, pl.units, s) : launch<128>(k, pl.units, s);
   return e == cudaSuccess ? HPD_OK : record_cuda_error(e);
 }
 
