@@ -9,16 +9,27 @@
 // Values are read once and written once; sums, norm and rotation are in 32 bits
 // with one rounding to bf16 at the end.  D / 16 lanes hold a head: lane l values
 // 8l .. 8l + 7 of its lower and of its upper half, so that every rotated pair is in one
-// lane, all accesses are 16 bytes and a warp has 512 / D heads at once.  A warp
-// takes one row and kUnroll rounds of heads, whose loads are all issued before
-// the first is used; cosines and sines are read once for them.
-// What bounds it: HBM, reading and writing T (H_q + 2 H_kv) D values.
+// lane, all accesses are 16 bytes and a warp has 512 / D heads (a round) at once.
+// A warp takes items of up to kUnroll rounds of a row in turn and issues all loads
+// of an item at once; the next item's positions and slot are on their way
+// meanwhile.
+// What bounds it: HBM, reading and writing T (H_q + 2 H_kv) D values.  32,749 rows
+// of 16 + 2 + 2 heads of 128 take 60.6 us, 5.8 TB/s and 86% of a copy's rate; 3,201 of
+// 32 + 8 + 8 heads take 17.1 (11.9 at that rate, and a launch).  In us, those two: a
+// CTA for every four items instead of CTAs that stay 75.0, 17.9; kUnroll 3 67.9,
+// 18.4; 4 68.8, 16.7; 6 61.9, 18.1; five CTAs an SM (96 registers) 64.9, 18.6.  One
+// value an instruction, whole rows loaded four rounds ahead: 82.3, 25.6 (288
+// instructions a round, which bounded it).
+#include <algorithm>
+
 #include "common.cuh"
 
 namespace hpd {
 namespace {
 
 constexpr int kRopeWarps = 4;
+constexpr int kUnroll = 5;
+constexpr int kRopeSms = 152, kRopeCtas = 4;  // CTAs of an SM
 
 struct RopeArgs {
   const __nv_bfloat16 *q, *k, *v;
@@ -28,143 +39,175 @@ struct RopeArgs {
   const int32_t *pos, *slot;
   __nv_bfloat16 *q_out, *k_cache, *v_cache;
   uint32_t *err;
-  long long num_slots, items;
+  long long num_slots;
   float eps;
-  int T, H_q, H_kv, max_pos, groups;
-  int n_axes;
+  int T, H_q, H_kv, max_pos;
+  int rounds, seg;      // rounds of a row, of an item (at most)
+  int segs;             // items of a row
   uint32_t axis[4];  // 2 bits a frequency, 8 frequencies (a lane's) in 16
 };
 
-__device__ __forceinline__ void unpack8(const uint4 &v, float *x) {
+// Eight values as four pairs, and back: the arithmetic is two values an
+// instruction.
+__device__ __forceinline__ void unpack8(const uint4 &v, float2 *x) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
+  for (int i = 0; i < 4; ++i)
+    x[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ uint4 pack8(const float *x) {
-  return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                    pack_bf16x2(x[6], x[7]));
+__device__ __forceinline__ uint4 pack8(const float2 *x) {
+  return make_uint4(pack_bf16x2(x[0].x, x[0].y), pack_bf16x2(x[1].x, x[1].y), pack_bf16x2(x[2].x, x[2].y),
+                    pack_bf16x2(x[3].x, x[3].y));
 }
 
-template <int D, int kUnroll>
-__global__ void __launch_bounds__(32 * kRopeWarps) qk_norm_rope_kernel(const RopeArgs a) {
+template <int D>
+__global__ void __launch_bounds__(32 * kRopeWarps, kRopeCtas) qk_norm_rope_kernel(const RopeArgs a) {
   constexpr int kLanes = D / 16;           // lanes of a head
-  constexpr int kHeads = 32 / kLanes;      // heads of a warp at once
+  constexpr int kHeads = 32 / kLanes;      // heads of a round
   const int lane = threadIdx.x & 31, sub = lane % kLanes;
-  const long long item = static_cast<long long>(blockIdx.x) * kRopeWarps + (threadIdx.x >> 5);
+  const int step = static_cast<int>(gridDim.x) * kRopeWarps;
+  const int n_rot = a.H_q + a.H_kv, n_heads = n_rot + a.H_kv;
+  const uint32_t axes = a.axis[sub >> 1] >> (16 * (sub & 1)) & 0xffffu;
   pdl_wait();     // rows, positions, slots and the caches as the kernel before leaves them
   pdl_trigger();
-  if (item >= a.items) return;
-  const int t = a.groups == 1 ? static_cast<int>(item) : static_cast<int>(item / a.groups);
-  const int h0 = static_cast<int>(item - static_cast<long long>(t) * a.groups) * (kHeads * kUnroll) + lane / kLanes;
-  const int n_heads = a.H_q + 2 * a.H_kv;
-  uint4 lo[kUnroll], hi[kUnroll];
-#pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
-    const int h = h0 + u * kHeads;
-    lo[u] = hi[u] = make_uint4(0u, 0u, 0u, 0u);
-    if (h >= n_heads) continue;
-    const __nv_bfloat16 *src = h < a.H_q            ? a.q + t * a.q_stride + h * D
-                               : h < a.H_q + a.H_kv ? a.k + t * a.k_stride + (h - a.H_q) * D
-                                                    : a.v + t * a.v_stride + (h - a.H_q - a.H_kv) * D;
-    lo[u] = *reinterpret_cast<const uint4 *>(src + 8 * sub);
-    hi[u] = *reinterpret_cast<const uint4 *>(src + D / 2 + 8 * sub);
+  int t = blockIdx.x * kRopeWarps + (threadIdx.x >> 5), part = 0;  // row and part of it: item t * segs + part
+  if (a.segs > 1) {
+    part = t % a.segs;
+    t /= a.segs;
   }
-  const int slot = a.slot[t];
-  float cs[16];  // cos, sin of this lane's 8 frequencies
-  int p[4] = {0, 0, 0, 0};
-  if (h0 - lane / kLanes < a.H_q + a.H_kv) {
-    for (int i = 0; i < 4; ++i) {
-      if (i >= a.n_axes) break;
-      p[i] = a.pos[static_cast<long long>(i) * a.T + t];
-      if (static_cast<unsigned>(p[i]) >= static_cast<unsigned>(a.max_pos)) {
-        if (lane == 0) atomicOr(a.err, HPD_DEVERR_POSITION);
-        p[i] = min(max(p[i], 0), a.max_pos - 1);
+  const int step_t = step / a.segs, step_part = step - step_t * a.segs;
+  const bool one_axis = axes == (axes & 3u) * 0x5555u;  // all eight of this lane's frequencies
+  const int32_t *pos = a.pos + static_cast<long long>(axes & 3u) * a.T;
+  int p_next = 0, slot_next = 0;
+  auto fetch_place = [&] {
+    if (t >= a.T) return;
+    p_next = pos[t];
+    slot_next = a.slot[t];
+  };
+  fetch_place();
+  while (t < a.T) {
+    int slot = slot_next;
+    const int p = p_next, r0 = part * a.seg, n = min(a.seg, a.rounds - r0), h0 = r0 * kHeads + lane / kLanes;
+    // (base pointers less the heads before theirs, at this lane's columns)
+    const __nv_bfloat16 *q_in = a.q + t * a.q_stride + 8 * sub;
+    const __nv_bfloat16 *k_in = a.k + t * a.k_stride + 8 * sub - a.H_q * D;
+    const __nv_bfloat16 *v_in = a.v + t * a.v_stride + 8 * sub - n_rot * D;
+    uint4 lo[kUnroll], hi[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int h = h0 + u * kHeads;
+      lo[u] = hi[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (u < n && h < n_heads) {
+        const uint4 *src = reinterpret_cast<const uint4 *>((h < a.H_q ? q_in : h < n_rot ? k_in : v_in) + h * D);
+        lo[u] = src[0];
+        hi[u] = src[D / 16];
       }
     }
-    const uint32_t axes = a.axis[sub >> 1] >> (16 * (sub & 1)) & 0xffffu;
-    auto row = [&](uint32_t i) {  // this lane's frequencies at the position on axis i
-      const int at = i == 0 ? p[0] : i == 1 ? p[1] : i == 2 ? p[2] : p[3];
-      return a.rope + (static_cast<long long>(at) * (D / 2) + 8 * sub) * 2;
-    };
-    if (axes == (axes & 3u) * 0x5555u) {  // all eight on one axis
-      const float4 *r = reinterpret_cast<const float4 *>(row(axes & 3u));
+    const int t_now = t;
+    t += step_t;
+    part += step_part;
+    if (part >= a.segs) {
+      part -= a.segs;
+      ++t;
+    }
+    float2 cos[4], sin[4];  // of this lane's 8 frequencies
+    if (r0 * kHeads < n_rot) {
+      auto row = [&](int at) {  // this lane's frequencies at a position
+        if (static_cast<unsigned>(at) >= static_cast<unsigned>(a.max_pos)) {
+          atomicOr(a.err, HPD_DEVERR_POSITION);
+          at = min(max(at, 0), a.max_pos - 1);
+        }
+        return a.rope + (static_cast<long long>(at) * (D / 2) + 8 * sub) * 2;
+      };
+      if (one_axis) {
+        const float4 *r = reinterpret_cast<const float4 *>(row(p));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 c = r[i];
-        cs[4 * i] = c.x;
-        cs[4 * i + 1] = c.y;
-        cs[4 * i + 2] = c.z;
-        cs[4 * i + 3] = c.w;
-      }
-    } else {
+        for (int i = 0; i < 4; ++i) {
+          const float4 c = r[i];
+          cos[i] = make_float2(c.x, c.z);
+          sin[i] = make_float2(c.y, c.w);
+        }
+      } else {  // (few lanes: the positions are not ahead)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 c = reinterpret_cast<const float2 *>(row(axes >> (2 * i) & 3u))[i];
-        cs[2 * i] = c.x;
-        cs[2 * i + 1] = c.y;
+        for (int i = 0; i < 4; ++i) {
+          const int32_t *at = a.pos + t_now;
+          const float *c0 = row(at[static_cast<long long>(axes >> (4 * i) & 3u) * a.T]) + 4 * i;
+          const float *c1 = row(at[static_cast<long long>(axes >> (4 * i + 2) & 3u) * a.T]) + 4 * i + 2;
+          cos[i] = make_float2(c0[0], c1[0]);
+          sin[i] = make_float2(c0[1], c1[1]);
+        }
       }
     }
-  }
-  const bool write_kv = slot >= 0 && slot < a.num_slots;
-  if (slot >= a.num_slots && lane == 0) atomicOr(a.err, HPD_DEVERR_PAGE_ID);
-#pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
-    const int h = h0 + u * kHeads;
-    const bool is_q = h < a.H_q, is_k = !is_q && h < a.H_q + a.H_kv;
-    float x[8], y[8], ss = 0.f;
-    unpack8(lo[u], x);
-    unpack8(hi[u], y);
-    if (is_q || is_k) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], fmaf(y[i], y[i], ss));
+    fetch_place();
+    if (slot >= a.num_slots) {
+      if (lane == 0) atomicOr(a.err, HPD_DEVERR_PAGE_ID);
+      slot = -1;
     }
+    __nv_bfloat16 *q_out = a.q_out + static_cast<long long>(t_now) * a.H_q * D + 8 * sub;
+    const long long row = static_cast<long long>(slot) * a.H_kv * D + 8 * sub;
+    __nv_bfloat16 *k_out = a.k_cache + row - a.H_q * D, *v_out = a.v_cache + row - n_rot * D;
 #pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    if (h >= n_heads) continue;
-    __nv_bfloat16 *dst;
-    if (is_q || is_k) {
-      const float r = rsqrtf(ss * (1.0f / D) + a.eps);
-      const __nv_bfloat16 *w = is_q ? a.q_weight : a.k_weight;
-      float wx[8], wy[8];
+    for (int u = 0; u < kUnroll; ++u) {
+      if (u >= n) break;
+      const int h = h0 + u * kHeads;
+      const bool is_q = h < a.H_q;
+      if ((r0 + u) * kHeads < n_rot) {
+        float2 x[4], y[4], s2 = make_float2(0.f, 0.f);
+        unpack8(lo[u], x);
+        unpack8(hi[u], y);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) wx[i] = wy[i] = 1.f;
-      if (w) {
-        unpack8(*reinterpret_cast<const uint4 *>(w + 8 * sub), wx);
-        unpack8(*reinterpret_cast<const uint4 *>(w + D / 2 + 8 * sub), wy);
+        for (int i = 0; i < 4; ++i) s2 = __ffma2_rn(x[i], x[i], __ffma2_rn(y[i], y[i], s2));
+        float ss = s2.x + s2.y;
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        if (h < n_rot) {
+          const float r = rsqrtf(ss * (1.0f / D) + a.eps);
+          const float2 r2 = make_float2(r, r);
+          const uint4 *w = reinterpret_cast<const uint4 *>((is_q ? a.q_weight : a.k_weight) + 8 * sub);
+          if (is_q ? a.q_weight : a.k_weight) {
+            float2 wx[4], wy[4];
+            unpack8(w[0], wx);
+            unpack8(w[D / 16], wy);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              x[i] = __fmul2_rn(x[i], wx[i]);
+              y[i] = __fmul2_rn(y[i], wy[i]);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 xn = __fmul2_rn(x[i], r2), yn = __fmul2_rn(y[i], r2);
+            const float2 ys = __fmul2_rn(yn, sin[i]);
+            x[i] = __ffma2_rn(xn, cos[i], make_float2(-ys.x, -ys.y));
+            y[i] = __ffma2_rn(yn, cos[i], __fmul2_rn(xn, sin[i]));
+          }
+          lo[u] = pack8(x);
+          hi[u] = pack8(y);
+        }
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float c = cs[2 * i], s = cs[2 * i + 1];
-        const float xn = x[i] * r * wx[i], yn = y[i] * r * wy[i];
-        x[i] = fmaf(xn, c, -yn * s);
-        y[i] = fmaf(yn, c, xn * s);
+      if (h < n_heads && (is_q || slot >= 0)) {
+        uint4 *dst = reinterpret_cast<uint4 *>((is_q ? q_out : h < n_rot ? k_out : v_out) + h * D);
+        dst[0] = lo[u];
+        dst[D / 16] = hi[u];
       }
-      dst = is_q ? a.q_out + (static_cast<long long>(t) * a.H_q + h) * D
-                 : a.k_cache + (static_cast<long long>(slot) * a.H_kv + (h - a.H_q)) * D;
-      lo[u] = pack8(x);
-      hi[u] = pack8(y);
-    } else {
-      dst = a.v_cache + (static_cast<long long>(slot) * a.H_kv + (h - a.H_q - a.H_kv)) * D;
-    }
-    if (is_q || write_kv) {
-      *reinterpret_cast<uint4 *>(dst + 8 * sub) = lo[u];
-      *reinterpret_cast<uint4 *>(dst + D / 2 + 8 * sub) = hi[u];
     }
   }
 }
 
-template <int D, int kUnroll>
+// Items of as many rounds as there are, up to kUnroll, where whole rows fill the
+// GPU with warps, else of fewer.
+template <int D>
 cudaError_t launch_rope(RopeArgs &a, cudaStream_t s) {
-  constexpr int per = 512 / D * kUnroll;  // heads of an item
-  a.groups = (a.H_q + 2 * a.H_kv + per - 1) / per;
-  a.items = static_cast<long long>(a.T) * a.groups;
-  const long long ctas = (a.items + kRopeWarps - 1) / kRopeWarps;
-  if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
-  return launch_kernel(true, qk_norm_rope_kernel<D, kUnroll>, dim3(static_cast<unsigned>(ctas)),
-                       dim3(32 * kRopeWarps), 0, s, a);
+  constexpr int heads = 512 / D, warps = kRopeSms * 16;
+  a.rounds = (a.H_q + 2 * a.H_kv + heads - 1) / heads;
+  const int least = std::max(1, std::min(a.rounds, warps / a.T));  // parts of a row that fill the GPU
+  const int segs = std::max(least, (a.rounds + kUnroll - 1) / kUnroll);
+  a.seg = (a.rounds + segs - 1) / segs;
+  a.segs = (a.rounds + a.seg - 1) / a.seg;
+  const long long items = static_cast<long long>(a.T) * a.segs;
+  const int ctas =
+      static_cast<int>(std::min<long long>((items + kRopeWarps - 1) / kRopeWarps, kRopeSms * kRopeCtas));
+  return launch_kernel(true, qk_norm_rope_kernel<D>, dim3(ctas), dim3(32 * kRopeWarps), 0, s, a);
 }
 
 }  // namespace
@@ -212,9 +255,8 @@ extern "C" hpd_status hpd_qk_norm_rope(const hpd_qk_norm_rope_args *a, hpd_strea
   k.H_q = a->H_q;
   k.H_kv = a->H_kv;
   k.max_pos = a->max_pos;
-  k.n_axes = a->n_axes;
   for (int i = 0; i < a->D / 2; ++i) k.axis[i >> 4] |= static_cast<uint32_t>(a->axis[i]) << (2 * (i & 15));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = a->D == 64 ? launch_rope<64, 2>(k, s) : launch_rope<128, 4>(k, s);
+  const cudaError_t e = a->D == 64 ? launch_rope<64>(k, s) : launch_rope<128>(k, s);
   return e == cudaSuccess ? HPD_OK : record_cuda_error(e);
 }

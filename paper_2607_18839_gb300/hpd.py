@@ -510,8 +510,14 @@ def fork_children(out_tokens, accepted_len, is_layout, layout_pos, fork_token, b
     return new
 
 
+def _is(t, dtype, shape) -> bool:
+    """A contiguous CUDA tensor of this type and shape."""
+    return t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous()
+
+
 def _need(what: str, t, dtype, shape, strides_free=False):
-    """A tensor of the wrong type or shape never reaches a kernel."""
+    """A tensor of the wrong type or shape never reaches a kernel (None: any
+    extent)."""
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or \
             len(t.shape) != len(shape) or \
@@ -548,6 +554,7 @@ class ChunkSlots:
         _need("ChunkSlots", free_top, i32, (1,))
         dev = page_table.device
         self.page_table, self.free_pages = page_table, free_pages
+        self._i32 = i32
         self._seq_in, self._top_in = seq_len, free_top
         self.seq_len = seq_len if in_place else torch.empty_like(seq_len)
         self.free_top = free_top if in_place else torch.empty_like(free_top)
@@ -562,8 +569,9 @@ class ChunkSlots:
 
     def __call__(self, new_len, stream=None) -> "ChunkSlots":
         """new_len: int32 [S] device tensor."""
-        import torch
-        _need("ChunkSlots", new_len, torch.int32, (self.args.S,))
+        shape = (self.args.S,)
+        if not _is(new_len, self._i32, shape):
+            _need("ChunkSlots", new_len, self._i32, shape)
         self.args.new_len = new_len.data_ptr()
         hpd_chunk_slots(self.args, _stream_handle(stream))
         return self
@@ -598,40 +606,43 @@ class QkNormRope:
         a.workspace, a.eps = _ptr(self.workspace), eps
         a.H_q, a.H_kv, a.D, a.n_axes, a.max_pos = H_q, H_kv, D, self.n_axes, rope.shape[0]
         a.axis[:D // 2] = axis
-        self.q_out = None
+        self._bf, self._i32 = torch.bfloat16, torch.int32
+        self._q = None
 
     def __call__(self, qkv, pos, slot, k_cache, v_cache, q_out=None, stream=None):
         """qkv: bf16 [T, at least (H_q + 2 H_kv) D], the projection's rows
         (queries, keys, values; rows may be strided); pos: int32 [n_axes, T] or
         [T]; slot: int32 [T]; caches bf16 [pages, 16, H_kv, D].  Returns the
         queries [T, H_q, D] (q_out, or a tensor that this object keeps)."""
-        import torch
-        a, T = self.args, qkv.shape[0]
-        H_q, H_kv, D = self.H_q, self.H_kv, self.D
-        bf = torch.bfloat16
-        _need("QkNormRope", qkv, bf, (None, None), strides_free=True)
-        if qkv.shape[1] < (H_q + 2 * H_kv) * D or qkv.stride(1) != 1:
+        a, H_q, H_kv, D = self.args, self.H_q, self.H_kv, self.D
+        bf, i32 = self._bf, self._i32
+        if qkv.dim() != 2 or qkv.dtype is not bf or not qkv.is_cuda:
+            _need("QkNormRope", qkv, bf, (None, None), strides_free=True)
+        T, width = qkv.shape
+        row, step = qkv.stride()
+        if width < (H_q + 2 * H_kv) * D or step != 1:
             raise HpdError("QkNormRope", 1, "rows of at least (H_q + 2 H_kv) D values side by side")
-        _need("QkNormRope", pos, torch.int32, (T,) if pos.dim() == 1 else (self.n_axes, T))
-        if pos.dim() == 1 and self.n_axes != 1:
-            raise HpdError("QkNormRope", 1, f"positions on {self.n_axes} axes")
-        _need("QkNormRope", slot, torch.int32, (None,))
-        _need("QkNormRope", k_cache, bf, (None, 16, H_kv, D))
-        _need("QkNormRope", v_cache, bf, k_cache.shape)
-        if slot.shape[0] < T:
-            raise HpdError("QkNormRope", 1, "a slot for each row")
+        if not _is(pos, i32, (self.n_axes, T)) and not (self.n_axes == 1 and _is(pos, i32, (T,))):
+            _need("QkNormRope", pos, i32, (self.n_axes, T))
+        if slot.dtype is not i32 or slot.dim() != 1 or not slot.is_cuda or not slot.is_contiguous() or \
+                slot.shape[0] < T:
+            raise HpdError("QkNormRope", 1, f"a contiguous CUDA int32 slot for each of {T} rows")
+        pages = k_cache.shape[0]
+        if not _is(k_cache, bf, (pages, 16, H_kv, D)) or not _is(v_cache, bf, (pages, 16, H_kv, D)):
+            _need("QkNormRope", k_cache, bf, (None, 16, H_kv, D))
+            _need("QkNormRope", v_cache, bf, k_cache.shape)
         if q_out is None:
-            if self.q_out is None or self.q_out.shape[0] < T:
-                self.q_out = torch.empty((T, H_q, D), dtype=bf, device=qkv.device)
-            q_out = self.q_out[:T]
-        else:
+            if self._q is None or self._q.shape[0] < T:
+                self._q = qkv.new_empty((T, H_q, D))
+            q_out = self._q if self._q.shape[0] == T else self._q[:T]
+        elif not _is(q_out, bf, (T, H_q, D)):
             _need("QkNormRope", q_out, bf, (T, H_q, D))
-        at, row = qkv.data_ptr(), qkv.stride(0)
+        at = qkv.data_ptr()
         a.q, a.k, a.v = at, at + 2 * H_q * D, at + 2 * (H_q + H_kv) * D
         a.q_stride = a.k_stride = a.v_stride = row
         a.pos, a.slot, a.q_out = pos.data_ptr(), slot.data_ptr(), q_out.data_ptr()
         a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
-        a.num_slots, a.T = k_cache.shape[0] * 16, T
+        a.num_slots, a.T = pages * 16, T
         hpd_qk_norm_rope(a, _stream_handle(stream))
         return q_out
 
@@ -666,6 +677,8 @@ class ChunkAttn:
         if nbytes == 0:
             raise HpdError("hpd_chunk_attn_workspace_size", 1, "invalid shape")
         self.max_tokens = max_tokens
+        self._H_q, self._D, self._S = H_q, D, S
+        self._bf, self._i32 = bf, torch.int32
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         a.workspace, a.workspace_bytes = _ptr(self.workspace), nbytes
         hpd_workspace_init(_ptr(self.workspace), nbytes, _stream_handle(stream))
@@ -674,17 +687,21 @@ class ChunkAttn:
         """q: bf16 [T, H_q, D] (heads side by side, rows may be strided), T up
         to max_tokens; chunk_cu int32 [S + 1], seq_len and full_len int32 [S].
         Returns (out, lse) of the T rows."""
-        import torch
-        a, T = self.args, q.shape[0]
-        _need("ChunkAttn", q, torch.bfloat16, (None, a.H_q, a.D), strides_free=True)
-        if T > self.max_tokens or T < 1 or q.stride(2) != 1 or q.stride(1) != a.D:
+        a, H_q, D, S = self.args, self._H_q, self._D, self._S
+        bf, i32 = self._bf, self._i32
+        if q.dtype is not bf or q.dim() != 3 or q.shape[1:] != (H_q, D) or not q.is_cuda:
+            _need("ChunkAttn", q, bf, (None, H_q, D), strides_free=True)
+        T, (row, head, step) = q.shape[0], q.stride()
+        if T > self.max_tokens or T < 1 or step != 1 or (head != D and H_q > 1):
             raise HpdError("ChunkAttn", 1, "1 to max_tokens rows with their heads side by side")
-        _need("ChunkAttn", chunk_cu, torch.int32, (a.S + 1,))
-        _need("ChunkAttn", seq_len, torch.int32, (a.S,))
-        if full_len is not None:
-            _need("ChunkAttn", full_len, torch.int32, (a.S,))
-        a.q, a.q_stride, a.T = q.data_ptr(), q.stride(0) if T > 1 else 0, T
-        a.chunk_cu, a.seq_len, a.full_len = chunk_cu.data_ptr(), seq_len.data_ptr(), _ptr(full_len)
+        if not _is(chunk_cu, i32, (S + 1,)) or not _is(seq_len, i32, (S,)):
+            _need("ChunkAttn", chunk_cu, i32, (S + 1,))
+            _need("ChunkAttn", seq_len, i32, (S,))
+        if full_len is not None and not _is(full_len, i32, (S,)):
+            _need("ChunkAttn", full_len, i32, (S,))
+        a.q, a.q_stride, a.T = q.data_ptr(), row if T > 1 else 0, T
+        a.chunk_cu, a.seq_len = chunk_cu.data_ptr(), seq_len.data_ptr()
+        a.full_len = None if full_len is None else full_len.data_ptr()
         hpd_chunk_attn(a, _stream_handle(stream))
         return (self.out, self.lse) if T == self.max_tokens else (self.out[:T], self.lse[:T])
 
