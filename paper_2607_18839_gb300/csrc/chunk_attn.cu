@@ -12,34 +12,40 @@
 // each, up to the last key that one of its rows sees.
 //
 // Work units: (tile, KV head, split of the tile's blocks).  One CTA per SM
-// takes units from an atomic counter; its roles run one unit apart, so that
-// nothing drains between units:
-//   warp 10     scheduler: finds the next unit in the step's lengths and puts
-//               its metadata into one of two slots while the other is in use
-//   warps 0, 11 TMA producers of K (and each unit's Q tile ahead of it) and V:
-//               three-stage rings, 128-byte swizzle; a block whose pages are
-//               consecutive in the pool is one box, else eight
-//   warp 1      Q tile into TMEM (tcgen05.cp), S = Q K^T into one of two buffers
-//   warp 12     O += P V, P read from TMEM where S was
-//   warps 2..9  softmax: two warpgroups, each with half of a block's keys and
-//               half of O's columns; a thread owns one row
-// A row's base is its maximum over the first block it sees keys of (the two
-// threads of a row exchange it there and nowhere else); later exponentials are
-// taken against it.  That is exact to the same relative error as a running
-// maximum as long as nothing overflows: a unit in which a score exceeds its base
-// by more than 2^64, or O is not finite, runs once more with running maxima.
-// Which units do is a matter of their own scores and values alone, so that a
-// call's bits do not depend on which CTA took which unit.
-// P goes to the tensor cores in two parts: while the exponentials of a half's
-// second 32 keys are taken, P V of the first 32 runs.
+// takes units from an atomic counter; its roles run apart, so that little drains
+// between units:
+//   warp 6      scheduler: finds the next unit in the step's lengths and puts
+//               its metadata into one of three slots
+//   warps 0..3  TMA producers, two of K (and each unit's Q tile ahead of it), two
+//               of V: three-stage rings, 128-byte swizzle.  A warp has four pages
+//               of each block, one box where they are consecutive in the pool, else
+//               four: a box takes its warp some 130 cycles to issue, the tensor map
+//               unit 68, so that two warps with eight boxes bounded the kernel.
+//   warp 4      Q tile into TMEM (tcgen05.cp), S = Q K^T into one of two buffers
+//   warp 5      O += P V, P read from TMEM where S was
+//   warps 8..15 softmax: two warpgroups, each with half of a block's keys and half
+//               of O's columns; a thread owns one row
+// A row's base is its maximum over the unit's first block (every row that sees
+// keys of the unit sees some there), over which its two threads exchange their
+// maxima.  Exponentials are taken against that base throughout, which is exact to
+// the same relative error as a running maximum as long as nothing overflows: a
+// unit in which a score exceeds its base by more than 2^64, or O is not finite, is
+// run again with its rows' true maxima, which a pass over S alone finds first.
+// Which units are is a matter of their own scores and values alone, so that a
+// call's bits do not depend on which CTA took which unit.  O is never rescaled.
+// A unit's output is written after the next unit's first exponentials, for which
+// the scores are there, while P V of its last block runs.  P goes to the tensor
+// cores in two parts: while the exponentials of a half's second 32 keys are taken,
+// P V of the first 32 runs.
 //
 // Rows that see no key are written by the scheduler.  Cache rows past a
 // sequence's end may hold anything: pages past it are not loaded (their box lies
-// outside the map and reads zeros), the rows behind it in its last page
-// are zeroed in shared memory before P V, and scores there are masked.
+// outside the map and reads zeros), scores behind it are masked, and the rows of V
+// behind it in its last page are zeroed in shared memory (a weight of zero would
+// not keep out what is not finite).
 // A value that is not finite in a row that some of a tile's rows see and others do
-// not would reach the others as 0 times it: rows whose O is not finite after
-// the second pass, and that such a value may have reached, are computed once
+// not would reach the others as 0 times it: rows whose O is not finite when
+// run again, and that such a value may have reached, are computed once
 // more from what they see, one row at a time.
 // All waits are bounded, as in the branch attention kernel.
 #include <algorithm>
@@ -56,13 +62,17 @@ using tc::kBlk;
 using tc::kRows;
 
 constexpr uint32_t kTmemCols = 512;
-constexpr int kPagesPerBlock = kBlk / kPage;
-constexpr int kSoftmaxWarps = 8;
-constexpr int kSchedWarp = 2 + kSoftmaxWarps;
-constexpr int kVWarp = kSchedWarp + 1;
-constexpr int kPvWarp = kVWarp + 1;
-constexpr int kThreads = 32 * (kPvWarp + 1);
-constexpr uint32_t kMetaConsumers = 4 + kSoftmaxWarps;
+constexpr int kPagesPerBlock = kBlk / kPage, kPagesEach = kPagesPerBlock / 2;  // of a producer
+constexpr int kProducers = 4;  // warps 0, 1: K; 2, 3: V
+constexpr int kQkWarp = 4, kPvWarp = 5, kSchedWarp = 6;
+constexpr int kSoftmaxWarp = 8, kSoftmaxWarps = 8;
+constexpr int kThreads = 32 * (kSoftmaxWarp + kSoftmaxWarps);
+// What a pass over a unit does: exponentials against the first block's maxima;
+// nothing but the rows' maxima; exponentials against those.
+enum Pass { kFirst, kMaxima, kAgain };
+constexpr int kMetaSlots = 3;
+// of a metadata slot: producers, two MMA issuers, softmax warps
+constexpr uint32_t kMetaConsumers = kProducers + 2 + kSoftmaxWarps;
 constexpr int kStages = 3;
 constexpr int kGroup = 256;      // sequences whose lengths the scheduler holds at once
 constexpr int kMaxSplits = 32;
@@ -100,7 +110,7 @@ struct UnitMeta {
   int full, L;   // keys that every token sees; tokens of the sequence
   int pages;     // pages up to the last key that the tile sees
   int blk_lo, n_blocks;
-  int exact;     // every block's base is the running maximum
+  int pass;
 };
 
 template <int D>
@@ -121,22 +131,22 @@ struct Layout {
 };
 
 struct __align__(8) Shared {
-  uint64_t meta_full[2], meta_empty[2];
+  uint64_t meta_full[kMetaSlots], meta_empty[kMetaSlots];
+  uint64_t taken;  // the K producer has begun a unit
   uint64_t k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages];
-  // per S buffer: scores written; P written, by part; P V done (the buffer is
-  // free and O holds the block)
+  // per S buffer: scores written; P written, by part; P V issued
   uint64_t s_full[2], p_full[2][2], s_free[2];
   uint64_t o_full, o_empty;
   uint64_t mma_done[2];
   uint32_t tmem_base;
   int abort;
-  float xmax[2][2][kRows];  // [half][block parity][row]
-  float xsum[2][2][kRows];  // [unit parity][half][row]
-  int xseq[2][2][4];        // [max | sum][half][quadrant]
+  float xmax[2][2][kRows];  // [unit parity][half][row]: maxima of a unit's first block
+  float xsum[2][2][kRows];  // [unit parity][half][row]: sums (pass over maxima: maxima)
+  int max_seq[4][2], sum_seq[4][2];  // [quadrant][half]: units published
   unsigned redo;            // units (by number in this CTA, modulo 32) to run once more
-  int units_done;           // softmax warps that finished a unit's epilogue
+  int units_done;           // softmax warps that wrote a unit's output
   int unit_id[32];          // the last units issued
-  UnitMeta meta[2];
+  UnitMeta meta[kMetaSlots];
   // the scheduler's group of sequences: units before each, first rows, lengths, splits
   int g_units[kGroup + 1], g_cu[kGroup + 1], g_len[kGroup], g_split[kGroup];
 };
@@ -178,15 +188,48 @@ __device__ __forceinline__ float lse_of(float m, float l) {
   return fmaf(static_cast<float>(e), kLn2, fmaf(m, kLn2, logf(f)));
 }
 
-// Half a block of a row's softmax against a base that is there (see
-// tc::softmax_half_based): publish(part) once P of the half's first (second) 32
-// keys is in TMEM.  hi: visible columns of the half.  Returns false when a score
-// lies above the window of the base.
-template <class Publish>
-__device__ __forceinline__ bool softmax_based(uint32_t s_addr, bool plain, int hi, float sl2, float m_run,
-                                              float &l_half, Publish publish) {
+__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
+// Largest score of a row's half block; hi: visible columns of the half.
+__device__ __forceinline__ float half_max(uint32_t s_addr, int hi, float sl2) {
   const float NEG_INF = -__int_as_float(0x7f800000);
-  if (!plain && __all_sync(0xffffffffu, hi <= 0)) {  // no row of the warp sees a key of the half
+  const bool raw = sl2 > 0.f;
+  float mx[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
+#pragma unroll 1
+  for (int part = 0; part < 2; ++part) {
+    uint32_t v[32];
+    tmem_ld32(s_addr + 32 * part, v);
+    tmem_ld_wait32(v);
+    tc::mask32(v, 0, hi - 32 * part, !raw, sl2);
+#pragma unroll
+    for (int c = 0; c < 32; c += 8)
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+        mx[a] = tc::fmax3(mx[a], __uint_as_float(v[c + 2 * a]), __uint_as_float(v[c + 2 * a + 1]));
+  }
+  return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * (raw ? sl2 : 1.f);
+}
+
+// A row's half block: P = exp2(scaled score - base) as bf16 pairs where the scores
+// were, and its sum; publish(part) once P of the half's first (second) 32 keys is
+// on its way.  PLAIN: every row of the warp sees every key, and the scale
+// is positive (its order is then the raw scores').  Returns false when a score
+// lies above the window of the base.
+template <bool PLAIN, class Publish>
+__device__ __forceinline__ bool softmax_half(uint32_t s_addr, int hi, float sl2, float m_run, float2 *l4,
+                                             Publish publish) {
+  const float NEG_INF = -__int_as_float(0x7f800000);
+  if (!PLAIN && __all_sync(0xffffffffu, hi <= 0)) {  // no row of the warp sees a key of the half
     uint32_t z[32];
 #pragma unroll
     for (int c = 0; c < 32; ++c) z[c] = 0u;
@@ -195,27 +238,20 @@ __device__ __forceinline__ bool softmax_based(uint32_t s_addr, bool plain, int h
     publish(1);
     return true;
   }
-  const bool raw = sl2 > 0.f;
+  const bool raw = PLAIN || sl2 > 0.f;
   const float mul = raw ? sl2 : 1.f, base = m_run == NEG_INF ? 0.f : m_run;
+  float mx4[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
   uint32_t v[64];
-  float2 sum4[4];
-  float mx4[4];
-#pragma unroll
-  for (int a = 0; a < 4; ++a) {
-    sum4[a] = make_float2(0.f, 0.f);
-    mx4[a] = NEG_INF;
-  }
   tmem_ld32(s_addr, v);
   tmem_ld_wait32(v);
   tmem_ld32(s_addr + 32, v + 32);
-  if (!plain) tc::mask32(v, 0, hi, !raw, sl2);
-  tc::exp32<true, false>(s_addr, v, mul, base, sum4, mx4);
+  if (!PLAIN) tc::mask32(v, 0, hi, !raw, sl2);
+  tc::exp32<true, false>(s_addr, v, mul, base, l4, mx4);
   publish(0);
   tmem_ld_wait32(v + 32);
-  if (!plain) tc::mask32(v + 32, 0, hi - 32, !raw, sl2);
-  tc::exp32<true, false>(s_addr + 16, v + 32, mul, base, sum4, mx4);
+  if (!PLAIN) tc::mask32(v + 32, 0, hi - 32, !raw, sl2);
+  tc::exp32<true, false>(s_addr + 16, v + 32, mul, base, l4, mx4);
   publish(1);
-  l_half += tc::sum_of(sum4);
   return fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * mul <= base + tc::kWindowLog2;
 }
 
@@ -284,8 +320,8 @@ __device__ __noinline__ void one_row(const ChunkParams &p, int seq, int token, i
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
-    chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                      const __grid_constant__ CUtensorMap tm_k8, const __grid_constant__ CUtensorMap tm_v8,
+    chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_k4,
+                      const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_v4,
                       const __grid_constant__ CUtensorMap tm_q, const ChunkParams p) {
   using L = Layout<D>;
   extern __shared__ uint8_t smem_raw[];
@@ -305,27 +341,30 @@ __global__ void __launch_bounds__(kThreads, 1)
     sh.redo = 0u;
     sh.units_done = 0;
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(bar(sh.k_full[s]), 1);
-      mbar_init(bar(sh.v_full[s]), 1);
+      mbar_init(bar(sh.k_full[s]), 2);
+      mbar_init(bar(sh.v_full[s]), 2);
       mbar_init(bar(sh.k_empty[s]), 1);
       mbar_init(bar(sh.v_empty[s]), 1);
     }
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < kMetaSlots; ++s) {
       mbar_init(bar(sh.meta_full[s]), 1);
       mbar_init(bar(sh.meta_empty[s]), kMetaConsumers);
+    }
+    for (int s = 0; s < 2; ++s) {
       mbar_init(bar(sh.s_full[s]), 1);
       mbar_init(bar(sh.p_full[s][0]), kSoftmaxWarps);
       mbar_init(bar(sh.p_full[s][1]), kSoftmaxWarps);
       mbar_init(bar(sh.s_free[s]), 1);
     }
+    mbar_init(bar(sh.taken), 1);
     mbar_init(bar(sh.o_full), 1);
     mbar_init(bar(sh.o_empty), kSoftmaxWarps);
     mbar_init(bar(sh.mma_done[0]), 1);
     mbar_init(bar(sh.mma_done[1]), 1);
     fence_mbar_init();
   }
-  if (tid < 16) (&sh.xseq[0][0][0])[tid] = 0;
-  if (warp == 1) {
+  if (tid < 16) (tid < 8 ? &sh.max_seq[0][0] : &sh.sum_seq[0][0])[tid & 7] = 0;
+  if (warp == kQkWarp) {
     tmem_alloc(smem_u32(&sh.tmem_base), kTmemCols);
     tmem_relinquish();
   }
@@ -396,7 +435,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
     };
     load_group(0, 0);
-    unsigned redo = 0;  // units to run once more
+    unsigned redo = 0;  // units to run again
+    int again = -1;     // the unit whose maxima the last pass took
+    int outputs = 0;    // passes that write a unit's output
     int nb_last = 0, nb_before = 0;
     auto take_redo = [&] {
       unsigned r = 0;
@@ -413,30 +454,37 @@ __global__ void __launch_bounds__(kThreads, 1)
       return u < kNoUnit;
     };
     for (int k = 0;; ++k) {
-      const int slot = k & 1;
-      if (k >= 2 && !wait_bar(sh.meta_empty[slot], ((k >> 1) - 1) & 1)) {
+      const int slot = k % kMetaSlots;
+      // a unit is taken when the K producer begins the one before: no earlier, as
+      // another CTA may come to it sooner
+      if ((k >= kMetaSlots && !wait_bar(sh.meta_empty[slot], (k / kMetaSlots - 1) & 1)) ||
+          (k >= 1 && !wait_bar(sh.taken, (k - 1) & 1))) {
         if (lane == 0) set_abort(sh, p.err);
         break;
       }
       UnitMeta &M = sh.meta[slot];
       bool have = false;
       for (;;) {
-        int u = 0;
+        int u = again, pass = kAgain;
         if (!redo) redo = take_redo();
-        const bool again = redo != 0;
-        if (again) {
-          u = sh.unit_id[__ffs(redo) - 1];
+        if (again >= 0) {
+          again = -1;
+        } else if (redo) {
+          u = again = sh.unit_id[__ffs(redo) - 1];
+          pass = kMaxima;
           redo &= redo - 1;
         } else {
+          pass = kFirst;
+          u = 0;
           if (lane == 0) u = atomicAdd(p.unit_ctr, 1);
           u = __shfl_sync(0xffffffffu, u, 0);
           if (__any_sync(0xffffffffu, aborted(sh))) break;
         }
         if (!locate(u)) {
-          // none left, once the units still running (the last two) need no second
-          // pass; who gives up here has set the abort word and the error
+          // none left, once the units still running (the last two) need not be run
+          // again; who gives up here has set the abort word and the error
           const uint64_t limit = kWaitLimitNs + (static_cast<uint64_t>(nb_last) + nb_before) * kBlockLimitNs;
-          if (!__all_sync(0xffffffffu, await_count(smem_u32(&sh.units_done), kSoftmaxWarps * k, &sh.abort, p.err,
+          if (!__all_sync(0xffffffffu, await_count(smem_u32(&sh.units_done), kSoftmaxWarps * outputs, &sh.abort, p.err,
                                                    HPD_DEVERR_TIMEOUT, limit)))
             break;
           redo = take_redo();
@@ -493,11 +541,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           M.pages = ceil_div_i(kmax, kPage);
           M.blk_lo = blk_lo;
           M.n_blocks = blk_hi - blk_lo;
-          M.exact = again;
+          M.pass = pass;
           sh.unit_id[k & 31] = u;
         }
         nb_before = nb_last;
         nb_last = blk_hi - blk_lo;
+        outputs += pass != kMaxima;
         have = true;
         break;
       }
@@ -507,72 +556,90 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) mbar_arrive(bar(sh.meta_full[slot]));
       if (!have) break;
     }
-  } else if (warp == 0 || warp == kVWarp) {
+  } else if (warp < kProducers) {
     // ------------------------------------------------------- producers --
-    const bool is_k = warp == 0;
+    const bool is_k = warp < 2;
+    const int half = warp & 1;
     if (lane == 0) {
       prefetch_tmap(&tm_q);
-      prefetch_tmap(&tm_k);
-      prefetch_tmap(&tm_v);
-      prefetch_tmap(&tm_k8);
-      prefetch_tmap(&tm_v8);
+      prefetch_tmap(is_k ? &tm_k : &tm_v);
+      prefetch_tmap(is_k ? &tm_k4 : &tm_v4);
     }
     __syncwarp();
     uint64_t *const full = is_k ? sh.k_full : sh.v_full, *const empty = is_k ? sh.k_empty : sh.v_empty;
-    const CUtensorMap *const page_map = is_k ? &tm_k : &tm_v, *const run_map = is_k ? &tm_k8 : &tm_v8;
-    const uint32_t ring = sbase + (is_k ? L::kK : L::kV);
+    const CUtensorMap *const page_map = is_k ? &tm_k : &tm_v, *const run_map = is_k ? &tm_k4 : &tm_v4;
+    const uint32_t ring = sbase + (is_k ? L::kK : L::kV), mine = half * (L::kTileBytes / 2);
     int issued = 0;  // ring entries
     bool ok = true;
     for (int k = 0; ok; ++k) {
-      const int slot = k & 1;
-      if (!(ok = wait_bar(sh.meta_full[slot], (k >> 1) & 1))) break;
+      const int slot = k % kMetaSlots;
+      if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
       const UnitMeta M = sh.meta[slot];
       __syncwarp();
-      if (lane == 0 && M.valid) mbar_arrive(bar(sh.meta_empty[slot]));
       if (!M.valid) break;
+      if (lane == 0) {
+        mbar_arrive(bar(sh.meta_empty[slot]));
+        if (warp == 0) mbar_arrive(bar(sh.taken));
+      }
+      if (!is_k && M.pass == kMaxima) continue;
       const int32_t *const row = p.page_table + static_cast<size_t>(M.seq) * p.max_pages;
-      // page i of a block in lane i < 8, looked up a block ahead; pages past the
-      // last one that the tile sees lie outside the map
+      // Ids of this warp's pages of eight blocks at once, looked up eight blocks
+      // ahead of their use (a look-up a block, one ahead, had the producers wait for
+      // it: some 700 cycles a block); pages past the last one that the tile sees lie
+      // outside the map, whose boxes read zeros.
+      constexpr int kIdBlocks = 32 / kPagesEach;
+      const int page0 = M.blk_lo * kPagesPerBlock + (lane / kPagesEach) * kPagesPerBlock + half * kPagesEach +
+                        lane % kPagesEach;
+      int ids = p.num_pages, ids_next = p.num_pages;
       auto look_up = [&](int j) {
-        const int i = (M.blk_lo + j) * kPagesPerBlock + lane;
-        return lane < kPagesPerBlock && j < M.n_blocks && i < M.pages ? row[i] : p.num_pages;
+        const int i = page0 + j * kPagesPerBlock;
+        ids_next = p.num_pages;
+        if (i < M.pages) ids_next = __ldg(row + i);
       };
-      int pg = look_up(0);
+      look_up(0);
 #pragma unroll 1
       for (int j = is_k ? -1 : 0; j < M.n_blocks; ++j) {
         const int e = issued, s = e % kStages;
         if (e >= kStages && !(ok = wait_bar(empty[s], ((e / kStages) - 1) & 1))) break;
         ++issued;
         const uint32_t dst = ring + s * L::kTileBytes, b = bar(full[s]);
-        if (j < 0) {  // the unit's Q tile
-          mbar_arrive_expect_tx_elect(b, L::kChunks * TT * G * 128);
-#pragma unroll 1
-          for (int c = 0; c < L::kChunks; ++c)
-            tma_load_3d_elect(dst + c * L::kChunkBytes, &tm_q, b, c * 64, M.g * G, M.tok0);
+        if (j < 0) {  // the unit's Q tile, 64 columns a warp
+          if (half < L::kChunks) {
+            mbar_arrive_expect_tx_elect(b, TT * G * 128);
+            tma_load_3d_elect(dst + half * L::kChunkBytes, &tm_q, b, half * 64, M.g * G, M.tok0);
+          } else if (lane == 0) {
+            mbar_arrive(b);
+          }
+          __syncwarp();
           continue;
         }
-        const int next = look_up(j + 1);
-        if (static_cast<unsigned>(pg) > static_cast<unsigned>(p.num_pages) ||
-            (pg == p.num_pages && lane < kPagesPerBlock &&
-             (M.blk_lo + j) * kPagesPerBlock + lane < M.pages)) {
-          flag_error(p.err, HPD_DEVERR_PAGE_ID);
-          pg = 0;
+        if (j % kIdBlocks == 0) {
+          ids = ids_next;
+          if (page0 + j * kPagesPerBlock < M.pages && static_cast<unsigned>(ids) >= static_cast<unsigned>(p.num_pages)) {
+            flag_error(p.err, HPD_DEVERR_PAGE_ID);
+            ids = 0;
+          }
+          look_up(j + kIdBlocks);
+          __syncwarp();
         }
-        mbar_arrive_expect_tx_elect(b, L::kTileBytes);
+        const int pg = __shfl_sync(0xffffffffu, ids, (j % kIdBlocks) * kPagesEach + (lane & (kPagesEach - 1)));
+        mbar_arrive_expect_tx_elect(b, L::kTileBytes / 2);
         const int right = __shfl_down_sync(0xffffffffu, pg, 1);
-        const unsigned run = __ballot_sync(0xffffffffu, lane < kPagesPerBlock - 1 && right == pg + 1);
-        const bool one = p.num_pages >= kPagesPerBlock && (run & 0x7fu) == 0x7fu;
-        if (lane < (one ? 1 : kPagesPerBlock))
-          tma_load_5d(dst + lane * L::kPageBytes, one ? run_map : page_map, b, 0, 0, 0, 2 * pg, M.g);
+        const unsigned run = __ballot_sync(0xffffffffu, lane < kPagesEach - 1 && right == pg + 1);
+        const bool one = p.num_pages >= kPagesEach && (run & 7u) == 7u;
+        if (lane < (one ? 1 : kPagesEach))
+          tma_load_5d(dst + mine + lane * L::kPageBytes, one ? run_map : page_map, b, 0, 0, 0, 2 * pg, M.g);
         __syncwarp();
-        pg = next;
       }
     }
     if (!ok && lane == 0) set_abort(sh, p.err);
     // no exit while a copy into this CTA's shared memory is in flight
-    for (int e = max(0, issued - kStages); e < issued; ++e) mbar_wait(bar(full[e % kStages]), (e / kStages) & 1);
-  } else if (warp == 1) {
+    for (int e = max(0, issued - kStages); e < issued; ++e)
+      mbar_wait(bar(full[e % kStages]), (e / kStages) & 1);
+  } else if (warp == kQkWarp) {
     // ---------------------------------------------------- Q K^T issuer --
+    // The MMA warps run their loops with warp-uniform values; one elected lane
+    // issues each group of MMAs and its commits.
     constexpr uint32_t idesc_qk = idesc_bf16_f32(kRows, kBlk, false);
     const uint64_t dq0 = smem_desc_sw128(sbase + L::kK, 16, 1024);
     const uint64_t dk0 = smem_desc_sw128(sbase + L::kK, 16, L::kGroupBytes);
@@ -581,18 +648,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     int jg = 0;               // blocks issued
     bool ok = true;
     for (int k = 0; ok; ++k) {
-      const int slot = k & 1;
-      if (!(ok = wait_bar(sh.meta_full[slot], (k >> 1) & 1))) break;
+      const int slot = k % kMetaSlots;
+      if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
       const bool valid = sh.meta[slot].valid != 0;
       const int nb = sh.meta[slot].n_blocks;
       __syncwarp();
       if (!valid) break;
       if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
-      // entry -1 of the unit: its Q, copied into TMEM slot k & 1 (in order with the
-      // MMAs: unit k - 2's Q K^T are done with the slot)
+      const uint32_t q_col = tmem + L::col_q(k & 1);
+      // entry -1 of the unit: its Q, copied into TMEM (in order with the MMAs: unit
+      // k - 2's Q K^T are done with the slot)
       for (int j = -1; j < nb; ++j) {
         if (!(ok = wait_bar(sh.k_full[sk], pk))) break;
-        // the S buffer is free once P V of the block before last has read P
+        // the S buffer is free for what is issued behind P V of the block before last
         if (j >= 0 && jg >= 2 && !(ok = wait_bar(sh.s_free[jg & 1], ((jg >> 1) - 1) & 1))) break;
         tc_fence_after();
         if (issuer) {
@@ -600,14 +668,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (j < 0) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
-              tmem_cp_128x256b(tmem + L::col_q(slot) + kk * 8,
-                               dq0 + off + (((kk >> 2) * L::kChunkBytes + (kk & 3) * 32) >> 4));
+              tmem_cp_128x256b(q_col + kk * 8, dq0 + off + (((kk >> 2) * L::kChunkBytes + (kk & 3) * 32) >> 4));
           } else {
             const uint32_t col = tmem + L::col_s(jg & 1);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
-              mma_ts_one(col, tmem + L::col_q(slot) + kk * 8, dk0 + off + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4),
-                         idesc_qk, kk > 0);
+              mma_ts_one(col, q_col + kk * 8, dk0 + off + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), idesc_qk, kk > 0);
             mma_commit_one(bar(sh.s_full[jg & 1]));
           }
           mma_commit_one(bar(sh.k_empty[sk]));
@@ -628,22 +694,34 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool issuer = elect_one();
     uint32_t sv = 0, pv = 0;  // V ring: stage, phase
     int jg = 0;               // blocks issued
+    int outputs = 0;          // units whose O was made
     bool ok = true;
     for (int k = 0; ok; ++k) {
-      const int slot = k & 1;
-      if (!(ok = wait_bar(sh.meta_full[slot], (k >> 1) & 1))) break;
-      const bool valid = sh.meta[slot].valid != 0;
+      const int slot = k % kMetaSlots;
+      if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
+      const bool valid = sh.meta[slot].valid != 0, maxima = sh.meta[slot].pass == kMaxima;
       const int nb = sh.meta[slot].n_blocks, len = sh.meta[slot].L;
       // the block with rows behind the sequence's end in its last page
       const int j_tail = len % kPage ? len / kBlk - sh.meta[slot].blk_lo : -1;
       __syncwarp();
       if (!valid) break;
       if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
-      // O last held the unit before, whose epilogue must have read it
-      if (k >= 1 && !(ok = wait_bar(sh.o_empty, (k - 1) & 1))) break;
+      if (maxima) {  // nothing to multiply: the scores are only read
+        for (int j = 0; j < nb; ++j, ++jg) {
+          if (!(ok = wait_bar(sh.p_full[jg & 1][0], (jg >> 1) & 1) && wait_bar(sh.p_full[jg & 1][1], (jg >> 1) & 1)))
+            break;
+          tc_fence_after();
+          tc_fence_before();
+          if (issuer) mbar_arrive(bar(sh.s_free[jg & 1]));
+          __syncwarp();
+        }
+        continue;
+      }
       for (int j = 0; j < nb; ++j) {
         if (!(ok = wait_bar(sh.v_full[sv], pv))) break;
-        if (j == j_tail) {  // a weight of zero would not keep out what is not finite there
+        // O last held the output before, which must have been read
+        if (j == 0 && outputs >= 1 && !(ok = wait_bar(sh.o_empty, (outputs - 1) & 1))) break;
+        if (j == j_tail) {
           const uint32_t v0 = sbase + L::kV + sv * L::kTileBytes;
           for (int i = (len % kBlk) * (L::kChunks * 8) + lane; i < (len % kBlk / kPage + 1) * kPage * (L::kChunks * 8);
                i += 32) {
@@ -676,7 +754,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!ok) break;
         if (issuer) {
-          mma_commit_one(bar(sh.s_free[jg & 1]));
+          // (Q K^T of the next block but one, into this S buffer, may be issued: MMAs
+          // run in the order of issue)
+          tc_fence_before();
+          mbar_arrive(bar(sh.s_free[jg & 1]));
           mma_commit_one(bar(sh.v_empty[sv]));
           if (j == nb - 1) mma_commit_one(bar(sh.o_full));
         }
@@ -687,196 +768,221 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         ++jg;
       }
+      ++outputs;
     }
     if (!ok && lane == 0) set_abort(sh, p.err);
-  } else {
+  } else if (warp >= kSoftmaxWarp) {
     // --------------------------------------------------------- softmax --
-    const int h = (warp - 2) >> 2;        // column half
-    const int quad = warp & 3;            // TMEM lane quadrant this warp may access
-    const int r_in = quad * 32 + lane;    // row within the tile
+    const int h = (warp - kSoftmaxWarp) >> 2;  // half of a block's keys, and of O's columns
+    const int quad = warp & 3;                 // TMEM lane quadrant this warp may access
+    const int r_in = quad * 32 + lane;         // row within the tile
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    const int rt = p.div_G(r_in);
     const float sl2 = p.scale_log2;
-    const uint32_t o_col = L::kColO + h * (D / 2);
-    int jbase = 0;
+    // The other half has published unit k, too.
+    auto await_other = [&](const int (*seq)[2], int k) {
+      return __all_sync(0xffffffffu, await_seq(&seq[quad][h ^ 1], k + 1, sh));
+    };
+    int k = 0, j = 0, jg = 0;    // unit, block of it, blocks in all
+    int outputs = 0;
+    int pending = -1;            // the unit whose output is to be written, its row's base
+    float m_pending = 0.f;
+    bool loaded = false;         // unit k's metadata
+    int nb = 0, blk_lo = 0, pass = kFirst, lim = 0, n_plain = 0;
+    bool valid_unit = false, idle = false;
+    float m_run = NEG_INF, given = NEG_INF, mx_run = NEG_INF;
+    float2 l4[4];                // the row's sum so far, in parts
+    bool inside = true;          // the scores stay in the window of their base
     bool ok = true;
-    for (int k = 0; ok; ++k) {
-      const int slot = k & 1;
-      if (!(ok = wait_bar(sh.meta_full[slot], (k >> 1) & 1))) break;
-      const UnitMeta M = sh.meta[slot];
-      __syncwarp();
-      if (!M.valid) break;
-      if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
-      const bool valid = r_in < M.nrows, idle = quad * 32 >= M.nrows;
-      const int rt = p.div_G(r_in), token = M.tok0 + rt, head = M.g * G + r_in - rt * G;
-      // (rows that are no query count as seeing everything, so that their warp
-      // needs no masks for them; their results are not stored)
-      const int lim = valid ? min(max(M.lim0 + rt, M.full), M.L) : 1 << 30;
-      const int n_plain = sl2 > 0.f ? max(__reduce_min_sync(0xffffffffu, lim), 0) / kBlk : 0;
-      const size_t pair = static_cast<size_t>(token) * p.H_q + head;
-      float m_run = NEG_INF, l_half = 0.f;
-      bool inside = true;  // the scores stay in the window of their base
-      bool based = false;  // every row of the warp has its base
-      auto await_s = [&](int jg) {
+    for (;;) {
+      // A unit's output comes after the next unit's first exponentials; at once
+      // when there is no next unit (yet).
+      if (pending >= 0 &&
+          (loaded ? !valid_unit || j > 0
+                  : !__all_sync(0xffffffffu, mbar_test_wait(bar(sh.meta_full[k % kMetaSlots]), (k / kMetaSlots) & 1)))) {
+        const UnitMeta &M = sh.meta[pending % kMetaSlots];
+        const bool valid = r_in < M.nrows, out_idle = quad * 32 >= M.nrows;
+        const int out_lim = min(max(M.lim0 + rt, M.full), M.L), out_pass = M.pass, nsplit = M.nsplit;
+        const int token = M.tok0 + rt, head = M.g * G + r_in - rt * G;
+        const size_t pair = static_cast<size_t>(token) * p.H_q + head;
+        const size_t slot_pair = static_cast<size_t>(M.split) * p.T * p.H_q + pair;
+        bool redo = false, mend = false;
+        if (!out_idle && !(ok = await_other(sh.sum_seq, pending))) break;
+        if (!(ok = wait_bar(sh.o_full, outputs & 1))) break;
+        ++outputs;
+        tc_fence_after();
+        if (!out_idle) {
+          const float l = sh.xsum[pending & 1][0][r_in] + sh.xsum[pending & 1][1][r_in];
+          // (a sum that is NaN stays one)
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          float2 finite = make_float2(0.f, 0.f);  // NaN once an infinity or NaN is added
+#pragma unroll 1
+          for (int c = 0; c < D / 2; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(t_lane + L::kColO + h * (D / 2) + c, o);
+            tmem_ld_wait32(o);
+            if (!valid) continue;
+#pragma unroll
+            for (int e = 0; e < 32; e += 2)
+              finite = __ffma2_rn(make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), make_float2(0.f, 0.f),
+                                  finite);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
+            const int dc = h * (D / 2) + c;  // output column
+            if (nsplit == 1) {
+              __nv_bfloat16 *dst = p.out + pair * D + dc;
+#pragma unroll
+              for (int e = 0; e < 32; e += 2)
+                o[e / 2] = pack_bf16x2(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
+              if (p.out_align32) {  // 32-byte stores: each fills a sector
+                st_global_v8(dst, o);
+                st_global_v8(dst + 16, o + 8);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                  reinterpret_cast<uint4 *>(dst)[e / 4] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+              }
+            } else {
+              float *dst = p.o_part + slot_pair * D + dc;
+#pragma unroll
+              for (int e = 0; e < 32; e += 8) st_global_v8(dst + e, o + e);
+            }
+          }
+          if (valid && h == 0) {
+            const float lse = l == 0.f ? NEG_INF : l > 0.f ? lse_of(m_pending, l) : l;
+            if (nsplit > 1) p.l_part[slot_pair] = lse;
+            else if (p.lse) p.lse[pair] = lse;
+          }
+          const bool odd = valid && !(finite.x == 0.f && finite.y == 0.f);
+          redo = __any_sync(0xffffffffu, out_pass == kFirst && (odd || (valid && l != l)));
+          // a key that the tile sees and this row does not
+          mend = out_pass == kAgain && odd && out_lim < M.pages * kPage && out_lim < M.L && l == l;
+        }
+        // O may be overwritten by the next unit once every warp has read it
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar(sh.o_empty));
+          if (redo) atomicOr(&sh.redo, 1u << (pending & 31));
+          __threadfence_block();
+          atomicAdd(&sh.units_done, 1);
+        }
+        for (unsigned rows = __ballot_sync(0xffffffffu, mend); rows; rows &= rows - 1) {
+          const int src = __ffs(rows) - 1;
+          const int row_token = __shfl_sync(0xffffffffu, token, src), row_head = __shfl_sync(0xffffffffu, head, src);
+          const int row_lim = __shfl_sync(0xffffffffu, out_lim, src);
+          const size_t at = static_cast<size_t>(row_token) * p.H_q + row_head;
+          const int k0 = M.blk_lo * kBlk, k1 = min(row_lim, (M.blk_lo + M.n_blocks) * kBlk);
+          one_row<D>(p, M.seq, row_token, row_head, k0, k1, h,
+                     nsplit == 1 ? nullptr : p.o_part + (static_cast<size_t>(M.split) * p.T * p.H_q + at) * D,
+                     p.out + at * D);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(sh.meta_empty[pending % kMetaSlots]));
+        pending = -1;
+      }
+      if (!loaded) {
+        const int slot = k % kMetaSlots;
+        if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
+        const UnitMeta &M = sh.meta[slot];
+        loaded = true;
+        valid_unit = M.valid != 0;
+        nb = M.n_blocks;
+        blk_lo = M.blk_lo;
+        pass = M.pass;
+        idle = quad * 32 >= M.nrows;
+        // (rows that are no query count as seeing everything, so that their warp
+        // needs no masks for them; their results are not stored)
+        lim = r_in < M.nrows ? min(max(M.lim0 + rt, M.full), M.L) : 1 << 30;
+        // blocks of the unit that every row of the warp sees all of
+        n_plain = sl2 > 0.f ? max(__reduce_min_sync(0xffffffffu, lim), 0) / kBlk - blk_lo : 0;
+        j = 0;
+        m_run = given;
+        mx_run = NEG_INF;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l4[i] = make_float2(0.f, 0.f);
+        inside = true;
+        if (!valid_unit && pending >= 0) continue;
+      }
+      if (!valid_unit) break;
+      if (j == nb) {  // the unit's sums (maxima), two buffers in turn
+        if (!idle) {
+          sh.xsum[k & 1][h][r_in] = pass == kMaxima ? mx_run : inside ? tc::sum_of(l4) : __int_as_float(0x7fffffff);
+          publish_seq(&sh.sum_seq[quad][h], k + 1);
+        }
+        if (pass == kMaxima) {
+          if (!idle) {
+            if (!(ok = await_other(sh.sum_seq, k))) break;
+            given = fmaxf(sh.xsum[k & 1][0][r_in], sh.xsum[k & 1][1][r_in]);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(sh.meta_empty[k % kMetaSlots]));
+        } else {
+          pending = k;
+          m_pending = m_run;
+        }
+        ++k;
+        loaded = false;
+        continue;
+      }
+      auto await_s = [&] {
         if (!wait_bar(sh.s_full[jg & 1], (jg >> 1) & 1)) return false;
         tc_fence_after();
         return true;
       };
-      for (int j = 0; j < M.n_blocks; ++j) {
-        const int jg = jbase + j, si = jg & 1;
-        auto publish = [&](int part) {
-          tmem_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(sh.p_full[si][part]));
-        };
-        if (!(ok = await_s(jg))) break;
-        if (idle) {  // whatever is there instead of P reaches only rows that are not stored
+      auto publish = [&](int part) {
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(sh.p_full[jg & 1][part]));
+      };
+      if (!(ok = await_s())) break;
+      const uint32_t s_addr = t_lane + L::col_s(jg & 1) + h * 64;
+      if (!idle) {  // (whatever is there instead of P reaches only rows that are not stored)
+        const int hi = min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64;
+        if (pass == kMaxima) {
+          mx_run = fmaxf(mx_run, half_max(s_addr, hi, sl2));
           publish(0);
           publish(1);
-          continue;
-        }
-        const uint32_t s_addr = t_lane + L::col_s(si) + h * 64;
-        const int jb = M.blk_lo + j;
-        if (based && !M.exact && jb < n_plain) {  // nothing to decide
-          inside &= softmax_based(s_addr, true, 64, sl2, m_run, l_half, publish);
-          continue;
-        }
-        const int hi = min(lim - jb * kBlk, kBlk);
-        const bool find_max =
-            M.exact || (!based && __any_sync(0xffffffffu, valid && m_run == NEG_INF && hi > 0));
-        if (!find_max) {
-          inside &= softmax_based(s_addr, false, hi - h * 64, sl2, m_run, l_half, publish);
-          continue;
-        }
-        const int par = jg & 1;
-        bool xok = true;
-        auto xchg = [&](float mx) {
-          sh.xmax[h][par][r_in] = mx;
-          publish_seq(&sh.xseq[0][h][quad], jg + 1);
-          xok = await_seq(&sh.xseq[0][h ^ 1][quad], jg + 1, sh);
-          return fmaxf(mx, sh.xmax[h ^ 1][par][r_in]);
-        };
-        const float alpha =
-            tc::softmax_half_max<false>(s_addr, -h * 64, hi - h * 64, sl2, m_run, l_half, xchg);
-        if (!(ok = __all_sync(0xffffffffu, xok))) break;
-        based = __all_sync(0xffffffffu, !valid || m_run != NEG_INF);
-        // Before O may be rescaled, P V of block jg - 1 must have landed.  The
-        // test is exact: P V (jg + 1) of the same buffer needs this block's first.
-        if (__any_sync(0xffffffffu, j > 0 && alpha != 1.f)) {
-          if (!(ok = wait_bar(sh.s_free[si ^ 1], ((jg - 1) >> 1) & 1))) break;
-          tc_fence_after();
-#pragma unroll 1
-          for (int c = 0; c < D / 2; c += 32) {
-            uint32_t o[32];
-            tmem_ld32(t_lane + o_col + c, o);
-            tmem_ld_wait32(o);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-            tmem_st32(t_lane + o_col + c, o);
+        } else {
+          if (j == 0 && pass == kFirst) {
+            sh.xmax[k & 1][h][r_in] = half_max(s_addr, hi, sl2);
+            publish_seq(&sh.max_seq[quad][h], k + 1);
+            if (!(ok = await_other(sh.max_seq, k))) break;
+            m_run = fmaxf(sh.xmax[k & 1][0][r_in], sh.xmax[k & 1][1][r_in]);
           }
+          inside &= softmax_half<false>(s_addr, hi, sl2, m_run, l4, publish);
         }
+      } else {
         publish(0);
         publish(1);
       }
-      if (!ok) break;
-      // ---------------------------------------------------- epilogue --
-      bool redo = false, mend = false;
-      if (!idle) {
-        // row sum over both halves (two buffers in turn: a half may be a unit ahead)
-        sh.xsum[k & 1][h][r_in] = l_half;
-        publish_seq(&sh.xseq[1][h][quad], k + 1);
-        if (!(ok = __all_sync(0xffffffffu, await_seq(&sh.xseq[1][h ^ 1][quad], k + 1, sh)))) break;
-      } else if (lane == 0) {  // (the count goes on for the units that this quadrant has rows of)
-        asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.xseq[1][h][quad])), "r"(k + 1)
-                     : "memory");
-      }
-      if (!(ok = wait_bar(sh.o_full, k & 1))) break;
-      tc_fence_after();
-      const size_t slot_pair = static_cast<size_t>(M.split) * p.T * p.H_q + pair;
-      if (!idle) {
-        const float l_run = l_half + sh.xsum[k & 1][h ^ 1][r_in];
-        // (a sum that is NaN stays one)
-        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-        const float lse = l_run == 0.f ? NEG_INF : l_run > 0.f ? lse_of(m_run, l_run) : l_run;
-        float2 finite = make_float2(0.f, 0.f);  // NaN once an infinity or NaN is added
-#pragma unroll 1
-        for (int c = 0; c < D / 2; c += 32) {
-          uint32_t o[32];
-          tmem_ld32(t_lane + o_col + c, o);
-          tmem_ld_wait32(o);
-          if (!valid) continue;
-#pragma unroll
-          for (int e = 0; e < 32; e += 2)
-            finite = __ffma2_rn(make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), make_float2(0.f, 0.f),
-                                finite);
-          const int dc = h * (D / 2) + c;  // output column
-          if (M.nsplit == 1) {
-            uint32_t w[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              w[e] = pack_bf16x2(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
-            __nv_bfloat16 *dst = p.out + pair * D + dc;
-            if (p.out_align32) {
-              st_global_v8(dst, w);
-              st_global_v8(dst + 16, w + 8);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 16; e += 4)
-                reinterpret_cast<uint4 *>(dst)[e / 4] = make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]);
-            }
-          } else {
-            float *dst = p.o_part + slot_pair * D + dc;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
-#pragma unroll
-            for (int e = 0; e < 32; e += 8) st_global_v8(dst + e, o + e);
-          }
+      ++jg;
+      ++j;
+      // blocks that every row of the warp sees all of: nothing to decide
+      if (pass != kMaxima && !idle && pending < 0) {
+        const int end = min(nb, n_plain);
+        while (j < end) {
+          if (!(ok = await_s())) break;
+          inside &= softmax_half<true>(t_lane + L::col_s(jg & 1) + h * 64, 64, sl2, m_run, l4, publish);
+          ++jg;
+          ++j;
         }
-        if (valid && h == 0) {
-          if (M.nsplit == 1) {
-            if (p.lse) p.lse[pair] = lse;
-          } else {
-            p.l_part[slot_pair] = lse;
-          }
-        }
-        const bool odd = valid && !(finite.x == 0.f && finite.y == 0.f);
-        redo = __any_sync(0xffffffffu, !M.exact && (odd || (valid && !inside)));
-        // a key that the tile sees and this row does not
-        mend = M.exact && odd && lim < M.pages * kPage && lim < M.L && l_run == l_run;
+        if (!ok) break;
       }
-      // O may be overwritten by the next unit once every warp has read it
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(bar(sh.o_empty));
-        if (redo) atomicOr(&sh.redo, 1u << (k & 31));
-        __threadfence_block();
-        atomicAdd(&sh.units_done, 1);
-      }
-      for (unsigned rows = __ballot_sync(0xffffffffu, mend); rows; rows &= rows - 1) {
-        const int src = __ffs(rows) - 1;
-        const int row_token = __shfl_sync(0xffffffffu, token, src), row_head = __shfl_sync(0xffffffffu, head, src);
-        const int row_lim = __shfl_sync(0xffffffffu, lim, src);
-        const size_t at = static_cast<size_t>(row_token) * p.H_q + row_head;
-        const int k0 = M.blk_lo * kBlk, k1 = min(row_lim, (M.blk_lo + M.n_blocks) * kBlk);
-        one_row<D>(p, M.seq, row_token, row_head, k0, k1, h,
-                   M.nsplit == 1 ? nullptr : p.o_part + (static_cast<size_t>(M.split) * p.T * p.H_q + at) * D,
-                   p.out + at * D);
-      }
-      jbase += M.n_blocks;
     }
     if (!ok && lane == 0) set_abort(sh, p.err);
   }
 
   // ------------------------------------------------------------ teardown --
-  if (warp == 1 || warp == kPvWarp) {
-    uint64_t &done = sh.mma_done[warp == 1 ? 0 : 1];
+  if (warp == kQkWarp || warp == kPvWarp) {
+    uint64_t &done = sh.mma_done[warp == kQkWarp ? 0 : 1];
     mma_commit(bar(done));
     mbar_wait(bar(done), 0);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) {
+  if (warp == kQkWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
   }
@@ -1010,13 +1116,13 @@ template <int D>
 cudaError_t launch(const ChunkParams &p, long long units, cudaStream_t s) {
   using L = Layout<D>;
   static_assert(L::kDynSmem + sizeof(Shared) <= 227 * 1024, "shared memory");
-  CUtensorMap tk, tv, tk8, tv8, tq;
-  const int run = std::min(kPagesPerBlock, p.num_pages);  // box never longer than the pool
+  CUtensorMap tk, tk4, tv, tv4, tq;
+  const int run = std::min(kPagesEach, p.num_pages);  // box never longer than the pool
   cudaError_t e = make_q_map(&tq, p, D);
   if (e == cudaSuccess) e = tc::make_page_map(&tk, p.k_cache, D, p.H_kv, p.num_pages);
   if (e == cudaSuccess) e = tc::make_page_map(&tv, p.v_cache, D, p.H_kv, p.num_pages);
-  if (e == cudaSuccess) e = tc::make_page_map(&tk8, p.k_cache, D, p.H_kv, p.num_pages, run);
-  if (e == cudaSuccess) e = tc::make_page_map(&tv8, p.v_cache, D, p.H_kv, p.num_pages, run);
+  if (e == cudaSuccess) e = tc::make_page_map(&tv4, p.v_cache, D, p.H_kv, p.num_pages, run);
+  if (e == cudaSuccess) e = tc::make_page_map(&tk4, p.k_cache, D, p.H_kv, p.num_pages, run);
   int dev = 0;
   if (e == cudaSuccess) e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -1034,7 +1140,7 @@ cudaError_t launch(const ChunkParams &p, long long units, cudaStream_t s) {
     configured.fetch_or(bit, std::memory_order_acq_rel);
   }
   const unsigned grid = static_cast<unsigned>(std::min<long long>(units, sms[dev & 63].load()));
-  e = launch_kernel(true, chunk_attn_kernel<D>, dim3(grid), dim3(kThreads), L::kDynSmem, s, tk, tv, tk8, tv8, tq, p);
+  e = launch_kernel(true, chunk_attn_kernel<D>, dim3(grid), dim3(kThreads), L::kDynSmem, s, tk, tk4, tv, tv4, tq, p);
   if (e != cudaSuccess || p.s_max == 1) return e;
   const size_t pairs = static_cast<size_t>(p.T) * p.H_q;
   return launch_kernel(true, chunk_merge_kernel<D>, dim3(static_cast<unsigned>((pairs + kMergeWarps - 1) / kMergeWarps)),
