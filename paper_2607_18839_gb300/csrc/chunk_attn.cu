@@ -23,19 +23,18 @@
 //               unit 68, so that two warps with eight boxes bounded the kernel.
 //   warp 4      Q tile into TMEM (tcgen05.cp), S = Q K^T into one of two buffers
 //   warp 5      O += P V, P read from TMEM where S was
-//   warps 8..15 softmax: two warpgroups, each with half of a block's keys and half
-//               of O's columns; a thread owns one row
+//   warps 8..15 softmax: two warpgroups, each with half of a block's keys; a
+//               thread owns one row
+//   warps 16..19 output: O of a finished unit, a row a thread, while the softmax
+//               warps are at the next unit
 // A row's base is its maximum over the unit's first block (every row that sees
-// keys of the unit sees some there), over which its two threads exchange their
-// maxima.  Exponentials are taken against that base throughout, which is exact to
+// keys of the unit sees some there), which both of its threads take.  Exponentials are taken against that base throughout, which is exact to
 // the same relative error as a running maximum as long as nothing overflows: a
 // unit in which a score exceeds its base by more than 2^64, or O is not finite, is
 // run again with its rows' true maxima, which a pass over S alone finds first.
 // Which units are is a matter of their own scores and values alone, so that a
 // call's bits do not depend on which CTA took which unit.  O is never rescaled.
-// A unit's output is written after the next unit's first exponentials, for which
-// the scores are there, while P V of its last block runs.  P goes to the tensor
-// cores in two parts: while the exponentials of a half's second 32 keys are taken,
+// P goes to the tensor cores in two parts: while the exponentials of a half's second 32 keys are taken,
 // P V of the first 32 runs.
 //
 // Rows that see no key are written by the scheduler.  Cache rows past a
@@ -66,13 +65,14 @@ constexpr int kPagesPerBlock = kBlk / kPage, kPagesEach = kPagesPerBlock / 2;  /
 constexpr int kProducers = 4;  // warps 0, 1: K; 2, 3: V
 constexpr int kQkWarp = 4, kPvWarp = 5, kSchedWarp = 6;
 constexpr int kSoftmaxWarp = 8, kSoftmaxWarps = 8;
-constexpr int kThreads = 32 * (kSoftmaxWarp + kSoftmaxWarps);
+constexpr int kOutputWarp = kSoftmaxWarp + kSoftmaxWarps, kOutputWarps = 4;
+constexpr int kThreads = 32 * (kOutputWarp + kOutputWarps);
 // What a pass over a unit does: exponentials against the first block's maxima;
 // nothing but the rows' maxima; exponentials against those.
 enum Pass { kFirst, kMaxima, kAgain };
 constexpr int kMetaSlots = 3;
-// of a metadata slot: producers, two MMA issuers, softmax warps
-constexpr uint32_t kMetaConsumers = kProducers + 2 + kSoftmaxWarps;
+// of a metadata slot: producers, two MMA issuers, softmax and output warps
+constexpr uint32_t kMetaConsumers = kProducers + 2 + kSoftmaxWarps + kOutputWarps;
 constexpr int kStages = 3;
 constexpr int kGroup = 256;      // sequences whose lengths the scheduler holds at once
 constexpr int kMaxSplits = 32;
@@ -96,7 +96,7 @@ struct ChunkParams {
   float *o_part;   // [s_max][T][H_q][D]
   float *l_part;   // [s_max][T][H_q]
   int *row_split;  // [T] splits of the row's tile
-  FastDiv div_G, div_Hkv;
+  FastDiv div_G, div_Hkv, div_tile;  // div_tile: tokens of a tile
 };
 
 // Metadata of one unit, written by the scheduler warp.
@@ -140,15 +140,16 @@ struct __align__(8) Shared {
   uint64_t mma_done[2];
   uint32_t tmem_base;
   int abort;
-  float xmax[2][2][kRows];  // [unit parity][half][row]: maxima of a unit's first block
-  float xsum[2][2][kRows];  // [unit parity][half][row]: sums (pass over maxima: maxima)
-  int max_seq[4][2], sum_seq[4][2];  // [quadrant][half]: units published
+  // of the last units: a row's base; its sums (pass over maxima: maxima) by half
+  float xbase[kMetaSlots][kRows], xsum[kMetaSlots][2][kRows];
+  int max_seq[4][2], sum_seq[4][2];  // [quadrant][half]: units whose maxima are taken, sums published
   unsigned redo;            // units (by number in this CTA, modulo 32) to run once more
-  int units_done;           // softmax warps that wrote a unit's output
+  int units_done;           // output warps that looked at a unit's output
   int unit_id[32];          // the last units issued
   UnitMeta meta[kMetaSlots];
-  // the scheduler's group of sequences: units before each, first rows, lengths, splits
-  int g_units[kGroup + 1], g_cu[kGroup + 1], g_len[kGroup], g_split[kGroup];
+  // the scheduler's group of sequences: units before each, first rows, rows, lengths,
+  // keys that all their rows see, splits
+  int g_units[kGroup], g_cu[kGroup], g_n[kGroup], g_len[kGroup], g_full[kGroup], g_split[kGroup];
 };
 
 __device__ __forceinline__ void set_abort(Shared &sh, uint32_t *err) {
@@ -188,31 +189,27 @@ __device__ __forceinline__ float lse_of(float m, float l) {
   return fmaf(static_cast<float>(e), kLn2, fmaf(m, kLn2, logf(f)));
 }
 
-__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
-// Largest score of a row's half block; hi: visible columns of the half.
-__device__ __forceinline__ float half_max(uint32_t s_addr, int hi, float sl2) {
+// Largest score of a row's 64 K columns (a pass over maxima: half a block; a
+// unit's first block: all of it, as reading the other thread's half costs less than
+// exchanging the maxima); hi: visible columns.
+template <int K>
+__device__ __forceinline__ float row_max(uint32_t s_addr, bool plain, int hi, float sl2) {
   const float NEG_INF = -__int_as_float(0x7f800000);
   const bool raw = sl2 > 0.f;
   float mx[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
 #pragma unroll 1
-  for (int part = 0; part < 2; ++part) {
-    uint32_t v[32];
-    tmem_ld32(s_addr + 32 * part, v);
+  for (int part = 0; part < K; ++part) {
+    uint32_t v[64];
+    tmem_ld32(s_addr + 64 * part, v);
+    tmem_ld32(s_addr + 64 * part + 32, v + 32);
     tmem_ld_wait32(v);
-    tc::mask32(v, 0, hi - 32 * part, !raw, sl2);
+    tmem_ld_wait32(v + 32);
+    if (!plain) {
+      tc::mask32(v, 0, hi - 64 * part, !raw, sl2);
+      tc::mask32(v + 32, 0, hi - 64 * part - 32, !raw, sl2);
+    }
 #pragma unroll
-    for (int c = 0; c < 32; c += 8)
+    for (int c = 0; c < 64; c += 8)
 #pragma unroll
       for (int a = 0; a < 4; ++a)
         mx[a] = tc::fmax3(mx[a], __uint_as_float(v[c + 2 * a]), __uint_as_float(v[c + 2 * a + 1]));
@@ -257,11 +254,11 @@ __device__ __forceinline__ bool softmax_half(uint32_t s_addr, int hi, float sl2,
 
 // One row over keys [lo, hi) of its sequence by one warp, from global memory and
 // nothing but what the row sees: for rows that a value of another row's keys may
-// have reached through the tensor cores.  Writes half h of the normalised row's
-// columns (o_f, or o_b if o_f is null).
+// have reached through the tensor cores.  Writes the normalised row (o_f, or o_b if
+// o_f is null).
 template <int D>
-__device__ __noinline__ void one_row(const ChunkParams &p, int seq, int token, int head, int lo, int hi, int h,
-                                     float *o_f, __nv_bfloat16 *o_b) {
+__device__ __noinline__ void one_row(const ChunkParams &p, int seq, int token, int head, int lo, int hi, float *o_f,
+                                     __nv_bfloat16 *o_b) {
   const int lane = threadIdx.x & 31, g = p.div_G(head);
   const float NEG_INF = -__int_as_float(0x7f800000);
   const __nv_bfloat16 *q = p.q + token * p.q_stride + head * D;
@@ -312,7 +309,6 @@ __device__ __noinline__ void one_row(const ChunkParams &p, int seq, int token, i
   const float inv = l > 0.f ? 1.f / l : l;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
-    if (c / (D / 64) != h) continue;
     if (o_f) o_f[c * 32 + lane] = o[c] * inv;
     else o_b[c * 32 + lane] = __float2bfloat16(o[c] * inv);
   }
@@ -358,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(bar(sh.taken), 1);
     mbar_init(bar(sh.o_full), 1);
-    mbar_init(bar(sh.o_empty), kSoftmaxWarps);
+    mbar_init(bar(sh.o_empty), kOutputWarps);
     mbar_init(bar(sh.mma_done[0]), 1);
     mbar_init(bar(sh.mma_done[1]), 1);
     fence_mbar_init();
@@ -383,31 +379,38 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto load_group = [&](int s0, int units_before) {
       g0 = s0;
       before = units_before;
-      int tiles[kGroup / 32], blocks[kGroup / 32];
+      const int count = min(kGroup, p.S - s0);
       long long total = 0;
-#pragma unroll
-      for (int k = 0; k < kGroup / 32; ++k) {
-        const int s = s0 + k * 32 + lane;
-        tiles[k] = blocks[k] = 0;
-        if (s < p.S) {
-          const int a0 = p.chunk_cu[s], a1 = p.chunk_cu[s + 1], len = p.seq_len[s];
-          const int c0 = min(max(a0, 0), p.T), c1 = max(c0, min(a1, p.T));
-          if (a0 != c0 || a1 != c1) flag_error(p.err, HPD_DEVERR_BRANCH_CU);
-          const int cap = p.max_pages * kPage, Ls = min(max(len, 0), cap);
-          if (Ls != len) flag_error(p.err, HPD_DEVERR_BRANCH_LEN);
-          tiles[k] = (c1 - c0 + TT - 1) / TT;
-          blocks[k] = ceil_div_i(Ls, kBlk);
-          total += static_cast<long long>(tiles[k]) * blocks[k];
-          sh.g_cu[k * 32 + lane] = c0;
-          // (a row range that the next sequence's offset contradicts)
-          sh.g_len[k * 32 + lane] = Ls;
-          if (k * 32 + lane == kGroup - 1 || s == p.S - 1) sh.g_cu[k * 32 + lane + 1] = c1;
-        }
+      // (loops left as loops, a step's loads ahead: code that runs once is bound by
+      // fetching it)
+      int a0 = 0, a1 = 0, len = 0, full = 0;
+      auto fetch = [&](int i) {
+        if (i >= count) return;
+        a0 = p.chunk_cu[s0 + i];
+        a1 = p.chunk_cu[s0 + i + 1];
+        len = p.seq_len[s0 + i];
+        if (p.full_len) full = p.full_len[s0 + i];
+      };
+      fetch(lane);
+#pragma unroll 1
+      for (int i = lane; i - lane < count; i += 32) {
+        const int b0 = a0, b1 = a1, b_len = len, b_full = full;
+        fetch(i + 32);
+        if (i >= count) continue;
+        const int c0 = min(max(b0, 0), p.T), c1 = max(c0, min(b1, p.T)), Ls = min(max(b_len, 0), p.max_pages * kPage);
+        if (b0 != c0 || b1 != c1) flag_error(p.err, HPD_DEVERR_BRANCH_CU);
+        if (Ls != b_len) flag_error(p.err, HPD_DEVERR_BRANCH_LEN);
+        const int tiles = p.div_tile(c1 - c0 + TT - 1);
+        total += static_cast<long long>(tiles) * ceil_div_i(Ls, kBlk);
+        sh.g_cu[i] = c0;
+        sh.g_n[i] = c1 - c0;
+        sh.g_len[i] = Ls;
+        sh.g_full[i] = min(max(b_full, 0), Ls);
       }
       // Blocks of a split: what one CTA's share of all blocks is.
       int per = 1 << 30;
       if (p.s_max > 1) {
-#pragma unroll
+#pragma unroll 1
         for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
         total *= p.H_kv;
         per = max(2, static_cast<int>((total + gridDim.x - 1) / gridDim.x));
@@ -415,20 +418,24 @@ __global__ void __launch_bounds__(kThreads, 1)
       // (sums that stop at kNoUnit, which offsets out of order could pass)
       auto add = [](int a, int b) { return min(a + b, kNoUnit); };
       int base = 0;
-#pragma unroll
-      for (int k = 0; k < kGroup / 32; ++k) {
-        if (s0 + k * 32 >= p.S) break;
-        const int nsplit = p.s_max > 1 ? min(p.s_max, max(1, (blocks[k] + per - 1) / per)) : 1;
-        const int units = min(tiles[k] * nsplit * p.H_kv, kNoUnit);
+#pragma unroll 1
+      for (int i = lane; i - lane < count; i += 32) {
+        int units = 0, nsplit = 1;
+        if (i < count) {
+          if (p.s_max > 1) nsplit = min(p.s_max, max(1, (ceil_div_i(sh.g_len[i], kBlk) + per - 1) / per));
+          units = min(p.div_tile(sh.g_n[i] + TT - 1) * nsplit * p.H_kv, kNoUnit);
+        }
         int incl = units;
-#pragma unroll
+#pragma unroll 1
         for (int o = 1; o < 32; o <<= 1) {
           const int v = __shfl_up_sync(0xffffffffu, incl, o);
           if (lane >= o) incl = add(incl, v);
         }
         const int prior = __shfl_up_sync(0xffffffffu, incl, 1);
-        sh.g_units[k * 32 + lane] = add(base, lane ? prior : 0);
-        sh.g_split[k * 32 + lane] = nsplit;
+        if (i < count) {
+          sh.g_units[i] = add(base, lane ? prior : 0);
+          sh.g_split[i] = nsplit;
+        }
         base = add(base, __shfl_sync(0xffffffffu, incl, 31));
       }
       group_units = base;
@@ -438,6 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     unsigned redo = 0;  // units to run again
     int again = -1;     // the unit whose maxima the last pass took
     int outputs = 0;    // passes that write a unit's output
+    bool asked = false;
     int nb_last = 0, nb_before = 0;
     auto take_redo = [&] {
       unsigned r = 0;
@@ -475,16 +483,19 @@ __global__ void __launch_bounds__(kThreads, 1)
           redo &= redo - 1;
         } else {
           pass = kFirst;
-          u = 0;
-          if (lane == 0) u = atomicAdd(p.unit_ctr, 1);
-          u = __shfl_sync(0xffffffffu, u, 0);
+          u = blockIdx.x;  // the first one asked for; then whatever is next
+          if (asked) {
+            if (lane == 0) u = gridDim.x + atomicAdd(p.unit_ctr, 1);
+            u = __shfl_sync(0xffffffffu, u, 0);
+          }
+          asked = true;
           if (__any_sync(0xffffffffu, aborted(sh))) break;
         }
         if (!locate(u)) {
           // none left, once the units still running (the last two) need not be run
           // again; who gives up here has set the abort word and the error
           const uint64_t limit = kWaitLimitNs + (static_cast<uint64_t>(nb_last) + nb_before) * kBlockLimitNs;
-          if (!__all_sync(0xffffffffu, await_count(smem_u32(&sh.units_done), kSoftmaxWarps * outputs, &sh.abort, p.err,
+          if (!__all_sync(0xffffffffu, await_count(smem_u32(&sh.units_done), kOutputWarps * outputs, &sh.abort, p.err,
                                                    HPD_DEVERR_TIMEOUT, limit)))
             break;
           redo = take_redo();
@@ -496,12 +507,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int mid = (lo + hi) >> 1;
           if (sh.g_units[mid] <= u - before) lo = mid; else hi = mid;
         }
-        const int c0 = sh.g_cu[lo], n = max(0, sh.g_cu[lo + 1] - c0), len = sh.g_len[lo], nsplit = sh.g_split[lo];
-        const int full = p.full_len ? min(max(p.full_len[g0 + lo], 0), len) : 0;
+        const int c0 = sh.g_cu[lo], n = sh.g_n[lo], len = sh.g_len[lo], full = sh.g_full[lo], nsplit = sh.g_split[lo];
         int idx = u - before - sh.g_units[lo];
         const int us = p.div_Hkv(idx), g = idx - us * p.H_kv;
         const int ut = nsplit > 1 ? us / nsplit : us, split = us - ut * nsplit;
-        const int tile = (n + TT - 1) / TT - 1 - ut;
+        const int tile = p.div_tile(n + TT - 1) - 1 - ut;
         const int i0 = tile * TT, ntok = min(TT, n - i0), nrows = ntok * G;
         const int lim0 = len - n + i0 + 1;
         const int kmax = min(max(max(lim0 + ntok - 1, full), 0), len);
@@ -771,160 +781,133 @@ __global__ void __launch_bounds__(kThreads, 1)
       ++outputs;
     }
     if (!ok && lane == 0) set_abort(sh, p.err);
+  } else if (warp >= kOutputWarp) {
+    // ---------------------------------------------------------- output --
+    const int quad = warp & 3;          // TMEM lane quadrant this warp may access
+    const int r_in = quad * 32 + lane;  // row within the tile
+    const uint32_t o_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::kColO;
+    const int rt = p.div_G(r_in);
+    int outputs = 0;
+    bool ok = true;
+    for (int k = 0; ok; ++k) {
+      const int slot = k % kMetaSlots;
+      if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
+      const UnitMeta &M = sh.meta[slot];
+      if (!M.valid) break;
+      const int pass = M.pass;
+      if (pass != kMaxima) {
+        const bool valid = r_in < M.nrows, idle = quad * 32 >= M.nrows;
+        const int lim = min(max(M.lim0 + rt, M.full), M.L), nsplit = M.nsplit;
+        const int token = M.tok0 + rt, head = M.g * G + r_in - rt * G;
+        const size_t pair = static_cast<size_t>(token) * p.H_q + head;
+        const size_t slot_pair = static_cast<size_t>(M.split) * p.T * p.H_q + pair;
+        float l = 0.f, inv = 0.f;
+        if (!idle) {
+          if (!(ok = __all_sync(0xffffffffu, await_seq(&sh.sum_seq[quad][0], k + 1, sh) &&
+                                                 await_seq(&sh.sum_seq[quad][1], k + 1, sh))))
+            break;
+          l = sh.xsum[slot][0][r_in] + sh.xsum[slot][1][r_in];
+          inv = l == 0.f ? 0.f : 1.f / l;  // (a sum that is NaN stays one)
+          if (valid) {
+            const float lse = l == 0.f ? NEG_INF : l > 0.f ? lse_of(sh.xbase[slot][r_in], l) : l;
+            if (nsplit > 1) p.l_part[slot_pair] = lse;
+            else if (p.lse) p.lse[pair] = lse;
+          }
+        }
+        if (!(ok = wait_bar(sh.o_full, outputs & 1))) break;
+        ++outputs;
+        tc_fence_after();
+        float2 finite = make_float2(0.f, 0.f);  // NaN once an infinity or NaN is added
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          if (!idle) {
+            tmem_ld32(o_addr + c, o);
+            tmem_ld_wait32(o);
+          }
+          if (c == D - 32) {  // O may be overwritten once every warp has read it
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.o_empty));
+          }
+          if (idle || !valid) continue;
+#pragma unroll
+          for (int e = 0; e < 32; e += 2)
+            finite = __ffma2_rn(make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), make_float2(0.f, 0.f),
+                                finite);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
+          if (nsplit == 1) {
+            __nv_bfloat16 *dst = p.out + pair * D + c;
+#pragma unroll
+            for (int e = 0; e < 32; e += 2)
+              o[e / 2] = pack_bf16x2(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
+            if (p.out_align32) {  // 32-byte stores: each fills a sector
+              st_global_v8(dst, o);
+              st_global_v8(dst + 16, o + 8);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 16; e += 4)
+                reinterpret_cast<uint4 *>(dst)[e / 4] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            }
+          } else {
+            float *dst = p.o_part + slot_pair * D + c;
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) st_global_v8(dst + e, o + e);
+          }
+        }
+        const bool odd = !idle && valid && !(finite.x == 0.f && finite.y == 0.f);
+        const bool redo = __any_sync(0xffffffffu, pass == kFirst && (odd || (!idle && valid && l != l)));
+        if (lane == 0) {
+          if (redo) atomicOr(&sh.redo, 1u << (k & 31));
+          asm volatile("red.release.cta.shared::cta.add.u32 [%0], 1;" ::"r"(smem_u32(&sh.units_done)) : "memory");
+        }
+        // a key that the tile sees and this row does not
+        const bool mend = pass == kAgain && odd && lim < M.pages * kPage && lim < M.L && l == l;
+        for (unsigned rows = __ballot_sync(0xffffffffu, mend); rows; rows &= rows - 1) {
+          const int src = __ffs(rows) - 1;
+          const int row_token = __shfl_sync(0xffffffffu, token, src), row_head = __shfl_sync(0xffffffffu, head, src);
+          const int row_lim = __shfl_sync(0xffffffffu, lim, src);
+          const size_t at = static_cast<size_t>(row_token) * p.H_q + row_head;
+          const int k0 = M.blk_lo * kBlk, k1 = min(row_lim, (M.blk_lo + M.n_blocks) * kBlk);
+          one_row<D>(p, M.seq, row_token, row_head, k0, k1,
+                     nsplit == 1 ? nullptr : p.o_part + (static_cast<size_t>(M.split) * p.T * p.H_q + at) * D,
+                     p.out + at * D);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
+    }
+    if (!ok && lane == 0) set_abort(sh, p.err);
   } else if (warp >= kSoftmaxWarp) {
     // --------------------------------------------------------- softmax --
-    const int h = (warp - kSoftmaxWarp) >> 2;  // half of a block's keys, and of O's columns
+    const int h = (warp - kSoftmaxWarp) >> 2;  // half of a block's keys
     const int quad = warp & 3;                 // TMEM lane quadrant this warp may access
     const int r_in = quad * 32 + lane;         // row within the tile
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     const int rt = p.div_G(r_in);
     const float sl2 = p.scale_log2;
-    // The other half has published unit k, too.
+    // The other half has published unit k.
     auto await_other = [&](const int (*seq)[2], int k) {
       return __all_sync(0xffffffffu, await_seq(&seq[quad][h ^ 1], k + 1, sh));
     };
-    int k = 0, j = 0, jg = 0;    // unit, block of it, blocks in all
-    int outputs = 0;
-    int pending = -1;            // the unit whose output is to be written, its row's base
-    float m_pending = 0.f;
-    bool loaded = false;         // unit k's metadata
-    int nb = 0, blk_lo = 0, pass = kFirst, lim = 0, n_plain = 0;
-    bool valid_unit = false, idle = false;
-    float m_run = NEG_INF, given = NEG_INF, mx_run = NEG_INF;
-    float2 l4[4];                // the row's sum so far, in parts
-    bool inside = true;          // the scores stay in the window of their base
+    int jg = 0;            // blocks in all
+    float given = NEG_INF;  // the row's maximum, which a pass over the maxima found
     bool ok = true;
-    for (;;) {
-      // A unit's output comes after the next unit's first exponentials; at once
-      // when there is no next unit (yet).
-      if (pending >= 0 &&
-          (loaded ? !valid_unit || j > 0
-                  : !__all_sync(0xffffffffu, mbar_test_wait(bar(sh.meta_full[k % kMetaSlots]), (k / kMetaSlots) & 1)))) {
-        const UnitMeta &M = sh.meta[pending % kMetaSlots];
-        const bool valid = r_in < M.nrows, out_idle = quad * 32 >= M.nrows;
-        const int out_lim = min(max(M.lim0 + rt, M.full), M.L), out_pass = M.pass, nsplit = M.nsplit;
-        const int token = M.tok0 + rt, head = M.g * G + r_in - rt * G;
-        const size_t pair = static_cast<size_t>(token) * p.H_q + head;
-        const size_t slot_pair = static_cast<size_t>(M.split) * p.T * p.H_q + pair;
-        bool redo = false, mend = false;
-        if (!out_idle && !(ok = await_other(sh.sum_seq, pending))) break;
-        if (!(ok = wait_bar(sh.o_full, outputs & 1))) break;
-        ++outputs;
-        tc_fence_after();
-        if (!out_idle) {
-          const float l = sh.xsum[pending & 1][0][r_in] + sh.xsum[pending & 1][1][r_in];
-          // (a sum that is NaN stays one)
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          float2 finite = make_float2(0.f, 0.f);  // NaN once an infinity or NaN is added
-#pragma unroll 1
-          for (int c = 0; c < D / 2; c += 32) {
-            uint32_t o[32];
-            tmem_ld32(t_lane + L::kColO + h * (D / 2) + c, o);
-            tmem_ld_wait32(o);
-            if (!valid) continue;
-#pragma unroll
-            for (int e = 0; e < 32; e += 2)
-              finite = __ffma2_rn(make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), make_float2(0.f, 0.f),
-                                  finite);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
-            const int dc = h * (D / 2) + c;  // output column
-            if (nsplit == 1) {
-              __nv_bfloat16 *dst = p.out + pair * D + dc;
-#pragma unroll
-              for (int e = 0; e < 32; e += 2)
-                o[e / 2] = pack_bf16x2(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
-              if (p.out_align32) {  // 32-byte stores: each fills a sector
-                st_global_v8(dst, o);
-                st_global_v8(dst + 16, o + 8);
-              } else {
-#pragma unroll
-                for (int e = 0; e < 16; e += 4)
-                  reinterpret_cast<uint4 *>(dst)[e / 4] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-              }
-            } else {
-              float *dst = p.o_part + slot_pair * D + dc;
-#pragma unroll
-              for (int e = 0; e < 32; e += 8) st_global_v8(dst + e, o + e);
-            }
-          }
-          if (valid && h == 0) {
-            const float lse = l == 0.f ? NEG_INF : l > 0.f ? lse_of(m_pending, l) : l;
-            if (nsplit > 1) p.l_part[slot_pair] = lse;
-            else if (p.lse) p.lse[pair] = lse;
-          }
-          const bool odd = valid && !(finite.x == 0.f && finite.y == 0.f);
-          redo = __any_sync(0xffffffffu, out_pass == kFirst && (odd || (valid && l != l)));
-          // a key that the tile sees and this row does not
-          mend = out_pass == kAgain && odd && out_lim < M.pages * kPage && out_lim < M.L && l == l;
-        }
-        // O may be overwritten by the next unit once every warp has read it
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(bar(sh.o_empty));
-          if (redo) atomicOr(&sh.redo, 1u << (pending & 31));
-          __threadfence_block();
-          atomicAdd(&sh.units_done, 1);
-        }
-        for (unsigned rows = __ballot_sync(0xffffffffu, mend); rows; rows &= rows - 1) {
-          const int src = __ffs(rows) - 1;
-          const int row_token = __shfl_sync(0xffffffffu, token, src), row_head = __shfl_sync(0xffffffffu, head, src);
-          const int row_lim = __shfl_sync(0xffffffffu, out_lim, src);
-          const size_t at = static_cast<size_t>(row_token) * p.H_q + row_head;
-          const int k0 = M.blk_lo * kBlk, k1 = min(row_lim, (M.blk_lo + M.n_blocks) * kBlk);
-          one_row<D>(p, M.seq, row_token, row_head, k0, k1, h,
-                     nsplit == 1 ? nullptr : p.o_part + (static_cast<size_t>(M.split) * p.T * p.H_q + at) * D,
-                     p.out + at * D);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(sh.meta_empty[pending % kMetaSlots]));
-        pending = -1;
-      }
-      if (!loaded) {
-        const int slot = k % kMetaSlots;
-        if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
-        const UnitMeta &M = sh.meta[slot];
-        loaded = true;
-        valid_unit = M.valid != 0;
-        nb = M.n_blocks;
-        blk_lo = M.blk_lo;
-        pass = M.pass;
-        idle = quad * 32 >= M.nrows;
-        // (rows that are no query count as seeing everything, so that their warp
-        // needs no masks for them; their results are not stored)
-        lim = r_in < M.nrows ? min(max(M.lim0 + rt, M.full), M.L) : 1 << 30;
-        // blocks of the unit that every row of the warp sees all of
-        n_plain = sl2 > 0.f ? max(__reduce_min_sync(0xffffffffu, lim), 0) / kBlk - blk_lo : 0;
-        j = 0;
-        m_run = given;
-        mx_run = NEG_INF;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) l4[i] = make_float2(0.f, 0.f);
-        inside = true;
-        if (!valid_unit && pending >= 0) continue;
-      }
-      if (!valid_unit) break;
-      if (j == nb) {  // the unit's sums (maxima), two buffers in turn
-        if (!idle) {
-          sh.xsum[k & 1][h][r_in] = pass == kMaxima ? mx_run : inside ? tc::sum_of(l4) : __int_as_float(0x7fffffff);
-          publish_seq(&sh.sum_seq[quad][h], k + 1);
-        }
-        if (pass == kMaxima) {
-          if (!idle) {
-            if (!(ok = await_other(sh.sum_seq, k))) break;
-            given = fmaxf(sh.xsum[k & 1][0][r_in], sh.xsum[k & 1][1][r_in]);
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(sh.meta_empty[k % kMetaSlots]));
-        } else {
-          pending = k;
-          m_pending = m_run;
-        }
-        ++k;
-        loaded = false;
-        continue;
-      }
+    for (int k = 0; ok; ++k) {
+      const int slot = k % kMetaSlots;
+      if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
+      const UnitMeta &M = sh.meta[slot];
+      if (!M.valid) break;
+      const int nb = M.n_blocks, blk_lo = M.blk_lo, pass = M.pass, nrows = M.nrows;
+      const bool idle = quad * 32 >= nrows;
+      // (rows that are no query count as seeing everything, so that their warp
+      // needs no masks for them; their results are not stored)
+      const int lim = r_in < nrows ? min(max(M.lim0 + rt, M.full), M.L) : 1 << 30;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
+      // blocks of the unit that every row of the warp sees all of
+      const int n_plain = sl2 > 0.f ? min(max(__reduce_min_sync(0xffffffffu, lim), 0) / kBlk - blk_lo, nb) : 0;
       auto await_s = [&] {
         if (!wait_bar(sh.s_full[jg & 1], (jg >> 1) & 1)) return false;
         tc_fence_after();
@@ -936,39 +919,55 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(sh.p_full[jg & 1][part]));
       };
-      if (!(ok = await_s())) break;
-      const uint32_t s_addr = t_lane + L::col_s(jg & 1) + h * 64;
-      if (!idle) {  // (whatever is there instead of P reaches only rows that are not stored)
-        const int hi = min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64;
-        if (pass == kMaxima) {
-          mx_run = fmaxf(mx_run, half_max(s_addr, hi, sl2));
+      if (idle) {  // (whatever is there instead of P reaches only rows that are not stored)
+        for (int j = 0; j < nb; ++j, ++jg) {
+          if (!(ok = await_s())) break;
           publish(0);
           publish(1);
-        } else {
-          if (j == 0 && pass == kFirst) {
-            sh.xmax[k & 1][h][r_in] = half_max(s_addr, hi, sl2);
-            publish_seq(&sh.max_seq[quad][h], k + 1);
-            if (!(ok = await_other(sh.max_seq, k))) break;
-            m_run = fmaxf(sh.xmax[k & 1][0][r_in], sh.xmax[k & 1][1][r_in]);
-          }
-          inside &= softmax_half<false>(s_addr, hi, sl2, m_run, l4, publish);
         }
-      } else {
-        publish(0);
-        publish(1);
+        continue;
       }
-      ++jg;
-      ++j;
-      // blocks that every row of the warp sees all of: nothing to decide
-      if (pass != kMaxima && !idle && pending < 0) {
-        const int end = min(nb, n_plain);
-        while (j < end) {
-          if (!(ok = await_s())) break;
-          inside &= softmax_half<true>(t_lane + L::col_s(jg & 1) + h * 64, 64, sl2, m_run, l4, publish);
-          ++jg;
-          ++j;
+      float m_run = given, mx_run = NEG_INF;
+      float2 l4[4];         // the row's sum so far, in parts
+      bool inside = true;   // the scores stay in the window of their base
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l4[i] = make_float2(0.f, 0.f);
+      for (int j = 0; j < nb; ++j, ++jg) {
+        // blocks that every row of the warp sees all of, once the base is there:
+        // nothing to decide
+        if (pass != kMaxima && (j > 0 || pass == kAgain)) {
+          for (; j < n_plain; ++j, ++jg) {
+            if (!(ok = await_s())) break;
+            inside &= softmax_half<true>(t_lane + L::col_s(jg & 1) + h * 64, 64, sl2, m_run, l4, publish);
+          }
+          if (!ok || j >= nb) break;
         }
-        if (!ok) break;
+        if (!(ok = await_s())) break;
+        const uint32_t s_addr = t_lane + L::col_s(jg & 1) + h * 64;
+        const int hi = min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64;
+        if (pass == kMaxima) {
+          mx_run = fmaxf(mx_run, row_max<1>(s_addr, j < n_plain, hi, sl2));
+          publish(0);
+          publish(1);
+          continue;
+        }
+        if (j == 0 && pass == kFirst) {
+          m_run = row_max<2>(t_lane + L::col_s(jg & 1), n_plain > 0, hi + h * 64, sl2);
+          // (P of either half may replace scores only once the other half has read them)
+          tc_fence_before();
+          publish_seq(&sh.max_seq[quad][h], k + 1);
+          if (!(ok = await_other(sh.max_seq, k))) break;
+          tc_fence_after();
+        }
+        inside &= softmax_half<false>(s_addr, hi, sl2, m_run, l4, publish);
+      }
+      if (!ok) break;
+      sh.xsum[slot][h][r_in] = pass == kMaxima ? mx_run : inside ? tc::sum_of(l4) : __int_as_float(0x7fffffff);
+      if (h == 0) sh.xbase[slot][r_in] = m_run;
+      publish_seq(&sh.sum_seq[quad][h], k + 1);
+      if (pass == kMaxima) {
+        if (!(ok = await_other(sh.sum_seq, k))) break;
+        given = fmaxf(sh.xsum[slot][0][r_in], sh.xsum[slot][1][r_in]);
       }
     }
     if (!ok && lane == 0) set_abort(sh, p.err);
@@ -1201,6 +1200,7 @@ hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *a, hpd_stream_t stream) {
   k.row_split = reinterpret_cast<int *>(ws + pl.off_rows);
   k.div_G.set(k.G);
   k.div_Hkv.set(k.H_kv);
+  k.div_tile.set(kRows / k.G);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e = a->D == 64 ? launch<64>(k, pl.units, s) : launch<128>(k, pl.units, s);
   return e == cudaSuccess ? HPD_OK : record_cuda_error(e);
