@@ -27,15 +27,17 @@
 //               thread owns one row
 //   warps 16..19 output: O of a finished unit, a row a thread, while the softmax
 //               warps are at the next unit
-// A row's base is its maximum over the unit's first block (every row that sees
-// keys of the unit sees some there), which both of its threads take.  Exponentials are taken against that base throughout, which is exact to
+// A row's base is its maximum over keys 0-31 and 64-95 of the unit's first block
+// (a row that sees any key of the unit sees key 0 of that): the scores that P does
+// not replace, so that both threads of the row read them and neither waits for the
+// other.  Exponentials are taken against that base throughout, which is exact to
 // the same relative error as a running maximum as long as nothing overflows: a
 // unit in which a score exceeds its base by more than 2^64, or O is not finite, is
 // run again with its rows' true maxima, which a pass over S alone finds first.
 // Which units are is a matter of their own scores and values alone, so that a
 // call's bits do not depend on which CTA took which unit.  O is never rescaled.
-// P goes to the tensor cores in two parts: while the exponentials of a half's second 32 keys are taken,
-// P V of the first 32 runs.
+// P goes to the tensor cores in two parts: while the exponentials of the second 32 keys of a half are
+// taken, P V of the first 32 runs.
 //
 // Rows that see no key are written by the scheduler.  Cache rows past a
 // sequence's end may hold anything: pages past it are not loaded (their box lies
@@ -88,7 +90,6 @@ struct ChunkParams {
   int S, T, H_q, H_kv, G, num_pages, max_pages;
   float scale_log2;
   __nv_bfloat16 *out;
-  bool out_align32;
   float *lse;
   uint32_t *err;
   int *unit_ctr;   // [2] next unit and finished CTAs, zero between calls
@@ -99,19 +100,25 @@ struct ChunkParams {
   FastDiv div_G, div_Hkv, div_tile;  // div_tile: tokens of a tile
 };
 
-// Metadata of one unit, written by the scheduler warp.
-struct UnitMeta {
+// Metadata of one unit, written by the scheduler warp, read 16 bytes at a time.
+struct __align__(16) UnitMeta {
   int valid;     // 0: no units left
-  int g, split, nsplit;
-  int seq;
-  int tok0;      // first row (of T) of the tile
+  int n_blocks, blk_lo;
+  int pass;
   int nrows;     // stacked rows
   int lim0;      // keys that the tile's first token sees by its place (a token more each)
   int full, L;   // keys that every token sees; tokens of the sequence
+  int seq, g;
+  int tok0;      // first row (of T) of the tile
   int pages;     // pages up to the last key that the tile sees
-  int blk_lo, n_blocks;
-  int pass;
+  int split, nsplit, pad[2];
 };
+__device__ __forceinline__ UnitMeta read_meta(const UnitMeta &m) {
+  UnitMeta r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<int4 *>(&r)[i] = reinterpret_cast<const int4 *>(&m)[i];
+  return r;
+}
 
 template <int D>
 struct Layout {
@@ -122,7 +129,8 @@ struct Layout {
   static constexpr uint32_t kGroupBytes = kChunks * 1024, kPageBytes = 2 * kGroupBytes;
   static constexpr uint32_t kK = 0;
   static constexpr uint32_t kV = kK + kStages * kTileBytes;
-  static constexpr uint32_t kBytes = kV + kStages * kTileBytes;
+  static constexpr uint32_t kStage = kV + kStages * kTileBytes;  // 128 bytes of each output row
+  static constexpr uint32_t kBytes = kStage + kRows * 128;
   static constexpr uint32_t kDynSmem = kBytes + 1024;   // slack to align to 1024
   // TMEM columns: S of block buffer i, O, Q rows of unit slot u
   static constexpr uint32_t kColO = 256;
@@ -130,19 +138,20 @@ struct Layout {
   static __device__ __forceinline__ uint32_t col_q(int u) { return u ? 448u : 384u; }
 };
 
-struct __align__(8) Shared {
+struct __align__(16) Shared {
   uint64_t meta_full[kMetaSlots], meta_empty[kMetaSlots];
   uint64_t taken;  // the K producer has begun a unit
   uint64_t k_full[kStages], v_full[kStages], k_empty[kStages], v_empty[kStages];
   // per S buffer: scores written; P written, by part; P V issued
   uint64_t s_full[2], p_full[2][2], s_free[2];
+  uint64_t sums[kMetaSlots];  // of the unit in the slot (softmax may be units ahead of its output)
   uint64_t o_full, o_empty;
   uint64_t mma_done[2];
   uint32_t tmem_base;
   int abort;
   // of the last units: a row's base; its sums (pass over maxima: maxima) by half
   float xbase[kMetaSlots][kRows], xsum[kMetaSlots][2][kRows];
-  int max_seq[4][2], sum_seq[4][2];  // [quadrant][half]: units whose maxima are taken, sums published
+  int max_seq[4][2];  // [quadrant][half]: units whose maxima are published
   unsigned redo;            // units (by number in this CTA, modulo 32) to run once more
   int units_done;           // output warps that looked at a unit's output
   int unit_id[32];          // the last units issued
@@ -182,6 +191,21 @@ __device__ __forceinline__ bool await_seq(const int *flag, int seq, const Shared
   return load_seq(flag) >= seq || await_seq_slow(flag, seq, &sh.abort);
 }
 
+// Wait until n output warps have looked at their units; false when the time is up
+// or a wait elsewhere gave up.
+__device__ __noinline__ bool await_outputs(Shared &sh, int n, uint64_t limit_ns, uint32_t *err) {
+  const uint64_t t0 = globaltimer();
+  for (uint32_t i = 1; load_seq(&sh.units_done) < n; ++i) {
+    if ((i & 63u) != 0) continue;
+    if (aborted(sh)) return false;
+    if (globaltimer() - t0 > limit_ns) {
+      set_abort(sh, err);
+      return false;
+    }
+  }
+  return true;
+}
+
 // Natural log of 2^m * l with one rounding at the result's size.
 __device__ __forceinline__ float lse_of(float m, float l) {
   const int e = static_cast<int>(__float_as_uint(l) >> 23) - 127;
@@ -189,66 +213,70 @@ __device__ __forceinline__ float lse_of(float m, float l) {
   return fmaf(static_cast<float>(e), kLn2, fmaf(m, kLn2, logf(f)));
 }
 
-// Largest score of a row's 64 K columns (a pass over maxima: half a block; a
-// unit's first block: all of it, as reading the other thread's half costs less than
-// exchanging the maxima); hi: visible columns.
-template <int K>
-__device__ __forceinline__ float row_max(uint32_t s_addr, bool plain, int hi, float sl2) {
+// Largest score of 32 columns at s_addr and of 32 at s_addr + apart; hi: visible
+// columns, the second 32 starting at `apart`.  (Out of line, one loop: code off the
+// inner loops exists once and keeps its loops, as the CTA is bound by fetching it.)
+__device__ __noinline__ float row_max(uint32_t s_addr, int apart, bool plain, int hi, float sl2) {
   const float NEG_INF = -__int_as_float(0x7f800000);
   const bool raw = sl2 > 0.f;
   float mx[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
 #pragma unroll 1
-  for (int part = 0; part < K; ++part) {
-    uint32_t v[64];
-    tmem_ld32(s_addr + 64 * part, v);
-    tmem_ld32(s_addr + 64 * part + 32, v + 32);
+  for (int part = 0; part < 2; ++part) {
+    uint32_t v[32];
+    tmem_ld32(s_addr, v);
     tmem_ld_wait32(v);
-    tmem_ld_wait32(v + 32);
-    if (!plain) {
-      tc::mask32(v, 0, hi - 64 * part, !raw, sl2);
-      tc::mask32(v + 32, 0, hi - 64 * part - 32, !raw, sl2);
-    }
+    if (!plain) tc::mask32(v, 0, hi, !raw, sl2);
 #pragma unroll
-    for (int c = 0; c < 64; c += 8)
+    for (int c = 0; c < 32; c += 8)
 #pragma unroll
       for (int a = 0; a < 4; ++a)
         mx[a] = tc::fmax3(mx[a], __uint_as_float(v[c + 2 * a]), __uint_as_float(v[c + 2 * a + 1]));
+    s_addr += apart;
+    hi -= apart;
   }
   return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * (raw ? sl2 : 1.f);
 }
 
-// A row's half block: P = exp2(scaled score - base) as bf16 pairs where the scores
-// were, and its sum; publish(part) once P of the half's first (second) 32 keys is
-// on its way.  PLAIN: every row of the warp sees every key, and the scale
-// is positive (its order is then the raw scores').  Returns false when a score
-// lies above the window of the base.
-template <bool PLAIN, class Publish>
-__device__ __forceinline__ bool softmax_half(uint32_t s_addr, int hi, float sl2, float m_run, float2 *l4,
-                                             Publish publish) {
+// A row's half block: P = exp2(scaled score - base) as bf16 pairs, and its sum.  P of
+// the half's keys 32-63 goes to the first 16 columns of their scores, then P of keys
+// 0-31 to the next 16: publish(part) once it is on its way.  (The scores of keys 0-31
+// stay until the next Q K^T.)  Returns false when a score lies above the window of
+// the base.  Here every row of the warp sees every key and the scale is positive (its
+// order is then the raw scores').
+template <class Publish>
+__device__ __forceinline__ bool softmax_plain(uint32_t s_addr, float sl2, float m_run, float2 *l4, Publish publish) {
   const float NEG_INF = -__int_as_float(0x7f800000);
-  if (!PLAIN && __all_sync(0xffffffffu, hi <= 0)) {  // no row of the warp sees a key of the half
-    uint32_t z[32];
-#pragma unroll
-    for (int c = 0; c < 32; ++c) z[c] = 0u;
-    tmem_st32(s_addr, z);
-    publish(0);
-    publish(1);
-    return true;
-  }
-  const bool raw = PLAIN || sl2 > 0.f;
-  const float mul = raw ? sl2 : 1.f, base = m_run == NEG_INF ? 0.f : m_run;
   float mx4[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
+  const float base = m_run == NEG_INF ? 0.f : m_run;
   uint32_t v[64];
-  tmem_ld32(s_addr, v);
+  tmem_ld32(s_addr + 32, v);
   tmem_ld_wait32(v);
-  tmem_ld32(s_addr + 32, v + 32);
-  if (!PLAIN) tc::mask32(v, 0, hi, !raw, sl2);
-  tc::exp32<true, false>(s_addr, v, mul, base, l4, mx4);
+  tmem_ld32(s_addr, v + 32);
+  tc::exp32<true, false>(s_addr + 32, v, sl2, base, l4, mx4);
   publish(0);
   tmem_ld_wait32(v + 32);
-  if (!PLAIN) tc::mask32(v + 32, 0, hi - 32, !raw, sl2);
-  tc::exp32<true, false>(s_addr + 16, v + 32, mul, base, l4, mx4);
+  tc::exp32<true, false>(s_addr + 48, v + 32, sl2, base, l4, mx4);
   publish(1);
+  return fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * sl2 <= base + tc::kWindowLog2;
+}
+// The same where rows see some of the keys, or the scale is not positive.  hi: visible
+// columns of the half.
+template <class Publish>
+__device__ __forceinline__ bool softmax_masked(uint32_t s_addr, int hi, float sl2, float m_run, float2 *l4,
+                                               Publish publish) {
+  const float NEG_INF = -__int_as_float(0x7f800000);
+  const bool raw = sl2 > 0.f;
+  const float mul = raw ? sl2 : 1.f, base = m_run == NEG_INF ? 0.f : m_run;
+  float mx4[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
+#pragma unroll 1
+  for (int part = 0; part < 2; ++part) {
+    uint32_t v[32];
+    tmem_ld32(s_addr + 32 - 32 * part, v);
+    tmem_ld_wait32(v);
+    tc::mask32(v, 0, hi - 32 + 32 * part, !raw, sl2);
+    tc::exp32<true, false>(s_addr + 32 + 16 * part, v, mul, base, l4, mx4);
+    publish(part);
+  }
   return fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * mul <= base + tc::kWindowLog2;
 }
 
@@ -345,6 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int s = 0; s < kMetaSlots; ++s) {
       mbar_init(bar(sh.meta_full[s]), 1);
       mbar_init(bar(sh.meta_empty[s]), kMetaConsumers);
+      mbar_init(bar(sh.sums[s]), kSoftmaxWarps);
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar(sh.s_full[s]), 1);
@@ -359,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(bar(sh.mma_done[1]), 1);
     fence_mbar_init();
   }
-  if (tid < 16) (tid < 8 ? &sh.max_seq[0][0] : &sh.sum_seq[0][0])[tid & 7] = 0;
+  if (tid < 8) (&sh.max_seq[0][0])[tid] = 0;
   if (warp == kQkWarp) {
     tmem_alloc(smem_u32(&sh.tmem_base), kTmemCols);
     tmem_relinquish();
@@ -441,7 +470,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       group_units = base;
       __syncwarp();
     };
-    load_group(0, 0);
     unsigned redo = 0;  // units to run again
     int again = -1;     // the unit whose maxima the last pass took
     int outputs = 0;    // passes that write a unit's output
@@ -454,7 +482,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     // The unit's place in the group held (moved there); false: no such unit.
     auto locate = [&](int u) {
-      if (u < before) load_group(0, 0);
+      if (u < before) {
+        g0 = -kGroup;
+        before = group_units = 0;
+      }
       while (u - before >= group_units) {
         if (g0 + kGroup >= p.S) return false;
         load_group(g0 + kGroup, min(before + group_units, kNoUnit));
@@ -493,11 +524,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!locate(u)) {
           // none left, once the units still running (the last two) need not be run
-          // again; who gives up here has set the abort word and the error
+          // again; who gives up here sets the abort word and the error
           const uint64_t limit = kWaitLimitNs + (static_cast<uint64_t>(nb_last) + nb_before) * kBlockLimitNs;
-          if (!__all_sync(0xffffffffu, await_count(smem_u32(&sh.units_done), kOutputWarps * outputs, &sh.abort, p.err,
-                                                   HPD_DEVERR_TIMEOUT, limit)))
-            break;
+          if (!__all_sync(0xffffffffu, await_outputs(sh, kOutputWarps * outputs, limit, p.err))) break;
           redo = take_redo();
           if (!redo) break;
           continue;
@@ -560,10 +589,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         have = true;
         break;
       }
-      if (!have && lane == 0) M.valid = 0;
-      __syncwarp();
-      __threadfence_block();
-      if (lane == 0) mbar_arrive(bar(sh.meta_full[slot]));
+      if (lane == 0) {  // (the arrival releases this lane's writes)
+        if (!have) M.valid = 0;
+        mbar_arrive(bar(sh.meta_full[slot]));
+      }
       if (!have) break;
     }
   } else if (warp < kProducers) {
@@ -584,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int k = 0; ok; ++k) {
       const int slot = k % kMetaSlots;
       if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
-      const UnitMeta M = sh.meta[slot];
+      const UnitMeta M = read_meta(sh.meta[slot]);
       __syncwarp();
       if (!M.valid) break;
       if (lane == 0) {
@@ -744,8 +773,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
-        // O (+)= P V: 16 keys per MMA, P in the S buffer (half h of the keys at
-        // column 64 h), the first 32 keys of both halves and then the second
+        // O (+)= P V: 16 keys per MMA, P in the S buffer: of half h, keys 32-63 at
+        // column 64 h + 32, then keys 0-31 at column 64 h + 48
         const uint64_t vd = dv0 + ((sv * L::kTileBytes) >> 4);
         const uint32_t col = tmem + L::col_s(jg & 1);
 #pragma unroll
@@ -755,9 +784,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (issuer) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int kk = (i >> 1) * 4 + part * 2 + (i & 1);
-              mma_ts_one(tmem + L::kColO, col + kk * 8 + (kk >= 4 ? 32 : 0), vd + kk * ((2 * L::kGroupBytes) >> 4),
-                         idesc_pv, (j > 0 || part > 0 || i > 0) ? 1u : 0u);
+              const int kk = (i >> 1) * 4 + (1 - part) * 2 + (i & 1);  // 16 keys of the block
+              mma_ts_one(tmem + L::kColO, col + (i >> 1) * 64 + 32 + part * 16 + (i & 1) * 8,
+                         vd + kk * ((2 * L::kGroupBytes) >> 4), idesc_pv, (j > 0 || part > 0 || i > 0) ? 1u : 0u);
             }
           }
           __syncwarp();
@@ -786,6 +815,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int quad = warp & 3;          // TMEM lane quadrant this warp may access
     const int r_in = quad * 32 + lane;  // row within the tile
     const uint32_t o_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::kColO;
+    const uint32_t stage = sbase + L::kStage + quad * 32 * 128;  // of this warp's rows
     const int rt = p.div_G(r_in);
     int outputs = 0;
     bool ok = true;
@@ -794,86 +824,111 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
       const UnitMeta &M = sh.meta[slot];
       if (!M.valid) break;
-      const int pass = M.pass;
-      if (pass != kMaxima) {
-        const bool valid = r_in < M.nrows, idle = quad * 32 >= M.nrows;
-        const int lim = min(max(M.lim0 + rt, M.full), M.L), nsplit = M.nsplit;
-        const int token = M.tok0 + rt, head = M.g * G + r_in - rt * G;
-        const size_t pair = static_cast<size_t>(token) * p.H_q + head;
-        const size_t slot_pair = static_cast<size_t>(M.split) * p.T * p.H_q + pair;
-        float l = 0.f, inv = 0.f;
-        if (!idle) {
-          if (!(ok = __all_sync(0xffffffffu, await_seq(&sh.sum_seq[quad][0], k + 1, sh) &&
-                                                 await_seq(&sh.sum_seq[quad][1], k + 1, sh))))
-            break;
-          l = sh.xsum[slot][0][r_in] + sh.xsum[slot][1][r_in];
-          inv = l == 0.f ? 0.f : 1.f / l;  // (a sum that is NaN stays one)
-          if (valid) {
-            const float lse = l == 0.f ? NEG_INF : l > 0.f ? lse_of(sh.xbase[slot][r_in], l) : l;
-            if (nsplit > 1) p.l_part[slot_pair] = lse;
-            else if (p.lse) p.lse[pair] = lse;
-          }
-        }
-        if (!(ok = wait_bar(sh.o_full, outputs & 1))) break;
-        ++outputs;
-        tc_fence_after();
-        float2 finite = make_float2(0.f, 0.f);  // NaN once an infinity or NaN is added
+      if (!(ok = wait_bar(sh.sums[slot], (k / kMetaSlots) & 1))) break;
+      const int pass = M.pass, nrows = M.nrows, nsplit = M.nsplit;
+      const bool idle = quad * 32 >= nrows, valid = r_in < nrows;
+      const int pair = (M.tok0 + rt) * p.H_q + M.g * G + r_in - rt * G;  // row and head
+      const size_t at_split = static_cast<size_t>(M.split) * p.T * p.H_q;
+      float *const part = nsplit > 1 ? p.o_part + (at_split + pair) * D : nullptr;
+      float inv = 0.f;
+      bool odd = false;
+      if (valid && pass != kMaxima) {
+        const float l = sh.xsum[slot][0][r_in] + sh.xsum[slot][1][r_in];
+        const float lse = l == 0.f ? NEG_INF : l > 0.f ? lse_of(sh.xbase[slot][r_in], l) : l;
+        if (part) p.l_part[at_split + pair] = lse;
+        else if (p.lse) p.lse[pair] = lse;
+        inv = l == 0.f ? 0.f : 1.f / l;  // (a sum that is NaN stays one)
+        odd = l != l;
+      }
+      __syncwarp();
+      // (a unit that was run again may have rows to be computed once more)
+      if (lane == 0 && pass != kAgain) mbar_arrive(bar(sh.meta_empty[slot]));
+      if (pass == kMaxima) continue;
+      if (!(ok = wait_bar(sh.o_full, outputs & 1))) break;
+      ++outputs;
+      tc_fence_after();
+      float2 finite = make_float2(0.f, 0.f);  // NaN once an infinity or NaN is added
+      // 64 columns at a time, through shared memory, so that a store instruction
+      // writes whole 128-byte lines of four rows instead of a sector of 32; O is
+      // read ahead of the stores, as the next unit's P V waits for that
 #pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t o[32];
-          if (!idle) {
-            tmem_ld32(o_addr + c, o);
-            tmem_ld_wait32(o);
-          }
-          if (c == D - 32) {  // O may be overwritten once every warp has read it
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(sh.o_empty));
-          }
-          if (idle || !valid) continue;
+      for (int half = 0; half <= D / 64; ++half) {
+        uint32_t keep[32];
+        if (half < D / 64) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 2)
-            finite = __ffma2_rn(make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), make_float2(0.f, 0.f),
-                                finite);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * inv);
-          if (nsplit == 1) {
-            __nv_bfloat16 *dst = p.out + pair * D + c;
-#pragma unroll
-            for (int e = 0; e < 32; e += 2)
-              o[e / 2] = pack_bf16x2(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
-            if (p.out_align32) {  // 32-byte stores: each fills a sector
-              st_global_v8(dst, o);
-              st_global_v8(dst + 16, o + 8);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 16; e += 4)
-                reinterpret_cast<uint4 *>(dst)[e / 4] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          for (int c = 0; c < 64; c += 32) {
+            uint32_t o[32];
+            if (!idle) {
+              tmem_ld32(o_addr + half * 64 + c, o);
+              tmem_ld_wait32(o);
             }
-          } else {
-            float *dst = p.o_part + slot_pair * D + c;
+            if (half == D / 64 - 1 && c == 32) {  // O may be overwritten once every warp has read it
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(sh.o_empty));
+            }
+            if (idle) continue;
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) st_global_v8(dst + e, o + e);
+            for (int e = 0; e < 32; e += 2) {
+              const float2 v = make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
+              finite = __ffma2_rn(v, make_float2(0.f, 0.f), finite);
+              const float2 x = __fmul2_rn(v, make_float2(inv, inv));
+              o[e] = __float_as_uint(x.x);
+              o[e + 1] = __float_as_uint(x.y);
+              keep[(c + e) / 2] = pack_bf16x2(x.x, x.y);
+            }
+            if (part && valid) {
+#pragma unroll
+              for (int e = 0; e < 32; e += 8) st_global_v8(part + half * 64 + c + e, o + e);
+            }
           }
         }
-        const bool odd = !idle && valid && !(finite.x == 0.f && finite.y == 0.f);
-        const bool redo = __any_sync(0xffffffffu, pass == kFirst && (odd || (!idle && valid && l != l)));
-        if (lane == 0) {
-          if (redo) atomicOr(&sh.redo, 1u << (k & 31));
-          asm volatile("red.release.cta.shared::cta.add.u32 [%0], 1;" ::"r"(smem_u32(&sh.units_done)) : "memory");
+        if (idle || part) continue;
+        if (half > 0) {  // the columns before these
+#pragma unroll 1
+          for (int i = 0; i < 32; i += 8) {
+            uint32_t w[2][4];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int r = (lane >> 3) + i + 4 * e;
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                           : "=r"(w[e][0]), "=r"(w[e][1]), "=r"(w[e][2]), "=r"(w[e][3])
+                           : "r"(stage + r * 128 + (((lane ^ r) & 7) << 4)));
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int r = (lane >> 3) + i + 4 * e, at = __shfl_sync(0xffffffffu, pair, r);
+              if (quad * 32 + r < nrows)
+                *reinterpret_cast<uint4 *>(p.out + static_cast<size_t>(at) * D + half * 64 - 64 + (lane & 7) * 8) =
+                    make_uint4(w[e][0], w[e][1], w[e][2], w[e][3]);
+            }
+          }
+          __syncwarp();
         }
-        // a key that the tile sees and this row does not
-        const bool mend = pass == kAgain && odd && lim < M.pages * kPage && lim < M.L && l == l;
-        for (unsigned rows = __ballot_sync(0xffffffffu, mend); rows; rows &= rows - 1) {
-          const int src = __ffs(rows) - 1;
-          const int row_token = __shfl_sync(0xffffffffu, token, src), row_head = __shfl_sync(0xffffffffu, head, src);
-          const int row_lim = __shfl_sync(0xffffffffu, lim, src);
-          const size_t at = static_cast<size_t>(row_token) * p.H_q + row_head;
-          const int k0 = M.blk_lo * kBlk, k1 = min(row_lim, (M.blk_lo + M.n_blocks) * kBlk);
-          one_row<D>(p, M.seq, row_token, row_head, k0, k1,
-                     nsplit == 1 ? nullptr : p.o_part + (static_cast<size_t>(M.split) * p.T * p.H_q + at) * D,
-                     p.out + at * D);
+        if (half < D / 64) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + lane * 128 + (((lane ^ e) & 7) << 4)),
+                         "r"(keep[4 * e]), "r"(keep[4 * e + 1]), "r"(keep[4 * e + 2]), "r"(keep[4 * e + 3])
+                         : "memory");
+          __syncwarp();
         }
+      }
+      const bool wild = valid && !(finite.x == 0.f && finite.y == 0.f);
+      const bool redo = __any_sync(0xffffffffu, pass == kFirst && (odd || wild));
+      if (lane == 0) {
+        if (redo) atomicOr(&sh.redo, 1u << (k & 31));
+        asm volatile("red.release.cta.shared::cta.add.u32 [%0], 1;" ::"r"(smem_u32(&sh.units_done)) : "memory");
+      }
+      if (pass != kAgain) continue;
+      // rows from which the tile's other rows' keys have to be kept out
+      const int lim = min(max(M.lim0 + rt, M.full), M.L), k0 = M.blk_lo * kBlk;
+      const bool mend = wild && !odd && lim < M.pages * kPage && lim < M.L;
+      for (unsigned rows = __ballot_sync(0xffffffffu, mend); rows; rows &= rows - 1) {
+        const int src = __ffs(rows) - 1;
+        const int at = __shfl_sync(0xffffffffu, pair, src), end = __shfl_sync(0xffffffffu, lim, src);
+        one_row<D>(p, M.seq, at / p.H_q, at % p.H_q, k0, min(end, k0 + M.n_blocks * kBlk),
+                   nsplit > 1 ? p.o_part + (at_split + at) * D : nullptr, p.out + static_cast<size_t>(at) * D);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
@@ -887,25 +942,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     const int rt = p.div_G(r_in);
     const float sl2 = p.scale_log2;
-    // The other half has published unit k.
-    auto await_other = [&](const int (*seq)[2], int k) {
-      return __all_sync(0xffffffffu, await_seq(&seq[quad][h ^ 1], k + 1, sh));
-    };
     int jg = 0;            // blocks in all
     float given = NEG_INF;  // the row's maximum, which a pass over the maxima found
     bool ok = true;
     for (int k = 0; ok; ++k) {
       const int slot = k % kMetaSlots;
       if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
-      const UnitMeta &M = sh.meta[slot];
+      const UnitMeta M = read_meta(sh.meta[slot]);
+      __syncwarp();
       if (!M.valid) break;
-      const int nb = M.n_blocks, blk_lo = M.blk_lo, pass = M.pass, nrows = M.nrows;
-      const bool idle = quad * 32 >= nrows;
+      if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
+      const int nb = M.n_blocks, blk_lo = M.blk_lo, pass = M.pass;
+      const bool idle = quad * 32 >= M.nrows;
       // (rows that are no query count as seeing everything, so that their warp
       // needs no masks for them; their results are not stored)
-      const int lim = r_in < nrows ? min(max(M.lim0 + rt, M.full), M.L) : 1 << 30;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
+      const int lim = r_in < M.nrows ? min(max(M.lim0 + rt, M.full), M.L) : 1 << 30;
       // blocks of the unit that every row of the warp sees all of
       const int n_plain = sl2 > 0.f ? min(max(__reduce_min_sync(0xffffffffu, lim), 0) / kBlk - blk_lo, nb) : 0;
       auto await_s = [&] {
@@ -925,6 +976,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           publish(0);
           publish(1);
         }
+        if (lane == 0) mbar_arrive(bar(sh.sums[slot]));
         continue;
       }
       float m_run = given, mx_run = NEG_INF;
@@ -932,41 +984,39 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool inside = true;   // the scores stay in the window of their base
 #pragma unroll
       for (int i = 0; i < 4; ++i) l4[i] = make_float2(0.f, 0.f);
-      for (int j = 0; j < nb; ++j, ++jg) {
-        // blocks that every row of the warp sees all of, once the base is there:
-        // nothing to decide
-        if (pass != kMaxima && (j > 0 || pass == kAgain)) {
-          for (; j < n_plain; ++j, ++jg) {
-            if (!(ok = await_s())) break;
-            inside &= softmax_half<true>(t_lane + L::col_s(jg & 1) + h * 64, 64, sl2, m_run, l4, publish);
-          }
-          if (!ok || j >= nb) break;
-        }
-        if (!(ok = await_s())) break;
-        const uint32_t s_addr = t_lane + L::col_s(jg & 1) + h * 64;
-        const int hi = min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64;
-        if (pass == kMaxima) {
-          mx_run = fmaxf(mx_run, row_max<1>(s_addr, j < n_plain, hi, sl2));
+      int j = 0;
+      if (pass == kMaxima) {
+        for (; j < nb; ++j, ++jg) {
+          if (!(ok = await_s())) break;
+          const int hi = min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64;
+          mx_run = fmaxf(mx_run, row_max(t_lane + L::col_s(jg & 1) + h * 64, 32, j < n_plain, hi, sl2));
           publish(0);
           publish(1);
-          continue;
         }
-        if (j == 0 && pass == kFirst) {
-          m_run = row_max<2>(t_lane + L::col_s(jg & 1), n_plain > 0, hi + h * 64, sl2);
-          // (P of either half may replace scores only once the other half has read them)
-          tc_fence_before();
-          publish_seq(&sh.max_seq[quad][h], k + 1);
-          if (!(ok = await_other(sh.max_seq, k))) break;
-          tc_fence_after();
+      } else {
+        if (!(ok = await_s())) break;
+        if (pass == kFirst)
+          m_run = row_max(t_lane + L::col_s(jg & 1), 64, n_plain > 0, min(lim - blk_lo * kBlk, kBlk), sl2);
+        // blocks that every row of the warp sees all of: nothing to decide
+        for (; j < n_plain; ++j, ++jg) {
+          if (j > 0 && !(ok = await_s())) break;
+          inside &= softmax_plain(t_lane + L::col_s(jg & 1) + h * 64, sl2, m_run, l4, publish);
         }
-        inside &= softmax_half<false>(s_addr, hi, sl2, m_run, l4, publish);
+        if (!ok) break;
+        for (; j < nb; ++j, ++jg) {
+          if (j > 0 && !(ok = await_s())) break;
+          const int hi = min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64;
+          inside &= softmax_masked(t_lane + L::col_s(jg & 1) + h * 64, hi, sl2, m_run, l4, publish);
+        }
       }
       if (!ok) break;
       sh.xsum[slot][h][r_in] = pass == kMaxima ? mx_run : inside ? tc::sum_of(l4) : __int_as_float(0x7fffffff);
       if (h == 0) sh.xbase[slot][r_in] = m_run;
-      publish_seq(&sh.sum_seq[quad][h], k + 1);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(sh.sums[slot]));
       if (pass == kMaxima) {
-        if (!(ok = await_other(sh.sum_seq, k))) break;
+        publish_seq(&sh.max_seq[quad][h], k + 1);
+        if (!(ok = __all_sync(0xffffffffu, await_seq(&sh.max_seq[quad][h ^ 1], k + 1, sh)))) break;
         given = fmaxf(sh.xsum[slot][0][r_in], sh.xsum[slot][1][r_in]);
       }
     }
@@ -1190,7 +1240,6 @@ hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *a, hpd_stream_t stream) {
   k.max_pages = a->max_pages;
   k.scale_log2 = (a->scale != 0.f ? a->scale : 1.0f / std::sqrt(static_cast<float>(a->D))) * kLog2e;
   k.out = static_cast<__nv_bfloat16 *>(a->out);
-  k.out_align32 = (reinterpret_cast<uintptr_t>(a->out) & 31u) == 0;
   k.lse = a->lse;
   k.err = reinterpret_cast<uint32_t *>(ws);
   k.unit_ctr = reinterpret_cast<int *>(ws + 8);

@@ -567,3 +567,21 @@ def test_gpu_attn_on_another_stream_and_in_a_graph(torch):
         g.replay()
     torch.cuda.synchronize()
     assert torch.equal(op.out, ref[0]) and torch.equal(op.lse, ref[1])
+
+
+@gpu
+@pytest.mark.parametrize("hq,hkv,D", [(32, 8, 128), (8, 8, 64)])
+def test_gpu_attn_many_short_units_one_after_another(torch, hq, hkv, D):
+    # some twenty units of one or two blocks on every SM, whose roles may be units
+    # apart: every call gives the first one's bits, and those the oracle's values
+    rng = np.random.default_rng(21)
+    S = 3200 // hkv
+    new, total = np.full(S, 2), rng.integers(2, 250, S)
+    c = _attn_case(torch, new, total, hq, hkv, D, seed=14)
+    op = _check_attn(torch, c)
+    first = op.out.clone(), op.lse.clone()
+    for _ in range(50):
+        op(c["q"], c["cu"], c["total"])
+    torch.cuda.synchronize()
+    assert op.errors() == 0
+    assert torch.equal(op.out, first[0]) and torch.equal(op.lse, first[1])
