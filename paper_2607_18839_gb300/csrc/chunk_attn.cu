@@ -237,6 +237,23 @@ __device__ __noinline__ float row_max(uint32_t s_addr, int apart, bool plain, in
   return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * (raw ? sl2 : 1.f);
 }
 
+// 16 consecutive 32-bit TMEM columns of this thread's lane, and the wait for them.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t *r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+  asm volatile(""
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]),
+                 "+r"(r[15])::"memory");
+}
+
 // A row's half block: P = exp2(scaled score - base) as bf16 pairs, and its sum.  P of
 // the half's keys 32-63 goes to the first 16 columns of their scores, then P of keys
 // 0-31 to the next 16: publish(part) once it is on its way.  (The scores of keys 0-31
@@ -248,15 +265,29 @@ __device__ __forceinline__ bool softmax_plain(uint32_t s_addr, float sl2, float 
   const float NEG_INF = -__int_as_float(0x7f800000);
   float mx4[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
   const float base = m_run == NEG_INF ? 0.f : m_run;
-  uint32_t v[64];
-  tmem_ld32(s_addr + 32, v);
-  tmem_ld_wait32(v);
-  tmem_ld32(s_addr, v + 32);
-  tc::exp32<true, false>(s_addr + 32, v, sl2, base, l4, mx4);
-  publish(0);
-  tmem_ld_wait32(v + 32);
-  tc::exp32<true, false>(s_addr + 48, v + 32, sl2, base, l4, mx4);
-  publish(1);
+  // 16 scores at a time, the next 16 on their way
+  uint32_t v[2][16], pk[16];
+  const float2 mul2 = make_float2(sl2, sl2), nbase2 = make_float2(-base, -base);
+  tmem_ld16(s_addr + 32, v[0]);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    uint32_t *const x = v[q & 1];
+    tmem_ld_wait16(x);
+    if (q < 3) tmem_ld16(s_addr + (q == 0 ? 48 : q == 1 ? 0 : 16), v[(q & 1) ^ 1]);
+#pragma unroll
+    for (int c = 0; c < 16; c += 2) {
+      const float2 a = make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+      const float2 arg = __ffma2_rn(a, mul2, nbase2);
+      const float2 e = make_float2(fast_exp2(arg.x), fast_exp2(arg.y));
+      l4[(c >> 1) & 3] = __fadd2_rn(l4[(c >> 1) & 3], e);
+      pk[(q & 1) * 8 + c / 2] = pack_bf16x2(e.x, e.y);
+      mx4[(c >> 1) & 3] = tc::fmax3(mx4[(c >> 1) & 3], a.x, a.y);
+    }
+    if (q & 1) {
+      tmem_st16(s_addr + 32 + (q >> 1) * 16, pk);
+      publish(q >> 1);
+    }
+  }
   return fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * sl2 <= base + tc::kWindowLog2;
 }
 // The same where rows see some of the keys, or the scale is not positive.  hi: visible
