@@ -78,8 +78,14 @@ constexpr uint32_t kMetaConsumers = kProducers + 2 + kSoftmaxWarps + kOutputWarp
 constexpr int kStages = 3;
 constexpr int kGroup = 256;      // sequences whose lengths the scheduler holds at once
 constexpr int kMaxSplits = 32;
+constexpr int kTailWaves = 4;    // most waves of the units of split tiles
 constexpr int kNoUnit = (1 << 30) - 1;  // every unit's number is below
 constexpr uint64_t kBlockLimitNs = 10000;  // of a unit's time: a block takes some 0.7 us
+
+// A unit of a tile whose blocks are split: what the merge needs to know.
+struct SlotInfo {
+  int tok0, nrows, g, split, nsplit, pad[3];
+};
 
 struct ChunkParams {
   const __nv_bfloat16 *q;
@@ -93,10 +99,12 @@ struct ChunkParams {
   float *lse;
   uint32_t *err;
   int *unit_ctr;   // [2] next unit and finished CTAs, zero between calls
-  int s_max;       // most splits of a tile; 1: none
-  float *o_part;   // [s_max][T][H_q][D]
-  float *l_part;   // [s_max][T][H_q]
-  int *row_split;  // [T] splits of the row's tile
+  int units;       // most units of whole tiles
+  int slots;       // most units of split tiles; 0: no tile is split
+  float *o_part;   // [slots][128][D]
+  float *l_part;   // [slots][128]
+  SlotInfo *slot;  // [slots]
+  int *n_slots;    // units of split tiles
   FastDiv div_G, div_Hkv, div_tile;  // div_tile: tokens of a tile
 };
 
@@ -111,7 +119,9 @@ struct __align__(16) UnitMeta {
   int seq, g;
   int tok0;      // first row (of T) of the tile
   int pages;     // pages up to the last key that the tile sees
-  int split, nsplit, pad[2];
+  int split, nsplit;
+  int slot;      // where a split tile's unit leaves its result
+  int pad;
 };
 __device__ __forceinline__ UnitMeta read_meta(const UnitMeta &m) {
   UnitMeta r;
@@ -157,8 +167,8 @@ struct __align__(16) Shared {
   int unit_id[32];          // the last units issued
   UnitMeta meta[kMetaSlots];
   // the scheduler's group of sequences: units before each, first rows, rows, lengths,
-  // keys that all their rows see, splits
-  int g_units[kGroup], g_cu[kGroup], g_n[kGroup], g_len[kGroup], g_full[kGroup], g_split[kGroup];
+  // keys that all their rows see, tiles left whole, splits of the others
+  int g_units[kGroup], g_cu[kGroup], g_n[kGroup], g_len[kGroup], g_full[kGroup], g_whole[kGroup], g_split[kGroup];
 };
 
 __device__ __forceinline__ void set_abort(Shared &sh, uint32_t *err) {
@@ -436,11 +446,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     // Units are numbered sequence by sequence, in each its tiles from the last
     // (longest) to the first, in each its splits and then its KV heads.
     int g0 = -kGroup, before = 0, group_units = 0;  // the group held, units before it and of it
+    int first_slot = kNoUnit;                       // the first unit of the tiles that may be split
     auto load_group = [&](int s0, int units_before) {
       g0 = s0;
       before = units_before;
       const int count = min(kGroup, p.S - s0);
-      long long total = 0;
       // (loops left as loops, a step's loads ahead: code that runs once is bound by
       // fetching it)
       int a0 = 0, a1 = 0, len = 0, full = 0;
@@ -460,44 +470,82 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int c0 = min(max(b0, 0), p.T), c1 = max(c0, min(b1, p.T)), Ls = min(max(b_len, 0), p.max_pages * kPage);
         if (b0 != c0 || b1 != c1) flag_error(p.err, HPD_DEVERR_BRANCH_CU);
         if (Ls != b_len) flag_error(p.err, HPD_DEVERR_BRANCH_LEN);
-        const int tiles = p.div_tile(c1 - c0 + TT - 1);
-        total += static_cast<long long>(tiles) * ceil_div_i(Ls, kBlk);
         sh.g_cu[i] = c0;
         sh.g_n[i] = c1 - c0;
         sh.g_len[i] = Ls;
         sh.g_full[i] = min(max(b_full, 0), Ls);
       }
-      // Blocks of a split: what one CTA's share of all blocks is.
-      int per = 1 << 30;
-      if (p.s_max > 1) {
-#pragma unroll 1
-        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-        total *= p.H_kv;
-        per = max(2, static_cast<int>((total + gridDim.x - 1) / gridDim.x));
-      }
       // (sums that stop at kNoUnit, which offsets out of order could pass)
       auto add = [](int a, int b) { return min(a + b, kNoUnit); };
-      int base = 0;
-#pragma unroll 1
-      for (int i = lane; i - lane < count; i += 32) {
-        int units = 0, nsplit = 1;
-        if (i < count) {
-          if (p.s_max > 1) nsplit = min(p.s_max, max(1, (ceil_div_i(sh.g_len[i], kBlk) + per - 1) / per));
-          units = min(p.div_tile(sh.g_n[i] + TT - 1) * nsplit * p.H_kv, kNoUnit);
-        }
-        int incl = units;
+      // exclusive prefix of x over the lanes, from base, which it adds their sum to
+      auto scan = [&](int x, int &base) {
+        int incl = x;
 #pragma unroll 1
         for (int o = 1; o < 32; o <<= 1) {
           const int v = __shfl_up_sync(0xffffffffu, incl, o);
           if (lane >= o) incl = add(incl, v);
         }
-        const int prior = __shfl_up_sync(0xffffffffu, incl, 1);
-        if (i < count) {
-          sh.g_units[i] = add(base, lane ? prior : 0);
-          sh.g_split[i] = nsplit;
-        }
+        const int prior = __shfl_up_sync(0xffffffffu, incl, 1), r = add(base, lane ? prior : 0);
         base = add(base, __shfl_sync(0xffffffffu, incl, 31));
+        return r;
+      };
+      auto tiles_of = [&](int i) { return i < count ? p.div_tile(sh.g_n[i] + TT - 1) : 0; };
+      int whole = kNoUnit, per = 1 << 30;  // tiles left whole; blocks of a split of the others
+      int tiles = 0;
+      if (p.slots > 0) {
+#pragma unroll 1
+        for (int i = lane; i - lane < count; i += 32) scan(tiles_of(i), tiles);
       }
+      // (offsets out of order can make more tiles than there are rows for)
+      const bool may_split = p.slots > 0 && static_cast<long long>(tiles) * p.H_kv <= p.units;
+      if (may_split) {
+        // (one group) The tiles of full waves stay whole; what is left over after them
+        // is split, into as many even waves as take the least time: a unit's start and
+        // end are worth some 3.5 blocks.
+        whole = static_cast<int>(static_cast<long long>(tiles) * p.H_kv / gridDim.x * gridDim.x / p.H_kv);
+        float blocks = 0.f;  // of the others, all heads
+        int at = 0;
+#pragma unroll 1
+        for (int i = lane; i - lane < count; i += 32) {
+          const int n = tiles_of(i), left = max(scan(n, at) + n - whole, 0);
+          if (i < count) blocks += static_cast<float>(min(left, n)) * ceil_div_i(sh.g_len[i], kBlk) * p.H_kv;
+        }
+#pragma unroll 1
+        for (int o = 16; o > 0; o >>= 1) blocks += __shfl_xor_sync(0xffffffffu, blocks, o);
+        const float units = static_cast<float>(tiles - whole) * p.H_kv, mean = units > 0.f ? blocks / units : 0.f;
+        float least = 0.f;
+#pragma unroll 1
+        for (int waves = 1; waves <= kTailWaves; ++waves) {
+          const int share = max(2, static_cast<int>(ceilf(blocks / (gridDim.x * waves))));
+          const float f = fmaxf(floorf(mean / share), 1.f);
+          const float cost = ceilf(units * f / gridDim.x) * (ceilf(mean / f) + 3.5f);
+          if (waves == 1 || cost < least) {
+            least = cost;
+            per = share;
+          }
+        }
+      }
+      int units = 0, at = 0;
+#pragma unroll 1
+      for (int pass = 0; pass < 2; ++pass) {
+        units = at = 0;
+#pragma unroll 1
+        for (int i = lane; i - lane < count; i += 32) {
+          const int n = tiles_of(i), w = max(min(whole - scan(n, at), n), 0);
+          const int f = i < count && n > w ? max(ceil_div_i(sh.g_len[i], kBlk) / per, 1) : 1;
+          const int first = scan(min((w + (n - w) * min(f, kMaxSplits)) * p.H_kv, kNoUnit), units);
+          if (i < count) {
+            sh.g_units[i] = first;
+            sh.g_whole[i] = w;
+            sh.g_split[i] = min(f, kMaxSplits);
+          }
+        }
+        if (!may_split || units - whole * p.H_kv <= p.slots) break;
+        per = 1 << 30;  // more than there is room for: nothing is split
+      }
+      const int base = units;
+      first_slot = may_split ? whole * p.H_kv : kNoUnit;
+      if (p.slots > 0 && blockIdx.x == 0 && lane == 0) *p.n_slots = max(units - first_slot, 0);
       group_units = base;
       __syncwarp();
     };
@@ -567,10 +615,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int mid = (lo + hi) >> 1;
           if (sh.g_units[mid] <= u - before) lo = mid; else hi = mid;
         }
-        const int c0 = sh.g_cu[lo], n = sh.g_n[lo], len = sh.g_len[lo], full = sh.g_full[lo], nsplit = sh.g_split[lo];
-        int idx = u - before - sh.g_units[lo];
-        const int us = p.div_Hkv(idx), g = idx - us * p.H_kv;
-        const int ut = nsplit > 1 ? us / nsplit : us, split = us - ut * nsplit;
+        const int c0 = sh.g_cu[lo], n = sh.g_n[lo], len = sh.g_len[lo], full = sh.g_full[lo];
+        const int w = sh.g_whole[lo], f = sh.g_split[lo];
+        const int idx = u - before - sh.g_units[lo], us = p.div_Hkv(idx), g = idx - us * p.H_kv;
+        const int nsplit = us < w ? 1 : f, ut = us < w || f == 1 ? us : w + (us - w) / f;
+        const int split = nsplit == 1 ? 0 : (us - w) - (ut - w) * f;
         const int tile = p.div_tile(n + TT - 1) - 1 - ut;
         const int i0 = tile * TT, ntok = min(TT, n - i0), nrows = ntok * G;
         const int lim0 = len - n + i0 + 1;
@@ -578,8 +627,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int N = ceil_div_i(kmax, kBlk);
         const int blk_lo = nsplit > 1 ? static_cast<int>(static_cast<long long>(split) * N / nsplit) : 0;
         const int blk_hi = nsplit > 1 ? static_cast<int>(static_cast<long long>(split + 1) * N / nsplit) : N;
-        if (p.s_max > 1 && g == 0 && split == 0)
-          for (int r = lane; r < ntok; r += 32) p.row_split[c0 + i0 + r] = nsplit;
+        const int slot_id = u - first_slot;  // of the units of tiles that may be split
+        if (slot_id >= 0 && lane == 0) p.slot[slot_id] = SlotInfo{c0 + i0, nrows, g, split, nsplit, {0, 0, 0}};
         if (blk_hi <= blk_lo) {
           // no key: zero output, or an empty partial
 #pragma unroll 1
@@ -592,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int c = 0; c < D / 8; ++c) o[c] = make_uint4(0u, 0u, 0u, 0u);
               if (p.lse) p.lse[pair] = NEG_INF;
             } else {
-              p.l_part[static_cast<size_t>(split) * p.T * p.H_q + pair] = NEG_INF;
+              p.l_part[static_cast<size_t>(slot_id) * kRows + r] = NEG_INF;
             }
           }
           continue;
@@ -602,6 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           M.g = g;
           M.split = split;
           M.nsplit = nsplit;
+          M.slot = slot_id;
           M.seq = g0 + lo;
           M.tok0 = c0 + i0;
           M.nrows = nrows;
@@ -859,14 +909,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int pass = M.pass, nrows = M.nrows, nsplit = M.nsplit;
       const bool idle = quad * 32 >= nrows, valid = r_in < nrows;
       const int pair = (M.tok0 + rt) * p.H_q + M.g * G + r_in - rt * G;  // row and head
-      const size_t at_split = static_cast<size_t>(M.split) * p.T * p.H_q;
-      float *const part = nsplit > 1 ? p.o_part + (at_split + pair) * D : nullptr;
+      const size_t part_row = static_cast<size_t>(M.slot) * kRows + r_in;
+      float *const part = nsplit > 1 ? p.o_part + part_row * D : nullptr;
       float inv = 0.f;
       bool odd = false;
       if (valid && pass != kMaxima) {
         const float l = sh.xsum[slot][0][r_in] + sh.xsum[slot][1][r_in];
         const float lse = l == 0.f ? NEG_INF : l > 0.f ? lse_of(sh.xbase[slot][r_in], l) : l;
-        if (part) p.l_part[at_split + pair] = lse;
+        if (part) p.l_part[part_row] = lse;
         else if (p.lse) p.lse[pair] = lse;
         inv = l == 0.f ? 0.f : 1.f / l;  // (a sum that is NaN stays one)
         odd = l != l;
@@ -959,7 +1009,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int src = __ffs(rows) - 1;
         const int at = __shfl_sync(0xffffffffu, pair, src), end = __shfl_sync(0xffffffffu, lim, src);
         one_row<D>(p, M.seq, at / p.H_q, at % p.H_q, k0, min(end, k0 + M.n_blocks * kBlk),
-                   nsplit > 1 ? p.o_part + (at_split + at) * D : nullptr, p.out + static_cast<size_t>(at) * D);
+                   part ? p.o_part + (part_row - lane + src) * D : nullptr, p.out + static_cast<size_t>(at) * D);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
@@ -1076,46 +1126,53 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// Joins the splits of the rows that have several: one warp a (row, head).
+// Joins the splits of a tile, a CTA for every split, each with its share of the rows,
+// a warp a row:
 //   lse = log sum_s exp(lse_s),  out = sum_s exp(lse_s - lse) out_s
-constexpr int kMergeWarps = 4;
+// What bounds it: the launch, and reading the partial results from L2.
+constexpr int kMergeWarps = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kMergeWarps) chunk_merge_kernel(const ChunkParams p) {
-  const int lane = threadIdx.x & 31;
-  const size_t pair = static_cast<size_t>(blockIdx.x) * kMergeWarps + (threadIdx.x >> 5);
-  const size_t pairs = static_cast<size_t>(p.T) * p.H_q;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
-  if (pair >= pairs) return;
-  const int t = static_cast<int>(pair / p.H_q);
-  const int n = min(p.row_split[t], p.s_max);
-  if (t >= p.chunk_cu[p.S] || n <= 1) return;
+  if (static_cast<int>(blockIdx.x) >= *p.n_slots) return;
+  const SlotInfo info = p.slot[blockIdx.x];
+  const int n = info.nsplit;
+  if (n <= 1) return;
+  const size_t slot0 = blockIdx.x - info.split * p.H_kv;  // of split 0; the next are H_kv on
   const float NEG_INF = -__int_as_float(0x7f800000);
-  const float l = lane < n ? p.l_part[lane * pairs + pair] : NEG_INF;
-  float m = l;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  const float base = m == NEG_INF ? 0.f : m;
-  float w = exp2f((l - base) * kLog2e), sum = w;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   constexpr int kV = D / 32;  // values of a lane
-  float acc[kV];
+  const int lo = info.split * info.nrows / n, hi = (info.split + 1) * info.nrows / n;
+  for (int r = lo + warp; r < hi; r += kMergeWarps) {
+    const int rt = p.div_G(r);
+    const size_t pair = static_cast<size_t>(info.tok0 + rt) * p.H_q + info.g * p.G + r - rt * p.G;
+    const float l = lane < n ? p.l_part[(slot0 + static_cast<size_t>(lane) * p.H_kv) * kRows + r] : NEG_INF;
+    float m = l;
 #pragma unroll
-  for (int c = 0; c < kV; ++c) acc[c] = 0.f;
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float base = m == NEG_INF ? 0.f : m;
+    const float w = exp2f((l - base) * kLog2e);
+    float sum = w;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    float acc[kV];
+#pragma unroll
+    for (int c = 0; c < kV; ++c) acc[c] = 0.f;
 #pragma unroll 4
-  for (int s = 0; s < n; ++s) {
-    const float ws = __shfl_sync(0xffffffffu, w, s);
-    if (ws == 0.f) continue;  // (an empty partial is not written)
-    const float *src = p.o_part + (s * pairs + pair) * D + lane * kV;
+    for (int s = 0; s < n; ++s) {
+      const float ws = __shfl_sync(0xffffffffu, w, s);
+      if (ws == 0.f) continue;  // (an empty partial is not written)
+      const float *src = p.o_part + ((slot0 + static_cast<size_t>(s) * p.H_kv) * kRows + r) * D + lane * kV;
 #pragma unroll
-    for (int c = 0; c < kV; ++c) acc[c] = fmaf(ws, src[c], acc[c]);
+      for (int c = 0; c < kV; ++c) acc[c] = fmaf(ws, src[c], acc[c]);
+    }
+    uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + pair * D) + lane * (kV / 2);
+#pragma unroll
+    for (int c = 0; c < kV; c += 2) dst[c / 2] = pack_bf16x2(acc[c] * inv, acc[c + 1] * inv);
+    if (lane == 0 && p.lse) p.lse[pair] = sum == 0.f ? NEG_INF : m + logf(sum);
   }
-  uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + pair * D) + lane * (kV / 2);
-#pragma unroll
-  for (int c = 0; c < kV; c += 2) dst[c / 2] = pack_bf16x2(acc[c] * inv, acc[c + 1] * inv);
-  if (lane == 0 && p.lse) p.lse[pair] = sum == 0.f ? NEG_INF : m + logf(sum);
 }
 
 // ------------------------------------------------------------------ host --
@@ -1140,41 +1197,40 @@ constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct ChunkPlan {
-  int s_max;
+  int slots;        // units of split tiles; 0: none is split
   long long units;  // upper bound
-  size_t off_opart, off_lpart, off_rows, bytes;
+  size_t off_opart, off_lpart, off_slot, bytes;
 };
 
-// Splits are allowed where the call's tiles are too few for the SMs.  Only host
-// scalars enter (the kernel then splits by the true lengths): the time of the
-// longest sequences' tiles, in blocks, unsplit against the best number of
-// splits, a unit's start and end counted as 3 blocks, the merge as 6.
+// Tiles may be split where the call's units leave SMs idle in their last (or only)
+// wave.  Only host scalars enter (the kernel then splits by the true lengths): the
+// time of units of the longest sequences, in blocks, whole against split after the
+// full waves, a unit's start and end counted as 3.5 blocks, the merge as 8.
 ChunkPlan make_plan(const hpd_chunk_attn_args *a) {
   ChunkPlan pl{};
   const int G = a->H_q / a->H_kv, TT = kRows / G;
   const long long seqs = std::min(a->S, a->T);
-  const long long tiles = std::max<long long>(seqs, (a->T + TT - 1) / TT) * a->H_kv;
+  const long long units = std::max<long long>(seqs, (a->T + TT - 1) / TT) * a->H_kv;
   const int cap = a->max_pages * kPage;
   const int longest = a->max_seq_len > 0 ? std::min(a->max_seq_len, cap) : cap;
   const int N = std::max(1, (longest + kBlk - 1) / kBlk);
-  auto time = [&](int sp) {
-    return (tiles * sp + kPlanSms - 1) / kPlanSms * ((N + sp - 1) / sp + 3) + (sp > 1 ? 6 : 0);
-  };
-  int best = 1;
-  if (a->S <= kGroup)
-    for (int sp = 2; sp <= std::min(N, kMaxSplits); ++sp)
-      if (time(sp) < time(best)) best = sp;
-  pl.s_max = best == 1 ? 1 : a->S == 1 ? best : std::min(kMaxSplits, 2 * best);
-  const long long tiles_max = (a->T + seqs * (TT - 1)) / TT;
-  pl.units = tiles_max * a->H_kv * pl.s_max;
-  const size_t pairs = static_cast<size_t>(a->T) * a->H_q;
-  pl.off_opart = kAlign;
-  pl.off_lpart = pl.off_rows = pl.bytes = kAlign;
-  if (pl.s_max > 1) {
-    pl.off_lpart = align_up(pl.off_opart + pl.s_max * pairs * a->D * sizeof(float));
-    pl.off_rows = align_up(pl.off_lpart + pl.s_max * pairs * sizeof(float));
-    pl.bytes = align_up(pl.off_rows + static_cast<size_t>(a->T) * sizeof(int));
+  const long long left = units % kPlanSms;
+  const double full = static_cast<double>(units / kPlanSms) * (N + 3.5), none = full + (left ? N + 3.5 : 0.0);
+  double split = none;
+  for (int waves = 1; waves <= kTailWaves && left; ++waves) {
+    const long long share = std::max<long long>(2, (left * N + kPlanSms * waves - 1) / (kPlanSms * waves));
+    const long long f = std::min<long long>(std::max<long long>(N / share, 1), kMaxSplits);
+    split = std::min(split, full + 8 + ((left * f + kPlanSms - 1) / kPlanSms) * ((N + f - 1) / f + 3.5));
   }
+  if (a->S <= kGroup && split < 0.97 * none)
+    // at most an SM's share of blocks a unit, and the units that are no longer than it
+    pl.slots = (kTailWaves + 1) * kPlanSms + 2 * a->H_kv;
+  const long long tiles_max = (a->T + seqs * (TT - 1)) / TT;
+  pl.units = tiles_max * a->H_kv + pl.slots;
+  pl.off_opart = kAlign;
+  pl.off_lpart = align_up(pl.off_opart + static_cast<size_t>(pl.slots) * kRows * a->D * sizeof(float));
+  pl.off_slot = align_up(pl.off_lpart + static_cast<size_t>(pl.slots) * kRows * sizeof(float));
+  pl.bytes = align_up(pl.off_slot + static_cast<size_t>(pl.slots) * sizeof(SlotInfo));
   return pl;
 }
 
@@ -1221,10 +1277,8 @@ cudaError_t launch(const ChunkParams &p, long long units, cudaStream_t s) {
   }
   const unsigned grid = static_cast<unsigned>(std::min<long long>(units, sms[dev & 63].load()));
   e = launch_kernel(true, chunk_attn_kernel<D>, dim3(grid), dim3(kThreads), L::kDynSmem, s, tk, tk4, tv, tv4, tq, p);
-  if (e != cudaSuccess || p.s_max == 1) return e;
-  const size_t pairs = static_cast<size_t>(p.T) * p.H_q;
-  return launch_kernel(true, chunk_merge_kernel<D>, dim3(static_cast<unsigned>((pairs + kMergeWarps - 1) / kMergeWarps)),
-                       dim3(32 * kMergeWarps), 0, s, p);
+  if (e != cudaSuccess || p.slots == 0) return e;
+  return launch_kernel(true, chunk_merge_kernel<D>, dim3(p.slots), dim3(32 * kMergeWarps), 0, s, p);
 }
 
 }  // namespace
@@ -1274,10 +1328,12 @@ hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *a, hpd_stream_t stream) {
   k.lse = a->lse;
   k.err = reinterpret_cast<uint32_t *>(ws);
   k.unit_ctr = reinterpret_cast<int *>(ws + 8);
-  k.s_max = pl.s_max;
+  k.units = static_cast<int>(pl.units);
+  k.slots = pl.slots;
   k.o_part = reinterpret_cast<float *>(ws + pl.off_opart);
   k.l_part = reinterpret_cast<float *>(ws + pl.off_lpart);
-  k.row_split = reinterpret_cast<int *>(ws + pl.off_rows);
+  k.slot = reinterpret_cast<SlotInfo *>(ws + pl.off_slot);
+  k.n_slots = reinterpret_cast<int *>(ws + 16);
   k.div_G.set(k.G);
   k.div_Hkv.set(k.H_kv);
   k.div_tile.set(kRows / k.G);

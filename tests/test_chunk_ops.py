@@ -585,3 +585,23 @@ def test_gpu_attn_many_short_units_one_after_another(torch, hq, hkv, D):
     torch.cuda.synchronize()
     assert op.errors() == 0
     assert torch.equal(op.out, first[0]) and torch.equal(op.lse, first[1])
+
+
+@gpu
+@pytest.mark.parametrize("new,total,hq,hkv,D", [
+    ([700], [3000], 40, 8, 128),            # 27 x 8 units on 152 SMs: some whole, the rest split
+    ([1], [20000], 32, 8, 128),             # nothing but splits
+    ([640, 3], [2500, 4000], 16, 4, 64),
+    ([1, 1, 1], [9000, 40, 0], 8, 2, 128),  # splits of one sequence, none of the others
+    ([300, 290], [2300, 300], 16, 16, 128)])
+def test_gpu_attn_split_tiles(torch, new, total, hq, hkv, D):
+    c = _attn_case(torch, new, total, hq, hkv, D, seed=15)
+    _check_attn(torch, c)
+    # offsets out of order beside splits: flagged, in bounds
+    op = H.ChunkAttn(hq, c["kc"], c["vc"], c["table"], max_tokens=c["q"].shape[0])
+    if len(new) > 1:
+        bad = c["cu"].clone()
+        bad[1] = c["q"].shape[0] + 5
+        op(c["q"], bad, c["total"])
+        torch.cuda.synchronize()
+        assert op.errors() & 0x2
