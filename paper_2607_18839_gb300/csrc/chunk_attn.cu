@@ -998,8 +998,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool wild = valid && !(finite.x == 0.f && finite.y == 0.f);
       const bool redo = __any_sync(0xffffffffu, pass == kFirst && (odd || wild));
       if (lane == 0) {
-        if (redo) atomicOr(&sh.redo, 1u << (k & 31));
-        asm volatile("red.release.cta.shared::cta.add.u32 [%0], 1;" ::"r"(smem_u32(&sh.units_done)) : "memory");
+        // (released only where there is something to release: it waits for the stores)
+        if (redo) {
+          atomicOr(&sh.redo, 1u << (k & 31));
+          __threadfence_block();
+        }
+        asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], 1;" ::"r"(smem_u32(&sh.units_done)) : "memory");
       }
       if (pass != kAgain) continue;
       // rows from which the tile's other rows' keys have to be kept out
@@ -1078,6 +1082,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!(ok = await_s())) break;
         if (pass == kFirst)
           m_run = row_max(t_lane + L::col_s(jg & 1), 64, n_plain > 0, min(lim - blk_lo * kBlk, kBlk), sl2);
+        // (scores of -inf alone give no base to a row that sees the unit's keys)
+        inside = pass != kFirst || m_run > NEG_INF || lim <= blk_lo * kBlk;
         // blocks that every row of the warp sees all of: nothing to decide
         for (; j < n_plain; ++j, ++jg) {
           if (j > 0 && !(ok = await_s())) break;

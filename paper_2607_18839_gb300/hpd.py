@@ -537,6 +537,15 @@ def rope_table(max_pos: int, D: int, theta: float = 1e6, device="cuda"):
     return torch.stack((a.cos(), a.sin()), -1).float().contiguous()
 
 
+def _ready_workspace(nbytes: int, device, stream=None):
+    """A cleared workspace that a call on any stream may use from now on."""
+    import torch
+    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    hpd_workspace_init(_ptr(t), nbytes, _stream_handle(stream))
+    torch.cuda.synchronize(device)
+    return t
+
+
 class ChunkSlots:
     """Pages and slots of each step's new tokens (hpd_chunk_slots) for the
     sequences of one page table.  Owns the outputs: chunk_cu [S + 1], slot and
@@ -561,7 +570,7 @@ class ChunkSlots:
         self.chunk_cu = torch.empty(S + 1, dtype=i32, device=dev)
         self.slot = torch.empty(max_tokens, dtype=i32, device=dev)
         self.pos = torch.empty(max_tokens, dtype=i32, device=dev)
-        self.workspace = torch.zeros(256, dtype=torch.uint8, device=dev)
+        self.workspace = _ready_workspace(256, dev)
         self.args = hpd_chunk_slots_args(
             None, _ptr(seq_len), _ptr(page_table), _ptr(free_pages), _ptr(free_top),
             _ptr(self.seq_len), _ptr(self.free_top), _ptr(self.chunk_cu), _ptr(self.slot),
@@ -599,7 +608,7 @@ class QkNormRope:
         self.H_q, self.H_kv, self.D = H_q, H_kv, D
         self._keep = (q_weight, k_weight, rope)
         self.n_axes = max(axis) + 1
-        self.workspace = torch.zeros(256, dtype=torch.uint8, device=rope.device)
+        self.workspace = _ready_workspace(256, rope.device)
         self.args = hpd_qk_norm_rope_args()
         a = self.args
         a.q_weight, a.k_weight, a.rope = _ptr(q_weight), _ptr(k_weight), _ptr(rope)
@@ -608,6 +617,7 @@ class QkNormRope:
         a.axis[:D // 2] = axis
         self._bf, self._i32 = torch.bfloat16, torch.int32
         self._q = None
+        self._outgrown = []  # still the target of captured graphs, or of calls on other streams
 
     def __call__(self, qkv, pos, slot, k_cache, v_cache, q_out=None, stream=None):
         """qkv: bf16 [T, at least (H_q + 2 H_kv) D], the projection's rows
@@ -633,7 +643,11 @@ class QkNormRope:
             _need("QkNormRope", v_cache, bf, k_cache.shape)
         if q_out is None:
             if self._q is None or self._q.shape[0] < T:
-                self._q = qkv.new_empty((T, H_q, D))
+                rows = T
+                if self._q is not None:  # (at least doubled, so that those kept stay below the last one's size)
+                    self._outgrown.append(self._q)
+                    rows = max(T, 2 * self._q.shape[0])
+                self._q = qkv.new_empty((rows, H_q, D))
             q_out = self._q if self._q.shape[0] == T else self._q[:T]
         elif not _is(q_out, bf, (T, H_q, D)):
             _need("QkNormRope", q_out, bf, (T, H_q, D))
@@ -679,9 +693,8 @@ class ChunkAttn:
         self.max_tokens = max_tokens
         self._H_q, self._D, self._S = H_q, D, S
         self._bf, self._i32 = bf, torch.int32
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        self.workspace = _ready_workspace(nbytes, dev, stream)
         a.workspace, a.workspace_bytes = _ptr(self.workspace), nbytes
-        hpd_workspace_init(_ptr(self.workspace), nbytes, _stream_handle(stream))
 
     def __call__(self, q, chunk_cu, seq_len, full_len=None, stream=None):
         """q: bf16 [T, H_q, D] (heads side by side, rows may be strided), T up
