@@ -605,3 +605,183 @@ def test_gpu_attn_split_tiles(torch, new, total, hq, hkv, D):
         op(c["q"], bad, c["total"])
         torch.cuda.synchronize()
         assert op.errors() & 0x2
+
+
+def _near_oracle(c, rows, out, lse):
+    """These rows of a call against the oracle, whatever the others hold."""
+    z = np.nan_to_num
+    ref, rl, size, reach = C.attn(_np(c["q"]), z(_np(c["kc"])), z(_np(c["vc"]), posinf=0.0, neginf=0.0),
+                                  c["table"].cpu().numpy(), c["cu"].cpu().numpy(), c["total"].cpu().numpy(),
+                                  None if c["full"] is None else c["full"].cpu().numpy(), c["scale"])
+    slip = 2.0 ** -20 * reach + 2.0 ** -19  # as in _check_attn
+    assert (np.abs(lse - rl)[rows] <= (slip + 2.0 ** -21 * np.abs(rl))[rows]).all()
+    assert (np.abs(out - ref)[rows] <= (2.0 ** -8 * (np.abs(ref) + size) * 1.02 + 2 * slip[..., None] * size)[rows]).all()
+
+
+@gpu
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("new,total,hq,hkv,D", [([40, 30], [300, 200], 8, 2, 128), ([40, 30], [300, 200], 8, 2, 64),
+                                                ([30], [6000], 8, 2, 128), ([300, 9], [700, 50], 32, 8, 128)])
+def test_gpu_attn_values_not_finite_stay_where_they_are_seen(torch, value, new, total, hq, hkv, D):
+    # a value in a chunk's own keys: the tokens before it share its tiles and must
+    # not see it (0 times it is not 0); lse knows nothing of values
+    c = _attn_case(torch, new, total, hq, hkv, D, seed=16)
+    G, first = hq // hkv, 20
+    at = total[0] - new[0] + first
+    c["vc"][int(c["table"][0, at // PAGE]), at % PAGE, 1, 5] = value
+    op = H.ChunkAttn(hq, c["kc"], c["vc"], c["table"], max_tokens=sum(new))
+    out, lse = op(c["q"], c["cu"], c["total"])
+    torch.cuda.synchronize()
+    assert op.errors() == 0
+    out, lse = _np(out), lse.cpu().numpy()
+    want = np.zeros(out.shape, bool)
+    want[first: new[0], G: 2 * G, 5] = True
+    assert np.array_equal(~np.isfinite(out), want)
+    seen = want.any(-1)
+    assert np.isfinite(lse).all()
+    # (rows that see it: their other columns are as good as any)
+    _near_oracle(c, ~seen, out, lse)
+    if value != value:
+        assert np.isnan(out[want]).all()
+    else:
+        assert (out[want] == value).all()
+
+
+@gpu
+def test_gpu_attn_scores_of_minus_infinity_before_the_others(torch):
+    # the keys whose scores give a tile its base at minus infinity, the others so low
+    # that no weight of base 0 is left: the softmax is of the others all the same
+    c = _attn_case(torch, [3, 2], [400, 128], 4, 2, 128, seed=17, scale=1.0)
+    c["q"].zero_()
+    c["q"][..., 0] = 16.0
+    for s, l in ((0, 400), (1, 128)):
+        for j in range(l):
+            low = (j % 128 < 32 or 64 <= j % 128 < 96) and j < 128
+            page = int(c["table"][s, j // PAGE])
+            c["kc"][page, j % PAGE, :, 0] = -3e38 if low else -12.5
+            c["vc"][page, j % PAGE] = 1000.0 if low else 3.0
+    op = H.ChunkAttn(4, c["kc"], c["vc"], c["table"], max_tokens=5, scale=1.0)
+    out, lse = op(c["q"], c["cu"], c["total"])
+    torch.cuda.synchronize()
+    assert op.errors() == 0 and bool((out == 3.0).all())
+    keys = np.array([398 - 64, 399 - 64, 400 - 64, 127 - 64, 128 - 64])
+    assert np.abs(lse.cpu().numpy() - (np.log(keys) - 200.0)[:, None]).max() <= 2.0 ** -12
+
+
+@gpu
+def test_gpu_attn_output_at_an_odd_multiple_of_16_bytes(torch):
+    c = _attn_case(torch, [60, 1], [300, 2900], 16, 2, 128, seed=18)
+    op = H.ChunkAttn(16, c["kc"], c["vc"], c["table"], max_tokens=61)
+    want = op(c["q"], c["cu"], c["total"])[0].clone()
+    room = torch.full((61 * 16 * 128 + 16,), 7.0, dtype=torch.bfloat16, device="cuda")
+    op.args.out = room.data_ptr() + 16
+    op(c["q"], c["cu"], c["total"])
+    torch.cuda.synchronize()
+    assert op.errors() == 0 and torch.equal(room[8:-8].view_as(want), want)
+    assert bool((room[:8] == 7.0).all()) and bool((room[-8:] == 7.0).all())
+
+
+@gpu
+def test_gpu_pages_beyond_32_bits_of_a_long_cache(torch):
+    # rows past 2^32 values (2^33 bytes) of the pool, written by the rotation and
+    # read by the attention; the same in a small pool gives the same bits
+    hq, hkv, D, new, total = 16, 8, 128, [37, 5], [37, 133]
+    far, pages = 264_000, sum(C.pages_of(l) for l in total)
+    assert far * PAGE * hkv * D > 2 ** 32
+    rng = np.random.default_rng(19)
+    qkv = _bf(torch, rng, sum(new), (hq + 2 * hkv) * D)
+    old = _bf(torch, rng, 2, pages, PAGE, hkv, D)
+    table, i32 = H.rope_table(200, D), dict(dtype=torch.int32, device="cuda")
+    got = []
+    for base in (0, far):
+        kc, vc = (torch.empty(base + pages, PAGE, hkv, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        kc[base:], vc[base:] = old[0], old[1]
+        top = torch.tensor([pages], **i32)
+        free = torch.arange(base + pages, **i32)[-pages:].flip(0).repeat(2)  # the last pages of the pool
+        pt = torch.zeros(2, 9, **i32)
+        pt[1, :8] = free[:8]
+        slots = H.ChunkSlots(pt, torch.tensor([0, 128], **i32), free, top, max_tokens=42)
+        # (ids up to the stack's size are valid to it: state the pool's)
+        slots.args.num_pages = base + pages
+        slots(torch.tensor(new, **i32))
+        rope = H.QkNormRope(hq, hkv, D, None, None, table)
+        q = rope(qkv, slots.pos, slots.slot, kc, vc)
+        op = H.ChunkAttn(hq, kc, vc, pt, max_tokens=42)
+        out, lse = op(q, slots.chunk_cu, slots.seq_len)
+        torch.cuda.synchronize()
+        assert slots.errors() == rope.errors() == op.errors() == 0
+        assert int(slots.slot.min()) >= base * PAGE
+        got.append((out.clone(), lse.clone(), kc[base:].clone(), vc[base:].clone()))
+        del kc, vc, op
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+@gpu
+def test_gpu_norm_rope_keeps_its_output_while_it_grows(torch):
+    rng = np.random.default_rng(20)
+    kc, vc = (torch.zeros(8, PAGE, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    op = H.QkNormRope(4, 2, 64, None, None, H.rope_table(64, 64))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    x = _bf(torch, rng, 40, 8 * 64)
+    run = lambda n: op(x[:n], torch.arange(n, **i32), torch.arange(n, **i32), kc, vc)  # noqa: E731
+    pos = torch.arange(4, **i32)
+    want = run(4).clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        q = op(x[:4], pos, pos, kc, vc)
+    big = run(40).clone()
+    q.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(q, want) and torch.equal(big[:4], want) and torch.equal(run(40), big)
+
+
+# ----------------------------------------- prefill of pages, then a decode step --
+
+@pytest.fixture(scope="module")
+def example():
+    import importlib.util
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "prefill_then_decode.py")
+    spec = importlib.util.spec_from_file_location("prefill_then_decode", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    return mod
+
+
+@gpu
+def test_gpu_prefill_in_chunks_then_decode(torch, example):
+    import oracle
+    from paper_2607_18839_gb300 import workloads as W
+    make = lambda room: example.Pages(example.Shape(), [(5, 7), (9, 9), (1, 1)], [30, 3, 77], room)  # noqa: E731
+    whole, parts = make(300), make(97)
+    a, b = whole.prefill(per_step=100), parts.prefill(per_step=11)
+    torch.cuda.synchronize()
+    # the same hidden states, but for what two layers' roundings to bf16 make of
+    # scores summed in other orders: 2^-8 of values of some units each
+    for x, y, n in zip(a, b, whole.total):
+        assert x.shape == (n, 256) and float((x.float() - y.float()).abs().max()) <= 8 * 2.0 ** -8 * float(x.abs().max())
+    assert int(whole.top) == int(parts.top) == 64
+    op = parts.branches(per_doc=3, m=4)
+    d, host = op.d, lambda t: t.cpu().numpy()  # noqa: E731
+    bits = lambda t: t.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)  # noqa: E731
+    cu, pt = host(d.prefix_cu), host(d.prefix_page_table)
+    rows = [[int(pt[s, j // PAGE]) * PAGE + j % PAGE for j in range(n)] for s, n in enumerate(parts.total)]
+    at = np.concatenate(rows)
+    inp = W.BranchDecodeInputs(
+        n_docs=3, B=9, m=4, H_q=16, H_kv=2, D=128, num_pages=d.num_pages, max_pages=d.max_pages, q=bits(d.q),
+        prefix_k=bits(d.k_cache).reshape(-1, 2, 128)[at], prefix_v=bits(d.v_cache).reshape(-1, 2, 128)[at],
+        prefix_cu=cu, branch_cu=host(d.branch_cu), k_cache=bits(d.k_cache), v_cache=bits(d.v_cache),
+        page_table=host(d.page_table), branch_len=host(d.branch_len), branch_prefix_len=host(d.branch_prefix_len))
+    ref, rl = oracle.branch_attn(inp)
+    assert np.abs(_np(op.out) - ref).max() <= 1e-2 and np.abs(host(op.lse) - rl).max() <= 1e-3
+    # (every branch has a page of its own)
+    assert (host(d.branch_len) == 4).all() and len(set(host(d.page_table)[:, 0])) == 9
+
+
+@gpu
+def test_gpu_prefill_refuses_what_has_no_room(torch, example):
+    pages = example.Pages(example.Shape(layers=1), [(9, 9)], [3], room=40)
+    with pytest.raises(ValueError):
+        pages.prefill(per_step=10)
