@@ -220,7 +220,7 @@ __device__ __noinline__ bool await_outputs(Shared &sh, int n, uint64_t limit_ns,
 __device__ __forceinline__ float lse_of(float m, float l) {
   const int e = static_cast<int>(__float_as_uint(l) >> 23) - 127;
   const float f = __uint_as_float((__float_as_uint(l) & 0x007fffffu) | 0x3f800000u);
-  return fmaf(static_cast<float>(e), kLn2, fmaf(m, kLn2, logf(f)));
+  return fmaf(static_cast<float>(e), kLn2, fmaf(m, kLn2, __log2f(f) * kLn2));
 }
 
 // Largest score of 32 columns at s_addr and of 32 at s_addr + apart; hi: visible
@@ -494,55 +494,58 @@ __global__ void __launch_bounds__(kThreads, 1)
       int tiles = 0;
       if (p.slots > 0) {
 #pragma unroll 1
-        for (int i = lane; i - lane < count; i += 32) scan(tiles_of(i), tiles);
+        for (int i = lane; i - lane < count; i += 32) {
+          const int prior = scan(tiles_of(i), tiles);
+          if (i < count) sh.g_whole[i] = prior;
+        }
       }
       // (offsets out of order can make more tiles than there are rows for)
       const bool may_split = p.slots > 0 && static_cast<long long>(tiles) * p.H_kv <= p.units;
+      // of a sequence with n tiles, those that stay whole
+      auto whole_of = [&](int i, int n) { return may_split ? max(min(whole - sh.g_whole[i], n), 0) : n; };
       if (may_split) {
         // (one group) The tiles of full waves stay whole; what is left over after them
         // is split, into as many even waves as take the least time: a unit's start and
         // end are worth some 3.5 blocks.
-        whole = static_cast<int>(static_cast<long long>(tiles) * p.H_kv / gridDim.x * gridDim.x / p.H_kv);
+        whole = tiles * p.H_kv / static_cast<int>(gridDim.x) * static_cast<int>(gridDim.x) / p.H_kv;
         float blocks = 0.f;  // of the others, all heads
-        int at = 0;
 #pragma unroll 1
-        for (int i = lane; i - lane < count; i += 32) {
-          const int n = tiles_of(i), left = max(scan(n, at) + n - whole, 0);
-          if (i < count) blocks += static_cast<float>(min(left, n)) * ceil_div_i(sh.g_len[i], kBlk) * p.H_kv;
+        for (int i = lane; i < count; i += 32) {
+          const int n = tiles_of(i);
+          blocks += static_cast<float>(n - whole_of(i, n)) * ceil_div_i(sh.g_len[i], kBlk) * p.H_kv;
         }
+        __syncwarp();
 #pragma unroll 1
         for (int o = 16; o > 0; o >>= 1) blocks += __shfl_xor_sync(0xffffffffu, blocks, o);
         const float units = static_cast<float>(tiles - whole) * p.H_kv, mean = units > 0.f ? blocks / units : 0.f;
-        float least = 0.f;
-#pragma unroll 1
-        for (int waves = 1; waves <= kTailWaves; ++waves) {
-          const int share = max(2, static_cast<int>(ceilf(blocks / (gridDim.x * waves))));
-          const float f = fmaxf(floorf(mean / share), 1.f);
-          const float cost = ceilf(units * f / gridDim.x) * (ceilf(mean / f) + 3.5f);
-          if (waves == 1 || cost < least) {
-            least = cost;
-            per = share;
-          }
-        }
+        const int waves = (lane & (kTailWaves - 1)) + 1;  // a lane tries one
+        const int share = max(2, static_cast<int>(ceilf(blocks / (gridDim.x * waves))));
+        const float f = fmaxf(floorf(mean / share), 1.f);
+        const float cost = ceilf(units * f / gridDim.x) * (ceilf(mean / f) + 3.5f);
+        // (costs are positive: their order is their bits')
+        const unsigned least = __reduce_min_sync(0xffffffffu, __float_as_uint(cost));
+        per = __shfl_sync(0xffffffffu, share, __ffs(__ballot_sync(0xffffffffu, __float_as_uint(cost) == least)) - 1);
       }
-      int units = 0, at = 0;
+      int units = 0;
 #pragma unroll 1
       for (int pass = 0; pass < 2; ++pass) {
-        units = at = 0;
+        units = 0;
 #pragma unroll 1
         for (int i = lane; i - lane < count; i += 32) {
-          const int n = tiles_of(i), w = max(min(whole - scan(n, at), n), 0);
-          const int f = i < count && n > w ? max(ceil_div_i(sh.g_len[i], kBlk) / per, 1) : 1;
-          const int first = scan(min((w + (n - w) * min(f, kMaxSplits)) * p.H_kv, kNoUnit), units);
+          const int n = tiles_of(i), w = i < count ? whole_of(i, n) : 0;
+          const int f = n > w ? min(max(ceil_div_i(sh.g_len[i], kBlk) / per, 1), kMaxSplits) : 1;
+          const int first = scan(min((w + (n - w) * f) * p.H_kv, kNoUnit), units);
           if (i < count) {
             sh.g_units[i] = first;
-            sh.g_whole[i] = w;
-            sh.g_split[i] = min(f, kMaxSplits);
+            sh.g_split[i] = f;
           }
         }
         if (!may_split || units - whole * p.H_kv <= p.slots) break;
         per = 1 << 30;  // more than there is room for: nothing is split
       }
+#pragma unroll 1
+      for (int i = lane; i < count; i += 32) sh.g_whole[i] = whole_of(i, tiles_of(i));
+      __syncwarp();
       const int base = units;
       first_slot = may_split ? whole * p.H_kv : kNoUnit;
       if (p.slots > 0 && blockIdx.x == 0 && lane == 0) *p.n_slots = max(units - first_slot, 0);
@@ -918,7 +921,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float lse = l == 0.f ? NEG_INF : l > 0.f ? lse_of(sh.xbase[slot][r_in], l) : l;
         if (part) p.l_part[part_row] = lse;
         else if (p.lse) p.lse[pair] = lse;
-        inv = l == 0.f ? 0.f : 1.f / l;  // (a sum that is NaN stays one)
+        inv = l == 0.f ? 0.f : __fdividef(1.f, l);  // (a sum that is NaN stays one; others are below 2^126)
         odd = l != l;
       }
       __syncwarp();
