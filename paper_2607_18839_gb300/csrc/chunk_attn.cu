@@ -398,7 +398,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   const float NEG_INF = -__int_as_float(0x7f800000);
   auto bar = [](uint64_t &b) { return smem_u32(&b); };
   auto wait_bar = [&](uint64_t &b, int parity) {
-    return __all_sync(0xffffffffu, mbar_wait(bar(b), parity, &sh.abort));
+    // (one look by the whole warp, then a branch that is the warp's: a branch lane by
+    // lane had 2 to 6 % of the kernel's time)
+    return __all_sync(0xffffffffu, mbar_try_wait(bar(b), parity)) ||
+           __all_sync(0xffffffffu, mbar_wait_slow(bar(b), parity, &sh.abort, kWaitLimitNs));
   };
 
   if (tid == 0) {
@@ -447,25 +450,29 @@ __global__ void __launch_bounds__(kThreads, 1)
     // (longest) to the first, in each its splits and then its KV heads.
     int g0 = -kGroup, before = 0, group_units = 0;  // the group held, units before it and of it
     int first_slot = kNoUnit;                       // the first unit of the tiles that may be split
+    // What a lane loads of a sequence, from the start on its way for its first one.
+    int a0 = 0, a1 = 0, len = 0, full = 0;
+    auto fetch = [&](int i) {
+      if (i >= p.S) return;
+      a0 = p.chunk_cu[i];
+      a1 = p.chunk_cu[i + 1];
+      len = p.seq_len[i];
+      if (p.full_len) full = p.full_len[i];
+    };
+    int fetched = 0;  // group whose first lengths are on their way
+    fetch(lane);
     auto load_group = [&](int s0, int units_before) {
       g0 = s0;
       before = units_before;
       const int count = min(kGroup, p.S - s0);
       // (loops left as loops, a step's loads ahead: code that runs once is bound by
       // fetching it)
-      int a0 = 0, a1 = 0, len = 0, full = 0;
-      auto fetch = [&](int i) {
-        if (i >= count) return;
-        a0 = p.chunk_cu[s0 + i];
-        a1 = p.chunk_cu[s0 + i + 1];
-        len = p.seq_len[s0 + i];
-        if (p.full_len) full = p.full_len[s0 + i];
-      };
-      fetch(lane);
+      if (fetched != s0) fetch(s0 + lane);
+      fetched = -1;
 #pragma unroll 1
       for (int i = lane; i - lane < count; i += 32) {
         const int b0 = a0, b1 = a1, b_len = len, b_full = full;
-        fetch(i + 32);
+        if (i + 32 < count) fetch(s0 + i + 32);
         if (i >= count) continue;
         const int c0 = min(max(b0, 0), p.T), c1 = max(c0, min(b1, p.T)), Ls = min(max(b_len, 0), p.max_pages * kPage);
         if (b0 != c0 || b1 != c1) flag_error(p.err, HPD_DEVERR_BRANCH_CU);
