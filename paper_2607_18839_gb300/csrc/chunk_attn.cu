@@ -939,6 +939,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ++outputs;
       tc_fence_after();
       float2 finite = make_float2(0.f, 0.f);  // NaN once an infinity or NaN is added
+      bool wild = false;                      // an output that is not finite
       // 64 columns at a time, through shared memory, so that a store instruction
       // writes whole 128-byte lines of four rows instead of a sector of 32; O is
       // read ahead of the stores, as the next unit's P V waits for that
@@ -974,6 +975,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
+        if (half == D / 64 - 1) {
+          // O has been looked at: the scheduler may go on, or end, beside the stores
+          wild = valid && !(finite.x == 0.f && finite.y == 0.f);
+          const bool redo = __any_sync(0xffffffffu, pass == kFirst && (odd || wild));
+          if (lane == 0) {
+            // (released only where there is something to release: it waits for the stores)
+            if (redo) {
+              atomicOr(&sh.redo, 1u << (k & 31));
+              __threadfence_block();
+            }
+            asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], 1;" ::"r"(smem_u32(&sh.units_done)) : "memory");
+          }
+        }
         if (idle || part) continue;
         if (half > 0) {  // the columns before these
 #pragma unroll 1
@@ -1004,16 +1018,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                          : "memory");
           __syncwarp();
         }
-      }
-      const bool wild = valid && !(finite.x == 0.f && finite.y == 0.f);
-      const bool redo = __any_sync(0xffffffffu, pass == kFirst && (odd || wild));
-      if (lane == 0) {
-        // (released only where there is something to release: it waits for the stores)
-        if (redo) {
-          atomicOr(&sh.redo, 1u << (k & 31));
-          __threadfence_block();
-        }
-        asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], 1;" ::"r"(smem_u32(&sh.units_done)) : "memory");
       }
       if (pass != kAgain) continue;
       // rows from which the tile's other rows' keys have to be kept out
