@@ -461,8 +461,8 @@ typedef struct {
   size_t workspace_bytes;
 } hpd_chunk_attn_args;       /* q, out and caches 16-byte aligned                   */
 
-/* Bytes of workspace hpd_chunk_attn needs for these host scalars; 0 if they are
- * invalid.  Device pointers are not read. */
+/* Bytes of workspace hpd_chunk_attn needs for these host scalars, and for the same
+ * with fewer rows T; 0 if they are invalid.  Device pointers are not read. */
 size_t hpd_chunk_attn_workspace_size(const hpd_chunk_attn_args *args);
 
 hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *args, hpd_stream_t stream);

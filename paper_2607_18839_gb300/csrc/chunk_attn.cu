@@ -1242,15 +1242,17 @@ ChunkPlan make_plan(const hpd_chunk_attn_args *a) {
     const long long f = std::min<long long>(std::max<long long>(N / share, 1), kMaxSplits);
     split = std::min(split, full + 8 + ((left * f + kPlanSms - 1) / kPlanSms) * ((N + f - 1) / f + 3.5));
   }
-  if (a->S <= kGroup && split < 0.97 * none)
-    // at most an SM's share of blocks a unit, and the units that are no longer than it
-    pl.slots = (kTailWaves + 1) * kPlanSms + 2 * a->H_kv;
+  // Room for split tiles wherever some number of rows up to T could have them (of four
+  // blocks at least), so that a workspace serves every call of no more rows.  At most
+  // an SM's share of blocks a unit, and the units that are no longer than it.
+  const int room = a->S <= kGroup && N >= 4 ? (kTailWaves + 1) * kPlanSms + 2 * a->H_kv : 0;
+  pl.slots = split < 0.97 * none ? room : 0;
   const long long tiles_max = (a->T + seqs * (TT - 1)) / TT;
   pl.units = tiles_max * a->H_kv + pl.slots;
   pl.off_opart = kAlign;
-  pl.off_lpart = align_up(pl.off_opart + static_cast<size_t>(pl.slots) * kRows * a->D * sizeof(float));
-  pl.off_slot = align_up(pl.off_lpart + static_cast<size_t>(pl.slots) * kRows * sizeof(float));
-  pl.bytes = align_up(pl.off_slot + static_cast<size_t>(pl.slots) * sizeof(SlotInfo));
+  pl.off_lpart = align_up(pl.off_opart + static_cast<size_t>(room) * kRows * a->D * sizeof(float));
+  pl.off_slot = align_up(pl.off_lpart + static_cast<size_t>(room) * kRows * sizeof(float));
+  pl.bytes = align_up(pl.off_slot + static_cast<size_t>(room) * sizeof(SlotInfo));
   return pl;
 }
 

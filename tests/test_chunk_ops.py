@@ -118,6 +118,14 @@ def test_attn_refuses(lib, bad, status):
         assert H.hpd_chunk_attn_workspace_size(a) == 0
 
 
+@pytest.mark.parametrize("S,H_q,H_kv,D,max_pages", [(4, 32, 8, 128, 1024), (1, 16, 2, 64, 64), (300, 8, 8, 128, 512),
+                                                    (64, 40, 8, 128, 30), (2, 8, 1, 128, 3)])
+def test_attn_workspace_serves_calls_of_fewer_rows(lib, S, H_q, H_kv, D, max_pages):
+    size = [H.hpd_chunk_attn_workspace_size(attn_args(S=S, T=T, H_q=H_q, H_kv=H_kv, D=D, max_pages=max_pages,
+                                                      num_pages=4096)) for T in range(1, 5000, 7)]
+    assert all(0 < a <= b for a, b in zip(size, size[1:]))
+
+
 def test_struct_layouts_match_the_header(tmp_path):
     if shutil.which("gcc") is None:
         pytest.skip("no gcc")
@@ -785,3 +793,18 @@ def test_gpu_prefill_refuses_what_has_no_room(torch, example):
     pages = example.Pages(example.Shape(layers=1), [(9, 9)], [3], room=40)
     with pytest.raises(ValueError):
         pages.prefill(per_step=10)
+
+
+@gpu
+def test_gpu_attn_calls_of_fewer_rows_than_the_operator_was_made_for(torch):
+    # 4,096 rows leave no SM idle, one row of a long context is split over all: the
+    # same operator, the oracle's values
+    c = _attn_case(torch, [1, 0], [3000, 9], 32, 8, 128, seed=22)
+    want, lse = H.ChunkAttn(32, c["kc"], c["vc"], c["table"], max_tokens=1)(c["q"], c["cu"], c["total"])
+    op = H.ChunkAttn(32, c["kc"], c["vc"], c["table"], max_tokens=4096)
+    for _ in range(2):
+        got = op(c["q"], c["cu"], c["total"])
+        torch.cuda.synchronize()
+        assert op.errors() == 0 and got[0].shape == want.shape
+        assert torch.equal(got[0], want) and torch.equal(got[1], lse)
+    _check_attn(torch, c)
