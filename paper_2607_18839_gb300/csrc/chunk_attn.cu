@@ -36,8 +36,10 @@
 // run again with its rows' true maxima, which a pass over S alone finds first.
 // Which units are is a matter of their own scores and values alone, so that a
 // call's bits do not depend on which CTA took which unit.  O is never rescaled.
-// P goes to the tensor cores in two parts: while the exponentials of the second 32 keys of a half are
-// taken, P V of the first 32 runs.
+// P is rounded to bf16, as the tensor cores take it (2^-9 of each weight, in either
+// direction); its sum is of the values before, in 32 bits, like scores and O.  P goes to
+// the tensor cores in two parts: while the exponentials of the second 32 keys of a
+// half are taken, P V of the first 32 runs.
 //
 // Rows that see no key are written by the scheduler.  Cache rows past a
 // sequence's end may hold anything: pages past it are not loaded (their box lies
@@ -49,6 +51,24 @@
 // run again, and that such a value may have reached, are computed once
 // more from what they see, one row at a time.
 // All waits are bounded, as in the branch attention kernel.
+//
+// What bounds it, and what it measured on a GB300 (calls one after another):
+//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 347-357 us, 1.44-1.49 PFLOP/s;
+//     the power limit.  At the full clock 289 us, 1.78 PFLOP/s, with the tensor pipe
+//     at work 87 % of the time.
+//   64 sequences that bring a token, contexts to 8,191, 32 / 8 heads of 128: 210 us,
+//     6.0 TB/s of 6.8: HBM.
+//   1,152 tokens of one page, 16 / 2 heads of 128: 15.5 us, of which the blocks have
+//     6: 3.4 us pass until the first scores (lengths, page ids, Q and K one after the
+//     other, through code that runs for the first time), 3.5 from the last P V to
+//     the end (O, its stores, the exit).
+//   A unit's change takes some 2 us and a block 0.63 with heads of 128 (0.53 of it MMAs);
+//     0.7 and 0.54 with heads of 64, where no pipe is full: a look at a barrier
+//     takes a warp 150 to 200 cycles while the others work, and each role makes
+//     two or three a block.
+// Halves of a block for the two softmax warpgroups, and not alternate blocks: those
+// took 0.67 us a block with heads of 128 and 0.52 with heads of 64 (three buffers of
+// scores, five stages).
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -83,9 +103,10 @@ constexpr int kNoUnit = (1 << 30) - 1;  // every unit's number is below
 constexpr uint64_t kBlockLimitNs = 10000;  // of a unit's time: a block takes some 0.7 us
 
 // A unit of a tile whose blocks are split: what the merge needs to know.
-struct SlotInfo {
+struct __align__(16) SlotInfo {
   int tok0, nrows, g, split, nsplit, pad[3];
 };
+static_assert(sizeof(SlotInfo) == 32, "read 16 bytes at a time");
 
 struct ChunkParams {
   const __nv_bfloat16 *q;
@@ -1149,25 +1170,42 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Joins the splits of a tile, a CTA for every split, each with its share of the rows,
 // a warp a row:
 //   lse = log sum_s exp(lse_s),  out = sum_s exp(lse_s - lse) out_s
-// What bounds it: the launch, and reading the partial results from L2.
-constexpr int kMergeWarps = 8;
+// What bounds it: the launch and three loads one after the other (the tile, then its
+// sums and results together), where rows are few; else reading the results from L2.
+constexpr int kMergeWarps = 16;
+constexpr int kMergeAhead = 8;  // splits whose results are on their way at once
 template <int D>
 __global__ void __launch_bounds__(32 * kMergeWarps) chunk_merge_kernel(const ChunkParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
-  if (static_cast<int>(blockIdx.x) >= *p.n_slots) return;
-  const SlotInfo info = p.slot[blockIdx.x];
-  const int n = info.nsplit;
-  if (n <= 1) return;
-  const size_t slot0 = blockIdx.x - info.split * p.H_kv;  // of split 0; the next are H_kv on
+  int n_slots, tok0, nrows, g, split, n;  // (both loads before the first decision)
+  asm volatile("ld.global.b32 %0, [%1];" : "=r"(n_slots) : "l"(p.n_slots));
+  asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(tok0), "=r"(nrows), "=r"(g), "=r"(split)
+               : "l"(&p.slot[blockIdx.x]));
+  asm volatile("ld.global.b32 %0, [%1];" : "=r"(n) : "l"(&p.slot[blockIdx.x].nsplit));
+  if (static_cast<int>(blockIdx.x) >= n_slots || n <= 1) return;
+  const size_t slot0 = blockIdx.x - split * p.H_kv;  // of split 0; the next are H_kv on
   const float NEG_INF = -__int_as_float(0x7f800000);
   constexpr int kV = D / 32;  // values of a lane
-  const int lo = info.split * info.nrows / n, hi = (info.split + 1) * info.nrows / n;
+  const size_t stride = static_cast<size_t>(p.H_kv) * kRows * D;
+  const int lo = split * nrows / n, hi = (split + 1) * nrows / n;
   for (int r = lo + warp; r < hi; r += kMergeWarps) {
-    const int rt = p.div_G(r);
-    const size_t pair = static_cast<size_t>(info.tok0 + rt) * p.H_q + info.g * p.G + r - rt * p.G;
+    const float *src = p.o_part + (slot0 * kRows + r) * D + lane * kV;
     const float l = lane < n ? p.l_part[(slot0 + static_cast<size_t>(lane) * p.H_kv) * kRows + r] : NEG_INF;
+    float v[kMergeAhead][kV];
+    auto load = [&](int s0) {
+#pragma unroll
+      for (int i = 0; i < kMergeAhead; ++i)
+        if (s0 + i < n) {
+          if constexpr (kV == 4)
+            *reinterpret_cast<float4 *>(v[i]) = *reinterpret_cast<const float4 *>(src + (s0 + i) * stride);
+          else
+            *reinterpret_cast<float2 *>(v[i]) = *reinterpret_cast<const float2 *>(src + (s0 + i) * stride);
+        }
+    };
+    load(0);
     float m = l;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -1180,14 +1218,18 @@ __global__ void __launch_bounds__(32 * kMergeWarps) chunk_merge_kernel(const Chu
     float acc[kV];
 #pragma unroll
     for (int c = 0; c < kV; ++c) acc[c] = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < n; ++s) {
-      const float ws = __shfl_sync(0xffffffffu, w, s);
-      if (ws == 0.f) continue;  // (an empty partial is not written)
-      const float *src = p.o_part + ((slot0 + static_cast<size_t>(s) * p.H_kv) * kRows + r) * D + lane * kV;
+#pragma unroll 1
+    for (int s0 = 0; s0 < n; s0 += kMergeAhead) {
+      if (s0 > 0) load(s0);
 #pragma unroll
-      for (int c = 0; c < kV; ++c) acc[c] = fmaf(ws, src[c], acc[c]);
+      for (int i = 0; i < kMergeAhead; ++i) {
+        const float ws = __shfl_sync(0xffffffffu, w, s0 + i);
+#pragma unroll
+        for (int c = 0; c < kV; ++c) acc[c] = ws == 0.f ? acc[c] : fmaf(ws, v[i][c], acc[c]);  // (an empty partial is not written)
+      }
     }
+    const int rt = p.div_G(r);
+    const size_t pair = static_cast<size_t>(tok0 + rt) * p.H_q + g * p.G + r - rt * p.G;
     uint32_t *dst = reinterpret_cast<uint32_t *>(p.out + pair * D) + lane * (kV / 2);
 #pragma unroll
     for (int c = 0; c < kV; c += 2) dst[c / 2] = pack_bf16x2(acc[c] * inv, acc[c + 1] * inv);

@@ -12,7 +12,9 @@
 // search of cu finds.  The first token of a page that is new enters it in the
 // table.  The last CTA to have read the lengths writes the new ones and the
 // stack's top, so that both may be updated in place.
-// What bounds it: the chain of lengths, scan, page id and store.
+// What bounds it: the chain of lengths, scan, page id and store.  4 sequences with 46
+// new tokens take 4.7 us, 512 with 63,260 take 6.2 (in a graph 4.4 and 6.0); their
+// bytes would take 0.08 at a copy's rate.
 #include <algorithm>
 
 #include "common.cuh"
