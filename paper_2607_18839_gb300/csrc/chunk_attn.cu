@@ -32,7 +32,7 @@
 // not replace, so that both threads of the row read them and neither waits for the
 // other.  Exponentials are taken against that base throughout, which is exact to
 // the same relative error as a running maximum as long as nothing overflows: a
-// unit in which a score exceeds its base by more than 2^64, or O is not finite, is
+// unit in which a weight would exceed 2^64, or O is not finite, is
 // run again with its rows' true maxima, which a pass over S alone finds first.
 // Which units are is a matter of their own scores and values alone, so that a
 // call's bits do not depend on which CTA took which unit.  O is never rescaled.
@@ -53,11 +53,11 @@
 // All waits are bounded, as in the branch attention kernel.
 //
 // What bounds it, and what it measured on a GB300 (calls one after another):
-//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 347-357 us, 1.44-1.49 PFLOP/s;
+//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 340-350 us, 1.47-1.51 PFLOP/s;
 //     the power limit.  At the full clock 289 us, 1.78 PFLOP/s, with the tensor pipe
 //     at work 87 % of the time.
-//   64 sequences that bring a token, contexts to 8,191, 32 / 8 heads of 128: 210 us,
-//     6.0 TB/s of 6.8: HBM.
+//   64 sequences that bring a token, contexts to 8,191, 32 / 8 heads of 128: 207 us,
+//     6.1 TB/s of 6.8: HBM.
 //   1,152 tokens of one page, 16 / 2 heads of 128: 15.5 us, of which the blocks have
 //     6: 3.4 us pass until the first scores (lengths, page ids, Q and K one after the
 //     other, through code that runs for the first time), 3.5 from the last P V to
@@ -1171,7 +1171,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 // a warp a row:
 //   lse = log sum_s exp(lse_s),  out = sum_s exp(lse_s - lse) out_s
 // What bounds it: the launch and three loads one after the other (the tile, then its
-// sums and results together), where rows are few; else reading the results from L2.
+// sums and results together) where rows are few; else reading the results from L2.
+// Without it, one token behind 3,999 takes 12.2 us, with it 13.2 (17.2 with 8 warps and a
+// split's result loaded behind its sums); 700 behind 2,300 with 40 heads 34, 40 (50).
 constexpr int kMergeWarps = 16;
 constexpr int kMergeAhead = 8;  // splits whose results are on their way at once
 template <int D>
@@ -1267,7 +1269,11 @@ struct ChunkPlan {
 // Tiles may be split where the call's units leave SMs idle in their last (or only)
 // wave.  Only host scalars enter (the kernel then splits by the true lengths): the
 // time of units of the longest sequences, in blocks, whole against split after the
-// full waves, a unit's start and end counted as 3.5 blocks, the merge as 8.
+// full waves, a unit's start and end counted as 3.5 blocks, the merge as 10.  (16 / 4
+// heads of 64, 500 tokens behind 2,000: 18.8 us whole; with 8, and so split, 21.7.  16 / 2
+// heads of 128, one token behind 1,799: 13.1 us split; with 13, and so whole, 16.7.
+// Split against whole: one token behind 2,499 13.1 and 19.2, 16 behind 8,984 16.8 and
+// 47.9, 2,048 behind 14,336 with 32 / 8 heads 341 and 346.)
 ChunkPlan make_plan(const hpd_chunk_attn_args *a) {
   ChunkPlan pl{};
   const int G = a->H_q / a->H_kv, TT = kRows / G;
@@ -1282,7 +1288,7 @@ ChunkPlan make_plan(const hpd_chunk_attn_args *a) {
   for (int waves = 1; waves <= kTailWaves && left; ++waves) {
     const long long share = std::max<long long>(2, (left * N + kPlanSms * waves - 1) / (kPlanSms * waves));
     const long long f = std::min<long long>(std::max<long long>(N / share, 1), kMaxSplits);
-    split = std::min(split, full + 8 + ((left * f + kPlanSms - 1) / kPlanSms) * ((N + f - 1) / f + 3.5));
+    split = std::min(split, full + 10 + ((left * f + kPlanSms - 1) / kPlanSms) * ((N + f - 1) / f + 3.5));
   }
   // Room for split tiles wherever some number of rows up to T could have them (of four
   // blocks at least), so that a workspace serves every call of no more rows.  At most
