@@ -13,8 +13,9 @@
 // table.  The last CTA to have read the lengths writes the new ones and the
 // stack's top, so that both may be updated in place.
 // What bounds it: the chain of lengths, scan, page id and store.  4 sequences with 46
-// new tokens take 4.7 us, 512 with 63,260 take 6.2 (in a graph 4.4 and 6.0); their
-// bytes would take 0.08 at a copy's rate.
+// new tokens take 4.2 us, 512 with 63,260 take 5.8; their bytes would take 0.08 at a
+// copy's rate.  (With every CTA waiting for the answer of the count before its tokens,
+// fences in a call of one CTA among them: 4.7 and 6.2.)
 #include <algorithm>
 
 #include "common.cuh"
@@ -55,7 +56,7 @@ __global__ void __launch_bounds__(kSlotThreads) chunk_slots_kernel(const SlotArg
   __shared__ int2 s_warp[kSlotThreads / 32];
   __shared__ int s_bad, s_last, s_top;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) s_bad = 0;
+  if (tid == 0) s_bad = s_cu[0] = s_pg[0] = 0;
   pdl_wait();     // the lengths, tables and the stack as the kernel before leaves them
   pdl_trigger();  // the next kernel may launch; it waits for this one
   if (tid == kSlotThreads - 1) s_top = *a.free_top;  // on its way with the lengths
@@ -93,29 +94,27 @@ __global__ void __launch_bounds__(kSlotThreads) chunk_slots_kernel(const SlotArg
     base = make_int2(add_sat(base.x, all.x), add_sat(base.y, all.y));
     __syncthreads();  // s_warp is reused
   }
-  if (tid == 0) {
-    s_cu[0] = 0;
-    s_pg[0] = 0;
-    // this CTA has read all lengths and the top into shared memory
+  // This CTA has read all lengths and the top into shared memory: who is the last to
+  // say so writes the new ones, once the answer is here.
+  int before = 0;
+  if (gridDim.x > 1 && tid == 0) {
     __threadfence();
-    s_last = gridDim.x == 1 || atomicAdd(a.ticket, 1) == static_cast<int>(gridDim.x) - 1;
-    if (s_last && gridDim.x > 1) *a.ticket = 0;
-    __threadfence();
+    before = atomicAdd(a.ticket, 1);
   }
-  __syncthreads();
   const int total = base.x, pages = base.y, top = s_top;
   const uint32_t why = s_bad                                                          ? HPD_DEVERR_BRANCH_LEN
                        : total > a.max_tokens                                         ? HPD_DEVERR_CHUNK_CAP
                        : top < 0 || top > a.num_pages || pages > top                  ? HPD_DEVERR_POOL
                                                                                       : 0u;
-  if (s_last) {
+  auto write_lengths = [&] {
     for (int s = tid; s < a.S; s += kSlotThreads)
       a.seq_len_out[s] = why ? s_len[s] : s_len[s] + (s_cu[s + 1] - s_cu[s]);
     if (tid == 0) {
       *a.free_top_out = why ? top : top - pages;
       if (why) atomicOr(a.err, why);
     }
-  }
+  };
+  if (gridDim.x == 1) write_lengths();
   if (blockIdx.x == 0)
     for (int s = tid; s <= a.S; s += kSlotThreads) a.chunk_cu[s] = why ? 0 : s_cu[s];
   const int end = why ? 0 : total, first = top - pages;
@@ -164,6 +163,17 @@ __global__ void __launch_bounds__(kSlotThreads) chunk_slots_kernel(const SlotArg
           if (a.pos) a.pos[t0 + i] = pos[i];
         }
     }
+  }
+  if (gridDim.x > 1) {
+    if (tid == 0) {
+      s_last = before == static_cast<int>(gridDim.x) - 1;
+      if (s_last) {
+        *a.ticket = 0;
+        __threadfence();
+      }
+    }
+    __syncthreads();
+    if (s_last) write_lengths();
   }
 }
 
