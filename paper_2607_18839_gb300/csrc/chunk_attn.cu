@@ -535,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // (one group) The tiles of full waves stay whole; what is left over after them
         // is split, into as many even waves as take the least time: a unit's start and
         // end are worth some 3.5 blocks.
-        whole = tiles * p.H_kv / static_cast<int>(gridDim.x) * static_cast<int>(gridDim.x) / p.H_kv;
+        whole = p.div_Hkv(tiles * p.H_kv / static_cast<int>(gridDim.x) * static_cast<int>(gridDim.x));
         float blocks = 0.f;  // of the others, all heads
 #pragma unroll 1
         for (int i = lane; i < count; i += 32) {
@@ -656,8 +656,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int lim0 = len - n + i0 + 1;
         const int kmax = min(max(max(lim0 + ntok - 1, full), 0), len);
         const int N = ceil_div_i(kmax, kBlk);
-        const int blk_lo = nsplit > 1 ? static_cast<int>(static_cast<long long>(split) * N / nsplit) : 0;
-        const int blk_hi = nsplit > 1 ? static_cast<int>(static_cast<long long>(split + 1) * N / nsplit) : N;
+        // (N below 2^23, at most 32 splits)
+        const int blk_lo = nsplit > 1 ? split * N / nsplit : 0, blk_hi = nsplit > 1 ? (split + 1) * N / nsplit : N;
         const int slot_id = u - first_slot;  // of the units of tiles that may be split
         if (slot_id >= 0 && lane == 0) p.slot[slot_id] = SlotInfo{c0 + i0, nrows, g, split, nsplit, {0, 0, 0}};
         if (blk_hi <= blk_lo) {
