@@ -462,8 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
-  pdl_wait();     // queries, cache, tables and lengths as the kernels before leave them
-  pdl_trigger();  // the merge of the splits may launch; it waits for this grid
+  // (each role waits for the kernels before where it starts, with its first code fetched)
 
   if (warp == kSchedWarp) {
     // ------------------------------------------------------- scheduler --
@@ -480,6 +479,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       len = p.seq_len[i];
       if (p.full_len) full = p.full_len[i];
     };
+    pdl_wait();     // queries, cache, tables and lengths as the kernels before leave them
+    pdl_trigger();  // the merge of the splits may launch; it waits for this grid
     int fetched = 0;  // group whose first lengths are on their way
     fetch(lane);
     auto load_group = [&](int s0, int units_before) {
@@ -717,6 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       prefetch_tmap(is_k ? &tm_k4 : &tm_v4);
     }
     __syncwarp();
+    pdl_wait();
     uint64_t *const full = is_k ? sh.k_full : sh.v_full, *const empty = is_k ? sh.k_empty : sh.v_empty;
     const CUtensorMap *const page_map = is_k ? &tm_k : &tm_v, *const run_map = is_k ? &tm_k4 : &tm_v4;
     const uint32_t ring = sbase + (is_k ? L::kK : L::kV), mine = half * (L::kTileBytes / 2);
@@ -795,6 +797,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t dq0 = smem_desc_sw128(sbase + L::kK, 16, 1024);
     const uint64_t dk0 = smem_desc_sw128(sbase + L::kK, 16, L::kGroupBytes);
     const bool issuer = elect_one();
+    pdl_wait();
     uint32_t sk = 0, pk = 0;  // K ring: stage, phase
     int jg = 0;               // blocks issued
     bool ok = true;
@@ -843,6 +846,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr uint32_t idesc_pv = idesc_bf16_f32(kRows, D, true);
     const uint64_t dv0 = smem_desc_sw128(sbase + L::kV, 1024, L::kGroupBytes);
     const bool issuer = elect_one();
+    pdl_wait();
     uint32_t sv = 0, pv = 0;  // V ring: stage, phase
     int jg = 0;               // blocks issued
     int outputs = 0;          // units whose O was made
@@ -928,6 +932,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int r_in = quad * 32 + lane;  // row within the tile
     const uint32_t o_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::kColO;
     const uint32_t stage = sbase + L::kStage + quad * 32 * 128;  // of this warp's rows
+    pdl_wait();
     const int rt = p.div_G(r_in);
     int outputs = 0;
     bool ok = true;
@@ -1062,6 +1067,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     const int rt = p.div_G(r_in);
     const float sl2 = p.scale_log2;
+    pdl_wait();
     int jg = 0;            // blocks in all
     float given = NEG_INF;  // the row's maximum, which a pass over the maxima found
     bool ok = true;
