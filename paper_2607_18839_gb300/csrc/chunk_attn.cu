@@ -1300,8 +1300,9 @@ ChunkPlan make_plan(const hpd_chunk_attn_args *a) {
   // blocks at least), so that a workspace serves every call of no more rows.  At most
   // an SM's share of blocks a unit, and the units that are no longer than it.
   const int room = a->S <= kGroup && N >= 4 ? (kTailWaves + 1) * kPlanSms + 2 * a->H_kv : 0;
-  pl.slots = split < 0.97 * none ? room : 0;
   const long long tiles_max = (a->T + seqs * (TT - 1)) / TT;
+  if (split < 0.97 * none)
+    pl.slots = static_cast<int>(std::min<long long>(room, tiles_max * a->H_kv * std::min(kMaxSplits, N)));
   pl.units = tiles_max * a->H_kv + pl.slots;
   pl.off_opart = kAlign;
   pl.off_lpart = align_up(pl.off_opart + static_cast<size_t>(room) * kRows * a->D * sizeof(float));
