@@ -711,8 +711,9 @@ class ChunkAttn:
         if q.dtype is not bf or q.dim() != 3 or q.shape[1:] != (H_q, D) or not q.is_cuda:
             _need("ChunkAttn", q, bf, (None, H_q, D), strides_free=True)
         T, (row, head, step) = q.shape[0], q.stride()
-        if T > self.max_tokens or T < 1 or step != 1 or (head != D and H_q > 1):
-            raise HpdError("ChunkAttn", 1, "1 to max_tokens rows with their heads side by side")
+        # (a row stride of 0, as expand() leaves it, is H_q * D to the C call)
+        if T > self.max_tokens or T < 1 or step != 1 or (head != D and H_q > 1) or (T > 1 and row < H_q * D):
+            raise HpdError("ChunkAttn", 1, "1 to max_tokens rows with their heads side by side, none over another")
         if not _is(chunk_cu, i32, (S + 1,)) or not _is(seq_len, i32, (S,)):
             _need("ChunkAttn", chunk_cu, i32, (S + 1,))
             _need("ChunkAttn", seq_len, i32, (S,))
