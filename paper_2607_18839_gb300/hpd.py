@@ -538,11 +538,12 @@ def rope_table(max_pos: int, D: int, theta: float = 1e6, device="cuda"):
     return torch.stack((a.cos(), a.sin()), -1).float().contiguous()
 
 
-def _ready_workspace(nbytes: int, device, stream=None):
-    """A cleared workspace that a call on any stream may use from now on."""
+def _ready_workspace(nbytes: int, device):
+    """A cleared workspace that a call on any stream may use from now on: cleared
+    on the stream that allocated it, behind what that has yet to write there."""
     import torch
     t = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    hpd_workspace_init(_ptr(t), nbytes, _stream_handle(stream))
+    hpd_workspace_init(_ptr(t), nbytes, _stream_handle(None))
     torch.cuda.synchronize(device)
     return t
 
@@ -673,7 +674,8 @@ class QkNormRope:
 class ChunkAttn:
     """Attention of up to max_tokens new tokens over the paged cache
     (hpd_chunk_attn).  Owns out [max_tokens, H_q, D], lse [max_tokens, H_q]
-    and the workspace."""
+    and the workspace, which is ready for calls on any stream once this is made
+    (on the current one, whatever ``stream``)."""
 
     def __init__(self, H_q, k_cache, v_cache, page_table, max_tokens, max_seq_len=0, scale=0.0,
                  stream=None):
@@ -699,7 +701,7 @@ class ChunkAttn:
         self.max_tokens = max_tokens
         self._H_q, self._D, self._S = H_q, D, S
         self._bf, self._i32 = bf, torch.int32
-        self.workspace = _ready_workspace(nbytes, dev, stream)
+        self.workspace = _ready_workspace(nbytes, dev)
         a.workspace, a.workspace_bytes = _ptr(self.workspace), nbytes
 
     def __call__(self, q, chunk_cu, seq_len, full_len=None, stream=None):

@@ -78,3 +78,11 @@ def test_attn_refuses_rows_that_share_storage(host):
     op(one.expand(1, 4, 64), host.i32(3), host.i32(2))  # one row has no stride
     op(host.bf(8, 5, 64)[:, :4], host.i32(3), host.i32(2))
     assert [c[0] for c in host.calls[n:]] == ["hpd_chunk_attn"] * 2 and host.calls[-1][1].q_stride == 5 * 64
+
+
+def test_attn_workspace_is_cleared_on_the_stream_that_allocated_it(host):
+    # what the current stream still has to write there comes before the clearing
+    for kw in ({}, dict(stream="side")):
+        host.calls.clear()
+        op = _attn_op(host, **kw)
+        assert host.calls == [("clear", op.workspace.data_ptr(), op.workspace.numel(), "current"), ("synchronize",)]
