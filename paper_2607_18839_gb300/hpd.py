@@ -617,7 +617,7 @@ class QkNormRope:
         a.workspace, a.eps = _ptr(self.workspace), eps
         a.H_q, a.H_kv, a.D, a.n_axes, a.max_pos = H_q, H_kv, D, self.n_axes, rope.shape[0]
         a.axis[:D // 2] = axis
-        self._bf, self._i32 = torch.bfloat16, torch.int32
+        self._bf, self._i32, self._on = torch.bfloat16, torch.int32, torch.cuda.stream
         self._q = None
         self._outgrown = []  # still the target of captured graphs, or of calls on other streams
 
@@ -654,7 +654,9 @@ class QkNormRope:
                 if self._q is not None:  # (at least doubled, so that those kept stay below the last one's size)
                     self._outgrown.append(self._q)
                     rows = max(T, 2 * self._q.shape[0])
-                self._q = qkv.new_empty((rows, H_q, D))
+                # (the call's stream allocates it: behind it lies what may still write there)
+                with self._on(stream):
+                    self._q = qkv.new_empty((rows, H_q, D))
             q_out = self._q if self._q.shape[0] == T else self._q[:T]
         elif not _is(q_out, bf, (T, H_q, D)):
             _need("QkNormRope", q_out, bf, (T, H_q, D))

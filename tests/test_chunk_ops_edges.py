@@ -40,7 +40,7 @@ class Host:
 
         @contextlib.contextmanager
         def on(stream):
-            before, self.stream = self.stream, stream
+            before, self.stream = self.stream, stream or self.stream  # (None: no other)
             yield
             self.stream = before
 
@@ -58,6 +58,27 @@ class Host:
 @pytest.fixture
 def host(lib, monkeypatch):
     return Host(pytest.importorskip("torch"), monkeypatch)
+
+
+# --------------------------------------------------- norms, rotation, write --
+
+def test_norm_rope_output_grows_on_the_stream_of_the_call(host, monkeypatch):
+    # memory of the current stream may still be written there by what was enqueued
+    # before; the call's kernel does not wait for that
+    made, cache = [], host.bf(2, PAGE, 2, 64)
+    new_empty = host.torch.Tensor.new_empty
+
+    def note(self, *a, **kw):
+        made.append(host.stream)
+        return new_empty(self, *a, **kw)
+
+    monkeypatch.setattr(host.torch.Tensor, "new_empty", note)
+    for stream in (None, "side"):
+        op = host.rope()
+        for T in (3, 2, 9):
+            op(host.bf(T, 8 * 64), host.i32(T), host.i32(T), cache, cache, stream=stream)
+            assert host.calls[-1][2] == (stream or "current")
+    assert made == ["current", "current", "side", "side"]
 
 
 # ---------------------------------------------------------------- attention --
