@@ -74,11 +74,12 @@ def test_norm_rope_output_grows_on_the_stream_of_the_call(host, monkeypatch):
 
     monkeypatch.setattr(host.torch.Tensor, "new_empty", note)
     for stream in (None, "side"):
+        made.clear()
         op = host.rope()
         for T in (3, 2, 9):
             op(host.bf(T, 8 * 64), host.i32(T), host.i32(T), cache, cache, stream=stream)
             assert host.calls[-1][2] == (stream or "current")
-    assert made == ["current", "current", "side", "side"]
+        assert set(made) == {stream or "current"}
 
 
 # ---------------------------------------------------------------- attention --
