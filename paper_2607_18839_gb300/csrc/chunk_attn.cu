@@ -747,7 +747,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto look_up = [&](int j) {
         const int i = page0 + j * kPagesPerBlock;
         ids_next = p.num_pages;
-        if (i < M.pages) ids_next = __ldg(row + i);
+        // (a coherent load: the kernel before may write the table while this one starts)
+        if (i < M.pages) ids_next = row[i];
       };
       look_up(0);
 #pragma unroll 1

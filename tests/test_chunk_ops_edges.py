@@ -2,6 +2,8 @@
 calls of no rows and of one, tensors that share their storage, streams, values
 that are not finite among long contexts."""
 import contextlib
+import os
+import re
 
 import pytest
 
@@ -108,3 +110,12 @@ def test_attn_workspace_is_cleared_on_the_stream_that_allocated_it(host):
         host.calls.clear()
         op = _attn_op(host, **kw)
         assert host.calls == [("clear", op.workspace.data_ptr(), op.workspace.numel(), "current"), ("synchronize",)]
+
+
+def test_no_loads_past_the_coherent_cache():
+    # kernels start while the one before them still writes what they read, and
+    # non-coherent loads are only for what nothing writes while a kernel runs
+    for path in B.sources() + [os.path.join(B.CSRC, f) for f in os.listdir(B.CSRC) if f.endswith(".cuh")]:
+        with open(path) as f:
+            text = f.read()
+        assert not re.search(r"__ldg\b|ld\.global\.(\w+\.)*nc\b", text), path
