@@ -47,9 +47,9 @@
 // behind it in its last page are zeroed in shared memory (a weight of zero would
 // not keep out what is not finite).
 // A value that is not finite in a row that some of a tile's rows see and others do
-// not would reach the others as 0 times it: rows whose O is not finite when
-// run again, and that such a value may have reached, are computed once
-// more from what they see, one row at a time.
+// not would reach the others as 0 times it: when a unit is run again, such values are
+// taken out of the blocks (two at most) that some of its rows see part of, and added to
+// the rows that see them.
 // All waits are bounded, as in the branch attention kernel.
 //
 // What bounds it, and what it measured on a GB300 (calls one after another):
@@ -185,6 +185,8 @@ struct __align__(16) Shared {
   int max_seq[4][2];  // [quadrant][half]: units whose maxima are published
   unsigned redo;            // units (by number in this CTA, modulo 32) to run once more
   int units_done;           // output warps that looked at a unit's output
+  uint32_t sieved[kMetaSlots][128];  // what sieve_block found in the unit of the slot, by column
+  int sieved_seq;                    // units of which that is complete
   int unit_id[32];          // the last units issued
   UnitMeta meta[kMetaSlots];
   // the scheduler's group of sequences: units before each, first rows, rows, lengths,
@@ -342,65 +344,63 @@ __device__ __forceinline__ bool softmax_masked(uint32_t s_addr, int hi, float sl
   return fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) * mul <= base + tc::kWindowLog2;
 }
 
-// One row over keys [lo, hi) of its sequence by one warp, from global memory and
-// nothing but what the row sees: for rows that a value of another row's keys may
-// have reached through the tensor cores.  Writes the normalised row (o_f, or o_b if
-// o_f is null).
+// Values that are not finite in a block of V that some of the tile's rows do not see all
+// of: they are taken out of shared memory, as 0 times them would reach those rows too,
+// and `first` keeps, for every column, the first key with NaN, +inf and -inf (10 bits
+// each, keys counted from key0 = 0 at the first such block; kNoKey: none).  A lane has
+// D / 32 columns, in `first` too.  v0: the block in shared memory.
+constexpr uint32_t kNoKey = 1023u;
 template <int D>
-__device__ __noinline__ void one_row(const ChunkParams &p, int seq, int token, int head, int lo, int hi, float *o_f,
-                                     __nv_bfloat16 *o_b) {
-  const int lane = threadIdx.x & 31, g = p.div_G(head);
-  const float NEG_INF = -__int_as_float(0x7f800000);
-  const __nv_bfloat16 *q = p.q + token * p.q_stride + head * D;
-  float m = NEG_INF, l = 0.f, o[D / 32];
+__device__ __noinline__ void sieve_block(uint32_t v0, int key0, uint32_t *first) {
+  using L = Layout<D>;
+  constexpr int kCols = D / 32;
+  const int c = (threadIdx.x & 31) * kCols;
+  uint32_t seen[kCols];
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) o[c] = 0.f;
+  for (int i = 0; i < kCols; ++i) seen[i] = first[c + i];
 #pragma unroll 1
-  for (int j0 = lo; j0 < hi; j0 += 32) {
-    const int j = j0 + lane;
-    int pg = 0;
-    float x = NEG_INF;
-    if (j < hi) {
-      pg = p.page_table[static_cast<size_t>(seq) * p.max_pages + j / kPage];
-      if (static_cast<unsigned>(pg) >= static_cast<unsigned>(p.num_pages)) pg = 0;
-      const __nv_bfloat162 *k = reinterpret_cast<const __nv_bfloat162 *>(
-          p.k_cache + ((static_cast<size_t>(pg) * kPage + j % kPage) * p.H_kv + g) * D);
-      const __nv_bfloat162 *q2 = reinterpret_cast<const __nv_bfloat162 *>(q);
-      x = 0.f;
-#pragma unroll 8
-      for (int c = 0; c < D / 2; ++c) {
-        const float2 a = __bfloat1622float2(q2[c]), b = __bfloat1622float2(k[c]);
-        x = fmaf(a.x, b.x, fmaf(a.y, b.y, x));
-      }
-      x *= p.scale_log2;
+  for (int r = 0; r < kBlk; ++r) {
+    const uint32_t at = v0 + (r >> 3) * L::kGroupBytes + (c / 64) * 1024 + (r & 7) * 128 +
+                        (((c % 64 / 8) ^ (r & 7)) << 4) + c % 8 * 2;
+    uint32_t w[kCols / 2];
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kCols / 2; ++i) {
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[i]) : "r"(at + 4 * i) : "memory");
+      any |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
     }
-    float mx = x;
-#pragma unroll 1
-    for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-    const float m_new = fmaxf(m, mx), base = m_new == NEG_INF ? 0.f : m_new;
-    const float alpha = exp2f(m - base), e = exp2f(x - base);
-    m = m_new;
-    float sum = e;
-#pragma unroll 1
-    for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-    l = l * alpha + sum;
+    if (!any) continue;
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) o[c] *= alpha;
-    const int n = min(32, hi - j0);
-#pragma unroll 1
-    for (int i = 0; i < n; ++i) {
-      const float ei = __shfl_sync(0xffffffffu, e, i);
-      const int pgi = __shfl_sync(0xffffffffu, pg, i);
-      const __nv_bfloat16 *v = p.v_cache + ((static_cast<size_t>(pgi) * kPage + (j0 + i) % kPage) * p.H_kv + g) * D;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) o[c] = fmaf(ei, __bfloat162float(v[c * 32 + lane]), o[c]);
+    for (int i = 0; i < kCols; ++i) {
+      const uint32_t x = w[i / 2] >> (16 * (i & 1)) & 0xffffu;
+      if ((x & 0x7f80u) != 0x7f80u) continue;
+      const int shift = x & 0x7fu ? 0 : x & 0x8000u ? 20 : 10;
+      if ((seen[i] >> shift & kNoKey) == kNoKey)
+        seen[i] = (seen[i] & ~(kNoKey << shift)) | static_cast<uint32_t>(key0 + r) << shift;
+      w[i / 2] &= ~(0xffffu << (16 * (i & 1)));
     }
+#pragma unroll
+    for (int i = 0; i < kCols / 2; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + 4 * i), "r"(w[i]) : "memory");
   }
-  const float inv = l > 0.f ? 1.f / l : l;
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) {
-    if (o_f) o_f[c * 32 + lane] = o[c] * inv;
-    else o_b[c * 32 + lane] = __float2bfloat16(o[c] * inv);
+  for (int i = 0; i < kCols; ++i) first[c + i] = seen[i];
+}
+// A row's sums with those values of its first `keys` keys (counted as above) added, in o_f,
+// or in o_b if o_f is null.  Their weights are positive: what they are does not matter.
+template <int D>
+__device__ __noinline__ void add_sieved(const uint32_t *first, int keys, float *o_f, __nv_bfloat16 *o_b) {
+#pragma unroll 1
+  for (int c = 0; c < D; ++c) {
+    const uint32_t f = first[c];
+    if (f == ((kNoKey << 20) | (kNoKey << 10) | kNoKey)) continue;
+    auto sees = [&](int shift) { return static_cast<int>(f >> shift & kNoKey) < keys; };
+    const float inf = __int_as_float(0x7f800000);
+    float add = sees(0) ? __int_as_float(0x7fffffff) : 0.f;
+    if (sees(10)) add += inf;
+    if (sees(20)) add -= inf;
+    if (add == 0.f) continue;
+    if (o_f) o_f[c] += add;
+    else o_b[c] = __float2bfloat16(__bfloat162float(o_b[c]) + add);
   }
 }
 
@@ -429,6 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     sh.abort = 0;
     sh.redo = 0u;
     sh.units_done = 0;
+    sh.sieved_seq = 0;
     for (int s = 0; s < kStages; ++s) {
       mbar_init(bar(sh.k_full[s]), 2);
       mbar_init(bar(sh.v_full[s]), 2);
@@ -855,14 +856,25 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int k = 0; ok; ++k) {
       const int slot = k % kMetaSlots;
       if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
-      const bool valid = sh.meta[slot].valid != 0, maxima = sh.meta[slot].pass == kMaxima;
+      const bool valid = sh.meta[slot].valid != 0;
+      const int pass = sh.meta[slot].pass;
       const int nb = sh.meta[slot].n_blocks, len = sh.meta[slot].L;
       // the block with rows behind the sequence's end in its last page
       const int j_tail = len % kPage ? len / kBlk - sh.meta[slot].blk_lo : -1;
+      // the first block that not every row of the tile sees all of (its first token sees
+      // least, the last one at most 127 keys more: two blocks at most), in a unit that is
+      // run again
+      int j_sieve = nb;
+      if (pass == kAgain)
+        j_sieve = max(max(min(max(sh.meta[slot].lim0, sh.meta[slot].full), len), 0) / kBlk - sh.meta[slot].blk_lo, 0);
       __syncwarp();
       if (!valid) break;
       if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
-      if (maxima) {  // nothing to multiply: the scores are only read
+      if (pass == kAgain) {
+        for (int c = lane; c < D; c += 32) sh.sieved[slot][c] = (kNoKey << 20) | (kNoKey << 10) | kNoKey;
+        __syncwarp();
+      }
+      if (pass == kMaxima) {  // nothing to multiply: the scores are only read
         for (int j = 0; j < nb; ++j, ++jg) {
           if (!(ok = wait_bar(sh.p_full[jg & 1][0], (jg >> 1) & 1) && wait_bar(sh.p_full[jg & 1][1], (jg >> 1) & 1)))
             break;
@@ -887,6 +899,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                          "r"(0)
                          : "memory");
           }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+        if (j >= j_sieve) {
+          sieve_block<D>(sbase + L::kV + sv * L::kTileBytes, (j - j_sieve) * kBlk, sh.sieved[slot]);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
@@ -925,6 +942,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++jg;
       }
       ++outputs;
+      if (pass == kAgain) publish_seq(&sh.sieved_seq, k + 1);
     }
     if (!ok && lane == 0) set_abort(sh, p.err);
   } else if (warp >= kOutputWarp) {
@@ -959,14 +977,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         odd = l != l;
       }
       __syncwarp();
-      // (a unit that was run again may have rows to be computed once more)
+      // (what was sieved from a unit that was run again is still to be read)
       if (lane == 0 && pass != kAgain) mbar_arrive(bar(sh.meta_empty[slot]));
       if (pass == kMaxima) continue;
       if (!(ok = wait_bar(sh.o_full, outputs & 1))) break;
       ++outputs;
       tc_fence_after();
       float2 finite = make_float2(0.f, 0.f);  // NaN once an infinity or NaN is added
-      bool wild = false;                      // an output that is not finite
       // 64 columns at a time, through shared memory, so that a store instruction
       // writes whole 128-byte lines of four rows instead of a sector of 32; O is
       // read ahead of the stores, as the next unit's P V waits for that
@@ -1004,7 +1021,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (half == D / 64 - 1) {
           // O has been looked at: the scheduler may go on, or end, beside the stores
-          wild = valid && !(finite.x == 0.f && finite.y == 0.f);
+          const bool wild = valid && !(finite.x == 0.f && finite.y == 0.f);  // an output that is not finite
           const bool redo = __any_sync(0xffffffffu, pass == kFirst && (odd || wild));
           if (lane == 0) {
             // (released only where there is something to release: it waits for the stores)
@@ -1047,15 +1064,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       if (pass != kAgain) continue;
-      // rows from which the tile's other rows' keys have to be kept out
-      const int lim = min(max(M.lim0 + rt, M.full), M.L), k0 = M.blk_lo * kBlk;
-      const bool mend = wild && !odd && lim < M.pages * kPage && lim < M.L;
-      for (unsigned rows = __ballot_sync(0xffffffffu, mend); rows; rows &= rows - 1) {
-        const int src = __ffs(rows) - 1;
-        const int at = __shfl_sync(0xffffffffu, pair, src), end = __shfl_sync(0xffffffffu, lim, src);
-        one_row<D>(p, M.seq, at / p.H_q, at % p.H_q, k0, min(end, k0 + M.n_blocks * kBlk),
-                   part ? p.o_part + (part_row - lane + src) * D : nullptr, p.out + static_cast<size_t>(at) * D);
-      }
+      // values that are not finite in the blocks that some rows see part of
+      if (!(ok = __all_sync(0xffffffffu, await_seq(&sh.sieved_seq, k + 1, sh)))) break;
+      const int lim = min(max(M.lim0 + rt, M.full), M.L);
+      const int sieve0 = max(max(min(max(M.lim0, M.full), M.L), 0) / kBlk, M.blk_lo) * kBlk;
+      __syncwarp();  // (rows of out were stored by other lanes)
+      if (valid && inv > 0.f)
+        add_sieved<D>(sh.sieved[slot], lim - sieve0, part, p.out + static_cast<size_t>(pair) * D);
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
     }

@@ -5,11 +5,14 @@ import contextlib
 import os
 import re
 
+import numpy as np
 import pytest
 
+import test_chunk_ops as K
 from paper_2607_18839_gb300 import build as B
 from paper_2607_18839_gb300 import hpd as H
 
+gpu = pytest.mark.gpu
 PAGE = 16
 
 
@@ -119,3 +122,108 @@ def test_no_loads_past_the_coherent_cache():
         with open(path) as f:
             text = f.read()
         assert not re.search(r"__ldg\b|ld\.global\.(\w+\.)*nc\b", text), path
+
+
+def _mark(c, s, j, head, col, value):
+    c["vc"][int(c["table"][s, j // PAGE]), j % PAGE, head, col] = value
+
+
+def _check_not_finite(torch, c, marks, op=None):
+    """A call with values that are not finite: sequence, key, KV head, column and
+    value of each.  A sum with a NaN or with infinities of both signs in it is NaN,
+    with those of one sign that infinity, whatever the (positive) weights."""
+    for m in marks:
+        _mark(c, *m)
+    hq, hkv = c["q"].shape[1], c["kc"].shape[2]
+    op = op or H.ChunkAttn(hq, c["kc"], c["vc"], c["table"], max_tokens=c["q"].shape[0])
+    full = None if c["full"] is None else c["full"]
+    out, lse = op(c["q"], c["cu"], c["total"], full)
+    torch.cuda.synchronize()
+    assert op.errors() == 0
+    out, lse = K._np(out), lse.cpu().numpy()
+    cu, total = c["cu"].cpu().numpy(), c["total"].cpu().numpy()
+    want = np.zeros(out.shape)
+    for s, j, g, col, value in marks:
+        n = cu[s + 1] - cu[s]
+        lim = total[s] - n + np.arange(n) + 1
+        if full is not None:
+            lim = np.minimum(np.maximum(lim, int(full[s])), total[s])
+        rows = cu[s] + np.flatnonzero(lim > j)
+        G = hq // hkv
+        with np.errstate(invalid="ignore"):
+            want[rows, g * G: (g + 1) * G, col] += value
+    off = ~np.isfinite(want)
+    assert np.array_equal(~np.isfinite(out), off) and np.isfinite(lse).all()
+    assert np.array_equal(out[off], want[off], equal_nan=True)
+    K._near_oracle(c, ~off.any(-1), out, lse)
+    return off
+
+
+INF, NAN = float("inf"), float("nan")
+
+
+@gpu
+@pytest.mark.parametrize("new,total,full,hq,hkv,D", [
+    ([100, 3], [300, 90], None, 16, 2, 128), ([100, 3], [300, 90], None, 16, 2, 64), ([128], [150], None, 1, 1, 128),
+    ([128, 5], [250, 5], None, 4, 4, 64), ([60], [3000], None, 40, 8, 128), ([90, 1], [200, 77], [150, 0], 10, 2, 128),
+    ([300], [300], [290], 8, 8, 64), ([33], [161], None, 6, 2, 128)])
+def test_gpu_attn_several_values_not_finite(torch, new, total, full, hq, hkv, D):
+    # among a tile's own keys, NaN and both infinities in one column at several
+    # keys; one before them that all see; the last key of all
+    c = K._attn_case(torch, new, total, hq, hkv, D, seed=30, full=full)
+    L, n = total[0], new[0]
+    at = lambda f: L - n + int(f * (n - 1))  # noqa: E731
+    g = hkv - 1
+    marks = [(0, at(.2), g, 5, INF), (0, at(.5), g, 5, INF), (0, at(.7), g, 5, -INF), (0, at(.4), g, 6, -INF),
+             (0, at(.3), g, 63, INF), (0, at(.6), g, 63, NAN), (0, 0, g, 9, INF), (0, at(.8), g, 9, -INF),
+             (0, L - 1, 0, 0, NAN), (0, at(.1), 0, D - 1, INF)]
+    off = _check_not_finite(torch, c, marks)
+    assert off.any() and (full or not off.all(-1).any())
+    # whole rows of values, keys whose scores they leave alone
+    for j in (at(.25), at(.55)):
+        c["vc"][int(c["table"][0, j // PAGE]), j % PAGE] = NAN
+    out, lse = H.ChunkAttn(hq, c["kc"], c["vc"], c["table"], max_tokens=sum(new))(c["q"], c["cu"], c["total"], c["full"])
+    torch.cuda.synchronize()
+    lim = L - n + np.arange(n) + 1
+    if full:
+        lim = np.minimum(np.maximum(lim, full[0]), L)
+    assert np.array_equal(np.isnan(K._np(out)[:n]).all((1, 2)), lim > at(.25)) and bool(torch.isfinite(lse).all())
+
+
+@gpu
+def test_gpu_attn_values_not_finite_behind_a_long_context(torch):
+    # more sequences than are split, so that one CTA has all of the long one, and
+    # units of others behind it: no wait runs out, every row is written
+    S, L, n = 700, 200_000, 40
+    new, total = [n] + [1] * (S - 1), [L] + [1 + i % 40 for i in range(S - 1)]
+    c = K._attn_case(torch, new, total, 4, 1, 64, seed=31)
+    op = H.ChunkAttn(4, c["kc"], c["vc"], c["table"], max_tokens=sum(new), max_seq_len=L)
+    op.out.fill_(7.0)
+    _check_not_finite(torch, c, [(0, L - 25, 0, 5, INF), (0, L - 9, 0, 5, NAN), (0, L - 12, 0, 40, -INF)], op)
+
+
+@gpu
+def test_gpu_attn_values_not_finite_cost_passes_and_no_more(torch):
+    # a unit with such values is run again, its maxima first: three times its blocks.
+    # Far from that lies what depends on one row at a time (hundreds of times).
+    S, L, n = 300, 8192, 40
+    new, total = [n] + [0] * (S - 1), [L] + [0] * (S - 1)
+    c = K._attn_case(torch, new, total, 4, 1, 128, seed=32)
+    op = H.ChunkAttn(4, c["kc"], c["vc"], c["table"], max_tokens=n, max_seq_len=L)
+
+    def us():
+        ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        best = 1e9
+        for _ in range(5):
+            ev[0].record()
+            op(c["q"], c["cu"], c["total"])
+            ev[1].record()
+            torch.cuda.synchronize()
+            best = min(best, 1e3 * ev[0].elapsed_time(ev[1]))
+        return best
+
+    plain = us()
+    _mark(c, 0, L - 3, 0, 7, INF)
+    again = us()
+    print(f"{plain:.0f} us, with an infinity among the last keys {again:.0f}")
+    assert op.errors() == 0 and again <= 10 * plain
