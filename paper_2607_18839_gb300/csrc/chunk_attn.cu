@@ -1239,6 +1239,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) chunk_merge_kernel(const Chu
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float w_or = l == NEG_INF ? -1.f : w;  // (an empty partial is not written; another's weight may be 0)
     float acc[kV];
 #pragma unroll
     for (int c = 0; c < kV; ++c) acc[c] = 0.f;
@@ -1247,9 +1248,9 @@ __global__ void __launch_bounds__(32 * kMergeWarps) chunk_merge_kernel(const Chu
       if (s0 > 0) load(s0);
 #pragma unroll
       for (int i = 0; i < kMergeAhead; ++i) {
-        const float ws = __shfl_sync(0xffffffffu, w, s0 + i);
+        const float ws = __shfl_sync(0xffffffffu, w_or, s0 + i);
 #pragma unroll
-        for (int c = 0; c < kV; ++c) acc[c] = ws == 0.f ? acc[c] : fmaf(ws, v[i][c], acc[c]);  // (an empty partial is not written)
+        for (int c = 0; c < kV; ++c) acc[c] = ws < 0.f ? acc[c] : fmaf(ws, v[i][c], acc[c]);
       }
     }
     const int rt = p.div_G(r);

@@ -227,3 +227,25 @@ def test_gpu_attn_values_not_finite_cost_passes_and_no_more(torch):
     again = us()
     print(f"{plain:.0f} us, with an infinity among the last keys {again:.0f}")
     assert op.errors() == 0 and again <= 10 * plain
+
+
+@gpu
+@pytest.mark.parametrize("value", [NAN, INF])
+def test_gpu_attn_values_not_finite_in_a_split_of_no_weight(torch, value):
+    # the keys of the first splits weigh e^-424 of the others: no weight in 32 bits, but
+    # a value among them that is not finite is in every row's sum
+    c = K._attn_case(torch, [1], [3000], 16, 8, 128, seed=33)
+    c["q"][..., 0] = 16.0
+    slot = torch.arange(3000, device="cuda")
+    at = c["table"][0][slot // PAGE].long() * PAGE + slot % PAGE
+    c["kc"].view(-1, 8, 128)[at[:1500], :, 0] = -300.0
+    c["kc"].view(-1, 8, 128)[at[1500:], :, 0] = 0.0
+    _mark(c, 0, 5, 1, 3, value)
+    op = H.ChunkAttn(16, c["kc"], c["vc"], c["table"], max_tokens=1)
+    out, lse = op(c["q"], c["cu"], c["total"])
+    torch.cuda.synchronize()
+    assert op.errors() == 0 and bool(torch.isfinite(lse).all())
+    off = ~np.isfinite(K._np(out)[0])
+    want = np.zeros((16, 128), bool)
+    want[2:4, 3] = True
+    assert np.array_equal(off, want)
