@@ -196,7 +196,7 @@ extern "C" hpd_status hpd_chunk_slots(const hpd_chunk_slots_args *a, hpd_stream_
                         static_cast<const void *>(a->slot), static_cast<const void *>(a->pos)})
     if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return HPD_ERR_INVALID_ARG;
   const size_t smem = (3 * static_cast<size_t>(a->S) + 2) * sizeof(int);
-  if (smem > 48 * 1024) {
+  if (smem > 47 * 1024) {  // (the default of 48 KB holds the kernel's own 144 bytes too)
     const cudaError_t e = cudaFuncSetAttribute(chunk_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                (3 * kMaxSeqs + 2) * static_cast<int>(sizeof(int)));
     if (e != cudaSuccess) return record_cuda_error(e);

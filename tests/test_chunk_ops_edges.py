@@ -4,6 +4,9 @@ that are not finite among long contexts."""
 import contextlib
 import os
 import re
+import subprocess
+import sys
+import textwrap
 
 import numpy as np
 import pytest
@@ -13,6 +16,7 @@ from paper_2607_18839_gb300 import build as B
 from paper_2607_18839_gb300 import hpd as H
 
 gpu = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PAGE = 16
 
 
@@ -63,6 +67,25 @@ class Host:
 @pytest.fixture
 def host(lib, monkeypatch):
     return Host(pytest.importorskip("torch"), monkeypatch)
+
+
+# ------------------------------------------------------------ pages and slots --
+
+@gpu
+def test_gpu_slots_sizes_where_shared_memory_passes_its_default(torch):
+    # the lengths of some 4,090 sequences fill the default size; each in a process of
+    # its own, as a larger call before lets a smaller one through
+    body = """
+        import sys, torch
+        sys.path[:0] = [%r, %r]
+        import test_chunk_ops as K
+        S = int(sys.argv[1])
+        new, ctx = K._random_lengths(S, 3, 20, seed=S)
+        K._check_slots(torch, K._slot_case(new, ctx, 3, extra=4, seed=1), int(new.sum()) + 1)
+    """ % (ROOT, os.path.join(ROOT, "tests"))
+    for S in (4083, 4084, 4095, 4096):
+        r = subprocess.run([sys.executable, "-c", textwrap.dedent(body), str(S)], capture_output=True, text=True)
+        assert r.returncode == 0, (S, r.stderr[-400:])
 
 
 # --------------------------------------------------- norms, rotation, write --
