@@ -418,7 +418,8 @@ typedef struct {
                                the error word                                      */
   int64_t num_slots;        /* >= 1 cache rows: 16 * num_pages                     */
   float eps;                /* >= 0                                                */
-  int T;                    /* >= 0 rows                                           */
+  int T;                    /* >= 0 rows; with none q, k, v, pos, slot and q_out
+                               may be NULL                                         */
   int H_q, H_kv, D;         /* D in {64, 128}; H_q, H_kv >= 1                      */
   int n_axes;               /* 1 .. 4                                              */
   int max_pos;              /* >= 1 rows of rope                                   */

@@ -220,8 +220,8 @@ extern "C" hpd_status hpd_qk_norm_rope(const hpd_qk_norm_rope_args *a, hpd_strea
     return HPD_ERR_INVALID_ARG;
   if (a->D != 64 && a->D != 128) return HPD_ERR_UNSUPPORTED;
   if (static_cast<long long>(a->H_q) + 2LL * a->H_kv > (1 << 20)) return HPD_ERR_UNSUPPORTED;
-  if (!a->q || !a->k || !a->v || !a->rope || !a->pos || !a->slot || !a->q_out || !a->k_cache || !a->v_cache)
-    return HPD_ERR_INVALID_ARG;
+  if (!a->rope || !a->k_cache || !a->v_cache) return HPD_ERR_INVALID_ARG;
+  if (a->T > 0 && (!a->q || !a->k || !a->v || !a->pos || !a->slot || !a->q_out)) return HPD_ERR_INVALID_ARG;
   if (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 255u) != 0) return HPD_ERR_WORKSPACE;
   for (const void *p : {a->q, a->k, a->v, a->q_weight, a->k_weight, static_cast<const void *>(a->rope),
                         static_cast<const void *>(a->q_out), static_cast<const void *>(a->k_cache),

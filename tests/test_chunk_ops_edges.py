@@ -90,6 +90,22 @@ def test_gpu_slots_sizes_where_shared_memory_passes_its_default(torch):
 
 # --------------------------------------------------- norms, rotation, write --
 
+def test_norm_rope_of_no_rows(lib, host, monkeypatch):
+    # nothing to do, and tensors of no rows have no address
+    rows = dict.fromkeys(("q", "k", "v", "pos", "slot", "q_out"))
+    assert lib.hpd_qk_norm_rope(K.rope_args(T=0, **rows), None) == 0
+    assert lib.hpd_qk_norm_rope(K.rope_args(T=1, **rows), None) == 1
+    monkeypatch.setattr(H, "hpd_qk_norm_rope",
+                        lambda a, s: H._check("hpd_qk_norm_rope", lib.hpd_qk_norm_rope(a, None)))
+    cache = host.bf(2, PAGE, 2, 64)
+    op = host.rope()
+    op.args.workspace = op.args.rope = 4096
+    empty = host.bf(0, 8 * 64)
+    assert empty.data_ptr() == 0
+    for _ in range(2):
+        assert op(empty, host.i32(0), host.i32(0), cache, cache).shape == (0, 4, 64)
+
+
 def test_norm_rope_output_grows_on_the_stream_of_the_call(host, monkeypatch):
     # memory of the current stream may still be written there by what was enqueued
     # before; the call's kernel does not wait for that
