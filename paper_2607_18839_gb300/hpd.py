@@ -662,7 +662,7 @@ class QkNormRope:
             _need("QkNormRope", q_out, bf, (T, H_q, D))
         at = qkv.data_ptr()
         a.q, a.k, a.v = at, at + 2 * H_q * D, at + 2 * (H_q + H_kv) * D
-        a.q_stride = a.k_stride = a.v_stride = row
+        a.q_stride = a.k_stride = a.v_stride = row if T > 1 else 0  # (one row has none)
         a.pos, a.slot, a.q_out = pos.data_ptr(), slot.data_ptr(), q_out.data_ptr()
         a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
         a.num_slots, a.T = pages * 16, T

@@ -106,6 +106,16 @@ def test_norm_rope_of_no_rows(lib, host, monkeypatch):
         assert op(empty, host.i32(0), host.i32(0), cache, cache).shape == (0, 4, 64)
 
 
+def test_norm_rope_of_one_row_has_no_stride(host):
+    # (a stride between rows that are not there need not be a multiple of 8)
+    op, cache = host.rope(), host.bf(2, PAGE, 2, 64)
+    op(host.bf(5, 8 * 64 + 3)[:1], host.i32(1), host.i32(1), cache, cache)
+    a = host.calls[-1][1]
+    assert a.T == 1 and a.q_stride % 8 == a.k_stride % 8 == a.v_stride % 8 == 0
+    op(host.bf(5, 8 * 64 + 16)[:2], host.i32(2), host.i32(2), cache, cache)
+    assert a.T == 2 and a.q_stride == a.k_stride == a.v_stride == 8 * 64 + 16
+
+
 def test_norm_rope_output_grows_on_the_stream_of_the_call(host, monkeypatch):
     # memory of the current stream may still be written there by what was enqueued
     # before; the call's kernel does not wait for that
