@@ -599,6 +599,8 @@ class QkNormRope:
 
     def __init__(self, H_q, H_kv, D, q_weight, k_weight, rope, sections=None, axis=None, eps=1e-6):
         import torch
+        if D not in (64, 128):
+            raise HpdError("QkNormRope", 2, "heads of 64 or 128 values")
         if axis is None:
             axis = [a for a, n in enumerate(sections or (D // 2,)) for _ in range(n)]
         if len(axis) != D // 2 or not all(0 <= a < 4 for a in axis):

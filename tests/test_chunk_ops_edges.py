@@ -116,6 +116,13 @@ def test_norm_rope_of_one_row_has_no_stride(host):
     assert a.T == 2 and a.q_stride == a.k_stride == a.v_stride == 8 * 64 + 16
 
 
+@pytest.mark.parametrize("D", [0, 32, 96, 256, 512])
+def test_norm_rope_refuses_other_head_sizes(host, D):
+    with pytest.raises(H.HpdError) as e:
+        host.rope(D=D)
+    assert e.value.status == 2
+
+
 def test_norm_rope_output_grows_on_the_stream_of_the_call(host, monkeypatch):
     # memory of the current stream may still be written there by what was enqueued
     # before; the call's kernel does not wait for that
