@@ -94,15 +94,16 @@ class Pages:
         return x
 
     def prefill(self, per_step):
-        """Everything, per_step tokens of each document a step; a document's
-        vision tokens, which see one another, come in one piece.  Returns the
-        last hidden states of each document's tokens."""
+        """Everything, up to per_step tokens of each document a step, and no more
+        than a step has room for; a document's vision tokens, which see one
+        another, come in one piece.  Returns the last hidden states of each
+        document's tokens."""
         import torch
         got, done = [[] for _ in self.total], [0] * len(self.total)
         while done != self.total:
             chunk, left = [], self.room
             for d, n in enumerate(self.total):
-                want = max(min(per_step, n - done[d]), self.vision[d] - done[d])
+                want = max(min(per_step, n - done[d], left), self.vision[d] - done[d])
                 chunk.append(want if want <= left else 0)
                 left -= chunk[-1]
             if not any(chunk):

@@ -2,6 +2,7 @@
 calls of no rows and of one, tensors that share their storage, streams, values
 that are not finite among long contexts."""
 import contextlib
+import importlib.util
 import os
 import re
 import subprocess
@@ -305,3 +306,28 @@ def test_gpu_attn_values_not_finite_in_a_split_of_no_weight(torch, value):
     want = np.zeros((16, 128), bool)
     want[2:4, 3] = True
     assert np.array_equal(off, want)
+
+
+# -------------------------------------------------------- prefill in chunks --
+
+def test_prefill_takes_text_in_pieces_that_fit(host):
+    # text behind the vision tokens goes in whatever pieces a step has room for;
+    # vision tokens in one piece
+    path = os.path.join(ROOT, "examples", "prefill_then_decode.py")
+    spec = importlib.util.spec_from_file_location("prefill_example", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    pages, steps = object.__new__(mod.Pages), []
+    pages.vision, pages.total, pages.room = [30, 0, 12], [230, 300, 13], 100
+    pages.check = lambda: None
+
+    def step(chunk):
+        assert 0 < sum(chunk) <= pages.room and min(chunk) >= 0
+        steps.append(chunk)
+        return host.torch.zeros(sum(chunk), 1)
+
+    pages.step = step
+    got = pages.prefill(per_step=256)
+    assert [len(x) for x in got] == pages.total
+    first = [next(s[d] for s in steps if s[d]) for d in range(3)]
+    assert first[0] >= 30 and first[2] >= 12
