@@ -154,10 +154,8 @@ __device__ __forceinline__ void cluster_wait() {
 
 // grid (cluster size * B), cluster (cluster size, 1, 1): cluster = branch.
 __global__ void __launch_bounds__(kAcceptThreads)
-    accept_cluster_kernel(const __nv_bfloat16 *__restrict__ logits,
-                          const int32_t *__restrict__ drafts, int m, int V,
-                          int32_t *__restrict__ out_tokens, int32_t *__restrict__ accepted_len,
-                          bool beside) {
+    accept_cluster_kernel(const __nv_bfloat16 *logits, const int32_t *drafts, int m, int V,
+                          int32_t *out_tokens, int32_t *accepted_len, bool beside) {
   __shared__ float s_v[kAcceptThreads / 32];
   __shared__ int s_i[kAcceptThreads / 32];
   __shared__ int s_tok[kMaxRows];  // used in the leader CTA

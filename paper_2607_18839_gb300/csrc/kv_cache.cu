@@ -212,7 +212,7 @@ __global__ void kv_append_copy_kernel(KvArgs a, int rows_total) {
 // Rollback (one CTA): keep the first keep_b of the step's m rows, free the
 // logical pages past the new length, push their ids in branch order.
 __global__ void __launch_bounds__(kScanThreads)
-    kv_rollback_kernel(KvArgs a, const int32_t *__restrict__ accepted_len) {
+    kv_rollback_kernel(KvArgs a, const int32_t *accepted_len) {
   __shared__ int warp_sums[33];
   __shared__ int s_bad, s_free;
   const int tid = threadIdx.x;

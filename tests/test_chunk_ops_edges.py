@@ -181,6 +181,13 @@ def test_no_loads_past_the_coherent_cache():
         assert not re.search(r"__ldg\b|ld\.global\.(\w+\.)*nc\b", text), path
 
 
+def test_no_promise_that_inputs_are_not_written():
+    # const and __restrict__ together let the compiler choose such loads by itself
+    for path in B.sources():
+        with open(path) as f:
+            assert not re.search(r"\bconst\s+\w+\s*\*\s*__restrict__", f.read()), path
+
+
 def _mark(c, s, j, head, col, value):
     c["vc"][int(c["table"][s, j // PAGE]), j % PAGE, head, col] = value
 
