@@ -315,6 +315,45 @@ def test_gpu_attn_values_not_finite_in_a_split_of_no_weight(torch, value):
     assert np.array_equal(off, want)
 
 
+# --------------------------------------------------------------- branch step --
+
+@gpu
+def test_gpu_branch_units_ordered_where_shared_memory_passes_its_default(torch):
+    # 4,096 buckets, 240 pages and 3,470 branches of one row: what the ordering holds
+    # ends within 144 bytes of the default size
+    n_docs, B, hkv, D = 240, 3470, 64, 64
+    words = 4096 + 4 * n_docs + 1 + 2 * B + -(-B // 128) + n_docs
+    assert 48 * 1024 - 144 < 4 * words <= 48 * 1024
+    rng = np.random.default_rng(40)
+    t = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()  # noqa: E731
+    kc, vc = K._bf(torch, rng, 8, PAGE, hkv, D), K._bf(torch, rng, 8, PAGE, hkv, D)
+    pk, pv = K._bf(torch, rng, n_docs, hkv, D), K._bf(torch, rng, n_docs, hkv, D)
+    q = torch.randn(B, hkv, D, device="cuda", dtype=torch.bfloat16)
+    cu = np.minimum(np.arange(n_docs + 1) * 15, B)
+    cu[-1] = B
+    length, table = rng.integers(1, 129, B), rng.integers(0, 8, (B, 8))
+    d = H.DeviceInputs(q=q, prefix_k=pk, prefix_v=pv, prefix_cu=t(np.arange(n_docs + 1)), branch_cu=t(cu),
+                       branch_prefix_len=t(np.ones(B)), k_cache=kc, v_cache=vc, page_table=t(table), branch_len=t(length),
+                       n_docs=n_docs, B=B, m=1, H_q=hkv, H_kv=hkv, D=D, num_pages=8, max_pages=8, prefix_tokens=n_docs,
+                       max_prefix_len=1, scale=0.0)
+    op = H.BranchAttn(d)
+    assert H.hpd_branch_attn_kernel_name(op.args, 0) == "unit_order"
+    out, lse = op()
+    torch.cuda.synchronize()
+    assert op.errors() == 0
+    for b in rng.integers(0, B, 40):
+        page = int(np.searchsorted(cu, b, side="right")) - 1
+        n = int(length[b])
+        at = t(table[b]).long()
+        k = torch.cat((pk[page: page + 1], kc[at].flatten(0, 1)[:n])).double()
+        v = torch.cat((pv[page: page + 1], vc[at].flatten(0, 1)[:n])).double()
+        x = torch.einsum("hd,lhd->hl", q[b].double(), k) / 8.0
+        assert float((lse[b] - x.logsumexp(-1)).abs().max()) <= 1e-4
+        ref = torch.einsum("hl,lhd->hd", x.softmax(-1), v)
+        # one rounding to bf16 of each weight and of the result
+        assert float((out[b] - ref).abs().max()) <= 2.0 ** -7 * float(v.abs().max())
+
+
 # -------------------------------------------------------- prefill in chunks --
 
 def test_prefill_takes_text_in_pieces_that_fit(host):
