@@ -394,7 +394,8 @@ hpd_status hpd_chunk_slots(const hpd_chunk_slots_args *args, hpd_stream_t stream
  *   x' = x * rsqrt(mean(x^2) + eps) * weight        over the D values of a head
  *   (x'_i, x'_{i + D/2}) rotated by the angle of table row pos[axis[i]][t]:
  *   y_i = x'_i cos - x'_{i+D/2} sin,  y_{i+D/2} = x'_{i+D/2} cos + x'_i sin
- * in 32 bits, rounded once.  q_out[t] takes the queries; cache row slot[t] the
+ * in 32 bits, rounded once (a head's squares have to sum to less than 3.4e38).
+ * q_out[t] takes the queries; cache row slot[t] the
  * keys, and the values as they are.  A negative slot's keys and values are not
  * written.  With several axes (time, height and width of an image's tokens)
  * frequency i turns by the position on axis[i]; text has one axis.
@@ -437,7 +438,10 @@ hpd_status hpd_qk_norm_rope(const hpd_qk_norm_rope_args *args, hpd_stream_t stre
  * of page page_table[s][j / 16].  Scores, softmax, lse and heads as in
  * hpd_branch_attn; a row that sees no key (more new tokens than seq_len) gets
  * out 0 and lse -inf.  Cache rows at or past seq_len[s] may hold anything, NaN
- * too.  Rows at or past chunk_cu[S] are not written.
+ * too.  A value that is not finite reaches the rows that see its key and no
+ * others.  Rows at or past chunk_cu[S] are not written.
+ * Long contexts of few rows are shared out over the GPU (a second launch joins
+ * the parts) where S <= 256; beyond, a tile of rows is one CTA's.
  * Lengths out of range are clamped and flagged HPD_DEVERR_BRANCH_LEN, offsets
  * HPD_DEVERR_BRANCH_CU, page ids HPD_DEVERR_PAGE_ID (and read as page 0). */
 typedef struct {
@@ -449,11 +453,12 @@ typedef struct {
   const void *k_cache, *v_cache; /* bf16 [num_pages][16][H_kv][D]                  */
   const int32_t *page_table;  /* [S][max_pages]                                    */
   int S;                      /* >= 1 sequences                                    */
-  int T;                      /* >= 1 rows of q, out and lse                       */
+  int T;                      /* >= 1 rows of q, out and lse; T * H_q < 2^25       */
   int H_q, H_kv, D;           /* H_q % H_kv == 0, H_q / H_kv <= 16; D in {64, 128} */
-  int num_pages, max_pages;   /* >= 1                                              */
-  int max_seq_len;            /* host upper bound on seq_len, for planning only;
-                                 0 = 16 * max_pages                                */
+  int num_pages, max_pages;   /* >= 1; 16 * num_pages < 2^31, 16 * max_pages < 2^30 */
+  int max_seq_len;            /* host upper bound on seq_len, for planning only:
+                                 far above the lengths it costs short calls 2 to
+                                 7 us; 0 = 16 * max_pages                          */
   float scale;                /* softmax scale; 0 = 1/sqrt(D)                      */
   void *out;                  /* bf16 [T][H_q][D]                                  */
   float *lse;                 /* fp32 [T][H_q], natural log; may be NULL           */

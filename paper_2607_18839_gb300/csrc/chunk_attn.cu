@@ -36,8 +36,12 @@
 // run again with its rows' true maxima, which a pass over S alone finds first.
 // Which units are is a matter of their own scores and values alone, so that a
 // call's bits do not depend on which CTA took which unit.  O is never rescaled.
-// P is rounded to bf16, as the tensor cores take it (2^-9 of each weight, in either
-// direction); its sum is of the values before, in 32 bits, like scores and O.  P goes to
+// P is rounded to bf16, as the tensor cores take it (2^-8 of each weight at most, in
+// either direction: the output is off by 0.0023 of its size, where weights of 32 bits
+// leave 0.0017, the rounding of the output); its sum is of the values before, in 32
+// bits, like scores and O.  A second bf16 part of P, as the branch attention has for
+// head ratios that do not divide 128 (whose calls had one before), would take P V
+// twice: half as much again of the MMAs that bound long chunks.  P goes to
 // the tensor cores in two parts: while the exponentials of the second 32 keys of a
 // half are taken, P V of the first 32 runs.
 //
@@ -53,12 +57,12 @@
 // All waits are bounded, as in the branch attention kernel.
 //
 // What bounds it, and what it measured on a GB300 (calls one after another):
-//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 340-350 us, 1.47-1.51 PFLOP/s;
-//     the power limit.  At the full clock 289 us, 1.78 PFLOP/s, with the tensor pipe
+//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 337-349 us, 1.48-1.53 PFLOP/s;
+//     the power limit.  At the full clock 286 us, 1.80 PFLOP/s, with the tensor pipe
 //     at work 87 % of the time.
-//   64 sequences that bring a token, contexts to 8,191, 32 / 8 heads of 128: 207 us,
-//     6.1 TB/s of 6.8: HBM.
-//   1,152 tokens of one page, 16 / 2 heads of 128: 15.5 us, of which the blocks have
+//   64 sequences that bring a token, contexts to 8,191, 32 / 8 heads of 128: 203-207
+//     us, 6.1 TB/s of 6.8: HBM.
+//   1,152 tokens of one page, 16 / 2 heads of 128: 15.3 us, of which the blocks have
 //     6: 3.4 us pass until the first scores (lengths, page ids, Q and K one after the
 //     other, through code that runs for the first time), 3.5 from the last P V to
 //     the end (O, its stores, the exit).
@@ -66,6 +70,9 @@
 //     0.7 and 0.54 with heads of 64, where no pipe is full: a look at a barrier
 //     takes a warp 150 to 200 cycles while the others work, and each role makes
 //     two or three a block.
+// 640 threads leave 96 registers each.  What does not fit (32 bytes of spill stores, 60
+// of loads with heads of 128; 24 and 44 with 64) is not in the blocks' loops: 246 local
+// loads an SM in a call of some 400 blocks an SM.
 // Halves of a block for the two softmax warpgroups, and not alternate blocks: those
 // took 0.67 us a block with heads of 128 and 0.52 with heads of 64 (three buffers of
 // scores, five stages).
@@ -1194,8 +1201,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 //   lse = log sum_s exp(lse_s),  out = sum_s exp(lse_s - lse) out_s
 // What bounds it: the launch and three loads one after the other (the tile, then its
 // sums and results together) where rows are few; else reading the results from L2.
-// Without it, one token behind 3,999 takes 12.2 us, with it 13.2 (17.2 with 8 warps and a
-// split's result loaded behind its sums); 700 behind 2,300 with 40 heads 34, 40 (50).
+// With it, one token behind 3,999 (16 / 2 heads of 128) takes 12.6 us, some 1 us more than
+// without; 700 behind 2,300 with 40 / 8 heads 38.6, without 32.2.
 constexpr int kMergeWarps = 16;
 constexpr int kMergeAhead = 8;  // splits whose results are on their way at once
 template <int D>
@@ -1292,11 +1299,16 @@ struct ChunkPlan {
 // Tiles may be split where the call's units leave SMs idle in their last (or only)
 // wave.  Only host scalars enter (the kernel then splits by the true lengths): the
 // time of units of the longest sequences, in blocks, whole against split after the
-// full waves, a unit's start and end counted as 3.5 blocks, the merge as 10.  (16 / 4
-// heads of 64, 500 tokens behind 2,000: 18.8 us whole; with 8, and so split, 21.7.  16 / 2
-// heads of 128, one token behind 1,799: 13.1 us split; with 13, and so whole, 16.7.
-// Split against whole: one token behind 2,499 13.1 and 19.2, 16 behind 8,984 16.8 and
-// 47.9, 2,048 behind 14,336 with 32 / 8 heads 341 and 346.)
+// full waves, a unit's start and end counted as 3.5 blocks, the merge as 10.  (us,
+// split and whole, 16 / 2 heads of 128: one token behind 1,799 12.0 and 16.2, behind 2,499
+// 12.5 and 18.9, 16 behind 8,984 16.1 and 47.7; 2,048 behind 14,336 with 32 / 8 heads 295
+// and 310, in bursts of 40 calls; 500 behind 2,000 with 16 / 4 heads of 64 21.6 and 19.0,
+// which stays whole.  The other way: 700 behind 2,300 with 40 / 8 heads is split, and
+// 38.6 and 36.1.)
+// A bound far above the lengths costs short calls time: they are split, or have a merge
+// launched that finds nothing.  With a bound of 8,192 and with the exact one: one token
+// behind 255 11.2 and 9.5, 640 of one page 15.4 and 12.0, 1,300 23.6 and 18.7, 300 behind
+// 1,200 17.8 and 15.7, 500 alone with 16 / 4 heads of 64 17.0 and 9.7.
 ChunkPlan make_plan(const hpd_chunk_attn_args *a) {
   ChunkPlan pl{};
   const int G = a->H_q / a->H_kv, TT = kRows / G;

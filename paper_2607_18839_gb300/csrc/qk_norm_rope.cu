@@ -15,7 +15,8 @@
 // meanwhile.
 // What bounds it: HBM, reading and writing T (H_q + 2 H_kv) D values.  32,749 rows
 // of 16 + 2 + 2 heads of 128 take 60.6 us, 5.8 TB/s and 86% of a copy's rate; 3,201 of
-// 32 + 8 + 8 heads take 17.1 (11.9 at that rate, and a launch).  In us, those two: a
+// 32 + 8 + 8 heads take 17.2 (11.9 at that rate, and a launch; 13.4 where call after call
+// has the same rows, which L2 then holds).  In us, those two (17.1 that day): a
 // CTA for every four items instead of CTAs that stay 75.0, 17.9; kUnroll 3 67.9,
 // 18.4; 4 68.8, 16.7; 6 61.9, 18.1; five CTAs an SM (96 registers) 64.9, 18.6.  One
 // value an instruction, whole rows loaded four rounds ahead: 82.3, 25.6 (288

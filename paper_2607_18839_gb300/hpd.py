@@ -550,8 +550,10 @@ def _ready_workspace(nbytes: int, device):
 
 class ChunkSlots:
     """Pages and slots of each step's new tokens (hpd_chunk_slots) for the
-    sequences of one page table.  Owns the outputs: chunk_cu [S + 1], slot and
-    pos [max_tokens], and the error word's workspace.  in_place: lengths and
+    sequences of one page table.  free_pages has an entry for every page of the
+    pool: page ids from its length up are out of range.  Owns the outputs:
+    chunk_cu [S + 1], slot and pos [max_tokens], and the error word's workspace.
+    in_place: lengths and
     the stack's top are updated where they are; otherwise the new ones go to
     ``seq_len`` and ``free_top`` of this object and the given ones stay."""
 
@@ -679,7 +681,9 @@ class ChunkAttn:
     """Attention of up to max_tokens new tokens over the paged cache
     (hpd_chunk_attn).  Owns out [max_tokens, H_q, D], lse [max_tokens, H_q]
     and the workspace, which is ready for calls on any stream once this is made
-    (on the current one, whatever ``stream``)."""
+    (on the current one, whatever ``stream``).  max_seq_len: the longest
+    sequence to come, for planning (0: as long as the page table is wide); one far
+    above the lengths costs short calls time."""
 
     def __init__(self, H_q, k_cache, v_cache, page_table, max_tokens, max_seq_len=0, scale=0.0,
                  stream=None):
