@@ -65,6 +65,7 @@ typedef enum {
 #define HPD_DEVERR_FORK_CAP 0x100u  /* fork: more branches than the output capacity */
 #define HPD_DEVERR_CHUNK_CAP 0x200u /* chunk slots: more new tokens than max_tokens */
 #define HPD_DEVERR_POSITION 0x400u  /* a position outside [0, max_pos) */
+#define HPD_DEVERR_SCALE 0x800u     /* a scale of an 8-bit cache that is negative or not finite */
 
 /* Tokens per KV page of the paged private cache. */
 #define HPD_PAGE_TOKENS 16
@@ -472,6 +473,84 @@ typedef struct {
 size_t hpd_chunk_attn_workspace_size(const hpd_chunk_attn_args *args);
 
 hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *args, hpd_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The paged cache in 8 bits: e4m3 codes [num_pages][16][H_kv][D] of keys and of
+ * values, and for each a scale fp32 [num_pages][H_kv] for every page and head; row
+ * r of page p holds code * scale[p][h].  Half the memory of a bf16 cache, and half
+ * of the reading that bounds decoding.  hpd_chunk_slots serves it as it is.
+ * ------------------------------------------------------------------------ */
+
+/* hpd_qk_norm_rope into an 8-bit cache: rope.k_cache and rope.v_cache are codes,
+ * everything else means what it means there; keys are taken as they are before
+ * their rounding to bf16, values as they are.
+ * The rows of one page stand one after another in ascending slots (as
+ * hpd_chunk_slots leaves them), no page at two places of a call.  Of such a run, head
+ * h, with a = (largest finite magnitude) / 448:
+ *   first row at offset 0:   scale = max(a, 2^-100)
+ *   at offset o > 0:         the scale that is there, times 2^k with the least k >= 0
+ *                            for which a <= scale; the codes of rows below o times 2^-k
+ *   code = x / scale rounded to e4m3 (to nearest, ties to even); NaN where x is not
+ *   finite
+ * so that a code is rounded once, but for one that leaves the normal numbers of e4m3
+ * (below 2^-6 of 448) as its page's scale grows.  Rows behind the run are left as
+ * they are.
+ * A scale that is there but not in [2^-100, 2^120] counts as 2^-100 and is flagged
+ * HPD_DEVERR_SCALE.  Two launches at most. */
+typedef struct {
+  hpd_qk_norm_rope_args rope;
+  float *k_scale, *v_scale; /* fp32 [num_slots / 16][H_kv]; num_slots a multiple of 16 */
+} hpd_qk_norm_rope_fp8_args;
+
+hpd_status hpd_qk_norm_rope_fp8(const hpd_qk_norm_rope_fp8_args *args, hpd_stream_t stream);
+
+/* hpd_chunk_attn over an 8-bit cache: attn.k_cache and attn.v_cache are codes.  Codes
+ * and scales are taken as they are, without a rounding (keys and values of 2^127 and
+ * more become infinite).  A query row with a value that is not finite gives NaN.  A
+ * scale of a page that a tile of rows sees has to be at least 0 and finite; another
+ * one is flagged HPD_DEVERR_SCALE and read as 0.  Cache rows at or past
+ * seq_len may hold anything, and the scales of pages past it too. */
+typedef struct {
+  hpd_chunk_attn_args attn;
+  const float *k_scale, *v_scale; /* fp32 [num_pages][H_kv] */
+} hpd_chunk_attn_fp8_args;
+
+/* As hpd_chunk_attn_workspace_size. */
+size_t hpd_chunk_attn_fp8_workspace_size(const hpd_chunk_attn_fp8_args *args);
+
+hpd_status hpd_chunk_attn_fp8(const hpd_chunk_attn_fp8_args *args, hpd_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Log probabilities of given tokens (those that hpd_pmtp_accept returned, say),
+ * the entropy of the distributions they were taken from and the likeliest
+ * alternatives.  Of row r, with d_v = (logits[r][v] - max) * scale, Z = sum exp(d_v):
+ *   logprob[r] = d_token - log Z              entropy[r] = log Z - sum exp(d_v) d_v / Z
+ *   top_tokens[r][i], top_logprobs[r][i]      the `top` largest logits, largest first,
+ *                                             the lowest index first among equal ones
+ * Every row is read once (its largest values perhaps again, and all of it where very
+ * many equal those); sums are in 32 bits, and that of Z leaves out its largest term,
+ * so that a log probability near 0 keeps its digits.
+ * A logit of -inf has probability 0 (log probability -inf).  A row with NaN or +inf,
+ * or with nothing but -inf, has NaN for its log probabilities and entropy; NaN is
+ * never among the top tokens: where fewer than `top` logits are numbers the rest are
+ * -1, with NaN.  A token outside [0, V) has log probability -inf, NaN in such a row.
+ * One launch.
+ */
+typedef struct {
+  const void *logits;      /* [R][V], row r at logits + r * row_stride values       */
+  int64_t row_stride;      /* values; 0 = V                                         */
+  const int32_t *tokens;   /* [R]                                                   */
+  float *logprob;          /* [R]                                                   */
+  float *entropy;          /* [R], or NULL                                          */
+  int32_t *top_tokens;     /* [R][top]; NULL with top = 0                           */
+  float *top_logprobs;     /* [R][top]; NULL with top = 0                           */
+  int R, V;                /* R >= 0 rows (with none nothing is done), V >= 1       */
+  int top;                 /* 0 .. 32, at most V                                    */
+  int fp32;                /* 1: logits are fp32, 0: bf16                           */
+  float scale;             /* 1 / temperature, > 0 and finite; 0 = 1                */
+} hpd_token_logprobs_args; /* logits aligned to their type, the rest to 4 bytes     */
+
+hpd_status hpd_token_logprobs(const hpd_token_logprobs_args *args, hpd_stream_t stream);
 
 /* Self-test of the bounded device waits (no counterpart in the paper): one
  * warp waits on an mbarrier phase that nothing completes and for a

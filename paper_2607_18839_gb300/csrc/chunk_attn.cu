@@ -1388,16 +1388,8 @@ cudaError_t launch(const ChunkParams &p, long long units, cudaStream_t s) {
 }
 
 }  // namespace
-}  // namespace hpd
 
-extern "C" {
-
-size_t hpd_chunk_attn_workspace_size(const hpd_chunk_attn_args *a) {
-  return hpd::check_scalars(a) == HPD_OK ? hpd::make_plan(a).bytes : 0;
-}
-
-hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *a, hpd_stream_t stream) {
-  using namespace hpd;
+hpd_status check_chunk_attn(const hpd_chunk_attn_args *a) {
   const hpd_status st = check_scalars(a);
   if (st != HPD_OK) return st;
   if (!a->q || !a->chunk_cu || !a->seq_len || !a->k_cache || !a->v_cache || !a->page_table || !a->out)
@@ -1408,10 +1400,25 @@ hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *a, hpd_stream_t stream) {
                         static_cast<const void *>(a->full_len), static_cast<const void *>(a->page_table),
                         static_cast<const void *>(a->lse)})
     if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return HPD_ERR_INVALID_ARG;
-  const ChunkPlan pl = make_plan(a);
   if (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & (kAlign - 1)) != 0 ||
-      a->workspace_bytes < pl.bytes)
+      a->workspace_bytes < make_plan(a).bytes)
     return HPD_ERR_WORKSPACE;
+  return HPD_OK;
+}
+
+}  // namespace hpd
+
+extern "C" {
+
+size_t hpd_chunk_attn_workspace_size(const hpd_chunk_attn_args *a) {
+  return hpd::check_scalars(a) == HPD_OK ? hpd::make_plan(a).bytes : 0;
+}
+
+hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *a, hpd_stream_t stream) {
+  using namespace hpd;
+  const hpd_status st = check_chunk_attn(a);
+  if (st != HPD_OK) return st;
+  const ChunkPlan pl = make_plan(a);
   uint8_t *ws = static_cast<uint8_t *>(a->workspace);
   ChunkParams k{};
   k.q = static_cast<const __nv_bfloat16 *>(a->q);

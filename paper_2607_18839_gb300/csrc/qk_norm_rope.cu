@@ -212,10 +212,8 @@ cudaError_t launch_rope(RopeArgs &a, cudaStream_t s) {
 }
 
 }  // namespace
-}  // namespace hpd
 
-extern "C" hpd_status hpd_qk_norm_rope(const hpd_qk_norm_rope_args *a, hpd_stream_t stream) {
-  using namespace hpd;
+hpd_status check_norm_rope(const hpd_qk_norm_rope_args *a) {
   if (!a || a->T < 0 || a->H_q < 1 || a->H_kv < 1 || a->n_axes < 1 || a->n_axes > 4 || a->max_pos < 1 ||
       a->num_slots < 1 || !(a->eps >= 0.f) || a->eps > 3.4e38f)
     return HPD_ERR_INVALID_ARG;
@@ -233,7 +231,10 @@ extern "C" hpd_status hpd_qk_norm_rope(const hpd_qk_norm_rope_args *a, hpd_strea
   if (a->q_stride % 8 != 0 || a->k_stride % 8 != 0 || a->v_stride % 8 != 0) return HPD_ERR_INVALID_ARG;
   for (int i = 0; i < a->D / 2; ++i)
     if (a->axis[i] >= a->n_axes) return HPD_ERR_INVALID_ARG;
-  if (a->T == 0) return HPD_OK;
+  return HPD_OK;
+}
+
+cudaError_t launch_norm_rope(const hpd_qk_norm_rope_args *a, bool queries_only, cudaStream_t s) {
   RopeArgs k{};
   k.q = static_cast<const __nv_bfloat16 *>(a->q);
   k.k = static_cast<const __nv_bfloat16 *>(a->k);
@@ -254,10 +255,18 @@ extern "C" hpd_status hpd_qk_norm_rope(const hpd_qk_norm_rope_args *a, hpd_strea
   k.eps = a->eps;
   k.T = a->T;
   k.H_q = a->H_q;
-  k.H_kv = a->H_kv;
+  k.H_kv = queries_only ? 0 : a->H_kv;
   k.max_pos = a->max_pos;
   for (int i = 0; i < a->D / 2; ++i) k.axis[i >> 4] |= static_cast<uint32_t>(a->axis[i]) << (2 * (i & 15));
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = a->D == 64 ? launch_rope<64>(k, s) : launch_rope<128>(k, s);
+  return a->D == 64 ? launch_rope<64>(k, s) : launch_rope<128>(k, s);
+}
+
+}  // namespace hpd
+
+extern "C" hpd_status hpd_qk_norm_rope(const hpd_qk_norm_rope_args *a, hpd_stream_t stream) {
+  using namespace hpd;
+  const hpd_status st = check_norm_rope(a);
+  if (st != HPD_OK || a->T == 0) return st;
+  const cudaError_t e = launch_norm_rope(a, false, reinterpret_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? HPD_OK : record_cuda_error(e);
 }

@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import Optional
+from typing import NamedTuple, Optional
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libhpd.so")
@@ -21,7 +21,7 @@ STATUS = {0: "HPD_OK", 1: "HPD_ERR_INVALID_ARG", 2: "HPD_ERR_UNSUPPORTED",
 
 DEVERR = {0x1: "PREFIX_CU", 0x2: "BRANCH_CU", 0x4: "BRANCH_LEN", 0x8: "PAGE_ID",
           0x10: "FORK_LEN", 0x40: "TIMEOUT", 0x80: "POOL", 0x100: "FORK_CAP",
-          0x200: "CHUNK_CAP", 0x400: "POSITION"}
+          0x200: "CHUNK_CAP", 0x400: "POSITION", 0x800: "SCALE"}
 
 # Every entry point declared in include/hpd.h.
 EXPORTS = ("hpd_branch_attn_workspace_size", "hpd_workspace_init", "hpd_branch_attn",
@@ -30,7 +30,8 @@ EXPORTS = ("hpd_branch_attn_workspace_size", "hpd_workspace_init", "hpd_branch_a
            "hpd_read_errors", "hpd_status_string", "hpd_last_cuda_error", "hpd_version",
            "hpd_branch_attn_noalloc", "hpd_wait_selftest", "hpd_kv_append", "hpd_kv_rollback",
            "hpd_fork_children", "hpd_chunk_slots", "hpd_qk_norm_rope",
-           "hpd_chunk_attn_workspace_size", "hpd_chunk_attn")
+           "hpd_chunk_attn_workspace_size", "hpd_chunk_attn", "hpd_qk_norm_rope_fp8",
+           "hpd_chunk_attn_fp8_workspace_size", "hpd_chunk_attn_fp8", "hpd_token_logprobs")
 
 # Scratch bytes built into libhpd for hpd_branch_attn_noalloc.
 NOALLOC_WORKSPACE_BYTES = 32 << 20
@@ -121,6 +122,26 @@ class hpd_chunk_attn_args(ctypes.Structure):
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class hpd_qk_norm_rope_fp8_args(ctypes.Structure):
+    """Mirror of the C struct of the same name."""
+
+    _fields_ = [("rope", hpd_qk_norm_rope_args), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class hpd_chunk_attn_fp8_args(ctypes.Structure):
+    """Mirror of the C struct of the same name."""
+
+    _fields_ = [("attn", hpd_chunk_attn_args), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class hpd_token_logprobs_args(ctypes.Structure):
+    """Mirror of the C struct of the same name."""
+
+    _fields_ = [("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64)] + [
+        (n, ctypes.c_void_p) for n in ("tokens", "logprob", "entropy", "top_tokens", "top_logprobs")] + [
+        (n, ctypes.c_int) for n in ("R", "V", "top", "fp32")] + [("scale", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -179,6 +200,14 @@ def load(path: str = LIB_PATH):
     lib.hpd_chunk_attn_workspace_size.argtypes = [ctypes.POINTER(hpd_chunk_attn_args)]
     lib.hpd_chunk_attn.restype = I
     lib.hpd_chunk_attn.argtypes = [ctypes.POINTER(hpd_chunk_attn_args), P]
+    lib.hpd_qk_norm_rope_fp8.restype = I
+    lib.hpd_qk_norm_rope_fp8.argtypes = [ctypes.POINTER(hpd_qk_norm_rope_fp8_args), P]
+    lib.hpd_chunk_attn_fp8_workspace_size.restype = S
+    lib.hpd_chunk_attn_fp8_workspace_size.argtypes = [ctypes.POINTER(hpd_chunk_attn_fp8_args)]
+    lib.hpd_chunk_attn_fp8.restype = I
+    lib.hpd_chunk_attn_fp8.argtypes = [ctypes.POINTER(hpd_chunk_attn_fp8_args), P]
+    lib.hpd_token_logprobs.restype = I
+    lib.hpd_token_logprobs.argtypes = [ctypes.POINTER(hpd_token_logprobs_args), P]
     _lib = lib
     return lib
 
@@ -288,6 +317,22 @@ def hpd_chunk_attn_workspace_size(args: hpd_chunk_attn_args) -> int:
 
 def hpd_chunk_attn(args: hpd_chunk_attn_args, stream_handle) -> None:
     _check("hpd_chunk_attn", load().hpd_chunk_attn(ctypes.byref(args), stream_handle))
+
+
+def hpd_qk_norm_rope_fp8(args: hpd_qk_norm_rope_fp8_args, stream_handle) -> None:
+    _check("hpd_qk_norm_rope_fp8", load().hpd_qk_norm_rope_fp8(ctypes.byref(args), stream_handle))
+
+
+def hpd_chunk_attn_fp8_workspace_size(args: hpd_chunk_attn_fp8_args) -> int:
+    return int(load().hpd_chunk_attn_fp8_workspace_size(ctypes.byref(args)))
+
+
+def hpd_chunk_attn_fp8(args: hpd_chunk_attn_fp8_args, stream_handle) -> None:
+    _check("hpd_chunk_attn_fp8", load().hpd_chunk_attn_fp8(ctypes.byref(args), stream_handle))
+
+
+def hpd_token_logprobs(args: hpd_token_logprobs_args, stream_handle) -> None:
+    _check("hpd_token_logprobs", load().hpd_token_logprobs(ctypes.byref(args), stream_handle))
 
 
 def hpd_branch_attn_noalloc(args: hpd_branch_attn_args, stream_handle: Optional[int]) -> None:
@@ -449,6 +494,65 @@ def pmtp_accept(logits, drafts, stream=None):
     return out_tokens, acc
 
 
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs returns, in the shape of its tokens; top_tokens and
+    top_logprobs have one more extent and are None with top = 0."""
+
+    logprob: object
+    entropy: object
+    top_tokens: object
+    top_logprobs: object
+
+
+def token_logprobs(logits, tokens, top=0, temperature=1.0, stream=None) -> TokenLogprobs:
+    """Log probabilities of given tokens (hpd_token_logprobs): logits bf16 or fp32
+    [..., V] (as pmtp_accept takes them; the rows of a matrix may be strided),
+    tokens int32 [...]: fp32 log probabilities under softmax(logits /
+    temperature), the distributions' entropies, and the `top` (up to 32) likeliest
+    tokens of each with their log probabilities.  The outputs are allocated on the
+    stream of the call."""
+    import torch
+    what = "token_logprobs"
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in (torch.bfloat16, torch.float32) or \
+            not logits.is_cuda or logits.dim() < 1:
+        _need(what, logits, torch.bfloat16, (None, None), strides_free=True)
+        raise HpdError(what, 1, "logits of at least one extent")
+    lead, V = logits.shape[:-1], logits.shape[-1]
+    _need(what, tokens, torch.int32, lead)
+    stride = 0
+    if logits.dim() == 2 and logits.shape[0] > 1:
+        stride = logits.stride(0)
+        if (V > 1 and logits.stride(1) != 1) or stride < V:
+            raise HpdError(what, 1, "rows with their values side by side, none over another")
+    elif not logits.is_contiguous() and not (logits.dim() == 2 and logits.stride(1) == 1):
+        raise HpdError(what, 1, "contiguous logits, or a matrix with strided rows")
+    if not temperature > 0 or not 1.0 / temperature < 3.4e38 or not 1.0 / temperature > 1e-37:
+        raise HpdError(what, 1, "a temperature above 0")
+    if not 0 <= top <= min(V, 32):
+        raise HpdError(what, 1 if top < 0 or top > V else 2, "0 to 32 alternatives, no more than there are tokens")
+    _need_current(what, logits, tokens)
+    R = tokens.numel()
+    with torch.cuda.stream(stream):
+        one = torch.empty((2,) + lead, dtype=torch.float32, device=logits.device)
+        ids = torch.empty(lead + (top,), dtype=torch.int32, device=logits.device) if top else None
+        lps = torch.empty(lead + (top,), dtype=torch.float32, device=logits.device) if top else None
+    logprob, entropy = one[0], one[1]
+    a = hpd_token_logprobs_args(_ptr(logits), stride, _ptr(tokens), _ptr(logprob), _ptr(entropy), _ptr(ids), _ptr(lps),
+                                R, V, top, int(logits.dtype is torch.float32), 1.0 / temperature)
+    hpd_token_logprobs(a, _stream_handle(stream))
+    return TokenLogprobs(logprob, entropy, ids, lps)
+
+
+def fp8_cache(num_pages, H_kv, D, device="cuda"):
+    """An empty paged cache in 8 bits: (k_cache, v_cache float8_e4m3fn [num_pages,
+    16, H_kv, D], k_scale, v_scale fp32 [num_pages, H_kv]), for QkNormRope and
+    ChunkAttn."""
+    import torch
+    code = lambda: torch.zeros((num_pages, 16, H_kv, D), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)  # noqa: E731
+    scale = lambda: torch.zeros((num_pages, H_kv), dtype=torch.float32, device=device)  # noqa: E731
+    return code(), code(), scale(), scale()
+
+
 class PagedKV:
     """Device state of the paged private KV (tensors owned here): the caches,
     the page table, the branch lengths and the free-page stack, plus a
@@ -529,6 +633,15 @@ def _need(what: str, t, dtype, shape, strides_free=False):
                                 f"{tuple('any' if n is None else n for n in shape)}, got {have}")
 
 
+def _need_current(what: str, *tensors):
+    """A launch goes to the current device: tensors of another one are refused."""
+    import torch
+    here = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t.get_device() != here:
+            raise HpdError(what, 1, f"a tensor on {t.device}, while device {here} is the current one")
+
+
 def rope_table(max_pos: int, D: int, theta: float = 1e6, device="cuda"):
     """cos and sin of position * theta^(-2 i / D) for qk_norm_rope: fp32
     [max_pos, D / 2, 2], the angles taken in 64 bits."""
@@ -597,7 +710,9 @@ class QkNormRope:
     """Per-head norms, rotation and cache write of a layer (hpd_qk_norm_rope).
     q_weight / k_weight: bf16 [D] or None; rope: fp32 [max_pos, D / 2, 2]
     (rope_table); sections: how many of the D / 2 frequencies turn by each
-    axis' position, in order, or ``axis``: the axis of every frequency."""
+    axis' position, in order, or ``axis``: the axis of every frequency.
+    The cache is bf16, or held in 8 bits (hpd_qk_norm_rope_fp8): codes with the
+    scales of their pages and heads (fp8_cache makes one)."""
 
     def __init__(self, H_q, H_kv, D, q_weight, k_weight, rope, sections=None, axis=None, eps=1e-6):
         import torch
@@ -615,22 +730,26 @@ class QkNormRope:
         self._keep = (q_weight, k_weight, rope)
         self.n_axes = max(axis) + 1
         self.workspace = _ready_workspace(256, rope.device)
-        self.args = hpd_qk_norm_rope_args()
-        a = self.args
+        self._fp8 = hpd_qk_norm_rope_fp8_args()
+        a = self.args = self._fp8.rope
         a.q_weight, a.k_weight, a.rope = _ptr(q_weight), _ptr(k_weight), _ptr(rope)
         a.workspace, a.eps = _ptr(self.workspace), eps
         a.H_q, a.H_kv, a.D, a.n_axes, a.max_pos = H_q, H_kv, D, self.n_axes, rope.shape[0]
         a.axis[:D // 2] = axis
         self._bf, self._i32, self._on = torch.bfloat16, torch.int32, torch.cuda.stream
+        self._f32, self._code = torch.float32, torch.float8_e4m3fn
         self._q = None
         self._outgrown = []  # still the target of captured graphs, or of calls on other streams
 
-    def __call__(self, qkv, pos, slot, k_cache, v_cache, q_out=None, stream=None):
+    def __call__(self, qkv, pos, slot, k_cache, v_cache, q_out=None, stream=None, k_scale=None, v_scale=None):
         """qkv: bf16 [T, at least (H_q + 2 H_kv) D], the projection's rows
         (queries, keys, values; rows may be strided); pos: int32 [n_axes, T] or
-        [T]; slot: int32 [T]; caches bf16 [pages, 16, H_kv, D].  Returns the
+        [T]; slot: int32 [T]; caches bf16 [pages, 16, H_kv, D], or float8_e4m3fn
+        with k_scale and v_scale fp32 [pages, H_kv]: the rows of a page then stand
+        one after another in ascending slots, no page at two places.  Returns the
         queries [T, H_q, D] (q_out, or a tensor that this object keeps)."""
         a, H_q, H_kv, D = self.args, self.H_q, self.H_kv, self.D
+        coded = k_scale is not None or v_scale is not None
         bf, i32 = self._bf, self._i32
         if qkv.dim() != 2 or qkv.dtype is not bf or not qkv.is_cuda:
             _need("QkNormRope", qkv, bf, (None, None), strides_free=True)
@@ -647,11 +766,17 @@ class QkNormRope:
             raise HpdError("QkNormRope", 1, f"a contiguous CUDA int32 slot for each of {T} rows")
         shape = k_cache.shape
         pages = shape[0]
-        if shape != (pages, 16, H_kv, D) or v_cache.shape != shape or k_cache.dtype is not bf or \
-                v_cache.dtype is not bf or not (k_cache.is_cuda and v_cache.is_cuda) or \
+        kind = self._code if coded else bf
+        if shape != (pages, 16, H_kv, D) or v_cache.shape != shape or k_cache.dtype is not kind or \
+                v_cache.dtype is not kind or not (k_cache.is_cuda and v_cache.is_cuda) or \
                 not (k_cache.is_contiguous() and v_cache.is_contiguous()):
-            _need("QkNormRope", k_cache, bf, (None, 16, H_kv, D))
-            _need("QkNormRope", v_cache, bf, shape)
+            _need("QkNormRope", k_cache, kind, (None, 16, H_kv, D))
+            _need("QkNormRope", v_cache, kind, shape)
+        if coded:
+            for t in (k_scale, v_scale):
+                if t is None or not _is(t, self._f32, (pages, H_kv)):
+                    _need("QkNormRope", t, self._f32, (pages, H_kv))
+            _need_current("QkNormRope", qkv, k_cache, v_cache, k_scale, v_scale)
         if q_out is None:
             if self._q is None or self._q.shape[0] < T:
                 rows = T
@@ -670,7 +795,11 @@ class QkNormRope:
         a.pos, a.slot, a.q_out = pos.data_ptr(), slot.data_ptr(), q_out.data_ptr()
         a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
         a.num_slots, a.T = pages * 16, T
-        hpd_qk_norm_rope(a, _stream_handle(stream))
+        if coded:
+            self._fp8.k_scale, self._fp8.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+            hpd_qk_norm_rope_fp8(self._fp8, _stream_handle(stream))
+        else:
+            hpd_qk_norm_rope(a, _stream_handle(stream))
         return q_out
 
     def errors(self, stream=None) -> int:
@@ -683,27 +812,37 @@ class ChunkAttn:
     and the workspace, which is ready for calls on any stream once this is made
     (on the current one, whatever ``stream``).  max_seq_len: the longest
     sequence to come, for planning (0: as long as the page table is wide); one far
-    above the lengths costs short calls time."""
+    above the lengths costs short calls time.
+    The cache is bf16, or held in 8 bits (hpd_chunk_attn_fp8): float8_e4m3fn codes
+    with k_scale and v_scale fp32 [pages, H_kv]."""
 
     def __init__(self, H_q, k_cache, v_cache, page_table, max_tokens, max_seq_len=0, scale=0.0,
-                 stream=None):
+                 stream=None, k_scale=None, v_scale=None):
         import torch
         bf = torch.bfloat16
-        _need("ChunkAttn", k_cache, bf, (None, 16, None, None))
-        _need("ChunkAttn", v_cache, bf, k_cache.shape)
+        self._coded = k_scale is not None or v_scale is not None
+        kind = torch.float8_e4m3fn if self._coded else bf
+        _need("ChunkAttn", k_cache, kind, (None, 16, None, None))
+        _need("ChunkAttn", v_cache, kind, k_cache.shape)
+        if self._coded:
+            for t in (k_scale, v_scale):
+                _need("ChunkAttn", t, torch.float32, (k_cache.shape[0], k_cache.shape[2]))
+            _need_current("ChunkAttn", k_cache, v_cache, k_scale, v_scale, page_table)
         _need("ChunkAttn", page_table, torch.int32, (None, None))
         num_pages, _, H_kv, D = k_cache.shape
         S, max_pages = page_table.shape
         dev = k_cache.device
-        self._keep = (k_cache, v_cache, page_table)
+        self._keep = (k_cache, v_cache, page_table, k_scale, v_scale)
         self.out = torch.empty((max_tokens, H_q, D), dtype=bf, device=dev)
         self.lse = torch.empty((max_tokens, H_q), dtype=torch.float32, device=dev)
-        a = self.args = hpd_chunk_attn_args()
+        self._fp8 = hpd_chunk_attn_fp8_args()
+        a = self.args = self._fp8.attn
+        self._fp8.k_scale, self._fp8.v_scale = _ptr(k_scale), _ptr(v_scale)
         a.k_cache, a.v_cache, a.page_table = _ptr(k_cache), _ptr(v_cache), _ptr(page_table)
         a.S, a.T, a.H_q, a.H_kv, a.D = S, max_tokens, H_q, H_kv, D
         a.num_pages, a.max_pages, a.max_seq_len, a.scale = num_pages, max_pages, max_seq_len, scale
         a.out, a.lse = _ptr(self.out), _ptr(self.lse)
-        nbytes = hpd_chunk_attn_workspace_size(a)
+        nbytes = hpd_chunk_attn_fp8_workspace_size(self._fp8) if self._coded else hpd_chunk_attn_workspace_size(a)
         if nbytes == 0:
             raise HpdError("hpd_chunk_attn_workspace_size", 1, "invalid shape")
         self.max_tokens = max_tokens
@@ -732,7 +871,11 @@ class ChunkAttn:
         a.q, a.q_stride, a.T = q.data_ptr(), row if T > 1 else 0, T
         a.chunk_cu, a.seq_len = chunk_cu.data_ptr(), seq_len.data_ptr()
         a.full_len = None if full_len is None else full_len.data_ptr()
-        hpd_chunk_attn(a, _stream_handle(stream))
+        if self._coded:
+            _need_current("ChunkAttn", q)
+            hpd_chunk_attn_fp8(self._fp8, _stream_handle(stream))
+        else:
+            hpd_chunk_attn(a, _stream_handle(stream))
         return (self.out, self.lse) if T == self.max_tokens else (self.out[:T], self.lse[:T])
 
     def errors(self, stream=None) -> int:
