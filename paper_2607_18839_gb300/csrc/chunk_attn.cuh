@@ -97,33 +97,33 @@ constexpr uint32_t kTmemCols = 512;
 constexpr int kPagesPerBlock = kBlk / kPage, kPagesEach = kPagesPerBlock / 2;  // of a producer
 constexpr int kSoftmaxWarp = 8, kSoftmaxWarps = 8;
 constexpr int kOutputWarp = kSoftmaxWarp + kSoftmaxWarps, kOutputWarps = 4;
+constexpr int kProducers = 4;  // warps 0, 1: K; 2, 3: V
+constexpr int kQkWarp = 4, kPvWarp = 5, kSchedWarp = 6;
+constexpr int kWideWarp = kOutputWarp + kOutputWarps, kWideWarps = 4;  // 8-bit cache: Q parts, V to f16
 template <bool kFp8>
-struct Roles {
-  static constexpr int kProducers = 4;  // warps 0, 1: K; 2, 3: V
-  static constexpr int kQkWarp = 4, kPvWarp = 5, kSchedWarp = 6;
-  static constexpr int kThreads = 32 * (kOutputWarp + kOutputWarps);
-  static constexpr int kStages = 3, kVStages = 3;  // of the K and V rings
-  static constexpr int kKArrivals = 2, kVArrivals = 2;
-};
-template <>
-struct Roles<true> {
-  static constexpr int kVWarp = 2, kVWarps = 4;  // warps 0, 1: K; 2 .. 5: V and Q
-  static constexpr int kProducers = kVWarp + kVWarps;
-  static constexpr int kQkWarp = 6, kPvWarp = 7, kSchedWarp = kOutputWarp + kOutputWarps;
-  static constexpr int kThreads = 32 * (kSchedWarp + 1);
-  static constexpr int kStages = 4, kVStages = 2;  // K codes, V in bf16
-  static constexpr int kCodeStages = 4;            // V codes, for each V warp
-  static constexpr int kKArrivals = 4, kVArrivals = kVWarps;
-};
+constexpr int kThreads = 32 * (kWideWarp + (kFp8 ? kWideWarps : 0));
 // What a pass over a unit does: exponentials against the first block's maxima;
 // nothing but the rows' maxima; exponentials against those.
 enum Pass { kFirst, kMaxima, kAgain };
 constexpr int kMetaSlots = 3;
 // of a metadata slot: producers, two MMA issuers, softmax and output warps
 template <bool kFp8>
-constexpr uint32_t kMetaConsumers = Roles<kFp8>::kProducers + 2 + kSoftmaxWarps + kOutputWarps;
+constexpr uint32_t kMetaConsumers = kProducers + 2 + kSoftmaxWarps + kOutputWarps + (kFp8 ? kWideWarps : 0);
+template <bool kFp8>
+struct Rings {
+  static constexpr int kStages = 3, kVStages = 3;  // of K and V
+};
+template <>
+struct Rings<true> {
+  static constexpr int kStages = 4, kVStages = 2;  // of K's codes, and of V as f16
+  static constexpr int kCodeStages = 4;            // of V's codes
+};
 constexpr int kMaxStages = 4;
 constexpr int kScaleBlocks = 8;  // blocks whose scales are held
+// 8-bit cache, a first pass, whose weights are f16: log2 of the weight of a row's base
+// (weights up to 2^12 above it fit, 2^-29 of it is not lost), and the least scale of V,
+// over that of its first block, at which none of 2^-4 and more loses digits.
+constexpr float kFirstLog2 = 4.f, kLeastVal = 0x1p-14f;
 constexpr int kGroup = 256;      // sequences whose lengths the scheduler holds at once
 constexpr int kMaxSplits = 32;
 constexpr int kTailWaves = 4;    // most waves of the units of split tiles
@@ -182,7 +182,7 @@ __device__ __forceinline__ UnitMeta read_meta(const UnitMeta &m) {
 
 template <int D, bool kFp8>
 struct Layout {
-  using R = Roles<kFp8>;
+  using R = Rings<kFp8>;
   static constexpr int kChunks = D / 64;                // 64-column (128-byte) boxes
   static constexpr uint32_t kChunkBytes = kRows * 128;  // 128 rows x 128 bytes
   static constexpr uint32_t kTileBytes = kChunks * kChunkBytes;
@@ -193,7 +193,8 @@ struct Layout {
   static constexpr uint32_t kK = 0;
   static constexpr uint32_t kV = kK + R::kStages * kKBytes;
   static constexpr uint32_t kCodes = kV + R::kVStages * kTileBytes;  // codes of V
-  static constexpr uint32_t kStage = kCodes + (kFp8 ? 4 * kCodeBytes : 0);  // 128 bytes of each output row
+  static constexpr int kCodeStages = kFp8 ? Rings<true>::kCodeStages : 0;
+  static constexpr uint32_t kStage = kCodes + kCodeStages * kCodeBytes;  // 128 bytes of each output row
   static constexpr uint32_t kBytes = kStage + kRows * 128;
   static constexpr uint32_t kDynSmem = kBytes + 1024;   // slack to align to 1024
   // TMEM columns: S of block buffer i, O, Q rows of unit slot u
@@ -201,7 +202,6 @@ struct Layout {
   static __device__ __forceinline__ uint32_t col_s(int i) { return i ? 128u : 0u; }
   static __device__ __forceinline__ uint32_t col_q(int u) { return u ? 448u : 384u; }
 };
-static_assert(Roles<true>::kCodeStages == 4, "Layout::kStage");
 
 struct __align__(16) Shared {
   uint64_t meta_full[kMetaSlots], meta_empty[kMetaSlots];
@@ -223,10 +223,10 @@ struct __align__(16) Shared {
   int sieved_seq;                    // units of which that is complete
   int unit_id[32];          // the last units issued
   UnitMeta meta[kMetaSlots];
-  // 8-bit cache: codes of V landed, by V warp; Q parts written and done with; a row's
+  // 8-bit cache: codes of V landed and widened; Q parts written and done with; a row's
   // factor of its parts; scales of a block's pages, of K and then of V
-  uint64_t code_full[4][4], q_full[2], q_free[2];
-  float q_scale[kMetaSlots][kRows];
+  uint64_t code_full[kMaxStages], code_empty[kMaxStages], q_full[2], q_free[2];
+  float q_scale[kMetaSlots][kRows], v_ref[kMetaSlots][kRows];  // (v_ref: what O is in units of)
   float __align__(16) scales[kScaleBlocks][2 * kPagesPerBlock];
   // the scheduler's group of sequences: units before each, first rows, rows, lengths,
   // keys that all their rows see, tiles left whole, splits of the others
@@ -446,8 +446,11 @@ __device__ __noinline__ void add_sieved(const uint32_t *first, int keys, float *
 // The same pieces over an 8-bit cache.  A raw score is that of the query's parts with
 // codes: what it is scaled by is row_mul (the softmax scale and the parts' factor) times
 // the key's scale, one for the 16 keys of a page.  A weight goes to the tensor cores
-// times its value's scale, rounded once; its sum is of the weight alone.  ks, vs: scales
-// of the first of the pages.
+// times its value's scale over the row's v_ref, rounded once; its sum is of the weight
+// alone.  In a first pass that is to f16, 2^-11 of it and as V's codes widen with one
+// instruction for two.  What f16 cannot hold is run again with bf16: a weight that is too
+// large becomes infinite, which the reader of O finds, and scales of V too far below
+// v_ref are found here (false).  ks, vs: scales of the first of the pages.
 __device__ __noinline__ float row_max_fp8(uint32_t s_addr, int apart, bool plain, int hi, float row_mul,
                                           const float *ks) {
   const float NEG_INF = -__int_as_float(0x7f800000);
@@ -471,91 +474,88 @@ __device__ __noinline__ float row_max_fp8(uint32_t s_addr, int apart, bool plain
   }
   return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
 }
+// Largest scale of V among a block's pages that have one of its first `keys` keys.
+__device__ __forceinline__ float largest_scale(const float *vs, int keys) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPagesPerBlock; ++i) m = i * kPage < keys ? fmaxf(m, vs[i]) : m;
+  return m;
+}
+// The power of two at or below it (2^-100 of less), and that over one.
+__device__ __forceinline__ float ref_of(float scale) {
+  return __uint_as_float(max(__float_as_uint(scale), 27u << 23) & 0x7f800000u);
+}
+__device__ __forceinline__ float over_ref(float ref) { return __uint_as_float((254u << 23) - __float_as_uint(ref)); }
 template <class Publish>
-__device__ __forceinline__ bool softmax_plain_fp8(uint32_t s_addr, float row_mul, const float *ks, const float *vs,
-                                                  float m_run, float2 *l4, Publish publish) {
-  const float NEG_INF = -__int_as_float(0x7f800000);
-  float mx4[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
-  const float base = m_run == NEG_INF ? 0.f : m_run;
+__device__ __forceinline__ bool softmax_plain_fp8(uint32_t s_addr, float row_mul, float val_mul, const float *ks,
+                                                  const float *vs, float base, float2 *l4, Publish publish) {
   uint32_t v[2][16], pk[16];
+  tmem_ld16(s_addr + 32, v[0]);
   const float2 nbase2 = make_float2(-base, -base);
   const float4 k4 = *reinterpret_cast<const float4 *>(ks), v4 = *reinterpret_cast<const float4 *>(vs);
-  const float mul[4] = {row_mul * k4.z, row_mul * k4.w, row_mul * k4.x, row_mul * k4.y};
-  const float val[4] = {v4.z, v4.w, v4.x, v4.y};
-  tmem_ld16(s_addr + 32, v[0]);
+  const float kq[4] = {k4.z, k4.w, k4.x, k4.y}, vq[4] = {v4.z, v4.w, v4.x, v4.y};
+  bool fits = true;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     uint32_t *const x = v[q & 1];
     tmem_ld_wait16(x);
     if (q < 3) tmem_ld16(s_addr + (q == 0 ? 48 : q == 1 ? 0 : 16), v[(q & 1) ^ 1]);
-    const float2 mul2 = make_float2(mul[q], mul[q]), val2 = make_float2(val[q], val[q]);
+    const float mul = row_mul * kq[q], val = val_mul * vq[q];
+    const float2 mul2 = make_float2(mul, mul), val2 = make_float2(val, val);
+    fits &= !(val < kLeastVal) || vq[q] == 0.f;
 #pragma unroll
     for (int c = 0; c < 16; c += 2) {
-      const float2 a = make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1]));
-      const float2 arg = __ffma2_rn(a, mul2, nbase2);
+      const float2 arg = __ffma2_rn(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), mul2, nbase2);
       const float2 e = make_float2(fast_exp2(arg.x), fast_exp2(arg.y));
       l4[(c >> 1) & 3] = __fadd2_rn(l4[(c >> 1) & 3], e);
       const float2 w = __fmul2_rn(e, val2);
-      pk[(q & 1) * 8 + c / 2] = pack_bf16x2(w.x, w.y);
-      mx4[(c >> 1) & 3] = tc::fmax3(mx4[(c >> 1) & 3], arg.x, arg.y);
+      pk[(q & 1) * 8 + c / 2] = pack_f16x2(w.x, w.y);
     }
     if (q & 1) {
       tmem_st16(s_addr + 32 + (q >> 1) * 16, pk);
       publish(q >> 1);
     }
   }
-  return fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) <= tc::kWindowLog2;
+  return fits;
 }
-template <class Publish>
-__device__ __forceinline__ bool softmax_masked_fp8(uint32_t s_addr, int hi, float row_mul, const float *ks,
-                                                   const float *vs, float m_run, float2 *l4, Publish publish) {
-  const float NEG_INF = -__int_as_float(0x7f800000);
-  const float base = m_run == NEG_INF ? 0.f : m_run;
-  float mx4[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
+template <bool kBf16, class Publish>
+__device__ __forceinline__ bool softmax_masked_fp8(uint32_t s_addr, int hi, float row_mul, float val_mul,
+                                                   const float *ks, const float *vs, float base, float2 *l4,
+                                                   Publish publish) {
+  bool fits = true;
 #pragma unroll 1
   for (int part = 0; part < 2; ++part) {
     uint32_t v[32], pk[16];
     tmem_ld32(s_addr + 32 - 32 * part, v);
     tmem_ld_wait32(v);
     const int p0 = 2 - 2 * part;
-    const float mul[2] = {row_mul * ks[p0], row_mul * ks[p0 + 1]}, val[2] = {vs[p0], vs[p0 + 1]};
+    const float mul[2] = {row_mul * ks[p0], row_mul * ks[p0 + 1]}, val[2] = {val_mul * vs[p0], val_mul * vs[p0 + 1]};
 #pragma unroll
     for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(fmaf(__uint_as_float(v[c]), mul[c / kPage], -base));
     tc::mask32(v, 0, hi - 32 + 32 * part, false, 1.f);
 #pragma unroll
     for (int c = 0; c < 32; c += 2) {
-      const float2 arg = make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-      const float2 e = make_float2(fast_exp2(arg.x), fast_exp2(arg.y));
+      const float2 e = make_float2(fast_exp2(__uint_as_float(v[c])), fast_exp2(__uint_as_float(v[c + 1])));
       l4[(c >> 1) & 3] = __fadd2_rn(l4[(c >> 1) & 3], e);
-      pk[c / 2] = pack_bf16x2(e.x * val[c / kPage], e.y * val[c / kPage]);
-      mx4[(c >> 1) & 3] = tc::fmax3(mx4[(c >> 1) & 3], arg.x, arg.y);
+      // (a key that the row does not see may have a page whose scale is any multiple of v_ref)
+      const float2 w = make_float2(e.x == 0.f ? 0.f : e.x * val[c / kPage], e.y == 0.f ? 0.f : e.y * val[c / kPage]);
+      pk[c / 2] = kBf16 ? pack_bf16x2(w.x, w.y) : pack_f16x2(w.x, w.y);
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) fits &= !(val[i] < kLeastVal) || vs[p0 + i] == 0.f;
     tmem_st16(s_addr + 32 + 16 * part, pk);
     publish(part);
   }
-  return fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])) <= tc::kWindowLog2;
-}
-
-// 16 codes of a row of V as bf16 in the tile that P V reads: columns 16 c .. 16 c + 15 of
-// key r of the tile at v0, the first 8 of them at `at`, the others beside.
-__device__ __forceinline__ void widen16(const uint32_t *w, uint32_t *b) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 lo = of_codes(w[i] & 0xffffu), hi = of_codes(w[i] >> 16);
-    b[2 * i] = pack_bf16x2(lo.x, lo.y);
-    b[2 * i + 1] = pack_bf16x2(hi.x, hi.y);
-  }
+  return kBf16 || fits;
 }
 
 template <int D, bool kFp8>
-__global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
+__global__ void __launch_bounds__(kThreads<kFp8>, 1)
     chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_k4,
                       const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_v4,
                       const __grid_constant__ CUtensorMap tm_q, const ChunkParams p) {
   using L = Layout<D, kFp8>;
-  using R = Roles<kFp8>;
-  constexpr int kProducers = R::kProducers, kQkWarp = R::kQkWarp, kPvWarp = R::kPvWarp, kSchedWarp = R::kSchedWarp;
-  constexpr int kStages = R::kStages, kVStages = R::kVStages;
+  constexpr int kStages = Rings<kFp8>::kStages, kVStages = Rings<kFp8>::kVStages;
   extern __shared__ uint8_t smem_raw[];
   __shared__ Shared sh;
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -577,17 +577,20 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
     sh.units_done = 0;
     sh.sieved_seq = 0;
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(bar(sh.k_full[s]), R::kKArrivals);
+      mbar_init(bar(sh.k_full[s]), kFp8 ? 4 : 2);
       mbar_init(bar(sh.k_empty[s]), 1);
     }
     for (int s = 0; s < kVStages; ++s) {
-      mbar_init(bar(sh.v_full[s]), R::kVArrivals);
+      mbar_init(bar(sh.v_full[s]), kFp8 ? kWideWarps : 2);
       mbar_init(bar(sh.v_empty[s]), 1);
     }
     if constexpr (kFp8) {
-      for (int i = 0; i < 16; ++i) mbar_init(bar(sh.code_full[0][0]) + 8 * i, 1);
+      for (int i = 0; i < Rings<true>::kCodeStages; ++i) {
+        mbar_init(bar(sh.code_full[i]), 2);
+        mbar_init(bar(sh.code_empty[i]), kWideWarps);
+      }
       for (int i = 0; i < 2; ++i) {
-        mbar_init(bar(sh.q_full[i]), R::kVWarps);
+        mbar_init(bar(sh.q_full[i]), kWideWarps);
         mbar_init(bar(sh.q_free[i]), 1);
       }
     }
@@ -864,303 +867,21 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
       }
       if (!have) break;
     }
-  } else if (kFp8 && warp < 2) {
-    if constexpr (kFp8) {
-    // ----------------------------------------------- K codes and scales --
-    const int half = warp;
-    if (lane == 0) {
-      prefetch_tmap(&tm_k);
-      prefetch_tmap(&tm_k4);
-    }
-    __syncwarp();
-    pdl_wait();
-    const uint32_t ring = sbase + L::kK + half * (L::kKBytes / 2);
-    int issued = 0;  // ring entries
-    bool ok = true;
-    for (int k = 0; ok; ++k) {
-      const int slot = k % kMetaSlots;
-      if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
-      const UnitMeta M = read_meta(sh.meta[slot]);
-      __syncwarp();
-      if (!M.valid) break;
-      if (lane == 0) {
-        mbar_arrive(bar(sh.meta_empty[slot]));
-        if (warp == 0) mbar_arrive(bar(sh.taken));
-      }
-      const int32_t *const row = p.page_table + static_cast<size_t>(M.seq) * p.max_pages;
-      // (ids of eight blocks at once, eight blocks ahead of their use, and the scales of
-      // those pages four ahead)
-      constexpr int kIdBlocks = 32 / kPagesEach;
-      const int page0 = M.blk_lo * kPagesPerBlock + (lane / kPagesEach) * kPagesPerBlock + half * kPagesEach +
-                        lane % kPagesEach;
-      int ids = p.num_pages, ids_next = p.num_pages;
-      float ks = 0.f, vs = 0.f, ks_next = 0.f, vs_next = 0.f;
-      auto seen = [&](int j) { return page0 + j * kPagesPerBlock < M.pages; };
-      auto look_up = [&](int j) {
-        ids_next = p.num_pages;
-        // (a coherent load: the kernel before may write the table while this one starts)
-        if (seen(j)) ids_next = row[page0 + j * kPagesPerBlock];
-      };
-      auto check = [&](int j) {  // ids_next of the blocks from j on
-        if (seen(j) && static_cast<unsigned>(ids_next) >= static_cast<unsigned>(p.num_pages)) {
-          flag_error(p.err, HPD_DEVERR_PAGE_ID);
-          ids_next = 0;
-        }
-      };
-      auto fetch_scales = [&](int j) {
-        ks_next = vs_next = 0.f;
-        if (seen(j)) {
-          const size_t at = static_cast<size_t>(ids_next) * p.H_kv + M.g;
-          ks_next = p.k_scale[at];
-          vs_next = p.v_scale[at];
-        }
-      };
-      look_up(0);
-#pragma unroll 1
-      for (int j = 0; j < M.n_blocks; ++j) {
-        const int e = issued, s = e % kStages, at = j % kIdBlocks;
-        if (e >= kStages && !(ok = wait_bar(sh.k_empty[s], ((e / kStages) - 1) & 1))) break;
-        ++issued;
-        if (at == 0) {
-          if (j == 0) {
-            check(0);
-            fetch_scales(0);
-          }
-          ids = ids_next;
-          look_up(j + kIdBlocks);
-          __syncwarp();
-        }
-        const int from = at * kPagesEach + (lane & (kPagesEach - 1));
-        const int pg = __shfl_sync(0xffffffffu, ids, from);
-        const uint32_t b = bar(sh.k_full[s]);
-        mbar_arrive_expect_tx_elect(b, L::kKBytes / 2);
-        const int right = __shfl_down_sync(0xffffffffu, pg, 1);
-        const unsigned run = __ballot_sync(0xffffffffu, lane < kPagesEach - 1 && right == pg + 1);
-        const bool one = p.num_pages >= kPagesEach && (run & 7u) == 7u;
-        if (lane < (one ? 1 : kPagesEach))
-          tma_load_3d(ring + s * L::kKBytes + lane * (kPage * D), one ? &tm_k4 : &tm_k, b, 0, M.g, kPage * pg);
-        __syncwarp();
-        if (at == 0) {
-          ks = ks_next;
-          vs = vs_next;
-          const float INF = __int_as_float(0x7f800000);
-          if (!(ks >= 0.f && ks < INF && vs >= 0.f && vs < INF)) {
-            flag_error(p.err, HPD_DEVERR_SCALE);
-            if (!(ks >= 0.f && ks < INF)) ks = 0.f;
-            if (!(vs >= 0.f && vs < INF)) vs = 0.f;
-          }
-          __syncwarp();
-        } else if (at == kIdBlocks / 2) {
-          check(j - at + kIdBlocks);
-          fetch_scales(j - at + kIdBlocks);
-          __syncwarp();
-        }
-        const float k1 = __shfl_sync(0xffffffffu, ks, from), v1 = __shfl_sync(0xffffffffu, vs, from);
-        if (lane < kPagesEach) {
-          sh.scales[e % kScaleBlocks][half * kPagesEach + lane] = k1;
-          sh.scales[e % kScaleBlocks][kPagesPerBlock + half * kPagesEach + lane] = v1;
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(b);
-      }
-    }
-    if (!ok && lane == 0) set_abort(sh, p.err);
-    // no exit while a copy into this CTA's shared memory is in flight
-    for (int e = max(0, issued - kStages); e < issued; ++e)
-      mbar_wait(bar(sh.k_full[e % kStages]), (e / kStages) & 1);
-    }
-  } else if (kFp8 && warp < kProducers) {
-    if constexpr (kFp8) {
-    // ------------------------------------------- Q parts, V codes to bf16 --
-    const int w = warp - R::kVWarp, quad = warp & 3;  // 32 keys of a block; 32 rows of a tile
-    if (lane == 0) {
-      prefetch_tmap(&tm_v);
-      prefetch_tmap(&tm_v4);
-    }
-    __syncwarp();
-    pdl_wait();
-    constexpr int kAhead = R::kCodeStages;
-    constexpr uint32_t kMine = 32 * D;  // bytes of this warp's codes of a block
-    const uint32_t codes = sbase + L::kCodes + w * (kAhead * kMine);
-    // Loads run ahead of what is converted, into the next units as well.
-    int iu = 0, ij = 0, inb = 0, iseq = 0, ig = 0, ipages = 0, ipage0 = 0;  // unit and block to load next
-    bool open = false, none = false;
-    int ids = 0, ids_next = 0;
-    int issued = 0, done = 0;  // blocks loaded and converted
-    constexpr int kIdBlocks = 16;  // two pages of a block are this warp's
-    auto look_up = [&](int j) {
-      const int i = ipage0 + j * kPagesPerBlock;
-      ids_next = p.num_pages;
-      if (i < ipages) ids_next = p.page_table[static_cast<size_t>(iseq) * p.max_pages + i];
-    };
-    auto open_unit = [&] {  // the next unit with blocks to load, if it is known
-      while (!open && !none && __all_sync(0xffffffffu, mbar_try_wait(bar(sh.meta_full[iu % kMetaSlots]), (iu / kMetaSlots) & 1))) {
-        const UnitMeta M = read_meta(sh.meta[iu % kMetaSlots]);
-        none = !M.valid;
-        if (none) break;
-        if (M.pass == kMaxima) {
-          ++iu;
-          continue;
-        }
-        open = true;
-        ij = 0;
-        inb = M.n_blocks;
-        iseq = M.seq;
-        ig = M.g;
-        ipages = M.pages;
-        ipage0 = (M.blk_lo + (lane >> 1)) * kPagesPerBlock + 2 * w + (lane & 1);
-        look_up(0);
-      }
-      __syncwarp();
-    };
-    auto issue = [&] {  // loads of as many blocks as are known and have room
-      while (issued - done < kAhead) {
-        if (!open) open_unit();
-        if (!open) return;
-        if (ij % kIdBlocks == 0) {
-          ids = ids_next;
-          if (ipage0 + ij * kPagesPerBlock < ipages && static_cast<unsigned>(ids) >= static_cast<unsigned>(p.num_pages)) {
-            flag_error(p.err, HPD_DEVERR_PAGE_ID);
-            ids = 0;
-          }
-          look_up(ij + kIdBlocks);
-          __syncwarp();
-        }
-        const int pg = __shfl_sync(0xffffffffu, ids, (ij % kIdBlocks) * 2 + (lane & 1));
-        const int right = __shfl_sync(0xffffffffu, pg, 1);
-        const bool one = p.num_pages >= 2 && __shfl_sync(0xffffffffu, pg, 0) + 1 == right;
-        const int st = issued % kAhead;
-        const uint32_t b = bar(sh.code_full[w][st]);
-        mbar_arrive_expect_tx_elect(b, kMine);
-        if (lane < (one ? 1 : 2))
-          tma_load_3d(codes + st * kMine + lane * (kPage * D), one ? &tm_v4 : &tm_v, b, 0, ig, kPage * pg);
-        __syncwarp();
-        ++issued;
-        if (++ij == inb) {
-          open = false;
-          ++iu;
-        }
-      }
-    };
-    uint32_t sv = 0, pv = 1;  // V ring: stage, phase of its being free
-    bool ok = true;
-    for (int k = 0; ok; ++k) {
-      const int slot = k % kMetaSlots;
-      if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
-      const UnitMeta M = read_meta(sh.meta[slot]);
-      __syncwarp();
-      if (!M.valid) break;
-      if (iu <= k && !open) open_unit();  // (known now, so that its slot may go)
-      if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
-      issue();
-      // Q: a row a thread.  q 2^t = q1 + q2 with the row's largest value between 2^7 and
-      // 2^8: q1 has four of bf16's eight bits, what is left of them fits into q2, but for
-      // values below 2^-9 of the largest.
-      if (k >= 2 && !(ok = wait_bar(sh.q_free[k & 1], ((k >> 1) - 1) & 1))) break;
-      tc_fence_after();
-      const int r_in = quad * 32 + lane;
-      if (quad * 32 < M.nrows) {
-        const int rt = p.div_G(r_in);
-        const bool valid = r_in < M.nrows;
-        const uint4 *const src = reinterpret_cast<const uint4 *>(
-            p.q + (valid ? (M.tok0 + rt) * p.q_stride + (M.g * G + r_in - rt * G) * D : 0));
-        unsigned most = 0u;
-        {
-          uint4 x[D / 8];
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) x[i] = valid ? src[i] : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i)
-            most = __vmaxu2(__vmaxu2(most, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu)),
-                            __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
-        }
-        most = max(most & 0xffffu, most >> 16);
-        const int t = min(134 - static_cast<int>(most >> 7), 126);
-        const float up = __uint_as_float(static_cast<uint32_t>(127 + t) << 23);
-        sh.q_scale[slot][r_in] =
-            most >= 0x7f80u ? __int_as_float(0x7fffffff) : __uint_as_float(static_cast<uint32_t>(127 - t) << 23);
-        const uint32_t q_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::col_q(k & 1);
-#pragma unroll 1
-        for (int i0 = 0; i0 < D / 8; i0 += 4) {  // 32 columns at a time, from L1 this time
-          uint32_t c1[8], c2[8];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint4 y = valid ? src[i0 + i] : make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t ab[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t a = ab[2 * e], b = ab[2 * e + 1];
-              const float q0 = __uint_as_float(a << 16) * up, q1 = __uint_as_float(a & 0xffff0000u) * up;
-              const float q2 = __uint_as_float(b << 16) * up, q3 = __uint_as_float(b & 0xffff0000u) * up;
-              const uint32_t lo = to_codes(q0, q1), hi = to_codes(q2, q3);
-              c1[2 * i + e] = lo | hi << 16;
-              const float2 f = of_codes(lo), g = of_codes(hi);
-              c2[2 * i + e] = to_codes4(q0 - f.x, q1 - f.y, q2 - g.x, q3 - g.y);
-            }
-          }
-          tmem_st8(q_addr + 2 * i0, c1);
-          tmem_st8(q_addr + D / 4 + 2 * i0, c2);
-        }
-        tmem_st_wait();
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(sh.q_full[k & 1]));
-      if (M.pass == kMaxima) continue;
-#pragma unroll 1
-      for (int j = 0; j < M.n_blocks; ++j) {
-        issue();
-        if (!(ok = wait_bar(sh.v_empty[sv], pv))) break;
-        const int st = done % kAhead;
-        if (!(ok = wait_bar(sh.code_full[w][st], (done / kAhead) & 1))) break;
-        const uint32_t from = codes + st * kMine, tile = sbase + L::kV + sv * L::kTileBytes;
-        // a lane has a row of each 8 keys and 16 columns of each 64 or 128
-        const int r = lane & 7, c0 = lane >> 3;
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const int group = D == 128 ? i >> 1 : i, c = D == 128 ? c0 + 4 * (i & 1) : c0;
-          const uint32_t at = D == 128 ? (c ^ r) << 4 : (c ^ (r >> 1 & 3)) << 4;
-          uint32_t x[4], y[8];
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                       : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
-                       : "r"(from + (group * 8 + r) * D + at)
-                       : "memory");
-          widen16(x, y);
-          const uint32_t dst = tile + (w * 4 + group) * L::kGroupBytes + (c >> 2) * 1024 + r * 128;
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + ((((c & 3) * 2 + e) ^ r) << 4)),
-                         "r"(y[4 * e]), "r"(y[4 * e + 1]), "r"(y[4 * e + 2]), "r"(y[4 * e + 3])
-                         : "memory");
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(sh.v_full[sv]));
-        ++done;
-        if (++sv == kVStages) {
-          sv = 0;
-          pv ^= 1u;
-        }
-      }
-    }
-    if (!ok && lane == 0) set_abort(sh, p.err);
-    for (int e = max(0, issued - kAhead); e < issued; ++e)
-      mbar_wait(bar(sh.code_full[w][e % kAhead]), (e / kAhead) & 1);
-    }
-  } else if (!kFp8 && warp < kProducers) {
+  } else if (warp < kProducers) {
     // ------------------------------------------------------- producers --
     const bool is_k = warp < 2;
     const int half = warp & 1;
     if (lane == 0) {
-      prefetch_tmap(&tm_q);
+      if (!kFp8) prefetch_tmap(&tm_q);
       prefetch_tmap(is_k ? &tm_k : &tm_v);
       prefetch_tmap(is_k ? &tm_k4 : &tm_v4);
     }
     __syncwarp();
     pdl_wait();
-    uint64_t *const full = is_k ? sh.k_full : sh.v_full, *const empty = is_k ? sh.k_empty : sh.v_empty;
+    uint64_t *const full = is_k ? sh.k_full : kFp8 ? sh.code_full : sh.v_full;
+    uint64_t *const empty = is_k ? sh.k_empty : kFp8 ? sh.code_empty : sh.v_empty;
     const CUtensorMap *const page_map = is_k ? &tm_k : &tm_v, *const run_map = is_k ? &tm_k4 : &tm_v4;
-    const uint32_t ring = sbase + (is_k ? L::kK : L::kV), mine = half * (L::kTileBytes / 2);
+    const uint32_t ring = sbase + (is_k ? L::kK : kFp8 ? L::kCodes : L::kV), mine = half * (L::kKBytes / 2);
     int issued = 0;  // ring entries
     bool ok = true;
     for (int k = 0; ok; ++k) {
@@ -1183,6 +904,16 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
       const int page0 = M.blk_lo * kPagesPerBlock + (lane / kPagesEach) * kPagesPerBlock + half * kPagesEach +
                         lane % kPagesEach;
       int ids = p.num_pages, ids_next = p.num_pages;
+      // (8-bit cache: scales of those pages, eight blocks' at once, four ahead)
+      float ks = 0.f, vs = 0.f, ks_next = 0.f, vs_next = 0.f;
+      auto seen = [&](int j) { return page0 + j * kPagesPerBlock < M.pages; };
+      auto fetch_scales = [&](int j, int id) {
+        ks_next = vs_next = 0.f;
+        if (!seen(j)) return;
+        const size_t at = static_cast<size_t>(static_cast<unsigned>(id) < static_cast<unsigned>(p.num_pages) ? id : 0) * p.H_kv + M.g;
+        ks_next = p.k_scale[at];
+        vs_next = p.v_scale[at];
+      };
       auto look_up = [&](int j) {
         const int i = page0 + j * kPagesPerBlock;
         ids_next = p.num_pages;
@@ -1191,12 +922,12 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
       };
       look_up(0);
 #pragma unroll 1
-      for (int j = is_k ? -1 : 0; j < M.n_blocks; ++j) {
+      for (int j = is_k && !kFp8 ? -1 : 0; j < M.n_blocks; ++j) {
         const int e = issued, s = e % kStages;
         if (e >= kStages && !(ok = wait_bar(empty[s], ((e / kStages) - 1) & 1))) break;
         ++issued;
-        const uint32_t dst = ring + s * L::kTileBytes, b = bar(full[s]);
-        if (j < 0) {  // the unit's Q tile, 64 columns a warp
+        const uint32_t dst = ring + s * L::kKBytes, b = bar(full[s]);
+        if (!kFp8 && j < 0) {  // the unit's Q tile, 64 columns a warp
           if (half < L::kChunks) {
             mbar_arrive_expect_tx_elect(b, TT * G * 128);
             tma_load_3d_elect(dst + half * L::kChunkBytes, &tm_q, b, half * 64, M.g * G, M.tok0);
@@ -1213,16 +944,45 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
             ids = 0;
           }
           look_up(j + kIdBlocks);
+          if (kFp8 && is_k && j == 0) fetch_scales(0, ids);
           __syncwarp();
         }
         const int pg = __shfl_sync(0xffffffffu, ids, (j % kIdBlocks) * kPagesEach + (lane & (kPagesEach - 1)));
-        mbar_arrive_expect_tx_elect(b, L::kTileBytes / 2);
+        mbar_arrive_expect_tx_elect(b, L::kKBytes / 2);
         const int right = __shfl_down_sync(0xffffffffu, pg, 1);
         const unsigned run = __ballot_sync(0xffffffffu, lane < kPagesEach - 1 && right == pg + 1);
         const bool one = p.num_pages >= kPagesEach && (run & 7u) == 7u;
-        if (lane < (one ? 1 : kPagesEach))
-          tma_load_5d(dst + mine + lane * L::kPageBytes, one ? run_map : page_map, b, 0, 0, 0, 2 * pg, M.g);
+        if (lane < (one ? 1 : kPagesEach)) {
+          if constexpr (kFp8)
+            tma_load_3d(dst + mine + lane * (kPage * D), one ? run_map : page_map, b, 0, M.g, kPage * pg);
+          else
+            tma_load_5d(dst + mine + lane * L::kPageBytes, one ? run_map : page_map, b, 0, 0, 0, 2 * pg, M.g);
+        }
         __syncwarp();
+        if (kFp8 && is_k) {
+          const int at = j % kIdBlocks;
+          if (at == 0) {
+            ks = ks_next;
+            vs = vs_next;
+            const float INF = __int_as_float(0x7f800000);
+            if (!(ks >= 0.f && ks < INF && vs >= 0.f && vs < INF)) {
+              flag_error(p.err, HPD_DEVERR_SCALE);
+              if (!(ks >= 0.f && ks < INF)) ks = 0.f;
+              if (!(vs >= 0.f && vs < INF)) vs = 0.f;
+            }
+          } else if (at == kIdBlocks / 2) {
+            fetch_scales(j - at + kIdBlocks, ids_next);
+          }
+          __syncwarp();
+          const int from = at * kPagesEach + (lane & (kPagesEach - 1));
+          const float k1 = __shfl_sync(0xffffffffu, ks, from), v1 = __shfl_sync(0xffffffffu, vs, from);
+          if (lane < kPagesEach) {
+            sh.scales[e % kScaleBlocks][half * kPagesEach + lane] = k1;
+            sh.scales[e % kScaleBlocks][kPagesPerBlock + half * kPagesEach + lane] = v1;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b);
+        }
       }
     }
     if (!ok && lane == 0) set_abort(sh, p.err);
@@ -1294,7 +1054,7 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
     if (!ok && lane == 0) set_abort(sh, p.err);
   } else if (warp == kPvWarp) {
     // ------------------------------------------------------ P V issuer --
-    constexpr uint32_t idesc_pv = idesc_bf16_f32(kRows, D, true);
+    constexpr uint32_t idesc_bf16 = idesc_bf16_f32(kRows, D, true), idesc_f16 = idesc_f16_f32(kRows, D, true);
     const uint64_t dv0 = smem_desc_sw128(sbase + L::kV, 1024, L::kGroupBytes);
     const bool issuer = elect_one();
     pdl_wait();
@@ -1307,6 +1067,7 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
       if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
       const bool valid = sh.meta[slot].valid != 0;
       const int pass = sh.meta[slot].pass;
+      const uint32_t idesc_pv = kFp8 && pass != kAgain ? idesc_f16 : idesc_bf16;
       const int nb = sh.meta[slot].n_blocks, len = sh.meta[slot].L;
       // the block with rows behind the sequence's end in its last page
       const int j_tail = len % kPage ? len / kBlk - sh.meta[slot].blk_lo : -1;
@@ -1394,6 +1155,125 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
       if (pass == kAgain) publish_seq(&sh.sieved_seq, k + 1);
     }
     if (!ok && lane == 0) set_abort(sh, p.err);
+  } else if (kFp8 && warp >= kWideWarp) {
+    if constexpr (kFp8) {
+      // -------------------------------------------- Q parts, V to f16 --
+      const int quad = warp & 3;  // its 32 rows of a tile, its 32 keys of a block
+      constexpr int kCodeStages = Rings<true>::kCodeStages;
+      pdl_wait();
+      int e = 0;                // blocks widened
+      uint32_t sv = 0, pv = 1;  // V ring: stage, phase of its being free
+      bool ok = true;
+      for (int k = 0; ok; ++k) {
+        const int slot = k % kMetaSlots;
+        if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
+        const UnitMeta M = read_meta(sh.meta[slot]);
+        __syncwarp();
+        if (!M.valid) break;
+        if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
+        // Q, a row a thread: q 2^t = q1 + q2 with the row's largest value from 2^7 to 2^8.
+        // q1 has four of bf16's eight bits, and what is left of them fits into q2, but for
+        // values below 2^-9 of the largest, which keep 2^-17 of that.
+        if (k >= 2 && !(ok = wait_bar(sh.q_free[k & 1], ((k >> 1) - 1) & 1))) break;
+        tc_fence_after();
+        const int r_in = quad * 32 + lane;
+        if (quad * 32 < M.nrows) {
+          const int rt = p.div_G(r_in);
+          const bool valid = r_in < M.nrows;
+          const uint4 *const src = reinterpret_cast<const uint4 *>(
+              p.q + (valid ? (M.tok0 + rt) * p.q_stride + (M.g * G + r_in - rt * G) * D : 0));
+          unsigned most = 0u;
+          {
+            uint4 x[D / 8];
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) x[i] = valid ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+              most = __vmaxu2(__vmaxu2(most, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu)),
+                              __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
+          }
+          most = max(most & 0xffffu, most >> 16);
+          const int t = min(134 - static_cast<int>(most >> 7), 126);
+          const float up = __uint_as_float(static_cast<uint32_t>(127 + t) << 23);
+          sh.q_scale[slot][r_in] =
+              most >= 0x7f80u ? __int_as_float(0x7fffffff) : __uint_as_float(static_cast<uint32_t>(127 - t) << 23);
+          const uint32_t q_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::col_q(k & 1);
+#pragma unroll 1
+          for (int i0 = 0; i0 < D / 8; i0 += 4) {  // 32 columns at a time, from L1 this time
+            uint32_t c1[8], c2[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint4 y = valid ? src[i0 + i] : make_uint4(0u, 0u, 0u, 0u);
+              const uint32_t ab[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const uint32_t a = ab[2 * e], b = ab[2 * e + 1];
+                const float q0 = __uint_as_float(a << 16) * up, q1 = __uint_as_float(a & 0xffff0000u) * up;
+                const float q2 = __uint_as_float(b << 16) * up, q3 = __uint_as_float(b & 0xffff0000u) * up;
+                const uint32_t lo = to_codes(q0, q1), hi = to_codes(q2, q3);
+                c1[2 * i + e] = lo | hi << 16;
+                const float2 f = of_codes(lo), g = of_codes(hi);
+                c2[2 * i + e] = to_codes4(q0 - f.x, q1 - f.y, q2 - g.x, q3 - g.y);
+              }
+            }
+            tmem_st8(q_addr + 2 * i0, c1);
+            tmem_st8(q_addr + D / 4 + 2 * i0, c2);
+          }
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(sh.q_full[k & 1]));
+        if (M.pass == kMaxima) continue;
+#pragma unroll 1
+        for (int j = 0; j < M.n_blocks; ++j, ++e) {
+          const int st = e % kCodeStages;
+          if (!(ok = wait_bar(sh.code_full[st], (e / kCodeStages) & 1))) break;
+          const uint32_t from = sbase + L::kCodes + st * L::kCodeBytes + quad * 32 * D;
+          // a lane has a row of each 8 keys and 16 columns of each 64: reads and writes of
+          // eight lanes are of eight rows, whose swizzles differ
+          const int r = lane & 7, c0 = lane >> 3;
+          uint32_t x[D / 16][4];
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            const int group = D == 128 ? i >> 1 : i, c = D == 128 ? c0 + 4 * (i & 1) : c0;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(x[i][0]), "=r"(x[i][1]), "=r"(x[i][2]), "=r"(x[i][3])
+                         : "r"(from + (group * 8 + r) * D + ((D == 128 ? c ^ r : c ^ (r >> 1 & 3)) << 4)));
+          }
+          if (!(ok = wait_bar(sh.v_empty[sv], pv))) break;
+          const uint32_t to = sbase + L::kV + sv * L::kTileBytes + quad * 4 * L::kGroupBytes + r * 128;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            const int group = D == 128 ? i >> 1 : i, half = D == 128 ? i & 1 : 0;
+            uint32_t y[8];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) y[n] = f16_of_codes((n & 1) ? x[i][n >> 1] >> 16 : x[i][n >> 1] & 0xffffu);
+            if (M.pass == kAgain) {
+#pragma unroll
+              for (int n = 0; n < 8; ++n) y[n] = bf16_of_f16(y[n]);
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + group * L::kGroupBytes + half * 1024 +
+                                                                           (((c0 * 2 + n) ^ r) << 4)),
+                           "r"(y[4 * n]), "r"(y[4 * n + 1]), "r"(y[4 * n + 2]), "r"(y[4 * n + 3])
+                           : "memory");
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bar(sh.v_full[sv]));
+            mbar_arrive(bar(sh.code_empty[st]));
+          }
+          if (++sv == kVStages) {
+            sv = 0;
+            pv ^= 1u;
+          }
+        }
+      }
+      if (!ok && lane == 0) set_abort(sh, p.err);
+    }
   } else if (warp >= kOutputWarp) {
     // ---------------------------------------------------------- output --
     const int quad = warp & 3;          // TMEM lane quadrant this warp may access
@@ -1422,7 +1302,7 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
         const float lse = l == 0.f ? NEG_INF : l > 0.f ? lse_of(sh.xbase[slot][r_in], l) : l;
         if (part) p.l_part[part_row] = lse;
         else if (p.lse) p.lse[pair] = lse;
-        inv = l == 0.f ? 0.f : __fdividef(1.f, l);  // (a sum that is NaN stays one; others are below 2^126)
+        inv = l == 0.f ? 0.f : __fdividef(kFp8 ? sh.v_ref[slot][r_in] : 1.f, l);  // (a sum that is NaN stays one; others are below 2^126)
         odd = l != l;
       }
       __syncwarp();
@@ -1561,7 +1441,7 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(sh.p_full[jg & 1][part]));
       };
-      float row_mul = sl2;
+      float row_mul = sl2, val_mul = 1.f, v_ref = 1.f;
       if constexpr (kFp8) {  // (the factor of the row's parts is there with its first scores)
         if (!idle) {
           if (!(ok = await_s())) break;
@@ -1590,10 +1470,12 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
           if (!(kFp8 && j == 0) && !(ok = await_s())) break;
           const int hi = min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64;
           const uint32_t at = t_lane + L::col_s(jg & 1) + h * 64;
-          if constexpr (kFp8)
-            mx_run = fmaxf(mx_run, row_max_fp8(at, 32, j < n_plain, hi, row_mul, sh.scales[jg % kScaleBlocks] + 4 * h));
-          else
+          if constexpr (kFp8) {
+            const float *const sc = sh.scales[jg % kScaleBlocks];
+            mx_run = fmaxf(mx_run, row_max_fp8(at, 32, j < n_plain, hi, row_mul, sc + 4 * h));
+          } else {
             mx_run = fmaxf(mx_run, row_max(at, 32, j < n_plain, hi, sl2));
+          }
           publish(0);
           publish(1);
         }
@@ -1602,18 +1484,29 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
         if (pass == kFirst) {
           const uint32_t at = t_lane + L::col_s(jg & 1);
           const int hi = min(lim - blk_lo * kBlk, kBlk);
-          if constexpr (kFp8) m_run = row_max_fp8(at, 64, n_plain > 0, hi, row_mul, sh.scales[jg % kScaleBlocks]);
-          else m_run = row_max(at, 64, n_plain > 0, hi, sl2);
+          if constexpr (kFp8) {
+            const float *const sc = sh.scales[jg % kScaleBlocks];
+            m_run = row_max_fp8(at, 64, n_plain > 0, hi, row_mul, sc) - kFirstLog2;
+            v_ref = ref_of(largest_scale(sc + kPagesPerBlock, hi));
+          } else {
+            m_run = row_max(at, 64, n_plain > 0, hi, sl2);
+          }
+        }
+        if constexpr (kFp8) {
+          val_mul = over_ref(v_ref);
+          if (h == 0) sh.v_ref[slot][r_in] = v_ref;
         }
         // (scores of -inf alone give no base to a row that sees the unit's keys)
         inside = pass != kFirst || m_run > NEG_INF || lim <= blk_lo * kBlk;
         // blocks that every row of the warp sees all of: nothing to decide
-        for (; j < n_plain; ++j, ++jg) {
+        for (; j < (kFp8 && pass == kAgain ? 0 : n_plain); ++j, ++jg) {
           if (j > 0 && !(ok = await_s())) break;
           const uint32_t at = t_lane + L::col_s(jg & 1) + h * 64;
           const float *const sc = sh.scales[jg % kScaleBlocks] + 4 * h;
-          if constexpr (kFp8) inside &= softmax_plain_fp8(at, row_mul, sc, sc + kPagesPerBlock, m_run, l4, publish);
-          else inside &= softmax_plain(at, sl2, m_run, l4, publish);
+          if constexpr (kFp8)
+            inside &= softmax_plain_fp8(at, row_mul, val_mul, sc, sc + kPagesPerBlock, m_run == NEG_INF ? 0.f : m_run, l4, publish);
+          else
+            inside &= softmax_plain(at, sl2, m_run, l4, publish);
         }
         if (!ok) break;
         for (; j < nb; ++j, ++jg) {
@@ -1621,8 +1514,13 @@ __global__ void __launch_bounds__(Roles<kFp8>::kThreads, 1)
           const int hi = min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64;
           const uint32_t at = t_lane + L::col_s(jg & 1) + h * 64;
           const float *const sc = sh.scales[jg % kScaleBlocks] + 4 * h;
-          if constexpr (kFp8) inside &= softmax_masked_fp8(at, hi, row_mul, sc, sc + kPagesPerBlock, m_run, l4, publish);
-          else inside &= softmax_masked(at, hi, sl2, m_run, l4, publish);
+          if constexpr (kFp8)
+            inside &= pass == kAgain ? softmax_masked_fp8<true>(at, hi, row_mul, 1.f, sc, sc + kPagesPerBlock,
+                                                                m_run == NEG_INF ? 0.f : m_run, l4, publish)
+                                     : softmax_masked_fp8<false>(at, hi, row_mul, val_mul, sc, sc + kPagesPerBlock,
+                                                                 m_run == NEG_INF ? 0.f : m_run, l4, publish);
+          else
+            inside &= softmax_masked(at, hi, sl2, m_run, l4, publish);
         }
       }
       if (!ok) break;
@@ -1846,7 +1744,7 @@ cudaError_t launch(const ChunkParams &p, long long units, cudaStream_t s) {
     e = make_code_map(&tk, p.k_cache, D, p.H_kv, p.num_pages, 1);
     if (e == cudaSuccess) e = make_code_map(&tk4, p.k_cache, D, p.H_kv, p.num_pages, run);
     if (e == cudaSuccess) e = make_code_map(&tv, p.v_cache, D, p.H_kv, p.num_pages, 1);
-    if (e == cudaSuccess) e = make_code_map(&tv4, p.v_cache, D, p.H_kv, p.num_pages, std::min(2, p.num_pages));
+    if (e == cudaSuccess) e = make_code_map(&tv4, p.v_cache, D, p.H_kv, p.num_pages, run);
     tq = tk;  // (not used)
   } else {
     e = make_q_map(&tq, p, D);
@@ -1872,7 +1770,7 @@ cudaError_t launch(const ChunkParams &p, long long units, cudaStream_t s) {
     configured.fetch_or(bit, std::memory_order_acq_rel);
   }
   const unsigned grid = static_cast<unsigned>(std::min<long long>(units, sms[dev & 63].load()));
-  e = launch_kernel(true, chunk_attn_kernel<D, kFp8>, dim3(grid), dim3(Roles<kFp8>::kThreads), L::kDynSmem, s, tk, tk4,
+  e = launch_kernel(true, chunk_attn_kernel<D, kFp8>, dim3(grid), dim3(kThreads<kFp8>), L::kDynSmem, s, tk, tk4,
                     tv, tv4, tq, p);
   if (e != cudaSuccess || p.slots == 0) return e;
   return launch_kernel(true, chunk_merge_kernel<D>, dim3(p.slots), dim3(32 * kMergeWarps), 0, s, p);
