@@ -1210,9 +1210,9 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
                 const uint32_t a = ab[2 * e], b = ab[2 * e + 1];
                 const float q0 = __uint_as_float(a << 16) * up, q1 = __uint_as_float(a & 0xffff0000u) * up;
                 const float q2 = __uint_as_float(b << 16) * up, q3 = __uint_as_float(b & 0xffff0000u) * up;
-                const uint32_t lo = to_codes(q0, q1), hi = to_codes(q2, q3);
-                c1[2 * i + e] = lo | hi << 16;
-                const float2 f = of_codes(lo), g = of_codes(hi);
+                c1[2 * i + e] = to_codes4(q0, q1, q2, q3);
+                float2 f, g;
+                of_codes4(c1[2 * i + e], f, g);
                 c2[2 * i + e] = to_codes4(q0 - f.x, q1 - f.y, q2 - g.x, q3 - g.y);
               }
             }
@@ -1248,7 +1248,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
             const int group = D == 128 ? i >> 1 : i, half = D == 128 ? i & 1 : 0;
             uint32_t y[8];
 #pragma unroll
-            for (int n = 0; n < 8; ++n) y[n] = f16_of_codes((n & 1) ? x[i][n >> 1] >> 16 : x[i][n >> 1] & 0xffffu);
+            for (int n = 0; n < 4; ++n) f16_of_codes(x[i][n], y[2 * n], y[2 * n + 1]);
             if (M.pass == kAgain) {
 #pragma unroll
               for (int n = 0; n < 8; ++n) y[n] = bf16_of_f16(y[n]);

@@ -148,7 +148,8 @@ __global__ void __launch_bounds__(32 * kWarps) put_codes_kernel(const PutArgs a)
         uint32_t *const w = reinterpret_cast<uint32_t *>(&v);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const float2 lo = of_codes(w[c] & 0xffffu), hi = of_codes(w[c] >> 16);
+          float2 lo, hi;
+          of_codes4(w[c], lo, hi);
           w[c] = to_codes4(lo.x * shrink, lo.y * shrink, hi.x * shrink, hi.y * shrink);
         }
         *p = v;
