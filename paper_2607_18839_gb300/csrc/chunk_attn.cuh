@@ -99,6 +99,7 @@ constexpr int kSoftmaxWarp = 8, kSoftmaxWarps = 8;
 constexpr int kOutputWarp = kSoftmaxWarp + kSoftmaxWarps, kOutputWarps = 4;
 constexpr int kProducers = 4;  // warps 0, 1: K; 2, 3: V
 constexpr int kQkWarp = 4, kPvWarp = 5, kSchedWarp = 6;
+constexpr int kScaleWarp = 7;  // 8-bit cache: the pages' scales
 constexpr int kWideWarp = kOutputWarp + kOutputWarps, kWideWarps = 4;  // 8-bit cache: Q parts, V to f16
 template <bool kFp8>
 constexpr int kThreads = 32 * (kWideWarp + (kFp8 ? kWideWarps : 0));
@@ -108,7 +109,7 @@ enum Pass { kFirst, kMaxima, kAgain };
 constexpr int kMetaSlots = 3;
 // of a metadata slot: producers, two MMA issuers, softmax and output warps
 template <bool kFp8>
-constexpr uint32_t kMetaConsumers = kProducers + 2 + kSoftmaxWarps + kOutputWarps + (kFp8 ? kWideWarps : 0);
+constexpr uint32_t kMetaConsumers = kProducers + 2 + kSoftmaxWarps + kOutputWarps + (kFp8 ? 1 + kWideWarps : 0);
 template <bool kFp8>
 struct Rings {
   static constexpr int kStages = 3, kVStages = 3;  // of K and V
@@ -549,6 +550,32 @@ __device__ __forceinline__ bool softmax_masked_fp8(uint32_t s_addr, int hi, floa
   return kBf16 || fits;
 }
 
+// 32 keys' codes at `from` as bf16 at `to`, both as the blocks hold them (of a unit that is
+// run again; out of line, as what is not in the blocks' loops is).
+template <int D>
+__device__ __noinline__ void widen_again(uint32_t from, uint32_t to) {
+  using L = Layout<D, true>;
+  const int lane = threadIdx.x & 31, r = lane & 7, c0 = lane >> 3;
+#pragma unroll 1
+  for (int i = 0; i < D / 16; ++i) {
+    const int group = D == 128 ? i >> 1 : i, h = D == 128 ? i & 1 : 0;
+    uint32_t x[4], y[8];
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                 : "r"(from + (group * 8 + r) * D + ((D == 128 ? (c0 + 4 * h) ^ r : c0 ^ (r >> 1 & 3)) << 4)));
+#pragma unroll
+    for (int n = 0; n < 4; ++n) f16_of_codes(x[n], y[2 * n], y[2 * n + 1]);
+#pragma unroll
+    for (int n = 0; n < 8; ++n) y[n] = bf16_of_f16(y[n]);
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + group * L::kGroupBytes + h * 1024 + r * 128 +
+                                                                   (((c0 * 2 + n) ^ r) << 4)),
+                   "r"(y[4 * n]), "r"(y[4 * n + 1]), "r"(y[4 * n + 2]), "r"(y[4 * n + 3])
+                   : "memory");
+  }
+}
+
 template <int D, bool kFp8>
 __global__ void __launch_bounds__(kThreads<kFp8>, 1)
     chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_k4,
@@ -577,7 +604,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
     sh.units_done = 0;
     sh.sieved_seq = 0;
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(bar(sh.k_full[s]), kFp8 ? 4 : 2);
+      mbar_init(bar(sh.k_full[s]), kFp8 ? 3 : 2);
       mbar_init(bar(sh.k_empty[s]), 1);
     }
     for (int s = 0; s < kVStages; ++s) {
@@ -904,16 +931,6 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
       const int page0 = M.blk_lo * kPagesPerBlock + (lane / kPagesEach) * kPagesPerBlock + half * kPagesEach +
                         lane % kPagesEach;
       int ids = p.num_pages, ids_next = p.num_pages;
-      // (8-bit cache: scales of those pages, eight blocks' at once, four ahead)
-      float ks = 0.f, vs = 0.f, ks_next = 0.f, vs_next = 0.f;
-      auto seen = [&](int j) { return page0 + j * kPagesPerBlock < M.pages; };
-      auto fetch_scales = [&](int j, int id) {
-        ks_next = vs_next = 0.f;
-        if (!seen(j)) return;
-        const size_t at = static_cast<size_t>(static_cast<unsigned>(id) < static_cast<unsigned>(p.num_pages) ? id : 0) * p.H_kv + M.g;
-        ks_next = p.k_scale[at];
-        vs_next = p.v_scale[at];
-      };
       auto look_up = [&](int j) {
         const int i = page0 + j * kPagesPerBlock;
         ids_next = p.num_pages;
@@ -944,7 +961,6 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
             ids = 0;
           }
           look_up(j + kIdBlocks);
-          if (kFp8 && is_k && j == 0) fetch_scales(0, ids);
           __syncwarp();
         }
         const int pg = __shfl_sync(0xffffffffu, ids, (j % kIdBlocks) * kPagesEach + (lane & (kPagesEach - 1)));
@@ -959,36 +975,75 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
             tma_load_5d(dst + mine + lane * L::kPageBytes, one ? run_map : page_map, b, 0, 0, 0, 2 * pg, M.g);
         }
         __syncwarp();
-        if (kFp8 && is_k) {
-          const int at = j % kIdBlocks;
-          if (at == 0) {
-            ks = ks_next;
-            vs = vs_next;
-            const float INF = __int_as_float(0x7f800000);
-            if (!(ks >= 0.f && ks < INF && vs >= 0.f && vs < INF)) {
-              flag_error(p.err, HPD_DEVERR_SCALE);
-              if (!(ks >= 0.f && ks < INF)) ks = 0.f;
-              if (!(vs >= 0.f && vs < INF)) vs = 0.f;
-            }
-          } else if (at == kIdBlocks / 2) {
-            fetch_scales(j - at + kIdBlocks, ids_next);
-          }
-          __syncwarp();
-          const int from = at * kPagesEach + (lane & (kPagesEach - 1));
-          const float k1 = __shfl_sync(0xffffffffu, ks, from), v1 = __shfl_sync(0xffffffffu, vs, from);
-          if (lane < kPagesEach) {
-            sh.scales[e % kScaleBlocks][half * kPagesEach + lane] = k1;
-            sh.scales[e % kScaleBlocks][kPagesPerBlock + half * kPagesEach + lane] = v1;
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(b);
-        }
       }
     }
     if (!ok && lane == 0) set_abort(sh, p.err);
     // no exit while a copy into this CTA's shared memory is in flight
     for (int e = max(0, issued - kStages); e < issued; ++e)
       mbar_wait(bar(full[e % kStages]), (e / kStages) & 1);
+  } else if (kFp8 && warp == kScaleWarp) {
+    if constexpr (kFp8) {
+      // ---------------------------------------------------------- scales --
+      // A lane has a page of four blocks at once: its id is looked up eight blocks ahead
+      // of their use, its scales four.
+      pdl_wait();
+      const float INF = __int_as_float(0x7f800000);
+      constexpr int kAtOnce = 32 / kPagesPerBlock;
+      int e = 0;  // blocks in all
+      bool ok = true;
+      for (int k = 0; ok; ++k) {
+        const int slot = k % kMetaSlots;
+        if (!(ok = wait_bar(sh.meta_full[slot], (k / kMetaSlots) & 1))) break;
+        const UnitMeta M = read_meta(sh.meta[slot]);
+        __syncwarp();
+        if (!M.valid) break;
+        if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
+        const int32_t *const row = p.page_table + static_cast<size_t>(M.seq) * p.max_pages;
+        int at = M.blk_lo * kPagesPerBlock + lane;  // the page whose id is looked up next
+        auto look_up = [&] {  // (one of no block: any page's scales, as 0)
+          const int id = at < M.pages ? row[at] : 0;
+          at += 32;
+          return id;
+        };
+        float ks = 0.f, vs = 0.f;
+        auto fetch = [&](int id, int of) {
+          ks = vs = 0.f;
+          if (of >= M.pages) return;
+          const size_t i = static_cast<size_t>(static_cast<unsigned>(id) < static_cast<unsigned>(p.num_pages) ? id : 0) * p.H_kv + M.g;
+          ks = p.k_scale[i];
+          vs = p.v_scale[i];
+        };
+        const int first = look_up();
+        int id = look_up();
+        fetch(first, at - 64);
+#pragma unroll 1
+        for (int j = 0; j < M.n_blocks; j += kAtOnce) {
+          float k1 = ks, v1 = vs;
+          if (j + kAtOnce < M.n_blocks) {
+            fetch(id, at - 32);
+            id = look_up();
+          }
+          if (!(k1 >= 0.f && k1 < INF && v1 >= 0.f && v1 < INF)) {
+            flag_error(p.err, HPD_DEVERR_SCALE);
+            if (!(k1 >= 0.f && k1 < INF)) k1 = 0.f;
+            if (!(v1 >= 0.f && v1 < INF)) v1 = 0.f;
+          }
+          __syncwarp();
+#pragma unroll 1
+          for (int i = 0; i < min(kAtOnce, M.n_blocks - j); ++i, ++e) {
+            if (e >= kStages && !(ok = wait_bar(sh.k_empty[e % kStages], ((e / kStages) - 1) & 1))) break;
+            if (lane / kPagesPerBlock == i) {
+              sh.scales[e % kScaleBlocks][lane % kPagesPerBlock] = k1;
+              sh.scales[e % kScaleBlocks][kPagesPerBlock + lane % kPagesPerBlock] = v1;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.k_full[e % kStages]));
+          }
+          if (!ok) break;
+        }
+      }
+      if (!ok && lane == 0) set_abort(sh, p.err);
+    }
   } else if (warp == kQkWarp) {
     // ---------------------------------------------------- Q K^T issuer --
     // The MMA warps run their loops with warp-uniform values; one elected lane
@@ -1233,32 +1288,41 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           // a lane has a row of each 8 keys and 16 columns of each 64: reads and writes of
           // eight lanes are of eight rows, whose swizzles differ
           const int r = lane & 7, c0 = lane >> 3;
-          uint32_t x[D / 16][4];
+          // (the next keys' codes are read before these are written: a block's codes at once
+          // would hold 32 registers)
+          constexpr int kPieces = D / 64;
+          uint32_t x[kPieces][4];
+          const uint32_t src = from + r * D + ((D == 128 ? c0 ^ r : c0 ^ (r >> 1 & 3)) << 4);
+          auto read = [&](int group) {
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            const int group = D == 128 ? i >> 1 : i, c = D == 128 ? c0 + 4 * (i & 1) : c0;
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(x[i][0]), "=r"(x[i][1]), "=r"(x[i][2]), "=r"(x[i][3])
-                         : "r"(from + (group * 8 + r) * D + ((D == 128 ? c ^ r : c ^ (r >> 1 & 3)) << 4)));
-          }
+            for (int h = 0; h < kPieces; ++h)
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                           : "=r"(x[h][0]), "=r"(x[h][1]), "=r"(x[h][2]), "=r"(x[h][3])
+                           : "r"((src ^ h << 6) + group * 8 * D));
+          };
+          read(0);
           if (!(ok = wait_bar(sh.v_empty[sv], pv))) break;
+          if (M.pass == kAgain) {
+            widen_again<D>(from, sbase + L::kV + sv * L::kTileBytes + quad * 4 * L::kGroupBytes);
+          } else {
           const uint32_t to = sbase + L::kV + sv * L::kTileBytes + quad * 4 * L::kGroupBytes + r * 128;
+          const uint32_t to0 = to + ((c0 * 2 ^ r) << 4), to1 = to + (((c0 * 2 + 1) ^ r) << 4);
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            const int group = D == 128 ? i >> 1 : i, half = D == 128 ? i & 1 : 0;
-            uint32_t y[8];
+          for (int group = 0; group < 4; ++group) {
+            uint32_t y[kPieces][8];
 #pragma unroll
-            for (int n = 0; n < 4; ++n) f16_of_codes(x[i][n], y[2 * n], y[2 * n + 1]);
-            if (M.pass == kAgain) {
+            for (int h = 0; h < kPieces; ++h)
 #pragma unroll
-              for (int n = 0; n < 8; ++n) y[n] = bf16_of_f16(y[n]);
-            }
+              for (int n = 0; n < 4; ++n) f16_of_codes(x[h][n], y[h][2 * n], y[h][2 * n + 1]);
+            if (group < 3) read(group + 1);
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + group * L::kGroupBytes + half * 1024 +
-                                                                           (((c0 * 2 + n) ^ r) << 4)),
-                           "r"(y[4 * n]), "r"(y[4 * n + 1]), "r"(y[4 * n + 2]), "r"(y[4 * n + 3])
-                           : "memory");
+            for (int h = 0; h < kPieces; ++h)
+#pragma unroll
+              for (int n = 0; n < 2; ++n)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((n ? to1 : to0) + group * L::kGroupBytes + h * 1024),
+                             "r"(y[h][4 * n]), "r"(y[h][4 * n + 1]), "r"(y[h][4 * n + 2]), "r"(y[h][4 * n + 3])
+                             : "memory");
+          }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
