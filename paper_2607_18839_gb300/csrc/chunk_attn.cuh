@@ -231,6 +231,7 @@ struct __align__(16) Shared {
   float __align__(16) scales[kScaleBlocks][2 * kPagesPerBlock];
   // the scheduler's group of sequences: units before each, first rows, rows, lengths,
   // keys that all their rows see, tiles left whole, splits of the others
+  uint8_t g_order[kGroup];  // (8-bit cache) sequences in the order of their units
   int g_units[kGroup], g_cu[kGroup], g_n[kGroup], g_len[kGroup], g_full[kGroup], g_whole[kGroup], g_split[kGroup];
 };
 
@@ -669,6 +670,8 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
     pdl_trigger();  // the merge of the splits may launch; it waits for this grid
     int fetched = 0;  // group whose first lengths are on their way
     fetch(lane);
+    bool sorted = false;
+    auto seq_at = [&](int i) { return kFp8 && sorted ? sh.g_order[i] : i; };
     auto load_group = [&](int s0, int units_before) {
       g0 = s0;
       before = units_before;
@@ -690,6 +693,30 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         sh.g_len[i] = Ls;
         sh.g_full[i] = min(max(b_full, 0), Ls);
       }
+      if constexpr (kFp8) {
+        // Longest sequences first, by eighths of the longest, where there is more than a unit
+        // an SM: a long one begun late has the others wait.
+        sorted = p.units > static_cast<int>(gridDim.x);
+        if (sorted) {
+          __syncwarp();
+          int most = 0;
+#pragma unroll 1
+          for (int i = lane; i < count; i += 32) most = max(most, sh.g_len[i]);
+          const float eighths = 8.f / (__reduce_max_sync(0xffffffffu, most) + 1);
+          int placed = 0;
+#pragma unroll 1
+          for (int c = 7; c >= 0; --c) {
+#pragma unroll 1
+            for (int i = lane; i - lane < count; i += 32) {
+              const bool here = i < count && min(static_cast<int>(sh.g_len[i] * eighths), 7) == c;
+              const unsigned all = __ballot_sync(0xffffffffu, here);
+              if (here) sh.g_order[placed + __popc(all & ((1u << lane) - 1u))] = static_cast<uint8_t>(i);
+              placed += __popc(all);
+            }
+          }
+          __syncwarp();
+        }
+      }
       // (sums that stop at kNoUnit, which offsets out of order could pass)
       auto add = [](int a, int b) { return min(a + b, kNoUnit); };
       // exclusive prefix of x over the lanes, from base, which it adds their sum to
@@ -704,7 +731,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         base = add(base, __shfl_sync(0xffffffffu, incl, 31));
         return r;
       };
-      auto tiles_of = [&](int i) { return i < count ? p.div_tile(sh.g_n[i] + TT - 1) : 0; };
+      auto tiles_of = [&](int i) { return i < count ? p.div_tile(sh.g_n[seq_at(i)] + TT - 1) : 0; };
       int whole = kNoUnit, per = 1 << 30;  // tiles left whole; blocks of a split of the others
       int tiles = 0;
       if (p.slots > 0) {
@@ -727,7 +754,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
 #pragma unroll 1
         for (int i = lane; i < count; i += 32) {
           const int n = tiles_of(i);
-          blocks += static_cast<float>(n - whole_of(i, n)) * ceil_div_i(sh.g_len[i], kBlk) * p.H_kv;
+          blocks += static_cast<float>(n - whole_of(i, n)) * ceil_div_i(sh.g_len[seq_at(i)], kBlk) * p.H_kv;
         }
         __syncwarp();
 #pragma unroll 1
@@ -748,7 +775,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
 #pragma unroll 1
         for (int i = lane; i - lane < count; i += 32) {
           const int n = tiles_of(i), w = i < count ? whole_of(i, n) : 0;
-          const int f = n > w ? min(max(ceil_div_i(sh.g_len[i], kBlk) / per, 1), kMaxSplits) : 1;
+          const int f = n > w ? min(max(ceil_div_i(sh.g_len[seq_at(i)], kBlk) / per, 1), kMaxSplits) : 1;
           const int first = scan(min((w + (n - w) * f) * p.H_kv, kNoUnit), units);
           if (i < count) {
             sh.g_units[i] = first;
@@ -833,7 +860,8 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           const int mid = (lo + hi) >> 1;
           if (sh.g_units[mid] <= u - before) lo = mid; else hi = mid;
         }
-        const int c0 = sh.g_cu[lo], n = sh.g_n[lo], len = sh.g_len[lo], full = sh.g_full[lo];
+        const int seq = seq_at(lo);
+        const int c0 = sh.g_cu[seq], n = sh.g_n[seq], len = sh.g_len[seq], full = sh.g_full[seq];
         const int w = sh.g_whole[lo], f = sh.g_split[lo];
         const int idx = u - before - sh.g_units[lo], us = p.div_Hkv(idx), g = idx - us * p.H_kv;
         const int nsplit = us < w ? 1 : f, ut = us < w || f == 1 ? us : w + (us - w) / f;
@@ -870,7 +898,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           M.split = split;
           M.nsplit = nsplit;
           M.slot = slot_id;
-          M.seq = g0 + lo;
+          M.seq = g0 + seq;
           M.tok0 = c0 + i0;
           M.nrows = nrows;
           M.lim0 = lim0;
