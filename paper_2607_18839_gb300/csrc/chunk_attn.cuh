@@ -121,6 +121,7 @@ struct Rings<true> {
 };
 constexpr int kMaxStages = 4;
 constexpr int kScaleBlocks = 8;  // blocks whose scales are held
+constexpr int kCopies = 4;       // of the rows of a tile of a quarter of its 128 at most
 // 8-bit cache, a first pass, whose weights are f16: log2 of the weight of a row's base
 // (weights up to 2^12 above it fit, 2^-29 of it is not lost), and the least scale of V,
 // over that of its first block, at which none of 2^-4 and more loses digits.
@@ -172,7 +173,7 @@ struct __align__(16) UnitMeta {
   int pages;     // pages up to the last key that the tile sees
   int split, nsplit;
   int slot;      // where a split tile's unit leaves its result
-  int pad;
+  int copies;    // of the tile's rows among the 128: 1, or kCopies (8-bit cache, few rows)
 };
 __device__ __forceinline__ UnitMeta read_meta(const UnitMeta &m) {
   UnitMeta r;
@@ -227,6 +228,7 @@ struct __align__(16) Shared {
   // 8-bit cache: codes of V landed and widened; Q parts written and done with; a row's
   // factor of its parts; scales of a block's pages, of K and then of V
   uint64_t code_full[kMaxStages], code_empty[kMaxStages], q_full[2], q_free[2];
+  uint64_t copied;  // the output warps are done with a piece of the copies' sums
   float q_scale[kMetaSlots][kRows], v_ref[kMetaSlots][kRows];  // (v_ref: what O is in units of)
   float __align__(16) scales[kScaleBlocks][2 * kPagesPerBlock];
   // the scheduler's group of sequences: units before each, first rows, rows, lengths,
@@ -551,6 +553,42 @@ __device__ __forceinline__ bool softmax_masked_fp8(uint32_t s_addr, int hi, floa
   return kBf16 || fits;
 }
 
+// The same of a row that the tile has kCopies times: a copy takes one of the half's pages
+// and leaves weights of 0 for the others.  (A thread's 64 columns bound the blocks of tiles
+// of few rows, where most softmax threads had no row.)
+template <class Publish>
+__device__ __forceinline__ bool softmax_share_fp8(uint32_t s_addr, int copy, int hi, float row_mul, float val_mul,
+                                                  const float *ks, const float *vs, float base, float2 *l4,
+                                                  Publish publish) {
+  static_assert(kCopies * kPage == kBlk / 2, "a page each");
+  const float NEG_INF = -__int_as_float(0x7f800000);
+  uint32_t v[16], pk[8];
+  tmem_ld16(s_addr + copy * kPage, v);
+  const float mul = row_mul * ks[copy], scale = vs[copy], val = val_mul * scale;
+  const int seen = hi - copy * kPage;
+  const float2 mul2 = make_float2(mul, mul), nbase2 = make_float2(-base, -base);
+  tmem_ld_wait16(v);
+#pragma unroll
+  for (int c = 0; c < kPage; c += 2) {
+    const float2 arg = __ffma2_rn(make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), mul2, nbase2);
+    const float2 e = make_float2(fast_exp2(c < seen ? arg.x : NEG_INF), fast_exp2(c + 1 < seen ? arg.y : NEG_INF));
+    l4[(c >> 1) & 3] = __fadd2_rn(l4[(c >> 1) & 3], e);
+    // (a key that the row does not see may have a page whose scale is any multiple of v_ref)
+    pk[c / 2] = pack_f16x2(e.x == 0.f ? 0.f : e.x * val, e.y == 0.f ? 0.f : e.y * val);
+  }
+#pragma unroll
+  for (int i = 0; i < kCopies; ++i) {  // pages 2, 3, 0, 1
+    if ((i ^ 2) == copy) {
+      tmem_st8(s_addr + 32 + 8 * i, pk);
+    } else {
+      const uint32_t zero[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+      tmem_st8(s_addr + 32 + 8 * i, zero);
+    }
+  }
+  publish();
+  return !(val < kLeastVal) || scale == 0.f;
+}
+
 // 32 keys' codes at `from` as bf16 at `to`, both as the blocks hold them (of a unit that is
 // run again; out of line, as what is not in the blocks' loops is).
 template <int D>
@@ -621,6 +659,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         mbar_init(bar(sh.q_full[i]), kWideWarps);
         mbar_init(bar(sh.q_free[i]), 1);
       }
+      mbar_init(bar(sh.copied), kOutputWarps);
     }
     for (int s = 0; s < kMetaSlots; ++s) {
       mbar_init(bar(sh.meta_full[s]), 1);
@@ -908,6 +947,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           M.blk_lo = blk_lo;
           M.n_blocks = blk_hi - blk_lo;
           M.pass = pass;
+          M.copies = kFp8 && pass == kFirst && nrows <= kRows / kCopies ? kCopies : 1;
           sh.unit_id[k & 31] = u;
         }
         nb_before = nb_last;
@@ -1259,12 +1299,12 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         // values below 2^-9 of the largest, which keep 2^-17 of that.
         if (k >= 2 && !(ok = wait_bar(sh.q_free[k & 1], ((k >> 1) - 1) & 1))) break;
         tc_fence_after();
-        const int r_in = quad * 32 + lane;
-        if (quad * 32 < M.nrows) {
-          const int rt = p.div_G(r_in);
-          const bool valid = r_in < M.nrows;
+        const int r_in = quad * 32 + lane, r = M.copies > 1 ? lane : r_in;
+        if (r - lane < M.nrows) {
+          const int rt = p.div_G(r);
+          const bool valid = r < M.nrows;
           const uint4 *const src = reinterpret_cast<const uint4 *>(
-              p.q + (valid ? (M.tok0 + rt) * p.q_stride + (M.g * G + r_in - rt * G) * D : 0));
+              p.q + (valid ? (M.tok0 + rt) * p.q_stride + (M.g * G + r - rt * G) * D : 0));
           unsigned most = 0u;
           {
             uint4 x[D / 8];
@@ -1375,6 +1415,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
     pdl_wait();
     const int rt = p.div_G(r_in);
     int outputs = 0;
+    unsigned copied = 0;  // phases of the barrier of that name
     bool ok = true;
     for (int k = 0; ok; ++k) {
       const int slot = k % kMetaSlots;
@@ -1383,6 +1424,108 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
       if (!M.valid) break;
       if (!(ok = wait_bar(sh.sums[slot], (k / kMetaSlots) & 1))) break;
       const int pass = M.pass, nrows = M.nrows, nsplit = M.nsplit;
+      if constexpr (kFp8) {
+        if (M.copies > 1) {
+          // A row's sums are those of its copies together.  O goes through shared memory, as
+          // many columns at once as the copies' rows have room for.
+          // (rows are 32 apart, a warp has a copy of each)
+          const int width = nrows <= 8 ? 128 : nrows <= 16 ? 64 : 32;
+          const int tok0 = M.tok0, head0 = M.g * G;
+          const size_t part_row = static_cast<size_t>(M.slot) * kRows;
+          const uint32_t base = sbase + L::kStage;
+          auto sum_of_row = [&](int row) {
+            float l = 0.f;
+            for (int c = 0; c < kRows; c += 32) l += sh.xsum[slot][0][row + c] + sh.xsum[slot][1][row + c];
+            return l;
+          };
+          bool odd = false;
+          if (r_in < nrows) {
+            const float l = sum_of_row(r_in), lse = l == 0.f ? NEG_INF : l > 0.f ? lse_of(sh.xbase[slot][r_in], l) : l;
+            if (nsplit > 1) p.l_part[part_row + r_in] = lse;
+            else if (p.lse) p.lse[(tok0 + rt) * p.H_q + head0 + r_in - rt * G] = lse;
+            odd = l != l;
+          }
+          // (the unit before may have rows on their way through the same memory)
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(sh.copied));
+          if (!(ok = wait_bar(sh.copied, copied & 1) && wait_bar(sh.o_full, outputs & 1))) break;
+          ++copied;
+          ++outputs;
+          tc_fence_after();
+#pragma unroll 1
+          for (int col = 0; col < D && ok; col += width) {
+            const int w = min(width, D - col);
+#pragma unroll 1
+            for (int c = 0; c < w; c += 32) {
+              uint32_t o[32];
+              tmem_ld32(o_addr + col + c, o);
+              tmem_ld_wait32(o);
+              if (lane < nrows) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + ((quad * nrows + lane) * width + c) * 4 +
+                                                                               (((e ^ lane) & 7) << 4)),
+                               "r"(o[4 * e]), "r"(o[4 * e + 1]), "r"(o[4 * e + 2]), "r"(o[4 * e + 3])
+                               : "memory");
+              }
+            }
+            if (col + width >= D) tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+              if (col + width >= D) mbar_arrive(bar(sh.o_empty));
+              mbar_arrive(bar(sh.copied));
+            }
+            if (!(ok = wait_bar(sh.copied, copied & 1))) break;
+            ++copied;
+            for (int i = r_in; i < nrows * (w / 4); i += kRows) {
+              const int row = i / (w / 4), c = i % (w / 4);  // four columns
+              float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+              for (int n = 0; n < kCopies; ++n) {
+                float4 x;
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
+                             : "r"(base + ((n * nrows + row) * width + (c & ~7) * 4) * 4 + (((c ^ row) & 7) << 4))
+                             : "memory");
+                v.x += x.x;
+                v.y += x.y;
+                v.z += x.z;
+                v.w += x.w;
+              }
+              const float l = sum_of_row(row), inv = l == 0.f ? 0.f : __fdividef(sh.v_ref[slot][row], l);
+              odd |= !(v.x * 0.f == 0.f && v.y * 0.f == 0.f && v.z * 0.f == 0.f && v.w * 0.f == 0.f);
+              v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+              if (nsplit > 1) {
+                *reinterpret_cast<float4 *>(p.o_part + (part_row + row) * D + col + 4 * c) = v;
+              } else {
+                const int t = p.div_G(row);
+                *reinterpret_cast<uint2 *>(p.out + (static_cast<size_t>(tok0 + t) * p.H_q + head0 + row - t * G) * D + col + 4 * c) =
+                    make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+              }
+            }
+            __syncwarp();
+            if (col + width >= D) break;
+            if (lane == 0) mbar_arrive(bar(sh.copied));
+            if (!(ok = wait_bar(sh.copied, copied & 1))) break;
+            ++copied;
+          }
+          if (!ok) break;
+          const bool redo = __any_sync(0xffffffffu, odd);
+          if (lane == 0) {
+            if (redo) {
+              atomicOr(&sh.redo, 1u << (k & 31));
+              __threadfence_block();
+            }
+            mbar_arrive(bar(sh.meta_empty[slot]));
+            asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], 1;" ::"r"(smem_u32(&sh.units_done)) : "memory");
+          }
+          // (the next unit's sums may come here once all have read these)
+          if (lane == 0) mbar_arrive(bar(sh.copied));
+          if (!(ok = wait_bar(sh.copied, copied & 1))) break;
+          ++copied;
+          continue;
+        }
+      }
       const bool idle = quad * 32 >= nrows, valid = r_in < nrows;
       const int pair = (M.tok0 + rt) * p.H_q + M.g * G + r_in - rt * G;  // row and head
       const size_t part_row = static_cast<size_t>(M.slot) * kRows + r_in;
@@ -1516,10 +1659,11 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
       if (!M.valid) break;
       if (!kFp8 && lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
       const int nb = M.n_blocks, blk_lo = M.blk_lo, pass = M.pass;
-      const bool idle = quad * 32 >= M.nrows;
+      const int r = kFp8 && M.copies > 1 ? lane : r_in;
+      const bool idle = r - lane >= M.nrows;
       // (rows that are no query count as seeing everything, so that their warp
       // needs no masks for them; their results are not stored)
-      const int lim = r_in < M.nrows ? min(max(M.lim0 + rt, M.full), M.L) : 1 << 30;
+      const int lim = r < M.nrows ? min(max(M.lim0 + (kFp8 ? p.div_G(r) : rt), M.full), M.L) : 1 << 30;
       // blocks of the unit that every row of the warp sees all of
       const int n_plain = kFp8 || sl2 > 0.f ? min(max(__reduce_min_sync(0xffffffffu, lim), 0) / kBlk - blk_lo, nb) : 0;
       auto await_s = [&] {
@@ -1542,6 +1686,15 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         }
         if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
       }
+      auto publish_both = [&] {
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar(sh.p_full[jg & 1][0]));
+          mbar_arrive(bar(sh.p_full[jg & 1][1]));
+        }
+      };
       if (idle) {  // (whatever is there instead of P reaches only rows that are not stored)
         for (int j = 0; j < nb; ++j, ++jg) {
           if (!(ok = await_s())) break;
@@ -1590,6 +1743,16 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         }
         // (scores of -inf alone give no base to a row that sees the unit's keys)
         inside = pass != kFirst || m_run > NEG_INF || lim <= blk_lo * kBlk;
+        if constexpr (kFp8) {
+          for (; M.copies > 1 && j < nb; ++j, ++jg) {
+            if (j > 0 && !(ok = await_s())) break;
+            const float *const sc = sh.scales[jg % kScaleBlocks] + 4 * h;
+            inside &= softmax_share_fp8(t_lane + L::col_s(jg & 1) + h * 64, quad,
+                                        min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64, row_mul, val_mul, sc,
+                                        sc + kPagesPerBlock, m_run == NEG_INF ? 0.f : m_run, l4, publish_both);
+          }
+          if (!ok) break;
+        }
         // blocks that every row of the warp sees all of: nothing to decide
         for (; j < (kFp8 && pass == kAgain ? 0 : n_plain); ++j, ++jg) {
           if (j > 0 && !(ok = await_s())) break;
