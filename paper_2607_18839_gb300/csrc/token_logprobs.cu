@@ -5,14 +5,24 @@
 //   logprob = d_token - log(1 + R),  entropy = log(1 + R) - sum exp(d_v) d_v / Z
 // Both terms of the entropy are positive, and log(1 + R) keeps the digits of a small
 // R: nothing cancels where a token is nearly sure.
+#include <cooperative_groups.h>
+
 #include <cmath>
 
 #include "common.cuh"
 
+namespace cg = cooperative_groups;
+
 namespace hpd {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kUnroll = 4;      // 16-byte loads of a thread on their way at once
+constexpr int kMaxCluster = 8;  // CTAs of a row
+constexpr int kTop = 32;
+constexpr int kGroups = 64;      // of threads, whose maxima bound the top values from below
+constexpr int kCandidates = 1024;
+constexpr int kLogpSms = 152;
 
 struct LogpArgs {
   const void *logits;
@@ -22,90 +32,413 @@ struct LogpArgs {
   int32_t *top_tokens;
   float *top_logprobs;
   int V, top;
-  float scale;
+  float scale, scale_log2;
 };
 
+__device__ __forceinline__ float inf() { return __int_as_float(0x7f800000); }
+__device__ __forceinline__ float nan() { return __int_as_float(0x7fffffff); }
+
 // A place in a row's order: larger values first, lower indices first among equal ones.
-// (NaN is in none: its value is never asked for.)
 struct Place {
   float x;
   int i;
 };
 __device__ __forceinline__ bool before(const Place &a, const Place &b) { return a.x > b.x || (a.x == b.x && a.i < b.i); }
 
-template <class T>
-__device__ __forceinline__ float value(const T *row, int i) {
-  return static_cast<float>(row[i]);
+// The order of values as whole numbers (-0 is +0).
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One CTA a row: the row is read for the maximum, for the sums, and once for each
-// alternative.
+// 16 bytes of a row, and their largest value (NaN only if there is nothing else).
 template <class T>
-__global__ void __launch_bounds__(kThreads) token_logprobs_kernel(const LogpArgs a) {
-  __shared__ Place s_place[kWarps];
-  __shared__ float s_sum[2][kWarps];
+struct Vec;
+template <>
+struct Vec<__nv_bfloat16> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ void unpack(const uint4 &v, float *x) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ float largest(const uint4 &v) {
+    auto h2 = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162 *>(&w); };
+    const __nv_bfloat162 m = __hmax2(__hmax2(h2(v.x), h2(v.y)), __hmax2(h2(v.z), h2(v.w)));
+    const uint32_t w = *reinterpret_cast<const uint32_t *>(&m);
+    return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+};
+template <>
+struct Vec<float> {
+  static constexpr int kN = 4;
+  static __device__ __forceinline__ void unpack(const uint4 &v, float *x) {
+    x[0] = __uint_as_float(v.x);
+    x[1] = __uint_as_float(v.y);
+    x[2] = __uint_as_float(v.z);
+    x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ float largest(const uint4 &v) {
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
+};
+
+// Of some values: the largest; with d = (x - m) scale log2(e) the sums of 2^d, one of the
+// largest values left out, and of 2^d d.  NaN among them is in `rest`.
+struct Sums {
+  float m, rest, mean;
+};
+__device__ __forceinline__ void add(Sums &s, float x, float base, float c) {
+  float d = (x - base) * c;
+  asm("max.NaN.f32 %0, %0, 0fC3480000;" : "+f"(d));  // (-200: 2^d is 0 there, and 0 times d a number)
+  const float e = fast_exp2(d);
+  s.rest += e;
+  s.mean = fmaf(e, d, s.mean);
+}
+// The sums so far against a new, larger m.
+__device__ __forceinline__ void raise(Sums &s, float m, float c) {
+  if (s.m > -inf()) {
+    const float d = (s.m - m) * c, w = fast_exp2(d), z = 1.f + s.rest;
+    s.mean = w == 0.f ? 0.f : w * fmaf(d, z, s.mean);
+    s.rest = w * z;
+  }
+  s.m = m;
+}
+template <int N>
+__device__ __forceinline__ void add_all(Sums &s, const float *x, float largest, float c) {
+  if (largest > s.m) {
+    raise(s, largest, c);
+    bool skip = true;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (skip && x[i] == largest) skip = false;
+      else add(s, x[i], s.m, c);
+    }
+    return;
+  }
+  const float base = s.m == -inf() ? 0.f : s.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) add(s, x[i], base, c);
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
+  if (b.m > a.m) {
+    const Sums t = a;
+    a = b;
+    b = t;
+  }
+  const float m = a.m;
+  if (b.m > -inf()) {
+    const float d = (b.m - m) * c, w = fast_exp2(d), z = 1.f + b.rest;
+    a.rest += w * z;
+    if (w != 0.f) a.mean += w * fmaf(d, z, b.mean);
+  } else {
+    a.rest += b.rest;
+  }
+  return a;
+}
+__device__ __forceinline__ Sums join_warp(Sums s, float c) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    Sums t;
+    t.m = __shfl_xor_sync(0xffffffffu, s.m, o);
+    t.rest = __shfl_xor_sync(0xffffffffu, s.rest, o);
+    t.mean = __shfl_xor_sync(0xffffffffu, s.mean, o);
+    // (the same order in both lanes)
+    s = threadIdx.x & o ? join(t, s, c) : join(s, t, c);
+  }
+  return s;
+}
+
+struct LogpShared {
+  Sums warp[kWarps];
+  float group[kGroups];
+  float least;     // a lower bound of the last of the top values
+  int found;       // candidates, some perhaps beyond their room
+  int count;       // of a scan
+  int per_warp[kWarps];
+  Place candidate[kCandidates];
+  Place best[kTop];
+  // of the CTAs of a row, in the first one
+  Sums part[kMaxCluster];
+  Place list[kMaxCluster][kTop];
+};
+
+// A CTA's share of a row: single values up to an aligned address (the first CTA's) and
+// behind the last whole 16 bytes (the last one's), and the 16-byte pieces between.
+template <class T>
+struct Share {
+  const T *row;
+  int head, tail0, tail;  // values before the pieces; first and number of those behind
+  int v0, v1;             // pieces
+  __device__ __forceinline__ uint4 piece(int v) const { return reinterpret_cast<const uint4 *>(row + head)[v]; }
+  __device__ __forceinline__ int index(int v) const { return head + v * Vec<T>::kN; }
+};
+
+// f(value, index) of every value of the share, a piece a thread.
+template <class T, class F>
+__device__ __forceinline__ void for_values(const Share<T> &s, F f) {
+  const int tid = threadIdx.x;
+  if (tid < s.head && s.v0 == 0) f(static_cast<float>(s.row[tid]), tid);
+  if (tid < s.tail) f(static_cast<float>(s.row[s.tail0 + tid]), s.tail0 + tid);
+#pragma unroll 1
+  for (int v = s.v0 + tid; v < s.v1; v += kThreads) {
+    float x[Vec<T>::kN];
+    Vec<T>::unpack(s.piece(v), x);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::kN; ++i) f(x[i], s.index(v) + i);
+  }
+}
+
+__device__ __forceinline__ void propose(LogpShared &sh, float x, int i) {
+  const int at = atomicAdd(&sh.found, 1);
+  if (at < kCandidates) sh.candidate[at] = Place{x, i};
+}
+
+// The first values of the share that equal x, in the order of their indices, `need` of
+// them at most, become candidates.
+template <class T>
+__device__ __noinline__ void propose_equal(LogpShared &sh, const Share<T> &s, float x, int need) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const float INF = __int_as_float(0x7f800000), nan = __int_as_float(0x7fffffff);
-  pdl_wait();
-  pdl_trigger();
-  const size_t r = blockIdx.x;
-  const T *row = static_cast<const T *>(a.logits) + static_cast<long long>(r) * a.row_stride;
-  // the first place behind `last`
-  auto next_of = [&](Place last) {
-    Place best{-INF, a.V};
-    for (int i = tid; i < a.V; i += kThreads) {
-      const Place p{value(row, i), i};
-      if (p.x == p.x && before(last, p) && before(p, best)) best = p;
-    }
-    for (int o = 16; o > 0; o >>= 1) {
-      const Place p{__shfl_xor_sync(0xffffffffu, best.x, o), __shfl_xor_sync(0xffffffffu, best.i, o)};
-      if (before(p, best)) best = p;
-    }
+  const int begin = s.v0 == 0 ? 0 : s.index(s.v0), end = s.tail ? s.tail0 + s.tail : s.index(s.v1);
+  for (int i0 = begin; i0 < end && need > 0; i0 += kThreads) {
+    const int i = i0 + tid;
+    const bool here = i < end && static_cast<float>(s.row[i]) == x;
+    const unsigned all = __ballot_sync(0xffffffffu, here);
+    if (lane == 0) sh.per_warp[warp] = __popc(all);
     __syncthreads();
-    if (lane == 0) s_place[warp] = best;
+    int at = __popc(all & ((1u << lane) - 1u)), total = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      at += w < warp ? sh.per_warp[w] : 0;
+      total += sh.per_warp[w];
+    }
+    if (here && at < need) propose(sh, x, i);
+    need -= total;
     __syncthreads();
-    for (int w = 0; w < kWarps; ++w)
-      if (before(s_place[w], best)) best = s_place[w];
-    return best;
-  };
-  const Place first = next_of(Place{INF, -1});
-  const float m = first.x;
-  float rest = 0.f, mean = 0.f;
-  for (int i = tid; i < a.V; i += kThreads) {
-    const float d = (value(row, i) - m) * a.scale, e = expf(d);
-    if (i != first.i) rest += e;
-    if (e > 0.f) mean = fmaf(e, d, mean);
   }
-  for (int o = 16; o > 0; o >>= 1) {
-    rest += __shfl_xor_sync(0xffffffffu, rest, o);
-    mean += __shfl_xor_sync(0xffffffffu, mean, o);
-  }
-  if (lane == 0) {
-    s_sum[0][warp] = rest;
-    s_sum[1][warp] = mean;
+}
+
+// Too many values reach the bound (ties, or an order that a thread's share of the row
+// follows): the last of the top values by halving the range of keys, a pass over the
+// share each time, then those above it and the first of its equals.
+template <class T>
+__device__ __noinline__ void select_by_halves(LogpShared &sh, const Share<T> &s, int top) {
+  uint32_t lo = key_of(sh.least), hi = 0xffffffffu;
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2 + 1;
+    __syncthreads();
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    int n = 0;
+    for_values(s, [&](float x, int) { n += x == x && key_of(x) >= mid; });
+    n = __reduce_add_sync(0xffffffffu, n);
+    if ((threadIdx.x & 31) == 0) atomicAdd(&sh.count, n);
+    __syncthreads();
+    if (sh.count >= top) lo = mid; else hi = mid - 1;
   }
   __syncthreads();
-  rest = mean = 0.f;
-  for (int w = 0; w < kWarps; ++w) {
-    rest += s_sum[0][w];
-    mean += s_sum[1][w];
+  if (threadIdx.x == 0) sh.found = 0;
+  __syncthreads();
+  for_values(s, [&](float x, int i) {
+    if (x == x && key_of(x) > lo) propose(sh, x, i);
+  });
+  __syncthreads();
+  const int need = top - sh.found;
+  propose_equal(sh, s, __uint_as_float(lo & 0x80000000u ? lo & 0x7fffffffu : ~lo), need);
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+
+// A row has a cluster of `ctas` CTAs, each with its share of the row, read once:
+//  - sums against each thread's own maximum, joined over the CTA;
+//  - top values: every thread's maximum is known, so that of 64 groups of threads; the
+//    top-th largest of those bounds the top values from below.  Only threads whose maximum
+//    reaches the bound (some 1.5 times `top` of them) look at their values again, in L2, a
+//    warp at each, and what reaches it is ranked against one another.
+// The first CTA joins the others' sums and lists, which come through distributed shared
+// memory.
+template <class T, bool kAlternatives>
+__global__ void __launch_bounds__(kThreads, 5) token_logprobs_kernel(const LogpArgs a, int ctas) {
+  using V = Vec<T>;
+  __shared__ LogpShared sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = ctas > 1 ? static_cast<int>(blockIdx.x % ctas) : 0;
+  const size_t r = ctas > 1 ? blockIdx.x / ctas : blockIdx.x;
+  const float c = a.scale_log2;
+  if (ctas > 1) cluster_arrive();
+  pdl_wait();
+  pdl_trigger();
+  Share<T> s;
+  s.row = static_cast<const T *>(a.logits) + static_cast<long long>(r) * a.row_stride;
+  s.head = min(a.V, static_cast<int>((16u - (reinterpret_cast<uintptr_t>(s.row) & 15u)) & 15u) / static_cast<int>(sizeof(T)));
+  const int pieces = (a.V - s.head) / V::kN;
+  s.v0 = static_cast<int>(static_cast<long long>(pieces) * rank / ctas);
+  s.v1 = static_cast<int>(static_cast<long long>(pieces) * (rank + 1) / ctas);
+  s.tail0 = s.head + pieces * V::kN;
+  s.tail = rank == ctas - 1 ? a.V - s.tail0 : 0;
+  float x_token = 0.f;
+  int token = -1;
+  if (rank == 0 && tid == 0) {
+    token = a.tokens[r];
+    if (token >= 0 && token < a.V) x_token = static_cast<float>(s.row[token]);
   }
-  if (first.i == a.V || !(fabsf(m) < INF)) rest = nan;
-  const float log_z = log1pf(rest);
-  if (tid == 0) {
-    const int t = a.tokens[r];
-    const float x = t >= 0 && t < a.V ? value(row, t) : -INF;
-    a.logprob[r] = rest == rest ? (x - m) * a.scale - log_z : nan;
-    if (a.entropy) a.entropy[r] = log_z - mean / (1.f + rest);
-  }
-  Place p = first;
-  for (int k = 0; k < a.top; ++k) {
-    if (tid == 0) {
-      a.top_tokens[r * a.top + k] = p.i < a.V ? p.i : -1;
-      a.top_logprobs[r * a.top + k] = p.i < a.V && rest == rest ? (p.x - m) * a.scale - log_z : nan;
+
+  Sums sums{-inf(), 0.f, 0.f};
+  auto single = [&](int i) {
+    const float x = static_cast<float>(s.row[i]);
+    add_all<1>(sums, &x, x, c);
+  };
+  if (tid < s.head && rank == 0) single(tid);
+  if (tid < s.tail) single(s.tail0 + tid);
+#pragma unroll 1
+  for (int v = s.v0 + tid; v < s.v1; v += kThreads * kUnroll) {
+    uint4 w[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (v + u * kThreads < s.v1) w[u] = s.piece(v + u * kThreads);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (v + u * kThreads >= s.v1) break;
+      float x[V::kN];
+      V::unpack(w[u], x);
+      add_all<V::kN>(sums, x, V::largest(w[u]), c);
     }
-    if (p.i < a.V && k + 1 < a.top) p = next_of(p);
   }
+  const float mine = sums.m;  // this thread's largest value
+  if constexpr (kAlternatives) {
+    float g = mine;
+#pragma unroll
+    for (int o = 1; o < kThreads / kGroups; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
+    if (lane % (kThreads / kGroups) == 0) sh.group[tid / (kThreads / kGroups)] = g;
+    if (tid == 0) sh.found = 0;
+  }
+  sums = join_warp(sums, c);
+  if (lane == 0) sh.warp[warp] = sums;
+  __syncthreads();
+
+  if constexpr (kAlternatives) {
+    const int top = a.top;
+    if (warp == 0) {  // the top-th largest of the groups' maxima
+#pragma unroll 1
+      for (int k = lane; k < kGroups; k += 32) {
+        const Place p{sh.group[k], k};
+        int ahead = 0;
+#pragma unroll 8
+        for (int j = 0; j < kGroups; ++j) ahead += before(Place{sh.group[j], j}, p);
+        if (ahead == top - 1) sh.least = p.x;
+      }
+    }
+    __syncthreads();
+    const float least = sh.least;
+    const bool any = least > -inf();  // (else fewer than `top` groups have a value above -inf: those are looked for)
+    unsigned hot = __ballot_sync(0xffffffffu, any ? mine >= least : mine > least);
+    auto look = [&](float x, int i) {
+      if (any ? x >= least : x > least) propose(sh, x, i);
+    };
+    while (hot) {
+      const int t = warp * 32 + __ffs(hot) - 1;  // the thread whose values the warp looks at
+      hot &= hot - 1;
+      if (lane == 0 && t < s.head && rank == 0) look(static_cast<float>(s.row[t]), t);
+      if (lane == 1 && t < s.tail) look(static_cast<float>(s.row[s.tail0 + t]), s.tail0 + t);
+#pragma unroll 1
+      for (int v = s.v0 + t + lane * kThreads; v < s.v1; v += 32 * kThreads) {
+        const uint4 w = s.piece(v);
+        if (any ? !(V::largest(w) >= least) : !(V::largest(w) > least)) continue;
+        float x[V::kN];
+        V::unpack(w, x);
+#pragma unroll
+        for (int i = 0; i < V::kN; ++i) look(x[i], s.index(v) + i);
+      }
+    }
+    __syncthreads();
+    if (sh.found > kCandidates) select_by_halves(sh, s, top);
+    else if (!any && sh.found < top) propose_equal(sh, s, -inf(), top - sh.found);
+    __syncthreads();
+    const int found = min(sh.found, kCandidates);
+    if (tid < top) sh.best[tid] = Place{nan(), -1};
+    __syncthreads();
+    for (int k = tid; k < found; k += kThreads) {
+      const Place p = sh.candidate[k];
+      int ahead = 0;
+      for (int j = 0; j < found; ++j) ahead += before(sh.candidate[j], p);
+      if (ahead < top) sh.best[ahead] = p;
+    }
+    __syncthreads();
+  }
+
+  if (ctas > 1) {
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster_wait();  // (the first CTA runs: its shared memory may be written)
+    LogpShared *first = cluster.map_shared_rank(&sh, 0);
+    if (tid == 0) {
+      Sums t = sh.warp[0];
+      for (int w = 1; w < kWarps; ++w) t = join(t, sh.warp[w], c);
+      first->part[rank] = t;
+    }
+    if (kAlternatives && tid < a.top) first->list[rank][tid] = sh.best[tid];
+    cluster.sync();
+    if (rank != 0) return;
+  }
+  Sums all = ctas > 1 ? sh.part[0] : sh.warp[0];
+  for (int w = 1; w < (ctas > 1 ? ctas : kWarps); ++w) all = join(all, ctas > 1 ? sh.part[w] : sh.warp[w], c);
+  if (!(fabsf(all.m) < inf())) all.rest = nan();
+  const float log_z = log1pf(all.rest);
+  auto logprob = [&](float x) { return all.rest == all.rest ? (x - all.m) * a.scale - log_z : nan(); };
+  if (tid == 0) {
+    a.logprob[r] = logprob(token >= 0 && token < a.V ? x_token : -inf());
+    if (a.entropy) a.entropy[r] = log_z - all.mean * kLn2 / (1.f + all.rest);
+  }
+  if constexpr (kAlternatives) {
+    const int top = a.top;
+    auto put = [&](int k, const Place &p) {
+      a.top_tokens[r * top + k] = p.i;
+      a.top_logprobs[r * top + k] = p.i >= 0 ? logprob(p.x) : nan();
+    };
+    if (ctas == 1) {
+      if (tid < top) put(tid, sh.best[tid]);
+      return;
+    }
+    if (tid < top) sh.best[tid] = Place{nan(), -1};
+    __syncthreads();
+    if (tid < ctas * top) {
+      const Place p = sh.list[tid / top][tid % top];
+      int ahead = 0;
+      for (int w = 0; w < ctas; ++w)
+        for (int j = 0; j < top; ++j) ahead += before(sh.list[w][j], p);
+      if (p.i >= 0 && ahead < top) sh.best[ahead] = p;
+    }
+    __syncthreads();
+    if (tid < top) put(tid, sh.best[tid]);
+  }
+}
+
+template <class T, bool kAlternatives>
+cudaError_t launch_logprobs(const LogpArgs &k, int R, cudaStream_t s) {
+  // CTAs of a row: as many as keep the GPU's SMs busy, none with less than 8 KB.
+  int ctas = 1;
+  while (ctas < kMaxCluster && static_cast<long long>(R) * ctas * 2 <= 4 * kLogpSms &&
+         static_cast<long long>(k.V) * static_cast<int>(sizeof(T)) >= 2LL * ctas * 8192)
+    ctas *= 2;
+  static std::atomic<uint64_t> done{0};
+  // (five CTAs an SM need a quarter of its 228 KB shared; the rest is for the loads)
+  cudaError_t e = prefer_l1(token_logprobs_kernel<T, kAlternatives>, done, 28);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(R) * static_cast<unsigned>(ctas));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(ctas);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = ctas > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T, kAlternatives>, k, ctas);
 }
 
 }  // namespace
@@ -138,8 +471,9 @@ extern "C" hpd_status hpd_token_logprobs(const hpd_token_logprobs_args *a, hpd_s
   k.top = a->top;
   k.scale = a->scale != 0.f ? a->scale : 1.f;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e =
-      a->fp32 ? launch_kernel(true, token_logprobs_kernel<float>, dim3(a->R), dim3(kThreads), 0, s, k)
-              : launch_kernel(true, token_logprobs_kernel<__nv_bfloat16>, dim3(a->R), dim3(kThreads), 0, s, k);
+  k.scale_log2 = k.scale * kLog2e;
+  const cudaError_t e = a->fp32 ? (k.top ? launch_logprobs<float, true>(k, a->R, s) : launch_logprobs<float, false>(k, a->R, s))
+                        : k.top ? launch_logprobs<__nv_bfloat16, true>(k, a->R, s)
+                                : launch_logprobs<__nv_bfloat16, false>(k, a->R, s);
   return e == cudaSuccess ? HPD_OK : record_cuda_error(e);
 }
