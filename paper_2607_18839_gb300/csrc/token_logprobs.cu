@@ -17,7 +17,8 @@ namespace hpd {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kUnroll = 4;      // 16-byte loads of a thread on their way at once
+constexpr int kUnroll = 2;      // 16-byte loads of a thread at once, twice that on their way
+constexpr int kCtasPerSm = 5;
 constexpr int kMaxCluster = 8;  // CTAs of a row
 constexpr int kTop = 32;
 constexpr int kGroups = 64;      // of threads, whose maxima bound the top values from below
@@ -91,38 +92,102 @@ struct Vec<float> {
 struct Sums {
   float m, rest, mean;
 };
-__device__ __forceinline__ void add(Sums &s, float x, float base, float c) {
-  float d = (x - base) * c;
-  asm("max.NaN.f32 %0, %0, 0fC3480000;" : "+f"(d));  // (-200: 2^d is 0 there, and 0 times d a number)
-  const float e = fast_exp2(d);
-  s.rest += e;
-  s.mean = fmaf(e, d, s.mean);
-}
-// The sums so far against a new, larger m.
-__device__ __forceinline__ void raise(Sums &s, float m, float c) {
-  if (s.m > -inf()) {
-    const float d = (s.m - m) * c, w = fast_exp2(d), z = 1.f + s.rest;
-    s.mean = w == 0.f ? 0.f : w * fmaf(d, z, s.mean);
-    s.rest = w * z;
+
+// A thread's values.  Sums are taken against a base, the largest of its first pieces, which
+// moves only when a value passes it by 2^kWindow; the piece with the largest value so far
+// is kept apart, as what it is, and its values are added when another takes its place: no
+// branch depends on where a row's maxima stand (a branch at every new maximum had two in
+// three of the pieces in both of its sides).
+template <class T>
+struct Running {
+  static constexpr float kWindow = 60.f, kNothing = -300.f;  // log2: 2^kNothing is 0
+  float m, second;    // the largest value, and that of the other pieces than its own
+  float base;
+  float2 sum, mean;   // of 2^d and 2^d d, d against the base
+  uint4 best;         // the piece that holds m, and the index of its first value
+  int best_at;
+  uint32_t floor2;    // bf16: what is below has 2^d = 0
+
+  __device__ __forceinline__ void set_base(float b, float c) {
+    base = b;
+    // (2^-6 of the base: the floor stays that far below it once rounded)
+    const float f = b - fmaxf(-kNothing / c, fabsf(b) * 0x1p-6f);
+    floor2 = pack_bf16x2(f, f);
   }
-  s.m = m;
-}
-template <int N>
-__device__ __forceinline__ void add_all(Sums &s, const float *x, float largest, float c) {
-  if (largest > s.m) {
-    raise(s, largest, c);
-    bool skip = true;
+  __device__ __forceinline__ void start(float first, float c) {
+    m = second = -inf();
+    sum = mean = make_float2(0.f, 0.f);
+    constexpr uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+    best = make_uint4(none, none, none, none);
+    best_at = 0;
+    set_base(fabsf(first) < inf() ? first : 0.f, c);
+  }
+  // (0 times minus infinity is kept out: by the floor, or of d itself where that would not be
+  // a number of the type)
+  __device__ __forceinline__ void add(const uint4 &v, float c) {
+    const float2 nbase2 = make_float2(-base, -base), c2 = make_float2(c, c);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const bool far = sizeof(T) == 4 || base < -1e37f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (skip && x[i] == largest) skip = false;
-      else add(s, x[i], s.m, c);
+    for (int i = 0; i < 4; i += sizeof(T) == 2 ? 1 : 2) {
+      float2 x;
+      if constexpr (sizeof(T) == 2) {
+        uint32_t u = w[i];
+        if (!far) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(u) : "r"(floor2));
+        x = make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+      } else {
+        x = make_float2(__uint_as_float(w[i]), __uint_as_float(w[i + 1]));
+      }
+      float2 d = __fmul2_rn(__fadd2_rn(x, nbase2), c2);
+      if (far) {
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(d.x) : "f"(kNothing));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(d.y) : "f"(kNothing));
+      }
+      const float2 e = make_float2(fast_exp2(d.x), fast_exp2(d.y));
+      sum = __fadd2_rn(sum, e);
+      mean = __ffma2_rn(e, d, mean);
     }
-    return;
   }
-  const float base = s.m == -inf() ? 0.f : s.m;
+  __device__ __forceinline__ void take(const uint4 &v, int at, float c) {
+    const float largest = Vec<T>::largest(v);
+    if ((largest - base) * c > kWindow && largest < inf()) raise(largest, c);
+    const bool better = largest > m;
+    second = fmaxf(second, fminf(m, largest));  // (NaN, of a piece of nothing else, is passed over)
+    const uint4 w = make_uint4(better ? best.x : v.x, better ? best.y : v.y, better ? best.z : v.z, better ? best.w : v.w);
+    best = make_uint4(better ? v.x : best.x, better ? v.y : best.y, better ? v.z : best.z, better ? v.w : best.w);
+    best_at = better ? at : best_at;
+    m = better ? largest : m;
+    add(w, c);
+  }
+  __device__ __forceinline__ void raise(float to, float c) {
+    const float d = fmaxf((base - to) * c, kNothing), w = fast_exp2(d);
+    // (w is 0 where nothing is left; sums that are NaN stay NaN)
+    mean = make_float2(w * fmaf(d, sum.x, mean.x), w * fmaf(d, sum.y, mean.y));
+    sum = make_float2(w * sum.x, w * sum.y);
+    set_base(to, c);
+  }
+  __device__ __forceinline__ Sums result(float c) const {
+    Sums s{m, sum.x + sum.y, mean.x + mean.y};
+    if (m == -inf()) return s;
+    const float d = fmaxf((base - m) * c, kNothing), w = fast_exp2(d);
+    s.mean = w * fmaf(d, s.rest, s.mean);
+    s.rest *= w;
+    float x[Vec<T>::kN];
+    Vec<T>::unpack(best, x);
+    bool skip = true;  // one of the largest
 #pragma unroll
-  for (int i = 0; i < N; ++i) add(s, x[i], base, c);
-}
+    for (int i = 0; i < Vec<T>::kN; ++i) {
+      const bool here = skip && x[i] == m;
+      skip = skip && !here;
+      float e_d = (x[i] - m) * c;
+      asm("max.NaN.f32 %0, %0, %1;" : "+f"(e_d) : "f"(kNothing));
+      const float e = here ? 0.f : fast_exp2(e_d);
+      s.rest += e;
+      s.mean = fmaf(e, e_d, s.mean);
+    }
+    return s;
+  }
+};
 __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   if (b.m > a.m) {
     const Sums t = a;
@@ -261,7 +326,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 // The first CTA joins the others' sums and lists, which come through distributed shared
 // memory.
 template <class T, bool kAlternatives>
-__global__ void __launch_bounds__(kThreads, 5) token_logprobs_kernel(const LogpArgs a, int ctas) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(const LogpArgs a, int ctas) {
   using V = Vec<T>;
   __shared__ LogpShared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -286,30 +351,49 @@ __global__ void __launch_bounds__(kThreads, 5) token_logprobs_kernel(const LogpA
     if (token >= 0 && token < a.V) x_token = static_cast<float>(s.row[token]);
   }
 
-  Sums sums{-inf(), 0.f, 0.f};
+  Running<T> run;
+  // a single value, as a piece with nothing else
   auto single = [&](int i) {
-    const float x = static_cast<float>(s.row[i]);
-    add_all<1>(sums, &x, x, c);
+    uint4 w;
+    if constexpr (sizeof(T) == 2)
+      w = make_uint4(0xff800000u | *reinterpret_cast<const uint16_t *>(s.row + i), 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+    else
+      w = make_uint4(__float_as_uint(s.row[i]), 0xff800000u, 0xff800000u, 0xff800000u);
+    run.take(w, i, c);
   };
-  if (tid < s.head && rank == 0) single(tid);
-  if (tid < s.tail) single(s.tail0 + tid);
-#pragma unroll 1
-  for (int v = s.v0 + tid; v < s.v1; v += kThreads * kUnroll) {
-    uint4 w[kUnroll];
+  // (the next pieces on their way while these are summed)
+  constexpr int kStep = kThreads * kUnroll;
+  uint4 w[2][kUnroll];
+  auto load = [&](int v, uint4 *w) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
       if (v + u * kThreads < s.v1) w[u] = s.piece(v + u * kThreads);
+  };
+  auto take = [&](int v, const uint4 *w) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       if (v + u * kThreads >= s.v1) break;
-      float x[V::kN];
-      V::unpack(w[u], x);
-      add_all<V::kN>(sums, x, V::largest(w[u]), c);
+      run.take(w[u], s.index(v + u * kThreads), c);
     }
+  };
+  const bool started = s.v0 + tid < s.v1;
+  int v = s.v0 + tid;
+  load(v, w[0]);
+  if (started) run.start(V::largest(w[0][0]), c);
+#pragma unroll 1
+  while (v < s.v1) {
+    load(v + kStep, w[1]);
+    take(v, w[0]);
+    load(v + 2 * kStep, w[0]);
+    take(v + kStep, w[1]);
+    v += 2 * kStep;
   }
-  const float mine = sums.m;  // this thread's largest value
+  if (!started) run.start(0.f, c);
+  if (tid < s.head && rank == 0) single(tid);
+  if (tid < s.tail) single(s.tail0 + tid);
+  Sums sums = run.result(c);
   if constexpr (kAlternatives) {
-    float g = mine;
+    float g = run.m;
 #pragma unroll
     for (int o = 1; o < kThreads / kGroups; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
     if (lane % (kThreads / kGroups) == 0) sh.group[tid / (kThreads / kGroups)] = g;
@@ -321,23 +405,33 @@ __global__ void __launch_bounds__(kThreads, 5) token_logprobs_kernel(const LogpA
 
   if constexpr (kAlternatives) {
     const int top = a.top;
-    if (warp == 0) {  // the top-th largest of the groups' maxima
-#pragma unroll 1
-      for (int k = lane; k < kGroups; k += 32) {
-        const Place p{sh.group[k], k};
-        int ahead = 0;
-#pragma unroll 8
-        for (int j = 0; j < kGroups; ++j) ahead += before(Place{sh.group[j], j}, p);
-        if (ahead == top - 1) sh.least = p.x;
-      }
+    if (tid < top) sh.best[tid] = Place{nan(), -1};
+    {  // the top-th largest of the groups' maxima, a group's place by four threads
+      constexpr int kPer = kThreads / kGroups;
+      const Place p{sh.group[tid / kPer], tid / kPer};
+      int ahead = 0;
+#pragma unroll
+      for (int j = tid % kPer; j < kGroups; j += kPer) ahead += before(Place{sh.group[j], j}, p);
+#pragma unroll
+      for (int o = 1; o < kPer; o <<= 1) ahead += __shfl_xor_sync(0xffffffffu, ahead, o);
+      if (tid % kPer == 0 && ahead == top - 1) sh.least = p.x;
     }
     __syncthreads();
     const float least = sh.least;
     const bool any = least > -inf();  // (else fewer than `top` groups have a value above -inf: those are looked for)
-    unsigned hot = __ballot_sync(0xffffffffu, any ? mine >= least : mine > least);
+    auto reaches = [&](float x) { return any ? x >= least : x > least; };
     auto look = [&](float x, int i) {
-      if (any ? x >= least : x > least) propose(sh, x, i);
+      if (reaches(x)) propose(sh, x, i);
     };
+    // a thread's best piece is at hand; those with another one that reaches the bound are
+    // looked through
+    unsigned hot = __ballot_sync(0xffffffffu, reaches(run.second));
+    if (reaches(run.m) && !reaches(run.second)) {
+      float x[V::kN];
+      V::unpack(run.best, x);
+#pragma unroll
+      for (int i = 0; i < V::kN; ++i) look(x[i], run.best_at + i);
+    }
     while (hot) {
       const int t = warp * 32 + __ffs(hot) - 1;  // the thread whose values the warp looks at
       hot &= hot - 1;
@@ -346,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, 5) token_logprobs_kernel(const LogpA
 #pragma unroll 1
       for (int v = s.v0 + t + lane * kThreads; v < s.v1; v += 32 * kThreads) {
         const uint4 w = s.piece(v);
-        if (any ? !(V::largest(w) >= least) : !(V::largest(w) > least)) continue;
+        if (!reaches(V::largest(w))) continue;
         float x[V::kN];
         V::unpack(w, x);
 #pragma unroll
@@ -358,13 +452,20 @@ __global__ void __launch_bounds__(kThreads, 5) token_logprobs_kernel(const LogpA
     else if (!any && sh.found < top) propose_equal(sh, s, -inf(), top - sh.found);
     __syncthreads();
     const int found = min(sh.found, kCandidates);
-    if (tid < top) sh.best[tid] = Place{nan(), -1};
-    __syncthreads();
-    for (int k = tid; k < found; k += kThreads) {
-      const Place p = sh.candidate[k];
+    if (found <= kThreads / 4) {  // a candidate's place by four threads
+      const Place p = sh.candidate[min(tid / 4, found - 1)];
       int ahead = 0;
-      for (int j = 0; j < found; ++j) ahead += before(sh.candidate[j], p);
-      if (ahead < top) sh.best[ahead] = p;
+      for (int j = tid % 4; j < found; j += 4) ahead += before(sh.candidate[j], p);
+      ahead += __shfl_xor_sync(0xffffffffu, ahead, 1);
+      ahead += __shfl_xor_sync(0xffffffffu, ahead, 2);
+      if (tid % 4 == 0 && tid / 4 < found && ahead < top) sh.best[ahead] = p;
+    } else {
+      for (int k = tid; k < found; k += kThreads) {
+        const Place p = sh.candidate[k];
+        int ahead = 0;
+        for (int j = 0; j < found; ++j) ahead += before(sh.candidate[j], p);
+        if (ahead < top) sh.best[ahead] = p;
+      }
     }
     __syncthreads();
   }

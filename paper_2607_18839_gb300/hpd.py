@@ -7,6 +7,7 @@ made without a CUDA device, the call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -513,32 +514,38 @@ def token_logprobs(logits, tokens, top=0, temperature=1.0, stream=None) -> Token
     stream of the call."""
     import torch
     what = "token_logprobs"
-    if not isinstance(logits, torch.Tensor) or logits.dtype not in (torch.bfloat16, torch.float32) or \
-            not logits.is_cuda or logits.dim() < 1:
-        _need(what, logits, torch.bfloat16, (None, None), strides_free=True)
+    bf = torch.bfloat16
+    # (checks written out, as for the rotation: they have a good part of a small call's time)
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dim() < 1 or \
+            not (logits.dtype is bf or logits.dtype is torch.float32):
+        _need(what, logits, bf, (None, None), strides_free=True)
         raise HpdError(what, 1, "logits of at least one extent")
-    lead, V = logits.shape[:-1], logits.shape[-1]
-    _need(what, tokens, torch.int32, lead)
+    shape = logits.shape
+    lead, V = shape[:-1], shape[-1]
+    if not isinstance(tokens, torch.Tensor) or not _is(tokens, torch.int32, lead):
+        _need(what, tokens, torch.int32, lead)
     stride = 0
-    if logits.dim() == 2 and logits.shape[0] > 1:
-        stride = logits.stride(0)
-        if (V > 1 and logits.stride(1) != 1) or stride < V:
+    if not logits.is_contiguous():
+        if len(shape) != 2:
+            raise HpdError(what, 1, "contiguous logits, or a matrix with strided rows")
+        stride, step = logits.stride()
+        if (V > 1 and step != 1) or (shape[0] > 1 and stride < V):
             raise HpdError(what, 1, "rows with their values side by side, none over another")
-    elif not logits.is_contiguous() and not (logits.dim() == 2 and logits.stride(1) == 1):
-        raise HpdError(what, 1, "contiguous logits, or a matrix with strided rows")
-    if not temperature > 0 or not 1.0 / temperature < 3.4e38 or not 1.0 / temperature > 1e-37:
+        stride = stride if shape[0] > 1 else 0  # (one row has none)
+    if not 1e-37 < temperature < 1e37:
         raise HpdError(what, 1, "a temperature above 0")
     if not 0 <= top <= min(V, 32):
         raise HpdError(what, 1 if top < 0 or top > V else 2, "0 to 32 alternatives, no more than there are tokens")
+    device = logits.device
     _need_current(what, logits, tokens)
-    R = tokens.numel()
-    with torch.cuda.stream(stream):
-        one = torch.empty((2,) + lead, dtype=torch.float32, device=logits.device)
-        ids = torch.empty(lead + (top,), dtype=torch.int32, device=logits.device) if top else None
-        lps = torch.empty(lead + (top,), dtype=torch.float32, device=logits.device) if top else None
-    logprob, entropy = one[0], one[1]
+    R, ids, lps = tokens.numel(), None, None
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        logprob, entropy = torch.empty((2,) + lead, dtype=torch.float32, device=device)
+        if top:
+            ids = torch.empty(lead + (top,), dtype=torch.int32, device=device)
+            lps = torch.empty(lead + (top,), dtype=torch.float32, device=device)
     a = hpd_token_logprobs_args(_ptr(logits), stride, _ptr(tokens), _ptr(logprob), _ptr(entropy), _ptr(ids), _ptr(lps),
-                                R, V, top, int(logits.dtype is torch.float32), 1.0 / temperature)
+                                R, V, top, logits.dtype is not bf, 1.0 / temperature)
     hpd_token_logprobs(a, _stream_handle(stream))
     return TokenLogprobs(logprob, entropy, ids, lps)
 
