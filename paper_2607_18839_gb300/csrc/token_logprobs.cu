@@ -17,10 +17,13 @@ namespace hpd {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kUnroll = 2;      // 16-byte loads of a thread at once, twice that on their way
+constexpr int kUnroll = 4;      // 16-byte loads of a thread on their way at once
 constexpr int kCtasPerSm = 5;
 constexpr int kMaxCluster = 8;  // CTAs of a row
 constexpr int kTop = 32;
+// A sum of weights beside the largest one's 1 below which that is left out of them: 2^-24 of
+// it is 2^-22 of the rest here.
+constexpr float kSure = 0.25f;
 constexpr int kGroups = 64;      // of threads, whose maxima bound the top values from below
 constexpr int kCandidates = 1024;
 constexpr int kLogpSms = 152;
@@ -87,77 +90,71 @@ struct Vec<float> {
   }
 };
 
-// Of some values: the largest; with d = (x - m) scale log2(e) the sums of 2^d, one of the
-// largest values left out, and of 2^d d.  NaN among them is in `rest`.
+// Of some values: the largest; with d = (x - m) scale log2(e) the sums of 2^d, but for one
+// of the largest values (whose 2^d is 1), and of 2^d d.  NaN among them is in `rest`.
 struct Sums {
   float m, rest, mean;
 };
+constexpr float kWindow = 60.f, kNothing = -300.f;  // log2: 2^kNothing is 0
 
-// A thread's values.  Sums are taken against a base, the largest of its first pieces, which
-// moves only when a value passes it by 2^kWindow; the piece with the largest value so far
-// is kept apart, as what it is, and its values are added when another takes its place: no
-// branch depends on where a row's maxima stand (a branch at every new maximum had two in
-// three of the pieces in both of its sides).
+__device__ __forceinline__ float max_nan(float a, float b) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
+  return a;
+}
+
+// A thread's values.  Sums are taken against a base, the largest of its first piece, which
+// moves only when a value passes it by 2^kWindow: no branch depends on where a row's
+// maxima stand (one at every new maximum had two in three of the pieces in both of its
+// sides).  All values are in the sums; of a row whose other values have little weight
+// beside the largest, whoever has that sums once more without it.
 template <class T>
 struct Running {
-  static constexpr float kWindow = 60.f, kNothing = -300.f;  // log2: 2^kNothing is 0
-  float m, second;    // the largest value, and that of the other pieces than its own
-  float base;
-  float2 sum, mean;   // of 2^d and 2^d d, d against the base
-  uint4 best;         // the piece that holds m, and the index of its first value
-  int best_at;
+  float m;            // the largest value
+  float base, limit;  // and what moves it
   uint32_t floor2;    // bf16: what is below has 2^d = 0
+  float2 sum, mean;   // of 2^d and 2^d d, d against the base
 
   __device__ __forceinline__ void set_base(float b, float c) {
     base = b;
+    limit = b + kWindow / c;
     // (2^-6 of the base: the floor stays that far below it once rounded)
     const float f = b - fmaxf(-kNothing / c, fabsf(b) * 0x1p-6f);
     floor2 = pack_bf16x2(f, f);
   }
   __device__ __forceinline__ void start(float first, float c) {
-    m = second = -inf();
+    m = -inf();
     sum = mean = make_float2(0.f, 0.f);
-    constexpr uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
-    best = make_uint4(none, none, none, none);
-    best_at = 0;
     set_base(fabsf(first) < inf() ? first : 0.f, c);
   }
-  // (0 times minus infinity is kept out: by the floor, or of d itself where that would not be
-  // a number of the type)
-  __device__ __forceinline__ void add(const uint4 &v, float c) {
-    const float2 nbase2 = make_float2(-base, -base), c2 = make_float2(c, c);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    const bool far = sizeof(T) == 4 || base < -1e37f;
-#pragma unroll
-    for (int i = 0; i < 4; i += sizeof(T) == 2 ? 1 : 2) {
-      float2 x;
-      if constexpr (sizeof(T) == 2) {
-        uint32_t u = w[i];
-        if (!far) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(u) : "r"(floor2));
-        x = make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
-      } else {
-        x = make_float2(__uint_as_float(w[i]), __uint_as_float(w[i + 1]));
-      }
-      float2 d = __fmul2_rn(__fadd2_rn(x, nbase2), c2);
-      if (far) {
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(d.x) : "f"(kNothing));
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(d.y) : "f"(kNothing));
-      }
-      const float2 e = make_float2(fast_exp2(d.x), fast_exp2(d.y));
-      sum = __fadd2_rn(sum, e);
-      mean = __ffma2_rn(e, d, mean);
-    }
+  __device__ __forceinline__ void add2(float2 x, bool floored, float c) {
+    float2 d = __fmul2_rn(__fadd2_rn(x, make_float2(-base, -base)), make_float2(c, c));
+    // (0 times minus infinity is kept out)
+    if (!floored) d = make_float2(max_nan(d.x, kNothing), max_nan(d.y, kNothing));
+    const float2 e = make_float2(fast_exp2(d.x), fast_exp2(d.y));
+    sum = __fadd2_rn(sum, e);
+    mean = __ffma2_rn(e, d, mean);
   }
-  __device__ __forceinline__ void take(const uint4 &v, int at, float c) {
+  __device__ __forceinline__ void take(const uint4 &v, float c) {
     const float largest = Vec<T>::largest(v);
-    if ((largest - base) * c > kWindow && largest < inf()) raise(largest, c);
-    const bool better = largest > m;
-    second = fmaxf(second, fminf(m, largest));  // (NaN, of a piece of nothing else, is passed over)
-    const uint4 w = make_uint4(better ? best.x : v.x, better ? best.y : v.y, better ? best.z : v.z, better ? best.w : v.w);
-    best = make_uint4(better ? v.x : best.x, better ? v.y : best.y, better ? v.z : best.z, better ? v.w : best.w);
-    best_at = better ? at : best_at;
-    m = better ? largest : m;
-    add(w, c);
+    if (largest > limit) raise(largest, c);
+    m = fmaxf(m, largest);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (sizeof(T) == 4) {
+      add2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), false, c);
+      add2(make_float2(__uint_as_float(w[2]), __uint_as_float(w[3])), false, c);
+    } else if (base > -1e37f) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t u = w[i];
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(u) : "r"(floor2));
+        // (a product and not a shift: another pipe)
+        add2(make_float2(__uint_as_float(u * 65536u), __uint_as_float(u & 0xffff0000u)), true, c);
+      }
+    } else {  // no floor below the base is a bf16 number
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        add2(make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), false, c);
+    }
   }
   __device__ __forceinline__ void raise(float to, float c) {
     const float d = fmaxf((base - to) * c, kNothing), w = fast_exp2(d);
@@ -166,37 +163,27 @@ struct Running {
     sum = make_float2(w * sum.x, w * sum.y);
     set_base(to, c);
   }
+  // The sums against the thread's own largest value, that one among them.
   __device__ __forceinline__ Sums result(float c) const {
     Sums s{m, sum.x + sum.y, mean.x + mean.y};
     if (m == -inf()) return s;
     const float d = fmaxf((base - m) * c, kNothing), w = fast_exp2(d);
     s.mean = w * fmaf(d, s.rest, s.mean);
     s.rest *= w;
-    float x[Vec<T>::kN];
-    Vec<T>::unpack(best, x);
-    bool skip = true;  // one of the largest
-#pragma unroll
-    for (int i = 0; i < Vec<T>::kN; ++i) {
-      const bool here = skip && x[i] == m;
-      skip = skip && !here;
-      float e_d = (x[i] - m) * c;
-      asm("max.NaN.f32 %0, %0, %1;" : "+f"(e_d) : "f"(kNothing));
-      const float e = here ? 0.f : fast_exp2(e_d);
-      s.rest += e;
-      s.mean = fmaf(e, e_d, s.mean);
-    }
     return s;
   }
 };
+
+// Of two parts: kWhole: with each one's largest value in its `rest`, else without.
+template <bool kWhole>
 __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   if (b.m > a.m) {
     const Sums t = a;
     a = b;
     b = t;
   }
-  const float m = a.m;
   if (b.m > -inf()) {
-    const float d = (b.m - m) * c, w = fast_exp2(d), z = 1.f + b.rest;
+    const float d = (b.m - a.m) * c, w = fast_exp2(d), z = kWhole ? b.rest : 1.f + b.rest;
     a.rest += w * z;
     if (w != 0.f) a.mean += w * fmaf(d, z, b.mean);
   } else {
@@ -212,13 +199,14 @@ __device__ __forceinline__ Sums join_warp(Sums s, float c) {
     t.rest = __shfl_xor_sync(0xffffffffu, s.rest, o);
     t.mean = __shfl_xor_sync(0xffffffffu, s.mean, o);
     // (the same order in both lanes)
-    s = threadIdx.x & o ? join(t, s, c) : join(s, t, c);
+    s = threadIdx.x & o ? join<true>(t, s, c) : join<true>(s, t, c);
   }
   return s;
 }
 
 struct LogpShared {
   Sums warp[kWarps];
+  float2 again[kWarps];
   float group[kGroups];
   float least;     // a lower bound of the last of the top values
   int found;       // candidates, some perhaps beyond their room
@@ -359,39 +347,28 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
       w = make_uint4(0xff800000u | *reinterpret_cast<const uint16_t *>(s.row + i), 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
     else
       w = make_uint4(__float_as_uint(s.row[i]), 0xff800000u, 0xff800000u, 0xff800000u);
-    run.take(w, i, c);
+    run.take(w, c);
   };
-  // (the next pieces on their way while these are summed)
-  constexpr int kStep = kThreads * kUnroll;
-  uint4 w[2][kUnroll];
-  auto load = [&](int v, uint4 *w) {
+  bool started = false;
+#pragma unroll 1
+  for (int v = s.v0 + tid; v < s.v1; v += kThreads * kUnroll) {
+    uint4 w[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
       if (v + u * kThreads < s.v1) w[u] = s.piece(v + u * kThreads);
-  };
-  auto take = [&](int v, const uint4 *w) {
+    if (!started) {
+      run.start(V::largest(w[0]), c);
+      started = true;
+    }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       if (v + u * kThreads >= s.v1) break;
-      run.take(w[u], s.index(v + u * kThreads), c);
+      run.take(w[u], c);
     }
-  };
-  const bool started = s.v0 + tid < s.v1;
-  int v = s.v0 + tid;
-  load(v, w[0]);
-  if (started) run.start(V::largest(w[0][0]), c);
-#pragma unroll 1
-  while (v < s.v1) {
-    load(v + kStep, w[1]);
-    take(v, w[0]);
-    load(v + 2 * kStep, w[0]);
-    take(v + kStep, w[1]);
-    v += 2 * kStep;
   }
   if (!started) run.start(0.f, c);
   if (tid < s.head && rank == 0) single(tid);
   if (tid < s.tail) single(s.tail0 + tid);
-  Sums sums = run.result(c);
   if constexpr (kAlternatives) {
     float g = run.m;
 #pragma unroll
@@ -399,9 +376,57 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     if (lane % (kThreads / kGroups) == 0) sh.group[tid / (kThreads / kGroups)] = g;
     if (tid == 0) sh.found = 0;
   }
-  sums = join_warp(sums, c);
-  if (lane == 0) sh.warp[warp] = sums;
+  const Sums own = run.result(c);
+  Sums all = join_warp(own, c);
+  if (lane == 0) sh.warp[warp] = all;
   __syncthreads();
+  all = sh.warp[0];
+#pragma unroll 1
+  for (int w = 1; w < kWarps; ++w) all = join<true>(all, sh.warp[w], c);
+  all.rest -= 1.f;
+  // Calls f(value, index) for the share's values that thread t of this warp has, by n lanes
+  // (a power of two) from its first one on; reach: for pieces with such a largest value alone.
+  auto again = [&](int t, int sub, int n, float reach, auto f) {
+    if (sub == 0 && t < s.head && rank == 0) f(static_cast<float>(s.row[t]), t);
+    if (sub == n - 1 && t < s.tail) f(static_cast<float>(s.row[s.tail0 + t]), s.tail0 + t);
+#pragma unroll 1
+    for (int v = s.v0 + t + sub * kThreads; v < s.v1; v += n * kThreads) {
+      const uint4 w = s.piece(v);
+      if (V::largest(w) < reach) continue;
+      float x[V::kN];
+      V::unpack(w, x);
+#pragma unroll
+      for (int i = 0; i < V::kN; ++i) f(x[i], s.index(v) + i);
+    }
+  };
+  if (all.rest < kSure) {  // (as for all of the CTA) the largest value leaves its sum too few digits
+    const float m = all.m;
+    float2 part = make_float2(0.f, 0.f);
+    if (own.m > -inf() && own.m < m) {
+      const float d = (own.m - m) * c, w = fast_exp2(d);
+      part = make_float2(w * own.rest, w == 0.f ? 0.f : w * fmaf(d, own.rest, own.mean));
+    }
+    const unsigned has = __ballot_sync(0xffffffffu, own.m == m);  // one thread of the CTA
+    if (has)
+      again(warp * 32 + __ffs(has) - 1, lane, 32, -inf(), [&](float x, int) {
+        const float d = fmaxf((x - m) * c, kNothing), e = x == m ? 0.f : fast_exp2(d);
+        part.x += e;
+        part.y = fmaf(e, d, part.y);
+      });
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      part.x += __shfl_xor_sync(0xffffffffu, part.x, o);
+      part.y += __shfl_xor_sync(0xffffffffu, part.y, o);
+    }
+    if (lane == 0) sh.again[warp] = part;
+    __syncthreads();
+    all.rest = all.mean = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      all.rest += sh.again[w].x;
+      all.mean += sh.again[w].y;
+    }
+  }
 
   if constexpr (kAlternatives) {
     const int top = a.top;
@@ -423,29 +448,14 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     auto look = [&](float x, int i) {
       if (reaches(x)) propose(sh, x, i);
     };
-    // a thread's best piece is at hand; those with another one that reaches the bound are
-    // looked through
-    unsigned hot = __ballot_sync(0xffffffffu, reaches(run.second));
-    if (reaches(run.m) && !reaches(run.second)) {
-      float x[V::kN];
-      V::unpack(run.best, x);
-#pragma unroll
-      for (int i = 0; i < V::kN; ++i) look(x[i], run.best_at + i);
-    }
+    // threads whose largest value reaches the bound, some at once with a part of the warp each
+    unsigned hot = __ballot_sync(0xffffffffu, reaches(run.m));
+    int n = 1;  // lanes for each: as many as a thread has pieces
+    while (n < 32 && n * kThreads < s.v1 - s.v0) n *= 2;
     while (hot) {
-      const int t = warp * 32 + __ffs(hot) - 1;  // the thread whose values the warp looks at
-      hot &= hot - 1;
-      if (lane == 0 && t < s.head && rank == 0) look(static_cast<float>(s.row[t]), t);
-      if (lane == 1 && t < s.tail) look(static_cast<float>(s.row[s.tail0 + t]), s.tail0 + t);
-#pragma unroll 1
-      for (int v = s.v0 + t + lane * kThreads; v < s.v1; v += 32 * kThreads) {
-        const uint4 w = s.piece(v);
-        if (!reaches(V::largest(w))) continue;
-        float x[V::kN];
-        V::unpack(w, x);
-#pragma unroll
-        for (int i = 0; i < V::kN; ++i) look(x[i], s.index(v) + i);
-      }
+      const int t = __fns(hot, 0, lane / n + 1);
+      if (t >= 0 && t < 32) again(warp * 32 + t, lane & (n - 1), n, least, look);
+      for (int i = 0; i < 32 / n; ++i) hot &= hot - 1;
     }
     __syncthreads();
     if (sh.found > kCandidates) select_by_halves(sh, s, top);
@@ -474,17 +484,16 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     cg::cluster_group cluster = cg::this_cluster();
     cluster_wait();  // (the first CTA runs: its shared memory may be written)
     LogpShared *first = cluster.map_shared_rank(&sh, 0);
-    if (tid == 0) {
-      Sums t = sh.warp[0];
-      for (int w = 1; w < kWarps; ++w) t = join(t, sh.warp[w], c);
-      first->part[rank] = t;
-    }
+    if (tid == 0) first->part[rank] = all;
     if (kAlternatives && tid < a.top) first->list[rank][tid] = sh.best[tid];
     cluster.sync();
     if (rank != 0) return;
   }
-  Sums all = ctas > 1 ? sh.part[0] : sh.warp[0];
-  for (int w = 1; w < (ctas > 1 ? ctas : kWarps); ++w) all = join(all, ctas > 1 ? sh.part[w] : sh.warp[w], c);
+  if (ctas > 1) {
+    all = sh.part[0];
+#pragma unroll 1
+    for (int w = 1; w < ctas; ++w) all = join<false>(all, sh.part[w], c);
+  }
   if (!(fabsf(all.m) < inf())) all.rest = nan();
   const float log_z = log1pf(all.rest);
   auto logprob = [&](float x) { return all.rest == all.rest ? (x - all.m) * a.scale - log_z : nan(); };
