@@ -495,6 +495,9 @@ def pmtp_accept(logits, drafts, stream=None):
     return out_tokens, acc
 
 
+_NO_STREAM = contextlib.nullcontext()
+
+
 class TokenLogprobs(NamedTuple):
     """What token_logprobs returns, in the shape of its tokens; top_tokens and
     top_logprobs have one more extent and are None with top = 0."""
@@ -538,14 +541,15 @@ def token_logprobs(logits, tokens, top=0, temperature=1.0, stream=None) -> Token
         raise HpdError(what, 1 if top < 0 or top > V else 2, "0 to 32 alternatives, no more than there are tokens")
     device = logits.device
     _need_current(what, logits, tokens)
-    R, ids, lps = tokens.numel(), None, None
-    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-        logprob, entropy = torch.empty((2,) + lead, dtype=torch.float32, device=device)
+    empty, f32, ids, lps = torch.empty, torch.float32, None, None
+    with _NO_STREAM if stream is None else torch.cuda.stream(stream):
+        logprob = empty(lead, dtype=f32, device=device)
+        entropy = empty(lead, dtype=f32, device=device)
         if top:
-            ids = torch.empty(lead + (top,), dtype=torch.int32, device=device)
-            lps = torch.empty(lead + (top,), dtype=torch.float32, device=device)
-    a = hpd_token_logprobs_args(_ptr(logits), stride, _ptr(tokens), _ptr(logprob), _ptr(entropy), _ptr(ids), _ptr(lps),
-                                R, V, top, logits.dtype is not bf, 1.0 / temperature)
+            ids = empty((*lead, top), dtype=torch.int32, device=device)
+            lps = empty((*lead, top), dtype=f32, device=device)
+    a = hpd_token_logprobs_args(logits.data_ptr(), stride, tokens.data_ptr(), logprob.data_ptr(), entropy.data_ptr(),
+                                _ptr(ids), _ptr(lps), tokens.numel(), V, top, logits.dtype is not bf, 1.0 / temperature)
     hpd_token_logprobs(a, _stream_handle(stream))
     return TokenLogprobs(logprob, entropy, ids, lps)
 
