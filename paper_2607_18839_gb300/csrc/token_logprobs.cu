@@ -55,6 +55,10 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+__device__ __forceinline__ float value_of(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
+
 // 16 bytes of a row, and their largest value (NaN only if there is nothing else).
 template <class T>
 struct Vec;
@@ -69,11 +73,17 @@ struct Vec<__nv_bfloat16> {
       x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
-  static __device__ __forceinline__ float largest(const uint4 &v) {
-    auto h2 = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162 *>(&w); };
-    const __nv_bfloat162 m = __hmax2(__hmax2(h2(v.x), h2(v.y)), __hmax2(h2(v.z), h2(v.w)));
-    const uint32_t w = *reinterpret_cast<const uint32_t *>(&m);
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    asm("max.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    return a;
+  }
+  static __device__ __forceinline__ uint32_t fold(const uint4 &v) { return max2(max2(v.x, v.y), max2(v.z, v.w)); }
+  static __device__ __forceinline__ float of_fold(uint32_t w) {
     return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+  static __device__ __forceinline__ float largest(const uint4 &v) { return of_fold(fold(v)); }
+  static __device__ __forceinline__ float largest4(const uint4 *v) {
+    return of_fold(max2(max2(fold(v[0]), fold(v[1])), max2(fold(v[2]), fold(v[3]))));
   }
 };
 template <>
@@ -87,6 +97,9 @@ struct Vec<float> {
   }
   static __device__ __forceinline__ float largest(const uint4 &v) {
     return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
+  static __device__ __forceinline__ float largest4(const uint4 *v) {
+    return fmaxf(fmaxf(largest(v[0]), largest(v[1])), fmaxf(largest(v[2]), largest(v[3])));
   }
 };
 
@@ -110,16 +123,19 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 template <class T>
 struct Running {
   float m;            // the largest value
-  float base, limit;  // and what moves it
+  float base, limit;  // and what moves it (NaN: bf16, and no floor below the base is a number)
   uint32_t floor2;    // bf16: what is below has 2^d = 0
   float2 sum, mean;   // of 2^d and 2^d d, d against the base
 
   __device__ __forceinline__ void set_base(float b, float c) {
     base = b;
     limit = b + kWindow / c;
-    // (2^-6 of the base: the floor stays that far below it once rounded)
-    const float f = b - fmaxf(-kNothing / c, fabsf(b) * 0x1p-6f);
-    floor2 = pack_bf16x2(f, f);
+    if (sizeof(T) == 2) {
+      // (2^-6 of the base: the floor stays that far below it once rounded)
+      const float f = b - fmaxf(-kNothing / c, fabsf(b) * 0x1p-6f);
+      floor2 = pack_bf16x2(f, f);
+      if (b < -1e37f) limit = nan();
+    }
   }
   __device__ __forceinline__ void start(float first, float c) {
     m = -inf();
@@ -134,27 +150,36 @@ struct Running {
     sum = __fadd2_rn(sum, e);
     mean = __ffma2_rn(e, d, mean);
   }
-  __device__ __forceinline__ void take(const uint4 &v, float c) {
-    const float largest = Vec<T>::largest(v);
-    if (largest > limit) raise(largest, c);
-    m = fmaxf(m, largest);
+  template <bool kFloored>
+  __device__ __forceinline__ void add(const uint4 &v, float c) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     if constexpr (sizeof(T) == 4) {
       add2(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), false, c);
       add2(make_float2(__uint_as_float(w[2]), __uint_as_float(w[3])), false, c);
-    } else if (base > -1e37f) {
+    } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t u = w[i];
-        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(u) : "r"(floor2));
+        if (kFloored) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(u) : "r"(floor2));
         // (a product and not a shift: another pipe)
-        add2(make_float2(__uint_as_float(u * 65536u), __uint_as_float(u & 0xffff0000u)), true, c);
+        add2(make_float2(__uint_as_float(u * 65536u), __uint_as_float(u & 0xffff0000u)), kFloored, c);
       }
-    } else {  // no floor below the base is a bf16 number
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        add2(make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), false, c);
     }
+  }
+  // N pieces, the largest of whose values is given.
+  template <int N>
+  __device__ __forceinline__ void take(const uint4 *v, float largest, float c) {
+    m = fmaxf(m, largest);
+    if (!(largest <= limit)) {
+      if (largest > base + kWindow / c) raise(largest, c);
+      if (limit != limit) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) add<false>(v[i], c);
+        return;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) add<true>(v[i], c);
   }
   __device__ __forceinline__ void raise(float to, float c) {
     const float d = fmaxf((base - to) * c, kNothing), w = fast_exp2(d);
@@ -174,8 +199,7 @@ struct Running {
   }
 };
 
-// Of two parts: kWhole: with each one's largest value in its `rest`, else without.
-template <bool kWhole>
+// Of two parts, each without one of its largest values.
 __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   if (b.m > a.m) {
     const Sums t = a;
@@ -183,7 +207,7 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
     b = t;
   }
   if (b.m > -inf()) {
-    const float d = (b.m - a.m) * c, w = fast_exp2(d), z = kWhole ? b.rest : 1.f + b.rest;
+    const float d = (b.m - a.m) * c, w = fast_exp2(d), z = 1.f + b.rest;
     a.rest += w * z;
     if (w != 0.f) a.mean += w * fmaf(d, z, b.mean);
   } else {
@@ -191,15 +215,19 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
   }
   return a;
 }
-__device__ __forceinline__ Sums join_warp(Sums s, float c) {
+// Of the parts of n lanes (a power of two), each with its largest value in `rest`.
+__device__ __forceinline__ Sums join_lanes(Sums s, int n, float c) {
+  float m = s.m;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    Sums t;
-    t.m = __shfl_xor_sync(0xffffffffu, s.m, o);
-    t.rest = __shfl_xor_sync(0xffffffffu, s.rest, o);
-    t.mean = __shfl_xor_sync(0xffffffffu, s.mean, o);
-    // (the same order in both lanes)
-    s = threadIdx.x & o ? join<true>(t, s, c) : join<true>(s, t, c);
+  for (int o = 1; o < n; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float d = s.m == m ? 0.f : fmaxf((s.m - m) * c, kNothing), w = fast_exp2(d);
+  s.mean = w * fmaf(d, s.rest, s.mean);
+  s.rest *= w;
+  s.m = m;
+#pragma unroll
+  for (int o = 1; o < n; o <<= 1) {
+    s.rest += __shfl_xor_sync(0xffffffffu, s.rest, o);
+    s.mean += __shfl_xor_sync(0xffffffffu, s.mean, o);
   }
   return s;
 }
@@ -207,8 +235,8 @@ __device__ __forceinline__ Sums join_warp(Sums s, float c) {
 struct LogpShared {
   Sums warp[kWarps];
   float2 again[kWarps];
-  float group[kGroups];
-  float least;     // a lower bound of the last of the top values
+  uint32_t group[kGroups];  // keys of the groups' maxima, made different by the groups' numbers
+  uint32_t least;  // a lower bound of the last of the top values, as a key
   int found;       // candidates, some perhaps beyond their room
   int count;       // of a scan
   int per_warp[kWarps];
@@ -278,7 +306,7 @@ __device__ __noinline__ void propose_equal(LogpShared &sh, const Share<T> &s, fl
 // share each time, then those above it and the first of its equals.
 template <class T>
 __device__ __noinline__ void select_by_halves(LogpShared &sh, const Share<T> &s, int top) {
-  uint32_t lo = key_of(sh.least), hi = 0xffffffffu;
+  uint32_t lo = sh.least, hi = 0xffffffffu;
   while (lo < hi) {
     const uint32_t mid = lo + (hi - lo) / 2 + 1;
     __syncthreads();
@@ -299,7 +327,7 @@ __device__ __noinline__ void select_by_halves(LogpShared &sh, const Share<T> &s,
   });
   __syncthreads();
   const int need = top - sh.found;
-  propose_equal(sh, s, __uint_as_float(lo & 0x80000000u ? lo & 0x7fffffffu : ~lo), need);
+  propose_equal(sh, s, value_of(lo), need);
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
@@ -347,42 +375,49 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
       w = make_uint4(0xff800000u | *reinterpret_cast<const uint16_t *>(s.row + i), 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
     else
       w = make_uint4(__float_as_uint(s.row[i]), 0xff800000u, 0xff800000u, 0xff800000u);
-    run.take(w, c);
+    run.template take<1>(&w, V::largest(w), c);
   };
-  bool started = false;
-#pragma unroll 1
-  for (int v = s.v0 + tid; v < s.v1; v += kThreads * kUnroll) {
+  int v = s.v0 + tid;
+  if (v < s.v1) {
     uint4 w[kUnroll];
+    bool started = false;
+#pragma unroll 1
+    for (; v + (kUnroll - 1) * kThreads < s.v1; v += kUnroll * kThreads) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if (v + u * kThreads < s.v1) w[u] = s.piece(v + u * kThreads);
-    if (!started) {
-      run.start(V::largest(w[0]), c);
+      for (int u = 0; u < kUnroll; ++u) w[u] = s.piece(v + u * kThreads);
+      const float largest = V::largest4(w);
+      if (!started) run.start(largest, c);
       started = true;
+      run.template take<kUnroll>(w, largest, c);
     }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (v + u * kThreads >= s.v1) break;
-      run.take(w[u], c);
+#pragma unroll 1
+    for (; v < s.v1; v += kThreads) {
+      w[0] = s.piece(v);
+      const float largest = V::largest(w[0]);
+      if (!started) run.start(largest, c);
+      started = true;
+      run.template take<1>(w, largest, c);
     }
+  } else {
+    run.start(0.f, c);
   }
-  if (!started) run.start(0.f, c);
   if (tid < s.head && rank == 0) single(tid);
   if (tid < s.tail) single(s.tail0 + tid);
   if constexpr (kAlternatives) {
     float g = run.m;
 #pragma unroll
     for (int o = 1; o < kThreads / kGroups; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
-    if (lane % (kThreads / kGroups) == 0) sh.group[tid / (kThreads / kGroups)] = g;
+    if (lane % (kThreads / kGroups) == 0) {
+      const int k = tid / (kThreads / kGroups);
+      sh.group[k] = (key_of(g) & ~static_cast<uint32_t>(kGroups - 1)) | k;
+    }
     if (tid == 0) sh.found = 0;
   }
   const Sums own = run.result(c);
-  Sums all = join_warp(own, c);
+  Sums all = join_lanes(own, 32, c);
   if (lane == 0) sh.warp[warp] = all;
   __syncthreads();
-  all = sh.warp[0];
-#pragma unroll 1
-  for (int w = 1; w < kWarps; ++w) all = join<true>(all, sh.warp[w], c);
+  all = join_lanes(sh.warp[lane % kWarps], kWarps, c);
   all.rest -= 1.f;
   // Calls f(value, index) for the share's values that thread t of this warp has, by n lanes
   // (a power of two) from its first one on; reach: for pieces with such a largest value alone.
@@ -433,17 +468,21 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     if (tid < top) sh.best[tid] = Place{nan(), -1};
     {  // the top-th largest of the groups' maxima, a group's place by four threads
       constexpr int kPer = kThreads / kGroups;
-      const Place p{sh.group[tid / kPer], tid / kPer};
+      const uint32_t key = sh.group[tid / kPer];
       int ahead = 0;
 #pragma unroll
-      for (int j = tid % kPer; j < kGroups; j += kPer) ahead += before(Place{sh.group[j], j}, p);
+      for (int j = 0; j < kGroups / kPer; j += 4) {
+        const uint4 k = *reinterpret_cast<const uint4 *>(sh.group + tid % kPer * (kGroups / kPer) + j);
+        ahead += (k.x > key) + (k.y > key) + (k.z > key) + (k.w > key);
+      }
 #pragma unroll
       for (int o = 1; o < kPer; o <<= 1) ahead += __shfl_xor_sync(0xffffffffu, ahead, o);
-      if (tid % kPer == 0 && ahead == top - 1) sh.least = p.x;
+      if (tid % kPer == 0 && ahead == top - 1) sh.least = key & ~static_cast<uint32_t>(kGroups - 1);
     }
     __syncthreads();
-    const float least = sh.least;
-    const bool any = least > -inf();  // (else fewer than `top` groups have a value above -inf: those are looked for)
+    // (else fewer than `top` groups have a value above -inf: those are looked for)
+    const bool any = sh.least >= key_of(-3.4028235e38f);
+    const float least = any ? value_of(sh.least) : -inf();
     auto reaches = [&](float x) { return any ? x >= least : x > least; };
     auto look = [&](float x, int i) {
       if (reaches(x)) propose(sh, x, i);
@@ -452,10 +491,14 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     unsigned hot = __ballot_sync(0xffffffffu, reaches(run.m));
     int n = 1;  // lanes for each: as many as a thread has pieces
     while (n < 32 && n * kThreads < s.v1 - s.v0) n *= 2;
+    const int sub = lane & (n - 1);
     while (hot) {
-      const int t = __fns(hot, 0, lane / n + 1);
-      if (t >= 0 && t < 32) again(warp * 32 + t, lane & (n - 1), n, least, look);
-      for (int i = 0; i < 32 / n; ++i) hot &= hot - 1;
+      int t = -1;  // the one of this lane's part
+      for (int i = 0; i < 32 && hot; i += n) {
+        if (lane - sub == i) t = __ffs(hot) - 1;
+        hot &= hot - 1;
+      }
+      if (t >= 0) again(warp * 32 + t, sub, n, least, look);
     }
     __syncthreads();
     if (sh.found > kCandidates) select_by_halves(sh, s, top);
@@ -492,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
   if (ctas > 1) {
     all = sh.part[0];
 #pragma unroll 1
-    for (int w = 1; w < ctas; ++w) all = join<false>(all, sh.part[w], c);
+    for (int w = 1; w < ctas; ++w) all = join(all, sh.part[w], c);
   }
   if (!(fabsf(all.m) < inf())) all.rest = nan();
   const float log_z = log1pf(all.rest);
@@ -516,8 +559,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     if (tid < ctas * top) {
       const Place p = sh.list[tid / top][tid % top];
       int ahead = 0;
-      for (int w = 0; w < ctas; ++w)
-        for (int j = 0; j < top; ++j) ahead += before(sh.list[w][j], p);
+      for (int w = 0; w < ctas && ahead < top; ++w)  // (each in order)
+        for (int j = 0; j < top && before(sh.list[w][j], p); ++j) ++ahead;
       if (p.i >= 0 && ahead < top) sh.best[ahead] = p;
     }
     __syncthreads();
