@@ -246,10 +246,8 @@ inline cudaError_t prefer_l1(K *kernel, std::atomic<uint64_t> &done, int percent
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_acq_rel);
   return e;
 }
-// Host checks of an hpd_qk_norm_rope call, and its launch (T > 0; queries_only: keys,
-// values and the caches are left alone).
+// Host checks of an hpd_qk_norm_rope call.
 hpd_status check_norm_rope(const hpd_qk_norm_rope_args *a);
-cudaError_t launch_norm_rope(const hpd_qk_norm_rope_args *a, bool queries_only, cudaStream_t s);
 // Host checks of an hpd_chunk_attn call.
 hpd_status check_chunk_attn(const hpd_chunk_attn_args *a);
 // Remember `e` for hpd_last_cuda_error() and return HPD_ERR_CUDA.
