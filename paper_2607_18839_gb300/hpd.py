@@ -648,9 +648,9 @@ def _need_current(what: str, *tensors):
     """A launch goes to the current device: tensors of another one are refused."""
     import torch
     here = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t.get_device() != here:
-            raise HpdError(what, 1, f"a tensor on {t.device}, while device {here} is the current one")
+    if {here} != {t.get_device() for t in tensors}:
+        raise HpdError(what, 1, f"tensors on {', '.join(str(t.device) for t in tensors)}, while device {here} is the "
+                                "current one")
 
 
 def rope_table(max_pos: int, D: int, theta: float = 1e6, device="cuda"):
@@ -784,9 +784,11 @@ class QkNormRope:
             _need("QkNormRope", k_cache, kind, (None, 16, H_kv, D))
             _need("QkNormRope", v_cache, kind, shape)
         if coded:
-            for t in (k_scale, v_scale):
-                if t is None or not _is(t, self._f32, (pages, H_kv)):
-                    _need("QkNormRope", t, self._f32, (pages, H_kv))
+            one = (pages, H_kv)
+            if k_scale is None or v_scale is None or not _is(k_scale, self._f32, one) or \
+                    not _is(v_scale, self._f32, one):
+                _need("QkNormRope", k_scale, self._f32, one)
+                _need("QkNormRope", v_scale, self._f32, one)
             _need_current("QkNormRope", qkv, k_cache, v_cache, k_scale, v_scale)
         if q_out is None:
             if self._q is None or self._q.shape[0] < T:
