@@ -118,6 +118,7 @@ template <>
 struct Rings<true> {
   static constexpr int kStages = 4, kVStages = 2;  // of K's codes, and of V as f16
   static constexpr int kCodeStages = 4;            // of V's codes
+  static_assert(kCodeStages == kStages, "their barriers are made together");
 };
 constexpr int kMaxStages = 4;
 constexpr int kScaleBlocks = 8;  // blocks whose scales are held
@@ -589,6 +590,60 @@ __device__ __forceinline__ bool softmax_share_fp8(uint32_t s_addr, int copy, int
   return !(val < kLeastVal) || scale == 0.f;
 }
 
+// A row of Q (at src, if it is one) in two e4m3 parts at q_addr, one behind the other: q 2^t =
+// q1 + q2 with the row's largest value from 2^7 to 2^8.  q1 has four of bf16's eight bits, and
+// what is left of them fits into q2, but for values below 2^-9 of the largest, which keep 2^-17
+// of that.  factor: 2^-t; NaN for a row with a value that is not finite.
+template <int D>
+__device__ __forceinline__ void part_row(const uint4 *src, bool valid, uint32_t q_addr, float *factor) {
+  unsigned most = 0u;
+  {
+    uint4 x[D / 8];
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) x[i] = valid ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+      most = __vmaxu2(__vmaxu2(most, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu)),
+                      __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
+  }
+  most = max(most & 0xffffu, most >> 16);
+  const int t = min(134 - static_cast<int>(most >> 7), 126);
+  const float up = __uint_as_float(static_cast<uint32_t>(127 + t) << 23);
+  *factor =
+      most >= 0x7f80u ? __int_as_float(0x7fffffff) : __uint_as_float(static_cast<uint32_t>(127 - t) << 23);
+  uint4 next[4];
+  auto fetch = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) next[i] = valid ? src[i0 + i] : make_uint4(0u, 0u, 0u, 0u);
+  };
+  fetch(0);
+#pragma unroll 1
+  for (int i0 = 0; i0 < D / 8; i0 += 4) {  // 32 columns at a time, from L1 this time
+    uint32_t c1[8], c2[8];
+    uint4 now[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) now[i] = next[i];
+    if (i0 + 4 < D / 8) fetch(i0 + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t ab[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t a = ab[2 * e], b = ab[2 * e + 1];
+        const float q0 = __uint_as_float(a << 16) * up, q1 = __uint_as_float(a & 0xffff0000u) * up;
+        const float q2 = __uint_as_float(b << 16) * up, q3 = __uint_as_float(b & 0xffff0000u) * up;
+        c1[2 * i + e] = to_codes4(q0, q1, q2, q3);
+        float2 f, g;
+        of_codes4(c1[2 * i + e], f, g);
+        c2[2 * i + e] = to_codes4(q0 - f.x, q1 - f.y, q2 - g.x, q3 - g.y);
+      }
+    }
+    tmem_st8(q_addr + 2 * i0, c1);
+    tmem_st8(q_addr + D / 4 + 2 * i0, c2);
+  }
+  tmem_st_wait();
+}
+
 // 32 keys' codes at `from` as bf16 at `to`, both as the blocks hold them (of a unit that is
 // run again; out of line, as what is not in the blocks' loops is).
 template <int D>
@@ -642,41 +697,65 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
     sh.redo = 0u;
     sh.units_done = 0;
     sh.sieved_seq = 0;
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(bar(sh.k_full[s]), kFp8 ? 3 : 2);
-      mbar_init(bar(sh.k_empty[s]), 1);
+  }
+  if constexpr (!kFp8) {
+    if (tid == 0) {
+      for (int s = 0; s < kStages; ++s) {
+        mbar_init(bar(sh.k_full[s]), 2);
+        mbar_init(bar(sh.v_full[s]), 2);
+        mbar_init(bar(sh.k_empty[s]), 1);
+        mbar_init(bar(sh.v_empty[s]), 1);
+      }
+      for (int s = 0; s < kMetaSlots; ++s) {
+        mbar_init(bar(sh.meta_full[s]), 1);
+        mbar_init(bar(sh.meta_empty[s]), kMetaConsumers<kFp8>);
+        mbar_init(bar(sh.sums[s]), kSoftmaxWarps);
+      }
+      for (int s = 0; s < 2; ++s) {
+        mbar_init(bar(sh.s_full[s]), 1);
+        mbar_init(bar(sh.p_full[s][0]), kSoftmaxWarps);
+        mbar_init(bar(sh.p_full[s][1]), kSoftmaxWarps);
+        mbar_init(bar(sh.s_free[s]), 1);
+      }
+      mbar_init(bar(sh.taken), 1);
+      mbar_init(bar(sh.o_full), 1);
+      mbar_init(bar(sh.o_empty), kOutputWarps);
+      mbar_init(bar(sh.mma_done[0]), 1);
+      mbar_init(bar(sh.mma_done[1]), 1);
+      fence_mbar_init();
     }
-    for (int s = 0; s < kVStages; ++s) {
-      mbar_init(bar(sh.v_full[s]), kFp8 ? kWideWarps : 2);
+  } else if (tid < 32) {  // (a lane each: there are twice as many)
+    const int s = tid;
+    if (s < kStages) {
+      mbar_init(bar(sh.k_full[s]), 3);
+      mbar_init(bar(sh.k_empty[s]), 1);
+      mbar_init(bar(sh.code_full[s]), 2);
+      mbar_init(bar(sh.code_empty[s]), kWideWarps);
+    }
+    if (s < kVStages) {
+      mbar_init(bar(sh.v_full[s]), kWideWarps);
       mbar_init(bar(sh.v_empty[s]), 1);
     }
-    if constexpr (kFp8) {
-      for (int i = 0; i < Rings<true>::kCodeStages; ++i) {
-        mbar_init(bar(sh.code_full[i]), 2);
-        mbar_init(bar(sh.code_empty[i]), kWideWarps);
-      }
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(bar(sh.q_full[i]), kWideWarps);
-        mbar_init(bar(sh.q_free[i]), 1);
-      }
-      mbar_init(bar(sh.copied), kOutputWarps);
-    }
-    for (int s = 0; s < kMetaSlots; ++s) {
+    if (s < kMetaSlots) {
       mbar_init(bar(sh.meta_full[s]), 1);
       mbar_init(bar(sh.meta_empty[s]), kMetaConsumers<kFp8>);
       mbar_init(bar(sh.sums[s]), kSoftmaxWarps);
     }
-    for (int s = 0; s < 2; ++s) {
+    if (s < 2) {
       mbar_init(bar(sh.s_full[s]), 1);
       mbar_init(bar(sh.p_full[s][0]), kSoftmaxWarps);
       mbar_init(bar(sh.p_full[s][1]), kSoftmaxWarps);
       mbar_init(bar(sh.s_free[s]), 1);
+      mbar_init(bar(sh.q_full[s]), kWideWarps);
+      mbar_init(bar(sh.q_free[s]), 1);
+      mbar_init(bar(sh.mma_done[s]), 1);
     }
-    mbar_init(bar(sh.taken), 1);
-    mbar_init(bar(sh.o_full), 1);
-    mbar_init(bar(sh.o_empty), kOutputWarps);
-    mbar_init(bar(sh.mma_done[0]), 1);
-    mbar_init(bar(sh.mma_done[1]), 1);
+    if (s == 0) {
+      mbar_init(bar(sh.taken), 1);
+      mbar_init(bar(sh.o_full), 1);
+      mbar_init(bar(sh.o_empty), kOutputWarps);
+      mbar_init(bar(sh.copied), kOutputWarps);
+    }
     fence_mbar_init();
   }
   if (tid < 8) (&sh.max_seq[0][0])[tid] = 0;
@@ -711,10 +790,95 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
     fetch(lane);
     bool sorted = false;
     auto seq_at = [&](int i) { return kFp8 && sorted ? sh.g_order[i] : i; };
+    // A group of no more than 32 sequences, a lane each: what load_group does, in registers
+    // (which of a call's first microseconds has two less).
+    auto load_few = [&] {
+      const int count = p.S;
+      g0 = before = 0;
+      const int c0 = min(max(a0, 0), p.T), c1 = max(c0, min(a1, p.T)), Ls = min(max(len, 0), p.max_pages * kPage);
+      if (lane < count) {
+        if (a0 != c0 || a1 != c1) flag_error(p.err, HPD_DEVERR_BRANCH_CU);
+        if (Ls != len) flag_error(p.err, HPD_DEVERR_BRANCH_LEN);
+        sh.g_cu[lane] = c0;
+        sh.g_n[lane] = c1 - c0;
+        sh.g_len[lane] = Ls;
+        sh.g_full[lane] = min(max(full, 0), Ls);
+      }
+      int n = lane < count ? p.div_tile(c1 - c0 + TT - 1) : 0, blocks = (Ls + kBlk - 1) / kBlk;  // tiles; of a tile
+      const int grid = static_cast<int>(gridDim.x);
+      const unsigned most_tiles = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(n));
+      // (offsets out of order can make more tiles than there are rows for)
+      const bool in_order = static_cast<long long>(most_tiles) * p.H_kv <= p.units;
+      const int all = in_order ? static_cast<int>(most_tiles) * p.H_kv : kNoUnit;
+      sorted = in_order && all > grid;
+      if (sorted) {  // the longest first
+        int place = 0;
+#pragma unroll 4
+        for (int j = 0; j < 32; ++j) {
+          const int other = __shfl_sync(0xffffffffu, Ls, j);
+          place += j < count && (other > Ls || (other == Ls && j < lane));
+        }
+        if (lane < count) sh.g_order[place] = static_cast<uint8_t>(lane);
+        __syncwarp();
+        const int seq = sh.g_order[min(lane, count - 1)];
+        n = __shfl_sync(0xffffffffu, n, seq);
+        blocks = __shfl_sync(0xffffffffu, blocks, seq);
+        if (lane >= count) n = 0;
+      }
+      auto scan = [&](int x, int &sum) {  // those of the lanes before; sums that stop at kNoUnit
+        int incl = x;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, incl, o);
+          if (lane >= o) incl = min(incl + v, kNoUnit);
+        }
+        sum = __shfl_sync(0xffffffffu, incl, 31);
+        const int prior = __shfl_up_sync(0xffffffffu, incl, 1);
+        return lane ? prior : 0;
+      };
+      const bool may_split = p.slots > 0 && in_order;
+      int whole = kNoUnit, w = n, splits = 1;
+      if (may_split) {
+        int sum;
+        whole = p.div_Hkv(all / grid * grid);
+        w = max(min(whole - scan(n, sum), n), 0);
+        const float left = static_cast<float>(
+            __reduce_add_sync(0xffffffffu, min(static_cast<unsigned>(n - w) * static_cast<unsigned>(blocks), 1u << 26)));
+        const float units = static_cast<float>(all - whole * p.H_kv), total = left * p.H_kv;
+        const float mean = units > 0.f ? __fdividef(total, units) : 0.f;
+        const int waves = (lane & (kTailWaves - 1)) + 1;  // a lane tries one
+        const int share = max(2, static_cast<int>(ceilf(__fdividef(total, grid * waves))));
+        const float f = fmaxf(floorf(__fdividef(mean, share)), 1.f);
+        const float cost = ceilf(__fdividef(units * f, grid)) * (ceilf(__fdividef(mean, f)) + 3.5f);
+        const unsigned least = __reduce_min_sync(0xffffffffu, __float_as_uint(cost));
+        const int per = __shfl_sync(0xffffffffu, share, __ffs(__ballot_sync(0xffffffffu, __float_as_uint(cost) == least)) - 1);
+        if (n > w) splits = min(max(blocks / per, 1), kMaxSplits);
+      }
+      int units, first = scan(min((w + (n - w) * splits) * p.H_kv, kNoUnit), units);
+      if (may_split && units - whole * p.H_kv > p.slots) {  // more than there is room for: nothing is split
+        splits = 1;
+        first = scan(n * p.H_kv, units);
+      }
+      if (lane < count) {
+        sh.g_units[lane] = first;
+        sh.g_split[lane] = splits;
+        sh.g_whole[lane] = w;
+      }
+      first_slot = may_split ? whole * p.H_kv : kNoUnit;
+      if (p.slots > 0 && blockIdx.x == 0 && lane == 0) *p.n_slots = max(units - first_slot, 0);
+      group_units = units;
+      __syncwarp();
+    };
     auto load_group = [&](int s0, int units_before) {
       g0 = s0;
       before = units_before;
       const int count = min(kGroup, p.S - s0);
+      if constexpr (kFp8) {
+        if (p.S <= 32) {
+          load_few();
+          return;
+        }
+      }
       // (loops left as loops, a step's loads ahead: code that runs once is bound by
       // fetching it)
       if (fetched != s0) fetch(s0 + lane);
@@ -735,7 +899,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
       if constexpr (kFp8) {
         // Longest sequences first, by eighths of the longest, where there is more than a unit
         // an SM: a long one begun late has the others wait.
-        sorted = p.units > static_cast<int>(gridDim.x);
+        sorted = p.units - p.slots > static_cast<int>(gridDim.x);
         if (sorted) {
           __syncwarp();
           int most = 0;
@@ -1294,55 +1458,15 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         __syncwarp();
         if (!M.valid) break;
         if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
-        // Q, a row a thread: q 2^t = q1 + q2 with the row's largest value from 2^7 to 2^8.
-        // q1 has four of bf16's eight bits, and what is left of them fits into q2, but for
-        // values below 2^-9 of the largest, which keep 2^-17 of that.
         if (k >= 2 && !(ok = wait_bar(sh.q_free[k & 1], ((k >> 1) - 1) & 1))) break;
         tc_fence_after();
-        const int r_in = quad * 32 + lane, r = M.copies > 1 ? lane : r_in;
-        if (r - lane < M.nrows) {
-          const int rt = p.div_G(r);
-          const bool valid = r < M.nrows;
-          const uint4 *const src = reinterpret_cast<const uint4 *>(
-              p.q + (valid ? (M.tok0 + rt) * p.q_stride + (M.g * G + r - rt * G) * D : 0));
-          unsigned most = 0u;
-          {
-            uint4 x[D / 8];
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i) x[i] = valid ? src[i] : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-              most = __vmaxu2(__vmaxu2(most, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu)),
-                              __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
-          }
-          most = max(most & 0xffffu, most >> 16);
-          const int t = min(134 - static_cast<int>(most >> 7), 126);
-          const float up = __uint_as_float(static_cast<uint32_t>(127 + t) << 23);
-          sh.q_scale[slot][r_in] =
-              most >= 0x7f80u ? __int_as_float(0x7fffffff) : __uint_as_float(static_cast<uint32_t>(127 - t) << 23);
-          const uint32_t q_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::col_q(k & 1);
-#pragma unroll 1
-          for (int i0 = 0; i0 < D / 8; i0 += 4) {  // 32 columns at a time, from L1 this time
-            uint32_t c1[8], c2[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint4 y = valid ? src[i0 + i] : make_uint4(0u, 0u, 0u, 0u);
-              const uint32_t ab[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const uint32_t a = ab[2 * e], b = ab[2 * e + 1];
-                const float q0 = __uint_as_float(a << 16) * up, q1 = __uint_as_float(a & 0xffff0000u) * up;
-                const float q2 = __uint_as_float(b << 16) * up, q3 = __uint_as_float(b & 0xffff0000u) * up;
-                c1[2 * i + e] = to_codes4(q0, q1, q2, q3);
-                float2 f, g;
-                of_codes4(c1[2 * i + e], f, g);
-                c2[2 * i + e] = to_codes4(q0 - f.x, q1 - f.y, q2 - g.x, q3 - g.y);
-              }
-            }
-            tmem_st8(q_addr + 2 * i0, c1);
-            tmem_st8(q_addr + D / 4 + 2 * i0, c2);
-          }
-          tmem_st_wait();
+        const int r_in = quad * 32 + lane, row = M.copies > 1 ? lane : r_in;
+        if (row - lane < M.nrows) {
+          const bool valid = row < M.nrows;
+          const int t = p.div_G(row);
+          part_row<D>(reinterpret_cast<const uint4 *>(
+                          p.q + (valid ? (M.tok0 + t) * p.q_stride + (M.g * G + row - t * G) * D : 0)),
+                      valid, tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::col_q(k & 1), &sh.q_scale[slot][r_in]);
         }
         tc_fence_before();
         __syncwarp();
@@ -1444,6 +1568,8 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
             if (nsplit > 1) p.l_part[part_row + r_in] = lse;
             else if (p.lse) p.lse[(tok0 + rt) * p.H_q + head0 + r_in - rt * G] = lse;
             odd = l != l;
+            // (what O's sums are to be multiplied by, in the base's place)
+            sh.xbase[slot][r_in] = l == 0.f ? 0.f : __fdividef(sh.v_ref[slot][r_in], l);
           }
           // (the unit before may have rows on their way through the same memory)
           __syncwarp();
@@ -1492,7 +1618,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
                 v.z += x.z;
                 v.w += x.w;
               }
-              const float l = sum_of_row(row), inv = l == 0.f ? 0.f : __fdividef(sh.v_ref[slot][row], l);
+              const float inv = sh.xbase[slot][row];
               odd |= !(v.x * 0.f == 0.f && v.y * 0.f == 0.f && v.z * 0.f == 0.f && v.w * 0.f == 0.f);
               v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
               if (nsplit > 1) {
