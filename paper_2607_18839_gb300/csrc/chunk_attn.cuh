@@ -1536,6 +1536,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
     const int r_in = quad * 32 + lane;  // row within the tile
     const uint32_t o_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::kColO;
     const uint32_t stage = sbase + L::kStage + quad * 32 * 128;  // of this warp's rows
+    constexpr int kOnce = kFp8 ? 16 : 32;  // columns of O at once (there are 80 registers, or 96)
     pdl_wait();
     const int rt = p.div_G(r_in);
     int outputs = 0;
@@ -1582,15 +1583,15 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           for (int col = 0; col < D && ok; col += width) {
             const int w = min(width, D - col);
 #pragma unroll 1
-            for (int c = 0; c < w; c += 32) {
-              uint32_t o[32];
-              tmem_ld32(o_addr + col + c, o);
-              tmem_ld_wait32(o);
+            for (int c = 0; c < w; c += 16) {
+              uint32_t o[16];
+              tmem_ld16(o_addr + col + c, o);
+              tmem_ld_wait16(o);
               if (lane < nrows) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + ((quad * nrows + lane) * width + c) * 4 +
-                                                                               (((e ^ lane) & 7) << 4)),
+                for (int e = 0; e < 4; ++e)
+                  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + ((quad * nrows + lane) * width + (c & ~31)) * 4 +
+                                                                               (((e + c / 4) ^ lane) & 7) * 16),
                                "r"(o[4 * e]), "r"(o[4 * e + 1]), "r"(o[4 * e + 2]), "r"(o[4 * e + 3])
                                : "memory");
               }
@@ -1682,20 +1683,25 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         uint32_t keep[32];
         if (half < D / 64) {
 #pragma unroll
-          for (int c = 0; c < 64; c += 32) {
-            uint32_t o[32];
+          for (int c = 0; c < 64; c += kOnce) {
+            uint32_t o[kOnce];
             if (!idle) {
-              tmem_ld32(o_addr + half * 64 + c, o);
-              tmem_ld_wait32(o);
+              if constexpr (kFp8) {
+                tmem_ld16(o_addr + half * 64 + c, o);
+                tmem_ld_wait16(o);
+              } else {
+                tmem_ld32(o_addr + half * 64 + c, o);
+                tmem_ld_wait32(o);
+              }
             }
-            if (half == D / 64 - 1 && c == 32) {  // O may be overwritten once every warp has read it
+            if (half == D / 64 - 1 && c == 64 - kOnce) {  // O may be overwritten once every warp has read it
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive(bar(sh.o_empty));
             }
             if (idle) continue;
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
+            for (int e = 0; e < kOnce; e += 2) {
               const float2 v = make_float2(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
               finite = __ffma2_rn(v, make_float2(0.f, 0.f), finite);
               const float2 x = __fmul2_rn(v, make_float2(inv, inv));
@@ -1705,7 +1711,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
             }
             if (part && valid) {
 #pragma unroll
-              for (int e = 0; e < 32; e += 8) st_global_v8(part + half * 64 + c + e, o + e);
+              for (int e = 0; e < kOnce; e += 8) st_global_v8(part + half * 64 + c + e, o + e);
             }
           }
         }
