@@ -495,7 +495,7 @@ hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *args, hpd_stream_t stream);
  * so that a code is rounded once, but for one that leaves the normal numbers of e4m3
  * (below 2^-6 of 448) as its page's scale grows.  Rows behind the run are left as
  * they are.
- * A scale that is there but not in [2^-100, 2^120] counts as 2^-100 and is flagged
+ * A scale that is there but not in [2^-100, 2^121] counts as 2^-100 and is flagged
  * HPD_DEVERR_SCALE.  One launch. */
 typedef struct {
   hpd_qk_norm_rope_args rope;

@@ -5,7 +5,7 @@ for each page and head, in 64 bits.
 import numpy as np
 
 PAGE = 16
-CODE_MAX, LEAST, MOST = 448.0, 2.0 ** -100, 2.0 ** 120
+CODE_MAX, LEAST, MOST = 448.0, 2.0 ** -100, 2.0 ** 121
 
 
 def _values():

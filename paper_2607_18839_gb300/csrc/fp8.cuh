@@ -7,7 +7,7 @@ namespace hpd {
 
 constexpr float kCodeMax = 448.f;                     // the largest e4m3 value
 constexpr float kLeastScale = 7.888609052210118e-31f;  // 2^-100, of a page of zeros
-constexpr float kMostScale = 1.329227995784916e+36f;   // 2^120, above the largest float / 448
+constexpr float kMostScale = 2.658455991569832e+36f;   // 2^121, above twice the largest float / 448
 
 // Four codes (the low byte first) as two pairs of f16, which holds every code.  (A half of
 // a register is an operand as it is: masks and shifts would be as many instructions again,

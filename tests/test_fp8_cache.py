@@ -369,6 +369,25 @@ def test_gpu_write_grows_scales_without_rounding_twice(torch):
 
 
 @gpu
+def test_gpu_write_keeps_the_largest_scales(torch):
+    # doublings end below twice the largest value / 448, which may pass 2^120
+    k, v, ks, vs = H.fp8_cache(1, 1, 64)
+    op = H.QkNormRope(1, 1, 64, None, None, H.rope_table(8, 64))
+    vs.fill_(1.1 * 2.0 ** -10)
+    ks.fill_(1.0)
+    rows = torch.ones(2, 3 * 64, dtype=torch.bfloat16, device="cuda")
+    rows[0, 2 * 64:] = 3.38e38
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    for t in range(2):
+        op(rows[t: t + 1], i32(t), i32(5 + t), k, v, k_scale=ks, v_scale=vs)
+    torch.cuda.synchronize()
+    assert op.errors() == 0
+    assert vs.item() == float(np.float32(1.1)) * 2.0 ** 120
+    got, x = F.decode(_u8(v)[0, 5]), float(rows[0, -1]) / vs.item()
+    assert (np.abs(got - x) <= 2.0 ** -4 * x).all() and not _u8(v)[0, 6].any()
+
+
+@gpu
 @pytest.mark.parametrize("bad", [0.0, -1.0, NAN, INF, 1e-35])
 def test_gpu_write_flags_scales_that_are_none(torch, bad):
     slot, pages = _slots(np.random.default_rng(6), [3, 20], [5, 0])
