@@ -179,8 +179,9 @@ __device__ __forceinline__ float settle_scale(const Fp8Args &f, const Run &r, fl
     }
     const int k = doublings(need, s);
     if (k > 0) {
-      s *= __uint_as_float(static_cast<uint32_t>(min(k, 127) + 127) << 23) *
-           __uint_as_float(static_cast<uint32_t>(max(k - 127, 0) + 127) << 23);
+      // (one after the other: 2^k alone may be out of range)
+      s *= __uint_as_float(static_cast<uint32_t>(min(k, 127) + 127) << 23);
+      s *= __uint_as_float(static_cast<uint32_t>(max(k - 127, 0) + 127) << 23);
       shrink_rows<D>((is_k ? f.k_cache : f.v_cache) + (page * kPage * f.H_kv + h) * D, static_cast<size_t>(f.H_kv) * D,
                      off, k);
     }
