@@ -544,10 +544,10 @@ typedef struct {
   float *entropy;          /* [R], or NULL                                          */
   int32_t *top_tokens;     /* [R][top]; NULL with top = 0                           */
   float *top_logprobs;     /* [R][top]; NULL with top = 0                           */
-  int R, V;                /* R >= 0 rows (with none nothing is done), V >= 1       */
+  int R, V;                /* R >= 0 rows (with none nothing is done), 1 <= V <= 2^30 */
   int top;                 /* 0 .. 32, at most V                                    */
   int fp32;                /* 1: logits are fp32, 0: bf16                           */
-  float scale;             /* 1 / temperature, > 0 and finite; 0 = 1                */
+  float scale;             /* 1 / temperature, from 2^-120 to 2^120; 0 = 1          */
 } hpd_token_logprobs_args; /* logits aligned to their type, the rest to 4 bytes     */
 
 hpd_status hpd_token_logprobs(const hpd_token_logprobs_args *args, hpd_stream_t stream);

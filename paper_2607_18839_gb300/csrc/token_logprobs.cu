@@ -7,7 +7,7 @@
 // R: nothing cancels where a token is nearly sure.
 #include <cooperative_groups.h>
 
-#include <cmath>
+#include <atomic>
 
 #include "common.cuh"
 
@@ -108,7 +108,9 @@ struct Vec<float> {
 struct Sums {
   float m, rest, mean;
 };
-constexpr float kWindow = 60.f, kNothing = -300.f;  // log2: 2^kNothing is 0
+// log2: a limit kWindow above a base may be twice that above it once rounded (a step of the
+// values may be as much), and sums of 2^30 terms have to fit all the same; 2^kNothing is 0.
+constexpr float kWindow = 45.f, kNothing = -300.f;
 
 __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(b));
@@ -506,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     __syncthreads();
     const int found = min(sh.found, kCandidates);
     if (found <= kThreads / 4) {  // a candidate's place by four threads
-      const Place p = sh.candidate[min(tid / 4, found - 1)];
+      const Place p = sh.candidate[min(tid / 4, max(found - 1, 0))];
       int ahead = 0;
       for (int j = tid % 4; j < found; j += 4) ahead += before(sh.candidate[j], p);
       ahead += __shfl_xor_sync(0xffffffffu, ahead, 1);
@@ -539,7 +541,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
   }
   if (!(fabsf(all.m) < inf())) all.rest = nan();
   const float log_z = log1pf(all.rest);
-  auto logprob = [&](float x) { return all.rest == all.rest ? (x - all.m) * a.scale - log_z : nan(); };
+  // (by halves, which are exact: a difference of two logits may be out of range)
+  auto logprob = [&](float x) {
+    return all.rest == all.rest ? (0.5f * x - 0.5f * all.m) * (2.f * a.scale) - log_z : nan();
+  };
   if (tid == 0) {
     a.logprob[r] = logprob(token >= 0 && token < a.V ? x_token : -inf());
     if (a.entropy) a.entropy[r] = log_z - all.mean * kLn2 / (1.f + all.rest);
@@ -599,10 +604,11 @@ cudaError_t launch_logprobs(const LogpArgs &k, int R, cudaStream_t s) {
 
 extern "C" hpd_status hpd_token_logprobs(const hpd_token_logprobs_args *a, hpd_stream_t stream) {
   using namespace hpd;
-  if (!a || a->R < 0 || a->V < 1 || a->top < 0 || a->top > a->V || a->row_stride < 0 || !std::isfinite(a->scale) ||
-      a->scale < 0.f || (a->fp32 != 0 && a->fp32 != 1))
+  // (of the logits' own range, the scale leaves neither differences nor the floor of the sums without a number)
+  if (!a || a->R < 0 || a->V < 1 || a->top < 0 || a->top > a->V || a->row_stride < 0 ||
+      !(a->scale == 0.f || (a->scale >= 0x1p-120f && a->scale <= 0x1p120f)) || (a->fp32 != 0 && a->fp32 != 1))
     return HPD_ERR_INVALID_ARG;
-  if (a->top > 32) return HPD_ERR_UNSUPPORTED;
+  if (a->top > 32 || a->V > 1 << 30) return HPD_ERR_UNSUPPORTED;
   if (a->R > 1 && a->row_stride != 0 && a->row_stride < a->V) return HPD_ERR_INVALID_ARG;
   if (a->R == 0) return HPD_OK;
   if (!a->logits || !a->tokens || !a->logprob || (a->top > 0 && (!a->top_tokens || !a->top_logprobs)))

@@ -535,8 +535,8 @@ def token_logprobs(logits, tokens, top=0, temperature=1.0, stream=None) -> Token
         if (V > 1 and step != 1) or (shape[0] > 1 and stride < V):
             raise HpdError(what, 1, "rows with their values side by side, none over another")
         stride = stride if shape[0] > 1 else 0  # (one row has none)
-    if not 1e-37 < temperature < 1e37:
-        raise HpdError(what, 1, "a temperature above 0")
+    if not 1e-36 <= temperature <= 1e36:
+        raise HpdError(what, 1, "a temperature above 0, from 1e-36 to 1e36")
     if not 0 <= top <= min(V, 32):
         raise HpdError(what, 1 if top < 0 or top > V else 2, "0 to 32 alternatives, no more than there are tokens")
     device = logits.device

@@ -41,6 +41,7 @@ def args(**kw):
 
 @pytest.mark.parametrize("bad,status", [
     (dict(R=-1), 1), (dict(V=0), 1), (dict(top=-1), 1), (dict(top=33), 2), (dict(V=3, top=4), 1), (dict(fp32=2), 1),
+    (dict(V=2 ** 30 + 1), 2), (dict(scale=2.0 ** -121), 1), (dict(scale=2.0 ** 121), 1),
     (dict(scale=-1.0), 1), (dict(scale=INF), 1), (dict(scale=NAN), 1), (dict(row_stride=99), 1), (dict(row_stride=-5), 1),
     (dict(logits=None), 1), (dict(tokens=None), 1), (dict(logprob=None), 1), (dict(top_tokens=None), 1),
     (dict(top_logprobs=None), 1), (dict(logits=4097), 1), (dict(logits=4098, fp32=1), 1), (dict(tokens=4098), 1),
@@ -79,7 +80,8 @@ def test_tensors_of_the_wrong_kind_are_refused(torch):
                 lambda: H.token_logprobs(bf, tok.cpu()), lambda: H.token_logprobs(bf[:, ::2], tok),
                 lambda: H.token_logprobs(bf[:1].expand(4, 100), tok), lambda: H.token_logprobs(bf, tok, top=-1),
                 lambda: H.token_logprobs(bf[:, :5], tok, top=6), lambda: H.token_logprobs(bf, tok, temperature=0.0),
-                lambda: H.token_logprobs(bf, tok, temperature=-1.0), lambda: H.token_logprobs(bf, tok, temperature=NAN),
+                lambda: H.token_logprobs(bf, tok, temperature=-1.0), lambda: H.token_logprobs(bf, tok, temperature=2e36),
+                lambda: H.token_logprobs(bf, tok, temperature=1e-37), lambda: H.token_logprobs(bf, tok, temperature=NAN),
                 lambda: H.token_logprobs(bf.T, tok), lambda: H.token_logprobs(bf.view(2, 2, 100)[:, :, :50], tok.view(2, 2))):
         with pytest.raises(H.HpdError) as e:
             bad()
@@ -94,6 +96,8 @@ def _check(torch, x, tokens, top=0, temperature=1.0, got=None):
     r = got or H.token_logprobs(x, torch.from_numpy(np.asarray(tokens, np.int32)).cuda(), top=top, temperature=temperature)
     torch.cuda.synchronize()
     lp, ent, ids, alt = O.logprobs(x.float().cpu().numpy(), tokens, top, temperature)
+    # (what lies beyond the largest number of 32 bits, 2^128 (1 - 2^-24), by half a step and more rounds to -inf)
+    lp, alt = (np.where(a <= -2.0 ** 128 * (1 - 2.0 ** -25), -INF, a) for a in (lp, alt))
     # Z: exponentials to 2^-22 of each, whose arguments d (a difference, a factor, log2 e
     # and its product: 2^-24 of it each, four times) are off by 2^-22 |d|; terms with
     # |d| above 88 are no numbers of 32 bits.  Sums in 32 bits of V / 512 terms in a thread at most
@@ -158,6 +162,30 @@ def test_gpu_rows_out_of_the_ordinary(torch, wide, V, top):
     tokens = [0, 1, 0, 1, V - 1, 3, 0, V - 1, 0, 3, 5, 1, V // 3, 2]
     x = torch.from_numpy(x).cuda()
     _check(torch, x if wide else x.to(torch.bfloat16), tokens, top)
+
+
+@gpu
+@pytest.mark.parametrize("temperature", [1e36, 1e30, 1e-30, 1e-36])
+@pytest.mark.parametrize("wide", [False, True])
+def test_gpu_temperatures_out_of_the_ordinary(torch, wide, temperature):
+    rng = np.random.default_rng(9)
+    x = _logits(torch, rng, 6, 9001, wide)
+    x[1, 5000:] = -INF
+    x[2, 1:] = -INF
+    x[3] = -3e38
+    x[3, 77] = 3e38
+    x[4] *= 2.0 ** 110
+    x[5] *= 2.0 ** -100
+    _check(torch, x, [3, 4, 5, 77, 6, 7], 5, temperature)
+
+
+@gpu
+def test_gpu_values_a_step_above_a_threads_first_ones(torch):
+    # a step of the values is more than 60 powers of two at this temperature, and a thread
+    # has some 2,900 values a step above its first ones: 2^117.6 each, were those its base
+    x = torch.full((8, 750000), 1.0 + 2.0 ** -23, device="cuda")
+    x[:, :4096] = 1.0
+    _check(torch, x.view(1, -1), [5000000], 0, temperature=0.51 * 2.0 ** -23 / 60 / np.log(2.0))
 
 
 @gpu
