@@ -674,6 +674,61 @@ def test_gpu_attn_on_another_stream_in_a_graph_and_of_fewer_rows(torch):
 
 
 @gpu
+@pytest.mark.parametrize("S", [20, 100])
+def test_gpu_attn_offsets_out_of_order(torch, S):
+    # every second sequence begins at row 0 again: more tiles than there are rows for; a
+    # sequence that has rows of its own alone keeps its results
+    c = _coded(torch, K._attn_case(torch, [3] * S, [200 + i for i in range(S)], 8, 2, 64, seed=15))
+    op = _op(c)
+    want = [x.clone() for x in op(c["q"], c["cu"], c["total"])]
+    cu = c["cu"].clone()
+    cu[1:S:2] = 3 * S
+    op(c["q"], cu, c["total"])
+    torch.cuda.synchronize()
+    assert op.errors() == 0x2
+    H.hpd_workspace_init(op.workspace.data_ptr(), op.workspace.numel(), H._stream_handle(None))
+    got = op(c["q"], c["cu"], c["total"])
+    torch.cuda.synchronize()
+    assert op.errors() == 0 and all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@gpu
+def test_gpu_calls_at_once_and_graphs_that_share_a_workspace(torch):
+    cases = [_coded(torch, K._attn_case(torch, new, total, 16, 2, 128, seed=16 + i))
+             for i, (new, total) in enumerate((([300, 1], [1500, 4000]), ([1] * 40, list(range(30, 1230, 30)))))]
+    ops = [_op(c) for c in cases]
+    run = lambda i, **kw: ops[i](cases[i]["q"], cases[i]["cu"], cases[i]["total"], **kw)  # noqa: E731
+    want = [[x.clone() for x in run(i)] for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for o in ops:
+        o.out.zero_(), o.lse.zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):  # an object a stream, at the same time
+        for i in range(2):
+            run(i, stream=streams[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in range(2) for a, b in zip(want[i], (ops[i].out, ops[i].lse)))
+    # one object in two graphs, of different numbers of rows, one after the other
+    c, op = cases[0], ops[0]
+    one = dict(cu=torch.tensor([0, 1, 1], dtype=torch.int32, device="cuda"), total=c["total"])
+    alone = [x.clone() for x in op(c["q"][:1], one["cu"], one["total"])]
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    with torch.cuda.graph(graphs[0]):
+        whole = op(c["q"], c["cu"], c["total"])
+    with torch.cuda.graph(graphs[1]):
+        first = op(c["q"][:1], one["cu"], one["total"])
+    for _ in range(3):
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want[0], whole))
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(alone, first))
+    assert ops[0].errors() == ops[1].errors() == 0
+
+
+@gpu
 def test_gpu_pages_beyond_32_bits_of_a_long_cache(torch):
     # 1.2 million pages of one head of 128: codes past 2^31
     pages, D = 1200000, 128
