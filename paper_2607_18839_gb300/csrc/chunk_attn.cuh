@@ -590,56 +590,60 @@ __device__ __forceinline__ bool softmax_share_fp8(uint32_t s_addr, int copy, int
   return !(val < kLeastVal) || scale == 0.f;
 }
 
-// A row of Q (at src, if it is one) in two e4m3 parts at q_addr, one behind the other: q 2^t =
-// q1 + q2 with the row's largest value from 2^7 to 2^8.  q1 has four of bf16's eight bits, and
-// what is left of them fits into q2, but for values below 2^-9 of the largest, which keep 2^-17
-// of that.  factor: 2^-t; NaN for a row with a value that is not finite.
+// Rows row0 to row0 + rows - 1 (32 at most) of a tile's queries in two e4m3 parts, one
+// behind the other, in TMEM at q_addr: q 2^t = q1 + q2 with the row's largest value from 2^7
+// to 2^8.  q1 has four of bf16's eight bits, and what is left of them fits into q2, but for
+// values below 2^-9 of the largest, which keep 2^-17 of that.  factor: 2^-t of each row; NaN
+// for one with a value that is not finite.  Four lanes have a row, eight of each 32 columns
+// a lane, so that it is loaded once, in pieces of 64 bytes.
 template <int D>
-__device__ __forceinline__ void part_row(const uint4 *src, bool valid, uint32_t q_addr, float *factor) {
-  unsigned most = 0u;
-  {
-    uint4 x[D / 8];
+__device__ __forceinline__ void part_rows(const __nv_bfloat16 *q, long long q_stride, int G, FastDiv div_G, int row0,
+                                          int rows, uint32_t q_addr, float *factor) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll(D == 64 ? 2 : 1)  // (with 128 columns the 80 registers hold 16 rows' pieces)
+  for (int r0 = lane >> 2; r0 - (lane >> 2) < rows; r0 += 16, q_addr += 16u << 16) {
+    uint4 x[2][D / 32];  // of rows r0 and r0 + 8
+    float up[2];
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) x[i] = valid ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+    for (int e = 0; e < 2; ++e) {
+      const int row = row0 + r0 + 8 * e, t = div_G(row);
+      const uint4 *const src = reinterpret_cast<const uint4 *>(q + t * q_stride + (row - t * G) * D) + (lane & 3);
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i)
-      most = __vmaxu2(__vmaxu2(most, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu)),
-                      __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
-  }
-  most = max(most & 0xffffu, most >> 16);
-  const int t = min(134 - static_cast<int>(most >> 7), 126);
-  const float up = __uint_as_float(static_cast<uint32_t>(127 + t) << 23);
-  *factor =
-      most >= 0x7f80u ? __int_as_float(0x7fffffff) : __uint_as_float(static_cast<uint32_t>(127 - t) << 23);
-  uint4 next[4];
-  auto fetch = [&](int i0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) next[i] = valid ? src[i0 + i] : make_uint4(0u, 0u, 0u, 0u);
-  };
-  fetch(0);
-#pragma unroll 1
-  for (int i0 = 0; i0 < D / 8; i0 += 4) {  // 32 columns at a time, from L1 this time
-    uint32_t c1[8], c2[8];
-    uint4 now[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) now[i] = next[i];
-    if (i0 + 4 < D / 8) fetch(i0 + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t ab[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint32_t a = ab[2 * e], b = ab[2 * e + 1];
-        const float q0 = __uint_as_float(a << 16) * up, q1 = __uint_as_float(a & 0xffff0000u) * up;
-        const float q2 = __uint_as_float(b << 16) * up, q3 = __uint_as_float(b & 0xffff0000u) * up;
-        c1[2 * i + e] = to_codes4(q0, q1, q2, q3);
-        float2 f, g;
-        of_codes4(c1[2 * i + e], f, g);
-        c2[2 * i + e] = to_codes4(q0 - f.x, q1 - f.y, q2 - g.x, q3 - g.y);
-      }
+      for (int g = 0; g < D / 32; ++g) x[e][g] = r0 + 8 * e < rows ? src[4 * g] : make_uint4(0u, 0u, 0u, 0u);
     }
-    tmem_st8(q_addr + 2 * i0, c1);
-    tmem_st8(q_addr + D / 4 + 2 * i0, c2);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      unsigned most = 0u;
+#pragma unroll
+      for (int g = 0; g < D / 32; ++g)
+        most = __vmaxu2(__vmaxu2(most, __vmaxu2(x[e][g].x & 0x7fff7fffu, x[e][g].y & 0x7fff7fffu)),
+                        __vmaxu2(x[e][g].z & 0x7fff7fffu, x[e][g].w & 0x7fff7fffu));
+      most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      most = max(most & 0xffffu, most >> 16);
+      const int t = min(134 - static_cast<int>(most >> 7), 126);
+      up[e] = __uint_as_float(static_cast<uint32_t>(127 + t) << 23);
+      if ((lane & 3) == 0 && r0 + 8 * e < rows)
+        factor[r0 + 8 * e] =
+            most >= 0x7f80u ? __int_as_float(0x7fffffff) : __uint_as_float(static_cast<uint32_t>(127 - t) << 23);
+    }
+#pragma unroll
+    for (int g = 0; g < D / 32; ++g) {
+      uint32_t c1[4], c2[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int e = i >> 1;
+        const uint32_t a = i & 1 ? x[e][g].z : x[e][g].x, b = i & 1 ? x[e][g].w : x[e][g].y;
+        const float q0 = __uint_as_float(a << 16) * up[e], q1 = __uint_as_float(a & 0xffff0000u) * up[e];
+        const float q2 = __uint_as_float(b << 16) * up[e], q3 = __uint_as_float(b & 0xffff0000u) * up[e];
+        c1[i] = to_codes4(q0, q1, q2, q3);
+        float2 f, h;
+        of_codes4(c1[i], f, h);
+        c2[i] = to_codes4(q0 - f.x, q1 - f.y, q2 - h.x, q3 - h.y);
+      }
+      tmem_st_rows(q_addr + 8 * g, c1);
+      tmem_st_rows(q_addr + D / 4 + 8 * g, c2);
+    }
   }
   tmem_st_wait();
 }
@@ -1460,14 +1464,9 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         if (lane == 0) mbar_arrive(bar(sh.meta_empty[slot]));
         if (k >= 2 && !(ok = wait_bar(sh.q_free[k & 1], ((k >> 1) - 1) & 1))) break;
         tc_fence_after();
-        const int r_in = quad * 32 + lane, row = M.copies > 1 ? lane : r_in;
-        if (row - lane < M.nrows) {
-          const bool valid = row < M.nrows;
-          const int t = p.div_G(row);
-          part_row<D>(reinterpret_cast<const uint4 *>(
-                          p.q + (valid ? (M.tok0 + t) * p.q_stride + (M.g * G + row - t * G) * D : 0)),
-                      valid, tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::col_q(k & 1), &sh.q_scale[slot][r_in]);
-        }
+        const int row0 = M.copies > 1 ? 0 : quad * 32;
+        part_rows<D>(p.q + M.tok0 * p.q_stride + M.g * G * D, p.q_stride, G, p.div_G, row0, min(M.nrows - row0, 32),
+                     tmem + (static_cast<uint32_t>(quad * 32) << 16) + L::col_q(k & 1), &sh.q_scale[slot][quad * 32]);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(sh.q_full[k & 1]));

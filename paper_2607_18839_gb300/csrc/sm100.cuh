@@ -246,6 +246,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
       "r"(r[15])
       : "memory");
 }
+// 8 columns of 16 lanes' rows (taddr's on): a thread has columns 2 (lane % 4) and the next of
+// rows lane / 4 (x[0], x[1]) and 8 further on (x[2], x[3]).
+__device__ __forceinline__ void tmem_st_rows(uint32_t taddr, const uint32_t *x) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(x[0]), "r"(x[1]),
+               "r"(x[2]), "r"(x[3])
+               : "memory");
+}
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
