@@ -1582,15 +1582,15 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           for (int col = 0; col < D && ok; col += width) {
             const int w = min(width, D - col);
 #pragma unroll 1
-            for (int c = 0; c < w; c += 16) {
-              uint32_t o[16];
-              tmem_ld16(o_addr + col + c, o);
-              tmem_ld_wait16(o);
+            for (int c = 0; c < w; c += 32) {
+              uint32_t o[32];
+              tmem_ld32(o_addr + col + c, o);
+              tmem_ld_wait32(o);
               if (lane < nrows) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + ((quad * nrows + lane) * width + (c & ~31)) * 4 +
-                                                                               (((e + c / 4) ^ lane) & 7) * 16),
+                for (int e = 0; e < 8; ++e)
+                  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + ((quad * nrows + lane) * width + c) * 4 +
+                                                                               ((e ^ lane) & 7) * 16),
                                "r"(o[4 * e]), "r"(o[4 * e + 1]), "r"(o[4 * e + 2]), "r"(o[4 * e + 3])
                                : "memory");
               }
