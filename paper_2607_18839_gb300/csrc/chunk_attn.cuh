@@ -82,6 +82,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "fp8.cuh"
 #include "tc_common.cuh"
@@ -794,83 +795,136 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
     fetch(lane);
     bool sorted = false;
     auto seq_at = [&](int i) { return kFp8 && sorted ? sh.g_order[i] : i; };
-    // A group of no more than 32 sequences, a lane each: what load_group does, in registers
-    // (which of a call's first microseconds has two less).
-    auto load_few = [&] {
-      const int count = p.S;
+    // A group of no more than 64 sequences, kPer to a lane (lane + 32 u of them): what
+    // load_group does, in registers (the first unit of 64 is known 4 us earlier, of 24 two).
+    auto load_few = [&](auto per_lane) {
+      constexpr int kPer = decltype(per_lane)::value;
+      const int count = p.S, grid = static_cast<int>(gridDim.x);
       g0 = before = 0;
-      const int c0 = min(max(a0, 0), p.T), c1 = max(c0, min(a1, p.T)), Ls = min(max(len, 0), p.max_pages * kPage);
-      if (lane < count) {
-        if (a0 != c0 || a1 != c1) flag_error(p.err, HPD_DEVERR_BRANCH_CU);
-        if (Ls != len) flag_error(p.err, HPD_DEVERR_BRANCH_LEN);
-        sh.g_cu[lane] = c0;
-        sh.g_n[lane] = c1 - c0;
-        sh.g_len[lane] = Ls;
-        sh.g_full[lane] = min(max(full, 0), Ls);
+      int n[kPer], blocks[kPer];  // tiles; blocks of one
+#pragma unroll
+      for (int u = 0; u < kPer; ++u) {
+        const int i = lane + 32 * u;
+        if (u > 0) fetch(i);
+        const int c0 = min(max(a0, 0), p.T), c1 = max(c0, min(a1, p.T)), Ls = min(max(len, 0), p.max_pages * kPage);
+        if (i < count) {
+          if (a0 != c0 || a1 != c1) flag_error(p.err, HPD_DEVERR_BRANCH_CU);
+          if (Ls != len) flag_error(p.err, HPD_DEVERR_BRANCH_LEN);
+          sh.g_cu[i] = c0;
+          sh.g_n[i] = c1 - c0;
+          sh.g_len[i] = Ls;
+          sh.g_full[i] = min(max(full, 0), Ls);
+        }
+        n[u] = i < count ? p.div_tile(c1 - c0 + TT - 1) : 0;
+        blocks[u] = ceil_div_i(Ls, kBlk);
       }
-      int n = lane < count ? p.div_tile(c1 - c0 + TT - 1) : 0, blocks = (Ls + kBlk - 1) / kBlk;  // tiles; of a tile
-      const int grid = static_cast<int>(gridDim.x);
-      const unsigned most_tiles = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(n));
+      auto sum_of = [&](auto f) {
+        unsigned x = f(0);
+        if (kPer > 1) x += f(kPer - 1);
+        return __reduce_add_sync(0xffffffffu, x);
+      };
+      const unsigned most_tiles = sum_of([&](int u) { return static_cast<unsigned>(n[u]); });
       // (offsets out of order can make more tiles than there are rows for)
       const bool in_order = static_cast<long long>(most_tiles) * p.H_kv <= p.units;
       const int all = in_order ? static_cast<int>(most_tiles) * p.H_kv : kNoUnit;
       sorted = in_order && all > grid;
-      if (sorted) {  // the longest first
-        int place = 0;
-#pragma unroll 4
-        for (int j = 0; j < 32; ++j) {
-          const int other = __shfl_sync(0xffffffffu, Ls, j);
-          place += j < count && (other > Ls || (other == Ls && j < lane));
-        }
-        if (lane < count) sh.g_order[place] = static_cast<uint8_t>(lane);
-        __syncwarp();
-        const int seq = sh.g_order[min(lane, count - 1)];
-        n = __shfl_sync(0xffffffffu, n, seq);
-        blocks = __shfl_sync(0xffffffffu, blocks, seq);
-        if (lane >= count) n = 0;
-      }
-      auto scan = [&](int x, int &sum) {  // those of the lanes before; sums that stop at kNoUnit
-        int incl = x;
+      if (sorted) {  // the longest first: a bitonic sort of lengths in blocks, with the sequences' numbers
+        unsigned key[kPer];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int v = __shfl_up_sync(0xffffffffu, incl, o);
-          if (lane >= o) incl = min(incl + v, kNoUnit);
+        for (int u = 0; u < kPer; ++u)
+          key[u] = lane + 32 * u < count ? static_cast<unsigned>(blocks[u] + 1) << 6 | (63 - lane - 32 * u) : 0u;
+#pragma unroll 1
+        for (int size = 2; size <= 32 * kPer; size *= 2)
+#pragma unroll 1
+          for (int apart = size / 2; apart > 0; apart /= 2) {
+            if (kPer > 1 && apart == 32) {
+              const unsigned a = key[0], b = key[kPer - 1];
+              key[0] = max(a, b);
+              key[kPer - 1] = min(a, b);
+              continue;
+            }
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) {
+              const unsigned other = __shfl_xor_sync(0xffffffffu, key[u], apart);
+              const bool larger = !(lane & apart) == !((lane + 32 * u) & size);
+              key[u] = larger ? max(key[u], other) : min(key[u], other);
+            }
+          }
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+          n[u] = blocks[u] = 0;
+          if (lane + 32 * u < count) {
+            const int seq = 63 - static_cast<int>(key[u] & 63u);
+            sh.g_order[lane + 32 * u] = static_cast<uint8_t>(seq);
+            n[u] = p.div_tile(sh.g_n[seq] + TT - 1);
+            blocks[u] = static_cast<int>(key[u] >> 6) - 1;
+          }
         }
-        sum = __shfl_sync(0xffffffffu, incl, 31);
-        const int prior = __shfl_up_sync(0xffffffffu, incl, 1);
-        return lane ? prior : 0;
+      }
+      auto scan = [&](const int *x, int *prior) {  // sums of those before (that stop at kNoUnit); of all
+        int sum = 0;
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+          int incl = x[u];
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl = min(incl + v, kNoUnit);
+          }
+          const int v = __shfl_up_sync(0xffffffffu, incl, 1);
+          prior[u] = min(sum + (lane ? v : 0), kNoUnit);
+          sum = min(sum + __shfl_sync(0xffffffffu, incl, 31), kNoUnit);
+        }
+        return sum;
       };
       const bool may_split = p.slots > 0 && in_order;
-      int whole = kNoUnit, w = n, splits = 1;
+      int whole = kNoUnit, w[kPer], splits[kPer], first[kPer], units[kPer];
+#pragma unroll
+      for (int u = 0; u < kPer; ++u) {
+        w[u] = n[u];
+        splits[u] = 1;
+      }
       if (may_split) {
-        int sum;
         whole = p.div_Hkv(all / grid * grid);
-        w = max(min(whole - scan(n, sum), n), 0);
+        scan(n, first);
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) w[u] = max(min(whole - first[u], n[u]), 0);
         const float left = static_cast<float>(
-            __reduce_add_sync(0xffffffffu, min(static_cast<unsigned>(n - w) * static_cast<unsigned>(blocks), 1u << 26)));
-        const float units = static_cast<float>(all - whole * p.H_kv), total = left * p.H_kv;
-        const float mean = units > 0.f ? __fdividef(total, units) : 0.f;
+            sum_of([&](int u) { return min(static_cast<unsigned>(n[u] - w[u]) * static_cast<unsigned>(blocks[u]), 1u << 25); }));
+        const float rest = static_cast<float>(all - whole * p.H_kv), total = left * p.H_kv;
+        const float mean = rest > 0.f ? __fdividef(total, rest) : 0.f;
         const int waves = (lane & (kTailWaves - 1)) + 1;  // a lane tries one
         const int share = max(2, static_cast<int>(ceilf(__fdividef(total, grid * waves))));
         const float f = fmaxf(floorf(__fdividef(mean, share)), 1.f);
-        const float cost = ceilf(__fdividef(units * f, grid)) * (ceilf(__fdividef(mean, f)) + 3.5f);
+        const float cost = ceilf(__fdividef(rest * f, grid)) * (ceilf(__fdividef(mean, f)) + 3.5f);
         const unsigned least = __reduce_min_sync(0xffffffffu, __float_as_uint(cost));
         const int per = __shfl_sync(0xffffffffu, share, __ffs(__ballot_sync(0xffffffffu, __float_as_uint(cost) == least)) - 1);
-        if (n > w) splits = min(max(blocks / per, 1), kMaxSplits);
+#pragma unroll
+        for (int u = 0; u < kPer; ++u)
+          if (n[u] > w[u]) splits[u] = min(max(blocks[u] / per, 1), kMaxSplits);
       }
-      int units, first = scan(min((w + (n - w) * splits) * p.H_kv, kNoUnit), units);
-      if (may_split && units - whole * p.H_kv > p.slots) {  // more than there is room for: nothing is split
-        splits = 1;
-        first = scan(n * p.H_kv, units);
+#pragma unroll
+      for (int u = 0; u < kPer; ++u) units[u] = min((w[u] + (n[u] - w[u]) * splits[u]) * p.H_kv, kNoUnit);
+      int sum = scan(units, first);
+      if (may_split && sum - whole * p.H_kv > p.slots) {  // more than there is room for: nothing is split
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+          splits[u] = 1;
+          units[u] = n[u] * p.H_kv;
+        }
+        sum = scan(units, first);
       }
-      if (lane < count) {
-        sh.g_units[lane] = first;
-        sh.g_split[lane] = splits;
-        sh.g_whole[lane] = w;
-      }
+#pragma unroll
+      for (int u = 0; u < kPer; ++u)
+        if (lane + 32 * u < count) {
+          sh.g_units[lane + 32 * u] = first[u];
+          sh.g_split[lane + 32 * u] = splits[u];
+          sh.g_whole[lane + 32 * u] = w[u];
+        }
       first_slot = may_split ? whole * p.H_kv : kNoUnit;
-      if (p.slots > 0 && blockIdx.x == 0 && lane == 0) *p.n_slots = max(units - first_slot, 0);
-      group_units = units;
+      if (p.slots > 0 && blockIdx.x == 0 && lane == 0) *p.n_slots = max(sum - first_slot, 0);
+      group_units = sum;
       __syncwarp();
     };
     auto load_group = [&](int s0, int units_before) {
@@ -878,8 +932,9 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
       before = units_before;
       const int count = min(kGroup, p.S - s0);
       if constexpr (kFp8) {
-        if (p.S <= 32) {
-          load_few();
+        if (p.S <= 64) {
+          if (p.S <= 32) load_few(std::integral_constant<int, 1>{});
+          else load_few(std::integral_constant<int, 2>{});
           return;
         }
       }

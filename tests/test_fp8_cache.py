@@ -570,7 +570,10 @@ def test_gpu_attn_many_short_units_one_after_another(torch):
 @gpu
 @pytest.mark.parametrize("new,total,hq,hkv,D", [
     ([1], [20000], 16, 2, 128), ([1, 1], [9000, 30], 32, 8, 128), ([16], [9000], 16, 2, 64), ([500], [2500], 16, 4, 64),
-    ([1] * 5, [3999, 1, 70, 2048, 2049], 8, 1, 128), ([700], [3000], 40, 8, 128)])
+    ([1] * 5, [3999, 1, 70, 2048, 2049], 8, 1, 128), ([700], [3000], 40, 8, 128),
+    # groups of one and two sequences a lane of the scheduler, in order of their lengths and not, some empty
+    ([1] * 33, [64 * i for i in range(33)], 8, 2, 64), ([i % 4 for i in range(64)], [9 + 40 * (i * 23 % 64) for i in range(64)], 32, 8, 128),
+    ([1] * 64, [5 + 2000 * (i == 40) for i in range(64)], 4, 4, 64), ([60] * 32, [60 + 37 * (i * 7 % 32) for i in range(32)], 16, 4, 64)])
 def test_gpu_attn_split_tiles(torch, new, total, hq, hkv, D):
     c = _coded(torch, K._attn_case(torch, new, total, hq, hkv, D, seed=7, max_seq_len=max(total)))
     _check(torch, c)
@@ -674,7 +677,7 @@ def test_gpu_attn_on_another_stream_in_a_graph_and_of_fewer_rows(torch):
 
 
 @gpu
-@pytest.mark.parametrize("S", [20, 100])
+@pytest.mark.parametrize("S", [20, 50, 100])
 def test_gpu_attn_offsets_out_of_order(torch, S):
     # every second sequence begins at row 0 again: more tiles than there are rows for; a
     # sequence that has rows of its own alone keeps its results
