@@ -1551,24 +1551,24 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           if (M.pass == kAgain) {
             widen_again<D>(from, sbase + L::kV + sv * L::kTileBytes + quad * 4 * L::kGroupBytes);
           } else {
-          const uint32_t to = sbase + L::kV + sv * L::kTileBytes + quad * 4 * L::kGroupBytes + r * 128;
-          const uint32_t to0 = to + ((c0 * 2 ^ r) << 4), to1 = to + (((c0 * 2 + 1) ^ r) << 4);
+            const uint32_t to = sbase + L::kV + sv * L::kTileBytes + quad * 4 * L::kGroupBytes + r * 128;
+            const uint32_t to0 = to + ((c0 * 2 ^ r) << 4), to1 = to + (((c0 * 2 + 1) ^ r) << 4);
 #pragma unroll
-          for (int group = 0; group < 4; ++group) {
-            uint32_t y[kPieces][8];
+            for (int group = 0; group < 4; ++group) {
+              uint32_t y[kPieces][8];
 #pragma unroll
-            for (int h = 0; h < kPieces; ++h)
+              for (int h = 0; h < kPieces; ++h)
 #pragma unroll
-              for (int n = 0; n < 4; ++n) f16_of_codes(x[h][n], y[h][2 * n], y[h][2 * n + 1]);
-            if (group < 3) read(group + 1);
+                for (int n = 0; n < 4; ++n) f16_of_codes(x[h][n], y[h][2 * n], y[h][2 * n + 1]);
+              if (group < 3) read(group + 1);
 #pragma unroll
-            for (int h = 0; h < kPieces; ++h)
+              for (int h = 0; h < kPieces; ++h)
 #pragma unroll
-              for (int n = 0; n < 2; ++n)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((n ? to1 : to0) + group * L::kGroupBytes + h * 1024),
-                             "r"(y[h][4 * n]), "r"(y[h][4 * n + 1]), "r"(y[h][4 * n + 2]), "r"(y[h][4 * n + 3])
-                             : "memory");
-          }
+                for (int n = 0; n < 2; ++n)
+                  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((n ? to1 : to0) + group * L::kGroupBytes + h * 1024),
+                               "r"(y[h][4 * n]), "r"(y[h][4 * n + 1]), "r"(y[h][4 * n + 2]), "r"(y[h][4 * n + 3])
+                               : "memory");
+            }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();

@@ -36,6 +36,7 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// Four values as codes, to nearest, ties to even; beyond 448 to 448; NaN stays NaN.
 __device__ __forceinline__ uint32_t to_codes4(float a, float b, float c, float d) {
   uint32_t r;
   asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 y, %4, %3;\n\t"

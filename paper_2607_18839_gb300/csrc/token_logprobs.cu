@@ -5,6 +5,29 @@
 //   logprob = d_token - log(1 + R),  entropy = log(1 + R) - sum exp(d_v) d_v / Z
 // Both terms of the entropy are positive, and log(1 + R) keeps the digits of a small
 // R: nothing cancels where a token is nearly sure.
+//
+// A row is read once, 16 bytes a load, by a CTA of 256 threads or, of few rows, by a cluster
+// of up to eight.  Every thread has sums in 32 bits against a base of its own, the largest of
+// its first pieces, moved only by a value 2^kWindow above it: no branch depends on where a
+// row's maxima stand.  All values are in the sums; where that leaves the rest of a row too few
+// digits beside its largest value (a rest below kSure), the thread that has that one sums its
+// values once more without it, and the others lose nothing.
+// Top values: every thread knows its own maximum.  The top-th largest maximum of 64 groups
+// of threads is a lower bound of the last of the top values, which only few threads (some
+// 1.5 times `top`) reach: their pieces are read again, from L2, by the whole CTA, and what
+// reaches the bound (a few more than `top`) is ranked, each against all.  Many equal values,
+// or an order that follows a thread's share, give too many: then the value that the last of
+// them has is found by halving the range of its bits, a pass over the share each.
+//
+// What bounds it, and what it measured on a GB300 (in a graph):
+//   6,144 rows of 32,000 in bf16, sums alone: 68.8 us, 5.7 TB/s, 85 % of a copy's rate; with
+//     8 alternatives 91.5: six barriers and two dependent reads of L2 a row, during which the
+//     SM's other four CTAs stream; with 32 alternatives 113.
+//   160 rows of 100,003 in fp32: 15.6 us; with 20 alternatives 22.6, of which 7 are those.
+//   64 rows of 32,000: 4.4 us, with 8 alternatives 6.3; one row of 151,936 4.3, with 20 11.3:
+//     latency: loads, join, bound, second reads, ranks, and the lists of a cluster's CTAs.
+// A warp a row, each value against a running maximum: 1,263 us for the 6,144 rows.  Rereading by the warps that have the hot threads (eight of them in one warp,
+// one after the other) and ranks by a scan of the cluster's lists: 160 rows 27.4, one 13.8.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -241,6 +264,8 @@ struct LogpShared {
   uint32_t least;  // a lower bound of the last of the top values, as a key
   int found;       // candidates, some perhaps beyond their room
   int count;       // of a scan
+  int hots;        // threads whose largest value reaches the bound, and which
+  uint8_t hot[kThreads];
   int per_warp[kWarps];
   Place candidate[kCandidates];
   Place best[kTop];
@@ -413,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
       const int k = tid / (kThreads / kGroups);
       sh.group[k] = (key_of(g) & ~static_cast<uint32_t>(kGroups - 1)) | k;
     }
-    if (tid == 0) sh.found = 0;
+    if (tid == 0) sh.found = sh.hots = 0;
   }
   const Sums own = run.result(c);
   Sums all = join_lanes(own, 32, c);
@@ -421,19 +446,17 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
   __syncthreads();
   all = join_lanes(sh.warp[lane % kWarps], kWarps, c);
   all.rest -= 1.f;
-  // Calls f(value, index) for the share's values that thread t of this warp has, by n lanes
-  // (a power of two) from its first one on; reach: for pieces with such a largest value alone.
-  auto again = [&](int t, int sub, int n, float reach, auto f) {
-    if (sub == 0 && t < s.head && rank == 0) f(static_cast<float>(s.row[t]), t);
-    if (sub == n - 1 && t < s.tail) f(static_cast<float>(s.row[s.tail0 + t]), s.tail0 + t);
+  // f(value) of the share's values that thread t of this warp has, by all of its lanes
+  auto again = [&](int t, auto f) {
+    if (lane == 0 && t < s.head && rank == 0) f(static_cast<float>(s.row[t]));
+    if (lane == 31 && t < s.tail) f(static_cast<float>(s.row[s.tail0 + t]));
 #pragma unroll 1
-    for (int v = s.v0 + t + sub * kThreads; v < s.v1; v += n * kThreads) {
+    for (int v = s.v0 + t + lane * kThreads; v < s.v1; v += 32 * kThreads) {
       const uint4 w = s.piece(v);
-      if (V::largest(w) < reach) continue;
       float x[V::kN];
       V::unpack(w, x);
 #pragma unroll
-      for (int i = 0; i < V::kN; ++i) f(x[i], s.index(v) + i);
+      for (int i = 0; i < V::kN; ++i) f(x[i]);
     }
   };
   if (all.rest < kSure) {  // (as for all of the CTA) the largest value leaves its sum too few digits
@@ -445,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     }
     const unsigned has = __ballot_sync(0xffffffffu, own.m == m);  // one thread of the CTA
     if (has)
-      again(warp * 32 + __ffs(has) - 1, lane, 32, -inf(), [&](float x, int) {
+      again(warp * 32 + __ffs(has) - 1, [&](float x) {
         const float d = fmaxf((x - m) * c, kNothing), e = x == m ? 0.f : fast_exp2(d);
         part.x += e;
         part.y = fmaf(e, d, part.y);
@@ -489,23 +512,39 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     auto look = [&](float x, int i) {
       if (reaches(x)) propose(sh, x, i);
     };
-    // threads whose largest value reaches the bound, some at once with a part of the warp each
-    unsigned hot = __ballot_sync(0xffffffffu, reaches(run.m));
-    int n = 1;  // lanes for each: as many as a thread has pieces
-    while (n < 32 && n * kThreads < s.v1 - s.v0) n *= 2;
-    const int sub = lane & (n - 1);
-    while (hot) {
-      int t = -1;  // the one of this lane's part
-      for (int i = 0; i < 32 && hot; i += n) {
-        if (lane - sub == i) t = __ffs(hot) - 1;
-        hot &= hot - 1;
-      }
-      if (t >= 0) again(warp * 32 + t, sub, n, least, look);
+    // threads whose largest value reaches the bound: their pieces, by all threads
+    if (reaches(run.m)) {
+      sh.hot[atomicAdd(&sh.hots, 1)] = static_cast<uint8_t>(tid);
+      if (tid < s.head && rank == 0) look(static_cast<float>(s.row[tid]), tid);
+      if (tid < s.tail) look(static_cast<float>(s.row[s.tail0 + tid]), s.tail0 + tid);
     }
     __syncthreads();
-    if (sh.found > kCandidates) select_by_halves(sh, s, top);
-    else if (!any && sh.found < top) propose_equal(sh, s, -inf(), top - sh.found);
+    const int each = (s.v1 - s.v0 + kThreads - 1) / kThreads, work = sh.hots * each;
+#pragma unroll 1
+    for (int i0 = tid; i0 - tid < work; i0 += kUnroll * kThreads) {
+      uint4 w[kUnroll];
+      int v[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int i = i0 + u * kThreads, t = i / each;
+        v[u] = i < work ? s.v0 + sh.hot[t] + (i - t * each) * kThreads : s.v1;
+        if (v[u] < s.v1) w[u] = s.piece(v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        if (v[u] >= s.v1 || V::largest(w[u]) < least) continue;
+        float x[V::kN];
+        V::unpack(w[u], x);
+#pragma unroll
+        for (int e = 0; e < V::kN; ++e) look(x[e], s.index(v[u]) + e);
+      }
+    }
     __syncthreads();
+    if (sh.found > kCandidates || (!any && sh.found < top)) {
+      if (sh.found > kCandidates) select_by_halves(sh, s, top);
+      else propose_equal(sh, s, -inf(), top - sh.found);
+      __syncthreads();
+    }
     const int found = min(sh.found, kCandidates);
     if (found <= kThreads / 4) {  // a candidate's place by four threads
       const Place p = sh.candidate[min(tid / 4, max(found - 1, 0))];
@@ -564,8 +603,15 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
     if (tid < ctas * top) {
       const Place p = sh.list[tid / top][tid % top];
       int ahead = 0;
-      for (int w = 0; w < ctas && ahead < top; ++w)  // (each in order)
-        for (int j = 0; j < top && before(sh.list[w][j], p); ++j) ++ahead;
+#pragma unroll 4
+      for (int w = 0; w < ctas; ++w) {  // how many of each list, which are in order, come before
+        int at = 0;
+#pragma unroll
+        for (int half = kTop / 2; half > 0; half /= 2)
+          if (at + half <= top && before(sh.list[w][at + half - 1], p)) at += half;
+        if (at < top && before(sh.list[w][at], p)) ++at;
+        ahead += at;
+      }
       if (p.i >= 0 && ahead < top) sh.best[ahead] = p;
     }
     __syncthreads();
@@ -575,10 +621,13 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
 
 template <class T, bool kAlternatives>
 cudaError_t launch_logprobs(const LogpArgs &k, int R, cudaStream_t s) {
-  // CTAs of a row: as many as keep the GPU's SMs busy, none with less than 8 KB.
+  // CTAs of a row: as many as keep the GPU's SMs busy, none with less than 32 KB (joining a
+  // cluster's lists costs some 2 us: 64 rows of 32,000 with 8 alternatives 9.3 us with 8 KB
+  // each, 8.0 with 16, 6.3 with 32, 7.1 with 64; one row of 151,936 4.3
+  // without alternatives, 5.3 with 64 KB each, 7.1 with 128).
   int ctas = 1;
   while (ctas < kMaxCluster && static_cast<long long>(R) * ctas * 2 <= 4 * kLogpSms &&
-         static_cast<long long>(k.V) * static_cast<int>(sizeof(T)) >= 2LL * ctas * 8192)
+         static_cast<long long>(k.V) * static_cast<int>(sizeof(T)) >= 2LL * ctas * 32768)
     ctas *= 2;
   static std::atomic<uint64_t> done{0};
   // (five CTAs an SM need a quarter of its 228 KB shared; the rest is for the loads)
