@@ -21,7 +21,7 @@
 //     bf16 form of the queries, keys and values 60.6).  Queries alone are at the memory; the
 //     8,188 runs have the rest, some 7 us each for a warp, 16 warps an SM: slots, rows and
 //     scale, the table's rows, maximum, codes, one after the other.
-//   3,201 to 3,459 rows of 32 + 8 + 8 heads: 22.4 us, 3.4 TB/s: the same in one wave.
+//   3,292 rows of 32 + 8 + 8 heads: 22.4 us, 3.4 TB/s: the same in one wave.
 //   256 tokens of 256 sequences, 32 + 8 + 8 heads: 7.2 us, latency: 4,096 runs of a row, some
 //     of which have to halve the codes before theirs.  16 tokens, 8 + 2 + 2 heads of 64: 2.5.
 // The table's rows a round ahead: 872 bytes of spills, 74.5 and 25.8 us; with the turned keys
@@ -368,7 +368,7 @@ cudaError_t launch_fp8(Fp8Args &f, cudaStream_t s) {
   constexpr int kMost = kRopeSms * kRopeCtas;
   const long long T = f.rope.T, parts = 2LL * f.H_kv;
   // Items of as many rows as leave one to each warp of the GPU (a row each: 32,749 rows 317
-  // us instead of 74, 3,300 rows of 32 + 8 + 8 heads 32 instead of 22).
+  // us instead of 74, 3,292 rows of 32 + 8 + 8 heads 32 instead of 22).
   f.chunk = 1;
   while (f.chunk < kPage && T * parts >= 2LL * f.chunk * kMost * kRopeWarps) f.chunk *= 2;
   const long long items = (T + f.chunk - 1) / f.chunk * parts, q_items = plan_items(f.rope, D);
