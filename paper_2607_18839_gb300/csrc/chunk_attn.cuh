@@ -107,7 +107,7 @@ constexpr int kThreads = 32 * (kWideWarp + (kFp8 ? kWideWarps : 0));
 // What a pass over a unit does: exponentials against the first block's maxima;
 // nothing but the rows' maxima; exponentials against those.
 enum Pass { kFirst, kMaxima, kAgain };
-constexpr int kMetaSlots = 3;
+constexpr int kMetaSlots = 3, kLastUnits = 16;
 // of a metadata slot: producers, two MMA issuers, softmax and output warps
 template <bool kFp8>
 constexpr uint32_t kMetaConsumers = kProducers + 2 + kSoftmaxWarps + kOutputWarps + (kFp8 ? 1 + kWideWarps : 0);
@@ -127,7 +127,7 @@ constexpr int kCopies = 4;       // of the rows of a tile of a quarter of its 12
 // 8-bit cache, a first pass, whose weights are f16: log2 of the weight of a row's base
 // (weights up to 2^12 above it fit, 2^-29 of it is not lost), and the least scale of V,
 // over that of its first block, at which none of 2^-4 and more loses digits.
-constexpr float kFirstLog2 = 4.f, kLeastVal = 0x1p-14f;
+constexpr float kFirstLog2 = 4.f, kLeastLog2 = -14.f, kLeastVal = 0x1p-14f;
 constexpr int kGroup = 256;      // sequences whose lengths the scheduler holds at once
 constexpr int kMaxSplits = 32;
 constexpr int kTailWaves = 4;    // most waves of the units of split tiles
@@ -221,18 +221,19 @@ struct __align__(16) Shared {
   // of the last units: a row's base; its sums (pass over maxima: maxima) by half
   float xbase[kMetaSlots][kRows], xsum[kMetaSlots][2][kRows];
   int max_seq[4][2];  // [quadrant][half]: units whose maxima are published
-  unsigned redo;            // units (by number in this CTA, modulo 32) to run once more
+  unsigned redo;            // units (by number in this CTA, modulo kLastUnits) to run once more
   int units_done;           // output warps that looked at a unit's output
   uint32_t sieved[kMetaSlots][128];  // what sieve_block found in the unit of the slot, by column
   int sieved_seq;                    // units of which that is complete
-  int unit_id[32];          // the last units issued
+  int unit_id[kLastUnits];  // the last units issued
   UnitMeta meta[kMetaSlots];
   // 8-bit cache: codes of V landed and widened; Q parts written and done with; a row's
-  // factor of its parts; scales of a block's pages, of K and then of V
+  // factor of its parts; scales of a block's pages, of K and then of V, log2 of V's over the
+  // largest of the unit's first block, and that over V's
   uint64_t code_full[kMaxStages], code_empty[kMaxStages], q_full[2], q_free[2];
   uint64_t copied;  // the output warps are done with a piece of the copies' sums
   float q_scale[kMetaSlots][kRows], v_ref[kMetaSlots][kRows];  // (v_ref: what O is in units of)
-  float __align__(16) scales[kScaleBlocks][2 * kPagesPerBlock];
+  float __align__(16) scales[kScaleBlocks][4 * kPagesPerBlock];
   // the scheduler's group of sequences: units before each, first rows, rows, lengths,
   // keys that all their rows see, tiles left whole, splits of the others
   uint8_t g_order[kGroup];  // (8-bit cache) sequences in the order of their units
@@ -492,37 +493,41 @@ __device__ __forceinline__ float ref_of(float scale) {
   return __uint_as_float(max(__float_as_uint(scale), 27u << 23) & 0x7f800000u);
 }
 __device__ __forceinline__ float over_ref(float ref) { return __uint_as_float((254u << 23) - __float_as_uint(ref)); }
+// Where every row of the warp sees every key, so that v_ref is the unit's: a weight times its
+// value's scale is an exponential with that scale's log2 among its addends, and what the sum
+// is of has it taken out once for 16 keys.  lv, iv: log2 and reciprocals of the scales over
+// v_ref, of the first of the pages (a scale of 0, whose weights count all the same, does not fit).
 template <class Publish>
-__device__ __forceinline__ bool softmax_plain_fp8(uint32_t s_addr, float row_mul, float val_mul, const float *ks,
-                                                  const float *vs, float base, float2 *l4, Publish publish) {
+__device__ __forceinline__ bool softmax_plain_fp8(uint32_t s_addr, float row_mul, const float *ks, const float *lv,
+                                                  const float *iv, float base, float2 *l4, Publish publish) {
   uint32_t v[2][16], pk[16];
   tmem_ld16(s_addr + 32, v[0]);
-  const float2 nbase2 = make_float2(-base, -base);
-  const float4 k4 = *reinterpret_cast<const float4 *>(ks), v4 = *reinterpret_cast<const float4 *>(vs);
-  const float kq[4] = {k4.z, k4.w, k4.x, k4.y}, vq[4] = {v4.z, v4.w, v4.x, v4.y};
-  bool fits = true;
+  const float4 k4 = *reinterpret_cast<const float4 *>(ks), v4 = *reinterpret_cast<const float4 *>(lv),
+               i4 = *reinterpret_cast<const float4 *>(iv);
+  const float kq[4] = {k4.z, k4.w, k4.x, k4.y}, vq[4] = {v4.z, v4.w, v4.x, v4.y}, iq[4] = {i4.z, i4.w, i4.x, i4.y};
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     uint32_t *const x = v[q & 1];
     tmem_ld_wait16(x);
     if (q < 3) tmem_ld16(s_addr + (q == 0 ? 48 : q == 1 ? 0 : 16), v[(q & 1) ^ 1]);
-    const float mul = row_mul * kq[q], val = val_mul * vq[q];
-    const float2 mul2 = make_float2(mul, mul), val2 = make_float2(val, val);
-    fits &= !(val < kLeastVal) || vq[q] == 0.f;
+    const float mul = row_mul * kq[q], add = vq[q] - base;
+    const float2 mul2 = make_float2(mul, mul), add2 = make_float2(add, add), inv2 = make_float2(iq[q], iq[q]);
+    float2 sum[2];
 #pragma unroll
     for (int c = 0; c < 16; c += 2) {
-      const float2 arg = __ffma2_rn(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), mul2, nbase2);
-      const float2 e = make_float2(fast_exp2(arg.x), fast_exp2(arg.y));
-      l4[(c >> 1) & 3] = __fadd2_rn(l4[(c >> 1) & 3], e);
-      const float2 w = __fmul2_rn(e, val2);
+      const float2 arg = __ffma2_rn(make_float2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), mul2, add2);
+      const float2 w = make_float2(fast_exp2(arg.x), fast_exp2(arg.y));
+      sum[(c >> 1) & 1] = c < 4 ? w : __fadd2_rn(sum[(c >> 1) & 1], w);
       pk[(q & 1) * 8 + c / 2] = pack_f16x2(w.x, w.y);
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) l4[(q & 1) * 2 + i] = __ffma2_rn(sum[i], inv2, l4[(q & 1) * 2 + i]);
     if (q & 1) {
       tmem_st16(s_addr + 32 + (q >> 1) * 16, pk);
       publish(q >> 1);
     }
   }
-  return fits;
+  return fminf(fminf(v4.x, v4.y), fminf(v4.z, v4.w)) >= kLeastLog2;
 }
 template <bool kBf16, class Publish>
 __device__ __forceinline__ bool softmax_masked_fp8(uint32_t s_addr, int hi, float row_mul, float val_mul,
@@ -1171,7 +1176,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           M.n_blocks = blk_hi - blk_lo;
           M.pass = pass;
           M.copies = kFp8 && pass == kFirst && nrows <= kRows / kCopies ? kCopies : 1;
-          sh.unit_id[k & 31] = u;
+          sh.unit_id[k & (kLastUnits - 1)] = u;
         }
         nb_before = nb_last;
         nb_last = blk_hi - blk_lo;
@@ -1307,6 +1312,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
         const int first = look_up();
         int id = look_up();
         fetch(first, at - 64);
+        float ref = 1.f;  // what V's scales are taken over
 #pragma unroll 1
         for (int j = 0; j < M.n_blocks; j += kAtOnce) {
           float k1 = ks, v1 = vs;
@@ -1320,12 +1326,16 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
             if (!(v1 >= 0.f && v1 < INF)) v1 = 0.f;
           }
           __syncwarp();
+          if (j == 0) ref = ref_of(__uint_as_float(__reduce_max_sync(0xffffffffu, lane < kPagesPerBlock ? __float_as_uint(v1) : 0u)));
+          const float over = v1 * over_ref(ref), lv = log2f(over), iv = __fdiv_rn(1.f, over);
 #pragma unroll 1
           for (int i = 0; i < min(kAtOnce, M.n_blocks - j); ++i, ++e) {
             if (e >= kStages && !(ok = wait_bar(sh.k_empty[e % kStages], ((e / kStages) - 1) & 1))) break;
             if (lane / kPagesPerBlock == i) {
               sh.scales[e % kScaleBlocks][lane % kPagesPerBlock] = k1;
               sh.scales[e % kScaleBlocks][kPagesPerBlock + lane % kPagesPerBlock] = v1;
+              sh.scales[e % kScaleBlocks][2 * kPagesPerBlock + lane % kPagesPerBlock] = lv;
+              sh.scales[e % kScaleBlocks][3 * kPagesPerBlock + lane % kPagesPerBlock] = iv;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sh.k_full[e % kStages]));
@@ -1694,7 +1704,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           const bool redo = __any_sync(0xffffffffu, odd);
           if (lane == 0) {
             if (redo) {
-              atomicOr(&sh.redo, 1u << (k & 31));
+              atomicOr(&sh.redo, 1u << (k & (kLastUnits - 1)));
               __threadfence_block();
             }
             mbar_arrive(bar(sh.meta_empty[slot]));
@@ -1776,7 +1786,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           if (lane == 0) {
             // (released only where there is something to release: it waits for the stores)
             if (redo) {
-              atomicOr(&sh.redo, 1u << (k & 31));
+              atomicOr(&sh.redo, 1u << (k & (kLastUnits - 1)));
               __threadfence_block();
             }
             asm volatile("red.relaxed.cta.shared::cta.add.u32 [%0], 1;" ::"r"(smem_u32(&sh.units_done)) : "memory");
@@ -1945,7 +1955,8 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           const uint32_t at = t_lane + L::col_s(jg & 1) + h * 64;
           const float *const sc = sh.scales[jg % kScaleBlocks] + 4 * h;
           if constexpr (kFp8)
-            inside &= softmax_plain_fp8(at, row_mul, val_mul, sc, sc + kPagesPerBlock, m_run == NEG_INF ? 0.f : m_run, l4, publish);
+            inside &= softmax_plain_fp8(at, row_mul, sc, sc + 2 * kPagesPerBlock, sc + 3 * kPagesPerBlock,
+                                        m_run == NEG_INF ? 0.f : m_run, l4, publish);
           else
             inside &= softmax_plain(at, sl2, m_run, l4, publish);
         }

@@ -11,10 +11,13 @@
 //   P V: V is widened to f16, which holds every code, and a weight goes to the tensor cores
 //      as f16 too, times its value's scale over v_ref (the largest of the unit's first block,
 //      a power of two), with its row's base at 2^4: up to 2^12 above the base it fits, 2^-29 of
-//      the base is lost at most, which is below what a sum in 32 bits loses.  2^-12 of a weight
+//      the base is lost at most, which is below what a sum in 32 bits loses.  2^-11 of a weight
 //      is what the rounding costs, an eighth of bf16's.  A unit whose O is not finite (a
 //      weight or a scale above f16's range) or which has scales below 2^-14 of v_ref is run
 //      again against true maxima with V and weights in bf16, which has the range.
+//      Where all rows see all of a block, v_ref is the unit's, and the scale's log2 is an addend
+//      of the weights' exponents: one product a weight less, and one for 16 keys more in the
+//      sums, which are of the weights alone.
 //   Roles beside those of chunk_attn.cuh: warps 2, 3 load V's codes; warp 7 has the pages'
 //      scales in shared memory a few blocks ahead; warps 20 to 23 part the queries, which go
 //      to TMEM as the tensor cores' A, and widen V's codes from one ring of shared memory into
@@ -29,11 +32,12 @@
 //   64 sequences of a token, 32 / 8 heads of 128, contexts of 100 to 8,191: 123 us [206],
 //     5.1 TB/s of 6.7: HBM, behind some 5 us until the first scores and 5 of tail.  19 of
 //     8,191: 60.6 us.
-//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 317 us, 1.62 PFLOP/s, 351 after seconds of
-//     it, 1.47, the power limit [345]; tensor pipe 69 % at work, a block 0.78 us.
-//   24 ragged chunks of up to 300, half of them a token, 40 / 8: 124 us [110 of other
+//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 308 us, 1.67 PFLOP/s, 341 to 351 after
+//     seconds of it, the power limit [345]; a block 0.76 us, whose MMAs have 0.65: the issue
+//     slots, of which a quarter of an SM's two softmax warps have most.
+//   24 ragged chunks of up to 300, half of them a token, 40 / 8: 120 to 123 us [110 of other
 //     lengths]: units' changes (a unit's queries are in parts some 3,000 cycles after its
-//     slot is free) and blocks, of which the single tokens' have four rows.
+//     slot is free) and blocks, of which the single tokens' have five rows.
 //   One token behind 255, 8 / 2 heads of 64: 8.4 us [8.3], latency.
 // Rows four times, and once: 64 sequences of a token 123 us and 132, 24 of 16 / 2 heads 18.4
 // and 19.9, 19 of 8,191 with heads of 64 48.0 and 51.3; at 32 rows (19 times 32 tokens) 66.7
@@ -41,7 +45,8 @@
 // Conversions are what V costs.  The long chunk: to bf16 by the warps that load it, three
 // instructions a pair, 606 us; to f16 by warps of their own 393; halves of registers as
 // operands of the conversions 328; queries parted by four lanes a row, which read it once,
-// instead of one 317.
+// instead of one 317; scales as addends of the exponents 308 (320 without in that run; the
+// ragged chunks 120 and 129, 19 times 32 tokens with heads of 64 52.7 and 54.8).
 #include "chunk_attn.cuh"
 
 extern "C" {
