@@ -29,10 +29,10 @@
 //
 // What bounds it, and what it measured on a GB300 (calls one after another; bf16 cache in
 // brackets):
-//   64 sequences of a token, 32 / 8 heads of 128, contexts of 100 to 8,191: 123 us [206],
+//   64 sequences of a token, 32 / 8 heads of 128, contexts of 100 to 8,191: 121 to 127 us [206],
 //     5.1 TB/s of 6.7: HBM, behind some 5 us until the first scores and 5 of tail.  19 of
 //     8,191: 60.6 us.
-//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 308 us, 1.67 PFLOP/s, 341 to 351 after
+//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 308 us, 1.67 PFLOP/s, 334 to 341 after
 //     seconds of it, the power limit [345]; a block 0.76 us, whose MMAs have 0.65: the issue
 //     slots, of which a quarter of an SM's two softmax warps have most.
 //   24 ragged chunks of up to 300, half of them a token, 40 / 8: 120 to 123 us [110 of other
