@@ -648,9 +648,10 @@ def _need_current(what: str, *tensors):
     """A launch goes to the current device: tensors of another one are refused."""
     import torch
     here = torch._C._cuda_getDevice()
-    if {here} != {t.get_device() for t in tensors}:
-        raise HpdError(what, 1, f"tensors on {', '.join(str(t.device) for t in tensors)}, while device {here} is the "
-                                "current one")
+    for t in tensors:
+        if t.get_device() != here:
+            raise HpdError(what, 1, f"tensors on {', '.join(str(t.device) for t in tensors)}, while device {here} is "
+                                    "the current one")
 
 
 def rope_table(max_pos: int, D: int, theta: float = 1e6, device="cuda"):
@@ -784,11 +785,12 @@ class QkNormRope:
             _need("QkNormRope", k_cache, kind, (None, 16, H_kv, D))
             _need("QkNormRope", v_cache, kind, shape)
         if coded:
-            one = (pages, H_kv)
-            if k_scale is None or v_scale is None or not _is(k_scale, self._f32, one) or \
-                    not _is(v_scale, self._f32, one):
-                _need("QkNormRope", k_scale, self._f32, one)
-                _need("QkNormRope", v_scale, self._f32, one)
+            one, f32 = (pages, H_kv), self._f32
+            if k_scale is None or v_scale is None or k_scale.dtype is not f32 or v_scale.dtype is not f32 or \
+                    k_scale.shape != one or v_scale.shape != one or not (k_scale.is_cuda and v_scale.is_cuda) or \
+                    not (k_scale.is_contiguous() and v_scale.is_contiguous()):
+                _need("QkNormRope", k_scale, f32, one)
+                _need("QkNormRope", v_scale, f32, one)
             _need_current("QkNormRope", qkv, k_cache, v_cache, k_scale, v_scale)
         if q_out is None:
             if self._q is None or self._q.shape[0] < T:
@@ -800,7 +802,7 @@ class QkNormRope:
                 with self._on(stream):
                     self._q = qkv.new_empty((rows, H_q, D))
             q_out = self._q if self._q.shape[0] == T else self._q[:T]
-        elif not _is(q_out, bf, (T, H_q, D)):
+        elif q_out.dtype is not bf or q_out.shape != (T, H_q, D) or not (q_out.is_cuda and q_out.is_contiguous()):
             _need("QkNormRope", q_out, bf, (T, H_q, D))
         at = qkv.data_ptr()
         a.q, a.k, a.v = at, at + 2 * H_q * D, at + 2 * (H_q + H_kv) * D
