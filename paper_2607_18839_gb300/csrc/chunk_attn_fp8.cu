@@ -32,11 +32,11 @@
 //   64 sequences of a token, 32 / 8 heads of 128, contexts of 100 to 8,191: 121 to 127 us [206],
 //     5.1 TB/s of 6.7: HBM, behind some 5 us until the first scores and 5 of tail.  19 of
 //     8,191: 60.6 us.
-//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 308 us, 1.67 PFLOP/s, 334 to 341 after
-//     seconds of it, the power limit [345]; a block 0.76 us, whose MMAs have 0.65: the issue
+//   2,048 tokens behind 14,336, 32 / 8 heads of 128: 308 us [295], 1.67 PFLOP/s, 334 to 341
+//     after seconds of it, the power limit [337 to 349]; a block 0.76 us, whose MMAs have 0.65: the issue
 //     slots, of which a quarter of an SM's two softmax warps have most.
-//   24 ragged chunks of up to 300, half of them a token, 40 / 8: 120 to 123 us [110 of other
-//     lengths]: units' changes (a unit's queries are in parts some 3,000 cycles after its
+//   24 ragged chunks of up to 300, half of them a token, 40 / 8: 120 to 123 us [97 to 110 of
+//     other lengths]: units' changes (a unit's queries are in parts some 3,000 cycles after its
 //     slot is free) and blocks, of which the single tokens' have five rows.
 //   One token behind 255, 8 / 2 heads of 64: 8.4 us [8.3], latency.
 // Rows four times, and once: 64 sequences of a token 123 us and 132, 24 of 16 / 2 heads 18.4
