@@ -8,8 +8,8 @@
 //
 // A row is read once, 16 bytes a load, by a CTA of 256 threads or, of few rows, by a cluster
 // of up to eight.  Every thread has sums in 32 bits against a base of its own, the largest of
-// its first pieces, moved only by a value 2^kWindow above it: no branch depends on where a
-// row's maxima stand.  All values are in the sums; where that leaves the rest of a row too few
+// its first pieces with a value above -inf, moved only by a value 2^kWindow above it: no branch
+// depends on where a row's maxima stand.  All values are in the sums; where that leaves the rest of a row too few
 // digits beside its largest value (a rest below kSure), the thread that has that one sums its
 // values once more without it, and the others lose nothing.
 // Top values: every thread knows its own maximum.  The top-th largest maximum of 64 groups
@@ -140,15 +140,16 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return a;
 }
 
-// A thread's values.  Sums are taken against a base, the largest of its first piece, which
-// moves only when a value passes it by 2^kWindow: no branch depends on where a row's
-// maxima stand (one at every new maximum had two in three of the pieces in both of its
-// sides).  All values are in the sums; of a row whose other values have little weight
+// A thread's values.  Sums are taken against a base, the largest of the first piece that has a
+// value above -inf, which moves only when a value passes it by 2^kWindow: no branch depends on
+// where a row's maxima stand (one at every new maximum had two in three of the pieces in both of
+// its sides).  Until then there is nothing to sum: a base of 0, say, would lose all of a row
+// that begins with -inf and whose other values are e^-88 and less.  All values are in the sums; of a row whose other values have little weight
 // beside the largest, whoever has that sums once more without it.
 template <class T>
 struct Running {
-  float m;            // the largest value
-  float base, limit;  // and what moves it (NaN: bf16, and no floor below the base is a number)
+  float m;            // the largest value; -inf: none yet
+  float base, limit;  // and what moves it (-inf: there is none yet; NaN: bf16, and no floor below it is a number)
   uint32_t floor2;    // bf16: what is below has 2^d = 0
   float2 sum, mean;   // of 2^d and 2^d d, d against the base
 
@@ -162,10 +163,11 @@ struct Running {
       if (b < -1e37f) limit = nan();
     }
   }
-  __device__ __forceinline__ void start(float first, float c) {
+  __device__ __forceinline__ void start(float c) {
     m = -inf();
     sum = mean = make_float2(0.f, 0.f);
-    set_base(fabsf(first) < inf() ? first : 0.f, c);
+    set_base(0.f, c);
+    limit = -inf();
   }
   __device__ __forceinline__ void add2(float2 x, bool floored, float c) {
     float2 d = __fmul2_rn(__fadd2_rn(x, make_float2(-base, -base)), make_float2(c, c));
@@ -196,7 +198,7 @@ struct Running {
   __device__ __forceinline__ void take(const uint4 *v, float largest, float c) {
     m = fmaxf(m, largest);
     if (!(largest <= limit)) {
-      if (largest > base + kWindow / c) raise(largest, c);
+      if (limit == -inf() || largest > base + kWindow / c) raise(largest, c);
       if (limit != limit) {
 #pragma unroll
         for (int i = 0; i < N; ++i) add<false>(v[i], c);
@@ -207,8 +209,8 @@ struct Running {
     for (int i = 0; i < N; ++i) add<true>(v[i], c);
   }
   __device__ __forceinline__ void raise(float to, float c) {
-    const float d = fmaxf((base - to) * c, kNothing), w = fast_exp2(d);
-    // (w is 0 where nothing is left; sums that are NaN stay NaN)
+    const float d = fminf(fmaxf((base - to) * c, kNothing), 0.f), w = fast_exp2(d);
+    // (w is 0 where nothing is left; sums that are NaN stay NaN; of a first base they are 0, or NaN)
     mean = make_float2(w * fmaf(d, sum.x, mean.x), w * fmaf(d, sum.y, mean.y));
     sum = make_float2(w * sum.x, w * sum.y);
     set_base(to, c);
@@ -404,29 +406,19 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
       w = make_uint4(__float_as_uint(s.row[i]), 0xff800000u, 0xff800000u, 0xff800000u);
     run.template take<1>(&w, V::largest(w), c);
   };
+  run.start(c);
   int v = s.v0 + tid;
-  if (v < s.v1) {
+#pragma unroll 1
+  for (; v + (kUnroll - 1) * kThreads < s.v1; v += kUnroll * kThreads) {
     uint4 w[kUnroll];
-    bool started = false;
-#pragma unroll 1
-    for (; v + (kUnroll - 1) * kThreads < s.v1; v += kUnroll * kThreads) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) w[u] = s.piece(v + u * kThreads);
-      const float largest = V::largest4(w);
-      if (!started) run.start(largest, c);
-      started = true;
-      run.template take<kUnroll>(w, largest, c);
-    }
+    for (int u = 0; u < kUnroll; ++u) w[u] = s.piece(v + u * kThreads);
+    run.template take<kUnroll>(w, V::largest4(w), c);
+  }
 #pragma unroll 1
-    for (; v < s.v1; v += kThreads) {
-      w[0] = s.piece(v);
-      const float largest = V::largest(w[0]);
-      if (!started) run.start(largest, c);
-      started = true;
-      run.template take<1>(w, largest, c);
-    }
-  } else {
-    run.start(0.f, c);
+  for (; v < s.v1; v += kThreads) {
+    const uint4 w = s.piece(v);
+    run.template take<1>(&w, V::largest(w), c);
   }
   if (tid < s.head && rank == 0) single(tid);
   if (tid < s.tail) single(s.tail0 + tid);

@@ -188,6 +188,47 @@ def test_gpu_values_a_step_above_a_threads_first_ones(torch):
     _check(torch, x.view(1, -1), [5000000], 0, temperature=0.51 * 2.0 ** -23 / 60 / np.log(2.0))
 
 
+def _check_lost(torch, x, tokens, top, temperature):
+    """_check where many terms of a row are below 2^-126 and count as 0: the entropy loses up to
+    (1 + |d|) 2^-126 of each, |d| at most 126 log 2 = 87.4 there (what is smaller loses less)."""
+    r = H.token_logprobs(x, torch.from_numpy(np.asarray(tokens, np.int32)).cuda(), top=top, temperature=temperature)
+    ent = torch.from_numpy(O.logprobs(x.float().cpu().numpy(), tokens, 0, temperature)[1]).cuda()
+    lost = (r.entropy - ent).abs() <= x.shape[1] * 88.4 * 2.0 ** -126
+    _check(torch, x, tokens, top, temperature, got=r._replace(entropy=torch.where(lost, ent, r.entropy)))
+
+
+@gpu
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("R,V,top", [(300, 32000, 8), (5, 32000, 0), (6, 151936, 20), (1, 70001, 32)])
+def test_gpu_values_far_below_zero_behind_those_that_have_none(torch, wide, R, V, top):
+    # a thread's first values are -inf, and those that follow are small: e^x is no number of 32 bits
+    rng = np.random.default_rng(R + V)
+    at = np.arange(V)
+    few = [rng.choice(V, V // 100, replace=False) for _ in range(R)]
+    some = np.zeros((R, V), bool)
+    for r, i in enumerate(few):
+        some[r, i] = True
+    for allowed, mean, std, temperature in (
+            (at >= 10000, -100.0, 2.0, 1.0), (at >= 10000, -12.0, 2.0, 0.1), (at >= V - 300, -82.0, 1.0, 1.0),
+            (some, 0.0, 4.0, 0.1), (some, -1.0, 3.0, 0.02), (some | (at < 3), -3e4, 1.0, 1.0)):
+        x = rng.standard_normal((R, V)).astype(np.float32) * std + np.float32(mean)
+        x = torch.from_numpy(np.where(allowed, x, -INF).astype(np.float32)).cuda()
+        tokens = np.where(rng.random(R) < 0.7, x.argmax(1).cpu().numpy(), rng.integers(0, V, R))
+        _check_lost(torch, x if wide else x.to(torch.bfloat16), tokens, top, temperature)
+
+
+@gpu
+@pytest.mark.parametrize("wide", [False, True])
+def test_gpu_a_few_values_far_below_zero(torch, wide):
+    # rows without a piece of 16 bytes, and with a value or more on either side of the pieces
+    rng = np.random.default_rng(11)
+    for V in list(range(1, 20)) + [2049, 8195]:
+        for shift in range(4):
+            whole = torch.from_numpy(rng.standard_normal((4, V + 9)).astype(np.float32) - 100).cuda()
+            x = (whole if wide else whole.to(torch.bfloat16))[:, shift: shift + V]
+            _check(torch, x, rng.integers(0, V, 4), min(V, 5))
+
+
 @gpu
 def test_gpu_tokens_that_are_none(torch):
     x = _logits(torch, np.random.default_rng(1), 6, 500, False)
