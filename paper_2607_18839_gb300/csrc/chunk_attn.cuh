@@ -124,10 +124,11 @@ struct Rings<true> {
 constexpr int kMaxStages = 4;
 constexpr int kScaleBlocks = 8;  // blocks whose scales are held
 constexpr int kCopies = 4;       // of the rows of a tile of a quarter of its 128 at most
-// 8-bit cache, a first pass, whose weights are f16: log2 of the weight of a row's base
-// (weights up to 2^12 above it fit, 2^-29 of it is not lost), and the least scale of V,
-// over that of its first block, at which none of 2^-4 and more loses digits.
-constexpr float kFirstLog2 = 4.f, kLeastLog2 = -14.f, kLeastVal = 0x1p-14f;
+// 8-bit cache, a first pass, whose weights times their values' scales are f16: log2 of what the
+// row's base has at least (2^11 times that fits; less is off by 2^-11 of it or by 2^-29 of the
+// base's), and how many powers of two scales may be below the unit's where these are addends of
+// the exponents (further away they would take digits from them).
+constexpr float kFirstLog2 = 4.f, kFarLog2 = 14.f;
 constexpr int kGroup = 256;      // sequences whose lengths the scheduler holds at once
 constexpr int kMaxSplits = 32;
 constexpr int kTailWaves = 4;    // most waves of the units of split tiles
@@ -455,31 +456,43 @@ __device__ __noinline__ void add_sieved(const uint32_t *first, int keys, float *
 // the key's scale, one for the 16 keys of a page.  A weight goes to the tensor cores
 // times its value's scale over the row's v_ref, rounded once; its sum is of the weight
 // alone.  In a first pass that is to f16, 2^-11 of it and as V's codes widen with one
-// instruction for two.  What f16 cannot hold is run again with bf16: a weight that is too
-// large becomes infinite, which the reader of O finds, and scales of V too far below
-// v_ref are found here (false).  ks, vs: scales of the first of the pages.
-__device__ __noinline__ float row_max_fp8(uint32_t s_addr, int apart, bool plain, int hi, float row_mul,
-                                          const float *ks) {
+// instruction for two.  The base is lowered by as many powers of two as the scale of its own page
+// is below v_ref: the products add up to 2^kFirstLog2 at least, so that what those below f16's
+// normal numbers lose, 2^-25 each, is 2^-29 of the sum at most, however small the scales are.
+// (Without, a row whose weight is all on pages of 2^-13 of v_ref was off by a sixth.)  What f16
+// cannot hold is run again with bf16: a product that is too large becomes infinite, which the
+// reader of O finds.  ks, vs: scales of the first of the pages.
+//
+// A row's largest score of 32 columns at s_addr and of 32 at s_addr + apart, and the scale of
+// V of its page (of none: the first one's).  sc: scales of K of the first of the pages, V's behind.
+__device__ __noinline__ float2 row_max_fp8(uint32_t s_addr, int apart, bool plain, int hi, float row_mul,
+                                           const float *sc) {
   const float NEG_INF = -__int_as_float(0x7f800000);
-  float mx[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
+  float2 best = make_float2(NEG_INF, sc[kPagesPerBlock]);
 #pragma unroll 1
   for (int part = 0; part < 2; ++part) {
     uint32_t v[32];
     tmem_ld32(s_addr, v);
     tmem_ld_wait32(v);
 #pragma unroll
-    for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(__uint_as_float(v[c]) * (row_mul * ks[c / kPage]));
+    for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(__uint_as_float(v[c]) * (row_mul * sc[c / kPage]));
     if (!plain) tc::mask32(v, 0, hi, false, 1.f);
 #pragma unroll
-    for (int c = 0; c < 32; c += 8)
+    for (int i = 0; i < 32 / kPage; ++i) {
+      float mx[2] = {NEG_INF, NEG_INF};
 #pragma unroll
-      for (int a = 0; a < 4; ++a)
-        mx[a] = tc::fmax3(mx[a], __uint_as_float(v[c + 2 * a]), __uint_as_float(v[c + 2 * a + 1]));
+      for (int c = i * kPage; c < (i + 1) * kPage; c += 4)
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+          mx[a] = tc::fmax3(mx[a], __uint_as_float(v[c + 2 * a]), __uint_as_float(v[c + 2 * a + 1]));
+      const float m = fmaxf(mx[0], mx[1]);
+      if (m > best.x) best = make_float2(m, sc[kPagesPerBlock + i]);
+    }
     s_addr += apart;
     hi -= apart;
-    ks += apart / kPage;
+    sc += apart / kPage;
   }
-  return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+  return best;
 }
 // Largest scale of V among a block's pages that have one of its first `keys` keys.
 __device__ __forceinline__ float largest_scale(const float *vs, int keys) {
@@ -488,9 +501,9 @@ __device__ __forceinline__ float largest_scale(const float *vs, int keys) {
   for (int i = 0; i < kPagesPerBlock; ++i) m = i * kPage < keys ? fmaxf(m, vs[i]) : m;
   return m;
 }
-// The power of two at or below it (2^-100 of less), and that over one.
+// The power of two at or below it (from 2^-100 to 2^126, which has a reciprocal), and that over one.
 __device__ __forceinline__ float ref_of(float scale) {
-  return __uint_as_float(max(__float_as_uint(scale), 27u << 23) & 0x7f800000u);
+  return __uint_as_float(min(max(__float_as_uint(scale), 27u << 23), 253u << 23) & 0x7f800000u);
 }
 __device__ __forceinline__ float over_ref(float ref) { return __uint_as_float((254u << 23) - __float_as_uint(ref)); }
 // Where every row of the warp sees every key, so that v_ref is the unit's: a weight times its
@@ -527,13 +540,12 @@ __device__ __forceinline__ bool softmax_plain_fp8(uint32_t s_addr, float row_mul
       publish(q >> 1);
     }
   }
-  return fminf(fminf(v4.x, v4.y), fminf(v4.z, v4.w)) >= kLeastLog2;
+  return fminf(fminf(v4.x, v4.y), fminf(v4.z, v4.w)) >= -kFarLog2;
 }
 template <bool kBf16, class Publish>
-__device__ __forceinline__ bool softmax_masked_fp8(uint32_t s_addr, int hi, float row_mul, float val_mul,
+__device__ __forceinline__ void softmax_masked_fp8(uint32_t s_addr, int hi, float row_mul, float val_mul,
                                                    const float *ks, const float *vs, float base, float2 *l4,
                                                    Publish publish) {
-  bool fits = true;
 #pragma unroll 1
   for (int part = 0; part < 2; ++part) {
     uint32_t v[32], pk[16];
@@ -552,26 +564,23 @@ __device__ __forceinline__ bool softmax_masked_fp8(uint32_t s_addr, int hi, floa
       const float2 w = make_float2(e.x == 0.f ? 0.f : e.x * val[c / kPage], e.y == 0.f ? 0.f : e.y * val[c / kPage]);
       pk[c / 2] = kBf16 ? pack_bf16x2(w.x, w.y) : pack_f16x2(w.x, w.y);
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) fits &= !(val[i] < kLeastVal) || vs[p0 + i] == 0.f;
     tmem_st16(s_addr + 32 + 16 * part, pk);
     publish(part);
   }
-  return kBf16 || fits;
 }
 
 // The same of a row that the tile has kCopies times: a copy takes one of the half's pages
 // and leaves weights of 0 for the others.  (A thread's 64 columns bound the blocks of tiles
 // of few rows, where most softmax threads had no row.)
 template <class Publish>
-__device__ __forceinline__ bool softmax_share_fp8(uint32_t s_addr, int copy, int hi, float row_mul, float val_mul,
+__device__ __forceinline__ void softmax_share_fp8(uint32_t s_addr, int copy, int hi, float row_mul, float val_mul,
                                                   const float *ks, const float *vs, float base, float2 *l4,
                                                   Publish publish) {
   static_assert(kCopies * kPage == kBlk / 2, "a page each");
   const float NEG_INF = -__int_as_float(0x7f800000);
   uint32_t v[16], pk[8];
   tmem_ld16(s_addr + copy * kPage, v);
-  const float mul = row_mul * ks[copy], scale = vs[copy], val = val_mul * scale;
+  const float mul = row_mul * ks[copy], val = val_mul * vs[copy];
   const int seen = hi - copy * kPage;
   const float2 mul2 = make_float2(mul, mul), nbase2 = make_float2(-base, -base);
   tmem_ld_wait16(v);
@@ -593,7 +602,6 @@ __device__ __forceinline__ bool softmax_share_fp8(uint32_t s_addr, int copy, int
     }
   }
   publish();
-  return !(val < kLeastVal) || scale == 0.f;
 }
 
 // Rows row0 to row0 + rows - 1 (32 at most) of a tile's queries in two e4m3 parts, one
@@ -1913,7 +1921,7 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           const uint32_t at = t_lane + L::col_s(jg & 1) + h * 64;
           if constexpr (kFp8) {
             const float *const sc = sh.scales[jg % kScaleBlocks];
-            mx_run = fmaxf(mx_run, row_max_fp8(at, 32, j < n_plain, hi, row_mul, sc + 4 * h));
+            mx_run = fmaxf(mx_run, row_max_fp8(at, 32, j < n_plain, hi, row_mul, sc + 4 * h).x);
           } else {
             mx_run = fmaxf(mx_run, row_max(at, 32, j < n_plain, hi, sl2));
           }
@@ -1927,8 +1935,12 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           const int hi = min(lim - blk_lo * kBlk, kBlk);
           if constexpr (kFp8) {
             const float *const sc = sh.scales[jg % kScaleBlocks];
-            m_run = row_max_fp8(at, 64, n_plain > 0, hi, row_mul, sc) - kFirstLog2;
+            const float2 first = row_max_fp8(at, 64, n_plain > 0, hi, row_mul, sc);
             v_ref = ref_of(largest_scale(sc + kPagesPerBlock, hi));
+            const int below =  // powers of two
+                static_cast<int>(__float_as_uint(v_ref) - __float_as_uint(ref_of(first.y))) >> 23;
+            m_run = first.x - (kFirstLog2 + below);
+            inside = below <= kFarLog2;
           } else {
             m_run = row_max(at, 64, n_plain > 0, hi, sl2);
           }
@@ -1938,14 +1950,13 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           if (h == 0) sh.v_ref[slot][r_in] = v_ref;
         }
         // (scores of -inf alone give no base to a row that sees the unit's keys)
-        inside = pass != kFirst || m_run > NEG_INF || lim <= blk_lo * kBlk;
+        inside &= pass != kFirst || m_run > NEG_INF || lim <= blk_lo * kBlk;
         if constexpr (kFp8) {
           for (; M.copies > 1 && j < nb; ++j, ++jg) {
             if (j > 0 && !(ok = await_s())) break;
             const float *const sc = sh.scales[jg % kScaleBlocks] + 4 * h;
-            inside &= softmax_share_fp8(t_lane + L::col_s(jg & 1) + h * 64, quad,
-                                        min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64, row_mul, val_mul, sc,
-                                        sc + kPagesPerBlock, m_run == NEG_INF ? 0.f : m_run, l4, publish_both);
+            softmax_share_fp8(t_lane + L::col_s(jg & 1) + h * 64, quad, min(lim - (blk_lo + j) * kBlk, kBlk) - h * 64,
+                              row_mul, val_mul, sc, sc + kPagesPerBlock, m_run == NEG_INF ? 0.f : m_run, l4, publish_both);
           }
           if (!ok) break;
         }
@@ -1967,15 +1978,18 @@ __global__ void __launch_bounds__(kThreads<kFp8>, 1)
           const uint32_t at = t_lane + L::col_s(jg & 1) + h * 64;
           const float *const sc = sh.scales[jg % kScaleBlocks] + 4 * h;
           if constexpr (kFp8)
-            inside &= pass == kAgain ? softmax_masked_fp8<true>(at, hi, row_mul, 1.f, sc, sc + kPagesPerBlock,
-                                                                m_run == NEG_INF ? 0.f : m_run, l4, publish)
-                                     : softmax_masked_fp8<false>(at, hi, row_mul, val_mul, sc, sc + kPagesPerBlock,
-                                                                 m_run == NEG_INF ? 0.f : m_run, l4, publish);
+            pass == kAgain ? softmax_masked_fp8<true>(at, hi, row_mul, 1.f, sc, sc + kPagesPerBlock,
+                                                      m_run == NEG_INF ? 0.f : m_run, l4, publish)
+                           : softmax_masked_fp8<false>(at, hi, row_mul, val_mul, sc, sc + kPagesPerBlock,
+                                                       m_run == NEG_INF ? 0.f : m_run, l4, publish);
           else
             inside &= softmax_masked(at, hi, sl2, m_run, l4, publish);
         }
       }
       if (!ok) break;
+      // (weights of pages whose scales are next to nothing may be beyond any product: the two halves'
+      // sum, and v_ref over it, have to be numbers)
+      if constexpr (kFp8) inside &= pass != kFirst || tc::sum_of(l4) <= fminf(over_ref(val_mul), 0x1p-26f) * 0x1p125f;
       sh.xsum[slot][h][r_in] = pass == kMaxima ? mx_run : inside ? tc::sum_of(l4) : __int_as_float(0x7fffffff);
       if (h == 0) sh.xbase[slot][r_in] = m_run;
       __syncwarp();

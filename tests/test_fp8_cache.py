@@ -548,6 +548,53 @@ def test_gpu_attn_scales_far_apart(torch, D):
 
 
 @gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("S,n", [(19, 1), (1, 608)])
+@pytest.mark.parametrize("ratio,low,zeros,most", [
+    (2.0 ** -10, 10, False, 1.0), (2.0 ** -13, 8, False, 1.0), (2.0 ** -13, 10, False, 1.0), (2.0 ** -13.9, 9, False, 1.0),
+    (2.0 ** -13.9, 11, False, 1.0), (2.0 ** -13, 10, True, 1.0), (2.0 ** -16, 10, False, 1.0), (2.0 ** 9, 11, False, 1.0),
+    (2.0 ** -13, 10, False, 2.0 ** 127), (2.0 ** -13, 10, False, 2.0 ** -80)])
+def test_gpu_attn_values_of_other_scales_than_the_first_blocks(torch, S, n, D, ratio, low, zeros, most):
+    # 16,000 keys of equal weights, e^-low of the largest, whose values' scales are `ratio` times the second page's;
+    # that has next to no weight, so that a row is of the small ones.  152 units of all keys: the sequences share
+    # their pages, the queries are the same.  zeros: pages of zeros with the least scale, of much weight.
+    hq, hkv, L = 32, 8, 16400
+    rng = np.random.default_rng(17)
+    pages = C.pages_of(L)
+    k, v = np.zeros((pages, PAGE, hkv, D)), 448.0 * 2.0 ** -rng.integers(0, 2, (pages, PAGE, hkv, D))
+    vs = np.full((pages, hkv), ratio, np.float32)
+    k[..., 0] = -low
+    k[0, 3, :, 0] = 0
+    k[1, :, :, 0], vs[1] = -40, 1.0
+    vs *= np.float32(most)
+    if zeros:
+        v[[20, 333]], vs[[20, 333]] = 0, 2.0 ** -100
+        k[[20, 333], 5, :, 0] = -1
+    code = lambda x: torch.from_numpy(x).cuda().float().to(torch.float8_e4m3fn)  # noqa: E731
+    i32 = lambda a: torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    ids = rng.permutation(pages)
+    back = np.argsort(ids)  # the page of a sequence that is held at a place of the cache
+    op = H.ChunkAttn(hq, code(k[back]), code(v[back]), i32(np.tile(ids, (S, 1))), max_tokens=S * n, scale=1.0,
+                     k_scale=torch.ones(pages, hkv, device="cuda"), v_scale=torch.from_numpy(vs[back]).cuda())
+    q = torch.zeros(S * n, hq, D, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 1.0
+    out, lse = op(q, i32(np.arange(S + 1) * n), i32([L] * S))
+    torch.cuda.synchronize()
+    assert op.errors() == 0
+    p = np.exp(k[..., 0].reshape(-1, hkv)[:L])
+    x = (v * vs[:, None, :, None].astype(np.float64)).reshape(-1, hkv, D)[:L]
+    lim = L - n + np.arange(n)
+    tot = np.cumsum(p, 0)[lim]
+    size = np.cumsum(p[..., None] * x, 0)[lim] / tot[..., None]  # (all values are positive: the output too)
+    rows = lambda a: np.repeat(np.tile(a, (S,) + (1,) * (a.ndim - 1)), hq // hkv, 1)  # noqa: E731
+    # roundings as in _near, of scores up to 40 whose queries lose nothing
+    slip = 2.0 ** -20 * 40 + 2.0 ** -19
+    assert (np.abs(lse.cpu().numpy() - rows(np.log(tot))) <= slip + 2.0 ** -21 * np.abs(rows(np.log(tot)))).all()
+    off = np.abs(K._np(out) / rows(size) - 1)
+    assert (off <= 2.0 ** -7 * 1.02 + 2 * slip).all(), off.max()
+
+
+@gpu
 def test_gpu_attn_rising_scores(torch):
     # scores that rise by more than the window of a fixed base
     c = K._attn_case(torch, [64, 1], [900, 2000], 8, 2, 128, seed=5)
