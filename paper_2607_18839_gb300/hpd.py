@@ -539,6 +539,9 @@ def token_logprobs(logits, tokens, top=0, temperature=1.0, stream=None) -> Token
         raise HpdError(what, 1, "a temperature above 0, from 1e-36 to 1e36")
     if not 0 <= top <= min(V, 32):
         raise HpdError(what, 1 if top < 0 or top > V else 2, "0 to 32 alternatives, no more than there are tokens")
+    rows = tokens.numel()
+    if V > 1 << 30 or rows >= 1 << 31:  # (the call's integers would hold other numbers)
+        raise HpdError(what, 2, "up to 2^30 tokens to choose from and fewer than 2^31 rows")
     device = logits.device
     _need_current(what, logits, tokens)
     empty, f32, ids, lps = torch.empty, torch.float32, None, None
@@ -549,7 +552,7 @@ def token_logprobs(logits, tokens, top=0, temperature=1.0, stream=None) -> Token
             ids = empty((*lead, top), dtype=torch.int32, device=device)
             lps = empty((*lead, top), dtype=f32, device=device)
     a = hpd_token_logprobs_args(logits.data_ptr(), stride, tokens.data_ptr(), logprob.data_ptr(), entropy.data_ptr(),
-                                _ptr(ids), _ptr(lps), tokens.numel(), V, top, logits.dtype is not bf, 1.0 / temperature)
+                                _ptr(ids), _ptr(lps), rows, V, top, logits.dtype is not bf, 1.0 / temperature)
     hpd_token_logprobs(a, _stream_handle(stream))
     return TokenLogprobs(logprob, entropy, ids, lps)
 

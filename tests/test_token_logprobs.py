@@ -56,6 +56,25 @@ def test_no_rows_need_no_device(lib):
     H.hpd_token_logprobs(args(R=0, logits=None, tokens=None, logprob=None), None)
 
 
+@pytest.mark.parametrize("R,V", [(1, 2 ** 32 + 100), (2, 2 ** 31), (3, 2 ** 30 + 1), (2 ** 32 + 5, 1), (2 ** 31, 1)])
+def test_sizes_that_do_not_fit_the_call_are_refused(lib, monkeypatch, R, V):
+    torch = pytest.importorskip("torch")
+    made = []
+
+    class OnDevice(torch.Tensor):
+        is_cuda = property(lambda self: True)
+
+    monkeypatch.setattr(H, "_need_current", lambda *a: None)
+    monkeypatch.setattr(H, "_stream_handle", lambda s: None)
+    monkeypatch.setattr(H, "hpd_token_logprobs", lambda a, s: made.append((a.R, a.V)))
+    on = lambda *n, **kw: torch.empty(n, device="meta", **kw).as_subclass(OnDevice)  # noqa: E731
+    with pytest.raises(H.HpdError) as e:
+        H.token_logprobs(on(R, V, dtype=torch.bfloat16), on(R, dtype=torch.int32))
+    assert e.value.status == 2 and not made
+    H.token_logprobs(on(7, 2 ** 30, dtype=torch.bfloat16), on(7, dtype=torch.int32))
+    assert made == [(7, 2 ** 30)]
+
+
 def test_struct_layout_matches_the_header(tmp_path):
     if shutil.which("gcc") is None:
         pytest.skip("no gcc")
