@@ -509,7 +509,7 @@ hpd_status hpd_qk_norm_rope_fp8(const hpd_qk_norm_rope_fp8_args *args, hpd_strea
  * is taken to 2^-17 of its row's largest value; scores, sums and lse are in 32 bits; a
  * weight, times its value's scale, is rounded to f16 or, where f16 has not the range for
  * a tile's weights and scales, to bf16: off by 2^-8 of that product at most, as in
- * hpd_chunk_attn, or by 2^-29 of the sum of the row's products (2^-12 of it in all with
+ * hpd_chunk_attn, or by 2^-28 of the sum of the row's products (2^-11 of it in all with
  * 2^17 keys).  A query row with a value that is not finite gives NaN.  A
  * scale of a page that a tile of rows sees has to be at least 0 and finite; another
  * one is flagged HPD_DEVERR_SCALE and read as 0.  Cache rows at or past

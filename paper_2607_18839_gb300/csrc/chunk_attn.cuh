@@ -125,10 +125,10 @@ constexpr int kMaxStages = 4;
 constexpr int kScaleBlocks = 8;  // blocks whose scales are held
 constexpr int kCopies = 4;       // of the rows of a tile of a quarter of its 128 at most
 // 8-bit cache, a first pass, whose weights times their values' scales are f16: log2 of what the
-// row's base has at least (2^11 times that fits; less is off by 2^-11 of it or by 2^-29 of the
+// row's base has at least (2^12 times that fits; less is off by 2^-11 of it or by 2^-28 of the
 // base's), and how many powers of two scales may be below the unit's where these are addends of
 // the exponents (further away they would take digits from them).
-constexpr float kFirstLog2 = 4.f, kFarLog2 = 14.f;
+constexpr float kFirstLog2 = 3.f, kFarLog2 = 14.f;
 constexpr int kGroup = 256;      // sequences whose lengths the scheduler holds at once
 constexpr int kMaxSplits = 32;
 constexpr int kTailWaves = 4;    // most waves of the units of split tiles
@@ -458,7 +458,7 @@ __device__ __noinline__ void add_sieved(const uint32_t *first, int keys, float *
 // alone.  In a first pass that is to f16, 2^-11 of it and as V's codes widen with one
 // instruction for two.  The base is lowered by as many powers of two as the scale of its own page
 // is below v_ref: the products add up to 2^kFirstLog2 at least, so that what those below f16's
-// normal numbers lose, 2^-25 each, is 2^-29 of the sum at most, however small the scales are.
+// normal numbers lose, 2^-25 each, is 2^-28 of the sum at most, however small the scales are.
 // (Without, a row whose weight is all on pages of 2^-13 of v_ref was off by a sixth.)  What f16
 // cannot hold is run again with bf16: a product that is too large becomes infinite, which the
 // reader of O finds.  ks, vs: scales of the first of the pages.

@@ -10,8 +10,8 @@
 //      long as one of bf16, and K is never widened.  Scales go to the scores, 16 at a time.
 //   P V: V is widened to f16, which holds every code, and a weight goes to the tensor cores
 //      as f16 too, times its value's scale over v_ref (the largest of the unit's first block,
-//      a power of two), with its row's base, so weighted, from 2^4 to 2^5: 2^11 times that fits,
-//      and the least that f16 keeps loses 2^-29 of it at most, whatever the scales are: the row's
+//      a power of two), with its row's base, so weighted, from 2^3 to 2^4: 2^12 times that fits,
+//      and the least that f16 keeps loses 2^-28 of it at most, whatever the scales are: the row's
 //      products add up to it at least.  2^-11 of a weight is what the rounding costs otherwise, an
 //      eighth of bf16's.  A unit whose O is not finite (a weight or a scale above f16's range) is
 //      run again against true maxima with V and weights in bf16, which has the range, and so is one
