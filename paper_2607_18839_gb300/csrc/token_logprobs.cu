@@ -262,7 +262,7 @@ __device__ __forceinline__ Sums join_lanes(Sums s, int n, float c) {
 struct LogpShared {
   Sums warp[kWarps];
   float2 again[kWarps];
-  uint32_t group[kGroups];  // keys of the groups' maxima, made different by the groups' numbers
+  uint32_t __align__(16) group[kGroups];  // keys of the groups' maxima, made different by the groups' numbers
   uint32_t least;  // a lower bound of the last of the top values, as a key
   int found;       // candidates, some perhaps beyond their room
   int count;       // of a scan
