@@ -20,11 +20,11 @@
 // them has is found by halving the range of its bits, a pass over the share each.
 //
 // What bounds it, and what it measured on a GB300 (in a graph):
-//   6,144 rows of 32,000 in bf16, sums alone: 68.8 us, 5.7 TB/s, 85 % of a copy's rate; with
-//     8 alternatives 91.5: six barriers and two dependent reads of L2 a row, during which the
-//     SM's other four CTAs stream; with 32 alternatives 113.
-//   160 rows of 100,003 in fp32: 15.6 us; with 20 alternatives 22.6, of which 7 are those.
-//   64 rows of 32,000: 4.4 us, with 8 alternatives 6.3; one row of 151,936 4.3, with 20 11.3:
+//   6,144 rows of 32,000 in bf16, sums alone: 68.4 us, 5.7 TB/s, 85 % of a copy's rate; with
+//     8 alternatives 92.0: six barriers and two dependent reads of L2 a row, during which the
+//     SM's other four CTAs stream; with 32 alternatives 114.
+//   160 rows of 100,003 in fp32: 15.1 us; with 20 alternatives 21.2, of which 6 are those.
+//   64 rows of 32,000: 4.1 us, with 8 alternatives 6.0; one row of 151,936 4.3, with 20 9.9:
 //     latency: loads, join, bound, second reads, ranks, and the lists of a cluster's CTAs.
 // A warp a row, each value against a running maximum: 1,263 us for the 6,144 rows.  Rereading by the warps that have the hot threads (eight of them in one warp,
 // one after the other) and ranks by a scan of the cluster's lists: 160 rows 27.4, one 13.8.
@@ -613,13 +613,18 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) token_logprobs_kernel(co
 
 template <class T, bool kAlternatives>
 cudaError_t launch_logprobs(const LogpArgs &k, int R, cudaStream_t s) {
-  // CTAs of a row: as many as keep the GPU's SMs busy, none with less than 32 KB (joining a
-  // cluster's lists costs some 2 us: 64 rows of 32,000 with 8 alternatives 9.3 us with 8 KB
-  // each, 8.0 with 16, 6.3 with 32, 7.1 with 64; one row of 151,936 4.3
-  // without alternatives, 5.3 with 64 KB each, 7.1 with 128).
+  // CTAs of a row: as many as keep the GPU's SMs busy, none with less than 32 KB, or 64 where the
+  // cluster has lists to join, which costs some 1 us a doubling.  One, two, four and eight CTAs, 64
+  // rows in bf16 (us, in a graph):
+  //                                    32,000               32,768               65,536               100,003
+  //   sums alone             4.1  4.1  4.1  5.7   3.9  3.5  3.4  5.5   5.7  4.4  4.0  6.0   8.1  5.7  5.0   7.2
+  //   with 8 alternatives    5.9  7.2  8.5 12.0   5.8  6.6  8.0 11.9   7.8  7.5  8.3 12.6  10.2  9.0  9.2  13.7
+  // (One row: 65,536 with 8 7.2, 7.1, 7.4 and 9.2; 100,003 in fp32 11.8, 9.3, 8.3 and 9.5, alone 10.0,
+  // 6.5, 4.7 and 4.1.)
+  constexpr long long kLeastBytes = kAlternatives ? 65536 : 32768;
   int ctas = 1;
   while (ctas < kMaxCluster && static_cast<long long>(R) * ctas * 2 <= 4 * kLogpSms &&
-         static_cast<long long>(k.V) * static_cast<int>(sizeof(T)) >= 2LL * ctas * 32768)
+         static_cast<long long>(k.V) * static_cast<int>(sizeof(T)) >= 2 * ctas * kLeastBytes)
     ctas *= 2;
   static std::atomic<uint64_t> done{0};
   // (five CTAs an SM need a quarter of its 228 KB shared; the rest is for the loads)
