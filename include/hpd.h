@@ -491,7 +491,8 @@ hpd_status hpd_chunk_attn(const hpd_chunk_attn_args *args, hpd_stream_t stream);
  *   at offset o > 0:         the scale that is there, times 2^k with the least k >= 0
  *                            for which a <= scale; the codes of rows below o times 2^-k
  *   code = x / scale rounded to e4m3 (to nearest, ties to even); NaN where x is not
- *   finite
+ *   finite.  The quotient is a product with 1 / scale in 32 bits, 2^-22 of it off at
+ *   most: next to a border between two codes it may be either
  * so that a code is rounded once, but for one that leaves the normal numbers of e4m3
  * (below 2^-6 of 448) as its page's scale grows.  Rows behind the run are left as
  * they are.
@@ -510,7 +511,12 @@ hpd_status hpd_qk_norm_rope_fp8(const hpd_qk_norm_rope_fp8_args *args, hpd_strea
  * weight, times its value's scale, is rounded to f16 or, where f16 has not the range for
  * a tile's weights and scales, to bf16: off by 2^-8 of that product at most, as in
  * hpd_chunk_attn, or by 2^-28 of the sum of the row's products (2^-11 of it in all with
- * 2^17 keys).  A query row with a value that is not finite gives NaN.  A
+ * 2^17 keys).  A tile of rows runs again where f16 has not the range, and a call all of
+ * whose tiles do takes some 3.5 times as long: where a row's score passes its largest one
+ * among some 64 of the first keys by 12 log 2 = 8.3 (with a value whose scale is no larger
+ * than that key's; by less with a larger one), or where scales of V are less than 2^-14 of
+ * the first pages'.  A
+ * query row with a value that is not finite gives NaN.  A
  * scale of a page that a tile of rows sees has to be at least 0 and finite; another
  * one is flagged HPD_DEVERR_SCALE and read as 0.  Cache rows at or past
  * seq_len may hold anything, and the scales of pages past it too. */

@@ -73,7 +73,8 @@
 //     two or three a block.
 // 640 threads leave 96 registers each.  What does not fit (32 bytes of spill stores, 60
 // of loads with heads of 128; 24 and 44 with 64) is not in the blocks' loops: 246 local
-// loads an SM in a call of some 400 blocks an SM.
+// loads an SM in a call of some 400 blocks an SM.  (With kFp8, 80 registers each: 108 bytes
+// of stores and 136 of loads, 116 and 156 with heads of 64; 541 local loads an SM in the same call.)
 // Halves of a block for the two softmax warpgroups, and not alternate blocks: those
 // took 0.67 us a block with heads of 128 and 0.52 with heads of 64 (three buffers of
 // scores, five stages).

@@ -40,6 +40,12 @@
 //     other lengths]: units' changes (a unit's queries are in parts some 3,000 cycles after its
 //     slot is free) and blocks, of which the single tokens' have five rows.
 //   One token behind 255, 8 / 2 heads of 64: 8.4 us [8.3], latency.
+// These are of normal scores with a standard deviation of 1.  A unit that is run again takes three
+// passes, two of which have its blocks one by one through the masked path.  Sharper scores (us; other
+// contexts of the 64 tokens, with a deviation of 1 101 [175]):
+//   deviation               2          2.5          3          4          5
+//   64 tokens          101 [175]    101 [176]   198 [176]  318 [175]  342 [175]
+//   long chunk         528 [295]    772 [295]  1,002 [294] 1,141 [293] 1,141 [293]
 // Rows four times, and once: 64 sequences of a token 123 us and 132, 24 of 16 / 2 heads 18.4
 // and 19.9, 19 of 8,191 with heads of 64 48.0 and 51.3; at 32 rows (19 times 32 tokens) 66.7
 // and 66.8.  Longest first, and in order: 123 and 139, 124 and 129.
