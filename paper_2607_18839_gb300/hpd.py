@@ -742,7 +742,7 @@ class QkNormRope:
                 _need("QkNormRope", w, torch.bfloat16, (D,))
         _need("QkNormRope", rope, torch.float32, (None, D // 2, 2))
         self.H_q, self.H_kv, self.D = H_q, H_kv, D
-        self._keep = (q_weight, k_weight, rope)
+        self._held = [t for t in (q_weight, k_weight, rope) if t is not None]
         self.n_axes = max(axis) + 1
         self.workspace = _ready_workspace(256, rope.device)
         self._fp8 = hpd_qk_norm_rope_fp8_args()
@@ -794,7 +794,6 @@ class QkNormRope:
                     not (k_scale.is_contiguous() and v_scale.is_contiguous()):
                 _need("QkNormRope", k_scale, f32, one)
                 _need("QkNormRope", v_scale, f32, one)
-            _need_current("QkNormRope", qkv, k_cache, v_cache, k_scale, v_scale)
         if q_out is None:
             if self._q is None or self._q.shape[0] < T:
                 rows = T
@@ -807,6 +806,8 @@ class QkNormRope:
             q_out = self._q if self._q.shape[0] == T else self._q[:T]
         elif q_out.dtype is not bf or q_out.shape != (T, H_q, D) or not (q_out.is_cuda and q_out.is_contiguous()):
             _need("QkNormRope", q_out, bf, (T, H_q, D))
+        if coded:
+            _need_current("QkNormRope", qkv, pos, slot, k_cache, v_cache, k_scale, v_scale, q_out, *self._held)
         at = qkv.data_ptr()
         a.q, a.k, a.v = at, at + 2 * H_q * D, at + 2 * (H_q + H_kv) * D
         a.q_stride = a.k_stride = a.v_stride = row if T > 1 else 0  # (one row has none)
@@ -890,7 +891,7 @@ class ChunkAttn:
         a.chunk_cu, a.seq_len = chunk_cu.data_ptr(), seq_len.data_ptr()
         a.full_len = None if full_len is None else full_len.data_ptr()
         if self._coded:
-            _need_current("ChunkAttn", q)
+            _need_current("ChunkAttn", q, chunk_cu, seq_len, q if full_len is None else full_len, self.out)
             hpd_chunk_attn_fp8(self._fp8, _stream_handle(stream))
         else:
             hpd_chunk_attn(a, _stream_handle(stream))

@@ -20,6 +20,7 @@ from paper_2607_18839_gb300 import hpd as H
 gpu = pytest.mark.gpu
 PAGE = 16
 INF, NAN = float("inf"), float("nan")
+NEED_CURRENT = H._need_current
 
 
 @pytest.fixture(scope="module")
@@ -181,6 +182,33 @@ def test_caches_and_scales_of_the_wrong_kind_are_refused(host):
     op = attn(code(8, 16, 2, 64), code(8, 16, 2, 64), **good)
     op(bf(8, 4, 64), i32(3), i32(2))
     assert host.calls[-1][0] == "hpd_chunk_attn_fp8" and host.calls[-1][1].v_scale == good["v_scale"].data_ptr()
+
+
+def test_every_tensor_of_another_device_is_refused(host, monkeypatch):
+    torch, bf, i32, f32, code = host.torch, host.bf, host.i32, host.f32, host.code
+
+    class Far(type(bf(1))):
+        get_device = lambda self: 1  # noqa: E731
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1, raising=False)  # (where the host's tensors are)
+    monkeypatch.setattr(H, "_need_current", NEED_CURRENT)
+    rope = host.rope()
+    put = dict(qkv=bf(4, 512), pos=i32(4), slot=i32(4), k_cache=code(8, 16, 2, 64), v_cache=code(8, 16, 2, 64),
+               q_out=bf(4, 4, 64), k_scale=f32(8, 2), v_scale=f32(8, 2))
+    op = H.ChunkAttn(4, code(8, 16, 2, 64), code(8, 16, 2, 64), i32(2, 4), max_tokens=8, k_scale=f32(8, 2), v_scale=f32(8, 2))
+    attn = dict(q=bf(4, 4, 64), chunk_cu=i32(3), seq_len=i32(2), full_len=i32(2))
+    for call, kw in ((rope, put), (op, attn)):
+        host.calls.clear()
+        call(**kw)
+        assert len(host.calls) == 1
+        for name in kw:
+            with pytest.raises(H.HpdError) as e:
+                call(**{**kw, name: kw[name].as_subclass(Far)})
+            assert e.value.status == 1 and len(host.calls) == 1, name
+    # and what the object was made with
+    far = H.QkNormRope(4, 2, 64, None, None, host.of(torch.zeros(8, 32, 2)).as_subclass(Far))
+    with pytest.raises(H.HpdError):
+        far(**put)
 
 
 @gpu
